@@ -46,6 +46,18 @@
  *   wf_switch_init/commit     host-side lazy catch-up bookkeeping: which
  *                             backlog is due after each round
  *
+ * and the same round with its two large streams in fewer bits, the KV cache
+ * in 8 and weights in 4 (elements and power-of-two block scales in the
+ * formats that gfx950's matrix instructions and conversions take):
+ *
+ *   wf_kv8_append             quantise K/V rows into the 8-bit cache
+ *   wf_kv8_only_prefill       the KV-only prefill into the 8-bit cache
+ *   wf_kv8_verify_attn        verify attention over the 8-bit cache
+ *   wf_kv8_verify_attn_tree   the same under a per-row ancestor mask
+ *   wf_kv8_compact_path       moves an accepted path's rows together
+ *   wf_w4_quantize            one-time 4-bit copy of a weight
+ *   wf_linear_w4              y = W x (+ residual) over a 4-bit weight
+ *
  * Conventions shared by every call
  *   - Every tensor pointer is DEVICE memory owned by the caller, 16-byte
  *     aligned, densely packed in the layout stated.  The library never
@@ -561,6 +573,168 @@ size_t wf_tiled_weight_bytes(int32_t rows, int32_t cols);
  * WF_ERR_WORKSPACE if tiled_bytes is too small. */
 wf_status_t wf_tile_weights(const void *w, int32_t rows, int32_t cols,
                             void *tiled, size_t tiled_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
+ * 8-bit KV cache.  Codes are OCP e4m3 (1 sign, 4 exponent and 3 mantissa
+ * bits, bias 7, largest 448, 0x7f and 0xff NaN); one scale byte s for each
+ * block of 32 tokens and KV head stands for 2^(s - 127), so
+ *   value = e4m3(code) * 2^(s - 127).
+ * A power of two costs e4m3 no precision (only its range matters), and rows
+ * of a block that is still filling up can take another scale exactly, except
+ * where they fall below the format's smallest normal value.
+ *
+ * With n_blocks = ceil(cap / 32), and row r of the cache in block r / 32:
+ *   k        [n_kv_heads][n_blocks][32][head_dim] codes
+ *   v        [n_kv_heads][n_blocks][head_dim][32] codes: each block
+ *            transposed, the layout in which the attention's matrix
+ *            instruction takes V^T
+ *   k_scale, v_scale  [n_kv_heads][n_blocks] bytes
+ * k and v 16-byte aligned, whole blocks allocated also where cap is no
+ * multiple of 32.  The struct is host memory read during the call.
+ *
+ * Writing rows start .. start+n-1 (append, compaction) makes rows below
+ * start+n the valid ones and re-encodes each block that a written row lies
+ * in: with amax the largest finite magnitude over the block's valid rows
+ * (those below start at the values they are held at, the written ones as
+ * given), e is the smallest integer with amax <= 448 * 2^e, at least -100
+ * and at most 120 (0 if amax is 0), the scale byte e + 127, and every valid
+ * row's code e4m3(value * 2^-e) rounded to nearest even; an element that is
+ * not finite is stored as NaN.  Codes of rows from start+n on are left as
+ * they were (their values change with the scale: they hold nothing).
+ * ---------------------------------------------------------------------- */
+#define WF_KV8_BLOCK 32
+
+typedef struct wf_kv8_cache {
+    void *k;
+    void *v;
+    uint8_t *k_scale;
+    uint8_t *v_scale;
+    int32_t n_kv_heads, cap, head_dim;
+} wf_kv8_cache_t;
+
+/* Bytes of one of the two code arrays, and of one of the two scale arrays,
+ * of a layer (0 for invalid arguments). */
+size_t wf_kv8_code_bytes(int32_t n_kv_heads, int32_t cap, int32_t head_dim);
+size_t wf_kv8_scale_bytes(int32_t n_kv_heads, int32_t cap);
+
+/* Appends n_tok tokens' K and V rows at cache rows start_pos .. .
+ * k, v     row (t, g) of head_dim elements (dtype dt: WF_BF16 or WF_F32) at
+ *          k + t * tok_stride + g * head_stride (strides in elements, the
+ *          same for k and v): [n_tok][n_kv_heads][head_dim] and
+ *          [n_kv_heads][n_tok][head_dim] are both read as they are.
+ * Limits:  0 <= n_tok (0 is a no-op); start_pos >= 0; start_pos + n_tok <=
+ *          cap; 1 <= n_kv_heads <= 256; head_dim in {64, 128}; k and v 16-byte
+ *          aligned, strides multiples of 16 bytes.  The rows must not overlap
+ *          the cache.
+ * No workspace. */
+wf_status_t wf_kv8_append(wf_dtype_t dt, const wf_kv8_cache_t *cache, const void *k,
+                          const void *v, int32_t n_tok, int32_t start_pos,
+                          size_t tok_stride, size_t head_stride, void *stream);
+
+/* wf_kv_only_prefill with its K/V appended to the 8-bit cache: the rows are
+ * formed as there (rounded to dt's storage) in the workspace and then
+ * appended.  Arguments and limits of both (dt: WF_F32, WF_BF16 or
+ * WF_BF16_TILED).
+ * workspace >= wf_kv8_only_prefill_workspace_bytes(...) bytes. */
+wf_status_t wf_kv8_only_prefill(wf_dtype_t dt, const void *x, const void *w_k,
+                                const void *w_v, const wf_kv8_cache_t *cache,
+                                int32_t n_tok, int32_t start_pos, int32_t d_in,
+                                double rope_base, void *workspace,
+                                size_t workspace_bytes, void *stream);
+size_t wf_kv8_only_prefill_workspace_bytes(wf_dtype_t dt, int32_t n_tok, int32_t d_in,
+                                           int32_t n_kv_heads, int32_t head_dim);
+
+/* ------------------------------------------------------------------------
+ * wf_kv8_verify_attn -- wf_verify_attn over the 8-bit cache: the definition,
+ * the order of rows and heads and the limits are that call's, with K and V
+ * the held values of cache rows [0, ctx_len + gamma) (the block's own rows
+ * appended before the call); cache->cap bounds ctx_len + gamma.  Codes and
+ * scales of later rows and blocks are not used, whatever they hold.
+ * q, out   [gamma][n_q_heads][head_dim], dtype dt.  WF_BF16: products of the
+ *          exact e4m3 keys with q in two e4m3 parts that together hold it to
+ *          2^-17 of the row's largest element, and of the values with weights
+ *          held likewise to about 2^-9, accumulated in fp32.  WF_F32: fp32
+ *          throughout.
+ * softmax_scale, num_splits and the workspace as there, with this call's
+ * own workspace query; block rows a row does not see have to hold finite
+ * values, as for wf_verify_attn_tree.
+ * ---------------------------------------------------------------------- */
+wf_status_t wf_kv8_verify_attn(wf_dtype_t dt, const void *q, const wf_kv8_cache_t *cache,
+                               void *out, int32_t gamma, int32_t ctx_len,
+                               int32_t n_q_heads, float softmax_scale,
+                               int32_t num_splits, void *workspace,
+                               size_t workspace_bytes, void *stream);
+
+/* wf_verify_attn_tree over the 8-bit cache; tree_mask as there. */
+wf_status_t wf_kv8_verify_attn_tree(wf_dtype_t dt, const void *q,
+                                    const wf_kv8_cache_t *cache, void *out,
+                                    const uint64_t *tree_mask, int32_t gamma,
+                                    int32_t ctx_len, int32_t n_q_heads,
+                                    float softmax_scale, int32_t num_splits,
+                                    void *workspace, size_t workspace_bytes,
+                                    void *stream);
+
+/* Workspace for both (0 for invalid arguments). */
+size_t wf_kv8_verify_attn_workspace_bytes(wf_dtype_t dt, int32_t gamma, int32_t ctx_len,
+                                          int32_t n_q_heads, int32_t n_kv_heads,
+                                          int32_t head_dim, int32_t num_splits);
+
+/* ------------------------------------------------------------------------
+ * wf_kv8_compact_path -- wf_kv_compact_path for the 8-bit cache: the held
+ * values of rows ctx_len + path[t], t = 0..n, are written to rows ctx_len + t
+ * as an append of n + 1 rows at ctx_len would write them (all sources read
+ * before any row is written).  accept, path and the treatment of entries
+ * outside [t, gamma) as there; row ctx_len + n ends the valid rows.
+ * Layer l's codes start l * code_layer_stride bytes after layer 0's and its
+ * scales l * scale_layer_stride bytes (k and v alike); both ignored when
+ * n_layers == 1.
+ * Limits: 1 <= gamma <= 64; ctx_len >= 0; ctx_len + gamma <= cap;
+ *         head_dim in {64, 128}; 1 <= n_layers <= 1024; for n_layers > 1
+ *         strides of at least one layer's bytes, code_layer_stride a multiple
+ *         of 16.
+ * ---------------------------------------------------------------------- */
+wf_status_t wf_kv8_compact_path(const wf_kv8_cache_t *cache, const int32_t *accept,
+                                const int32_t *path, int32_t gamma, int32_t ctx_len,
+                                int32_t n_layers, size_t code_layer_stride,
+                                size_t scale_layer_stride, void *stream);
+
+/* ------------------------------------------------------------------------
+ * 4-bit weights.  Codes are OCP e2m1 (magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6;
+ * bit 3 the sign), two to a byte with the lower column in the low nibble;
+ * one scale byte s for each group of 32 consecutive columns of a row stands
+ * for 2^(s - 127) (255: the group is NaN):
+ *   codes    [rows][cols / 2], scales [rows][cols / 32], cols % 32 == 0
+ *   W[r][c]  = e2m1(codes[r][c / 2] nibble c % 2) * 2^(scales[r][c / 32] - 127)
+ * the plain row-major form of such checkpoints, read as it is.
+ * ---------------------------------------------------------------------- */
+
+/* The 4-bit copy of the bf16 weight w [rows][cols]: per group, e is the
+ * smallest integer with amax <= 6 * 2^e, at least -100 and at most 120 (0 for
+ * a group of zeros), and each code e2m1(w * 2^-e) rounded to nearest, ties to
+ * the even code.  A group with an element that is not finite gets scale 255.
+ * w and codes 16-byte aligned; rows >= 1; cols a positive multiple of 32. */
+wf_status_t wf_w4_quantize(const void *w, int32_t rows, int32_t cols, void *codes,
+                           uint8_t *scales, void *stream);
+
+/* wf_linear_w4 -- y[r][o] = sum_i x[r][i] W[o][i] (+ res[r][o]) for a few
+ * rows: the products are exact (bf16 by e2m1), the sums fp32 in a fixed order.
+ *
+ * x        [n_rows][k_in] bf16.
+ * codes, scales  the 4-bit weight [n_out][k_in].
+ * res      [n_rows][n_out] bf16, or NULL.  May be y itself when out_dt is
+ *          WF_BF16.
+ * y        [n_rows][n_out], out_dt WF_BF16 (rounded once) or WF_F32 (as the
+ *          logits of wf_lmhead_accept_entropy and wf_lmhead_accept_tree).
+ * Limits:  1 <= n_rows <= 64; 1 <= n_out <= 2^30; k_in a positive multiple of 32, at
+ *          most 2^20; x, codes 16-byte aligned (rows of codes are 16-byte
+ *          aligned then, k_in / 2 being a multiple of 16).
+ * workspace >= wf_linear_w4_workspace_bytes(...) bytes (may be NULL when
+ *          that is 0). */
+wf_status_t wf_linear_w4(const void *x, const void *codes, const uint8_t *scales,
+                         const void *res, wf_dtype_t out_dt, void *y, int32_t n_rows,
+                         int32_t n_out, int32_t k_in, void *workspace,
+                         size_t workspace_bytes, void *stream);
+size_t wf_linear_w4_workspace_bytes(int32_t n_rows, int32_t n_out, int32_t k_in);
 
 /* ------------------------------------------------------------------------
  * wf_read_probe -- measurement support, not a step of the method: reads

@@ -8,6 +8,7 @@ kernels of libwf.so; there is no fallback path.  If the library has not been
 built, importing this package raises ImportError.
 """
 import ctypes
+import operator
 import os
 
 import torch  # loaded first so libwf binds to the same HIP runtime as torch
@@ -32,7 +33,12 @@ EXPORTED_SYMBOLS = (
     "wf_tiled_weight_bytes", "wf_tile_weights", "wf_verify_attn_noalloc",
     "wf_read_probe", "wf_read_probe_series", "wf_lmhead_accept_route_neural",
     "wf_lmhead_route_neural_workspace_bytes",
+    "wf_kv8_code_bytes", "wf_kv8_scale_bytes", "wf_kv8_append", "wf_kv8_only_prefill",
+    "wf_kv8_only_prefill_workspace_bytes", "wf_kv8_verify_attn", "wf_kv8_verify_attn_tree",
+    "wf_kv8_verify_attn_workspace_bytes", "wf_kv8_compact_path", "wf_w4_quantize",
+    "wf_linear_w4", "wf_linear_w4_workspace_bytes",
 )
+KV8_BLOCK = 32                       # WF_KV8_BLOCK
 NOALLOC_SCRATCH_BYTES = 32 << 20     # WF_NOALLOC_SCRATCH_BYTES
 WF_DRAFTER_AR, WF_DRAFTER_DIFFUSION = 0, 1
 
@@ -48,6 +54,15 @@ class DecoderLayer(ctypes.Structure):
         ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
         ("inter", ctypes.c_int32), ("rms_eps", ctypes.c_float),
         ("rope_base", ctypes.c_double)]
+
+
+class Kv8CacheStruct(ctypes.Structure):
+    """wf_kv8_cache_t: device pointers of one layer's 8-bit KV cache and its
+    shape."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("n_kv_heads", ctypes.c_int32), ("cap", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32)]
 
 
 class SwitchState(ctypes.Structure):
@@ -129,6 +144,30 @@ def _load():
     lib.wf_lmhead_accept_route_neural.restype = i32
     lib.wf_lmhead_route_neural_workspace_bytes.argtypes = [i32, i32, i32, i32, i32]
     lib.wf_lmhead_route_neural_workspace_bytes.restype = sz
+    lib.wf_kv8_code_bytes.argtypes = [i32, i32, i32]
+    lib.wf_kv8_code_bytes.restype = sz
+    lib.wf_kv8_scale_bytes.argtypes = [i32, i32]
+    lib.wf_kv8_scale_bytes.restype = sz
+    lib.wf_kv8_append.argtypes = [i32, p, p, p, i32, i32, sz, sz, p]
+    lib.wf_kv8_append.restype = i32
+    lib.wf_kv8_only_prefill.argtypes = [i32, p, p, p, p, i32, i32, i32, f64, p, sz, p]
+    lib.wf_kv8_only_prefill.restype = i32
+    lib.wf_kv8_only_prefill_workspace_bytes.argtypes = [i32, i32, i32, i32, i32]
+    lib.wf_kv8_only_prefill_workspace_bytes.restype = sz
+    lib.wf_kv8_verify_attn.argtypes = [i32, p, p, p, i32, i32, i32, f32, i32, p, sz, p]
+    lib.wf_kv8_verify_attn.restype = i32
+    lib.wf_kv8_verify_attn_tree.argtypes = [i32, p, p, p, p, i32, i32, i32, f32, i32, p, sz, p]
+    lib.wf_kv8_verify_attn_tree.restype = i32
+    lib.wf_kv8_verify_attn_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i32, i32]
+    lib.wf_kv8_verify_attn_workspace_bytes.restype = sz
+    lib.wf_kv8_compact_path.argtypes = [p, p, p, i32, i32, i32, sz, sz, p]
+    lib.wf_kv8_compact_path.restype = i32
+    lib.wf_w4_quantize.argtypes = [p, i32, i32, p, p, p]
+    lib.wf_w4_quantize.restype = i32
+    lib.wf_linear_w4.argtypes = [p, p, p, p, i32, p, i32, i32, i32, p, sz, p]
+    lib.wf_linear_w4.restype = i32
+    lib.wf_linear_w4_workspace_bytes.argtypes = [i32, i32, i32]
+    lib.wf_linear_w4_workspace_bytes.restype = sz
     lib.wf_read_probe.argtypes = [p, sz, p, sz, i32, p]
     lib.wf_read_probe.restype = i32
     lib.wf_read_probe_series.argtypes = [p, sz, sz, i32, i32, p, sz, i32, i32, p]
@@ -244,6 +283,18 @@ if _raw_stream is None or _device is None:
 
 def _stream(stream):
     return stream.cuda_stream if stream is not None else _raw_stream(_device())
+
+
+def _stream_at(t, stream):
+    """The stream of a call whose first tensor is t: without one given, the
+    current stream, which has to be one of t's device."""
+    if stream is not None:
+        return stream.cuda_stream
+    dev = _device()
+    at = getattr(t.device, "index", None)
+    if dev is not None and at is not None and at != dev:
+        raise ValueError("tensors must be on the current device")
+    return _raw_stream(dev)
 
 
 def _check(status, what):
@@ -582,6 +633,223 @@ def wf_drafter_catchup(layer, r, pos, k_cache, v_cache, out, workspace=None,
                                 _dev(workspace, "workspace"), workspace.numel(),
                                 _stream(stream))
     _check(st, "wf_drafter_catchup")
+    return out
+
+
+class Kv8Cache:
+    """An 8-bit KV cache of one layer, or of a stack of layers (wf.h: e4m3
+    codes, one power-of-two scale byte per 32 tokens and KV head).
+
+    k        [L?][Hkv][blocks][32][D] uint8 (or float8_e4m3fn) codes
+    v        [L?][Hkv][blocks][D][32], each block transposed
+    k_scale, v_scale  [L?][Hkv][blocks] uint8 (or float8_e8m0fnu)
+    cap      rows per head; blocks = ceil(cap / 32)
+
+    The calls on one layer take a cache without L; layer(l) is one layer of a
+    stack (a view of its memory)."""
+
+    def __init__(self, k, v, k_scale, v_scale, cap):
+        cap = operator.index(cap)
+        shape, blocks = tuple(k.shape), (cap + KV8_BLOCK - 1) // KV8_BLOCK
+        if len(shape) not in (4, 5) or cap < 1:
+            raise ValueError("k must be [L?][Hkv][blocks][32][D]")
+        lead, (b, rows, dh) = shape[:-3], shape[-3:]
+        if b != blocks or rows != KV8_BLOCK or tuple(v.shape) != lead + (b, dh, rows) or \
+                tuple(k_scale.shape) != lead + (b,) or tuple(v_scale.shape) != lead + (b,):
+            raise ValueError("cache shapes do not match each other and cap")
+        for t in (k, v, k_scale, v_scale):
+            if t.element_size() != 1 or t.device != k.device:
+                raise ValueError("cache tensors hold bytes, on one device")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.n_layers = lead[0] if len(lead) == 2 else None
+        self.n_kv_heads, self.cap, self.head_dim, self.device = lead[-1], cap, dh, k.device
+        self.struct = Kv8CacheStruct(_dev(k, "k"), _dev(v, "v"), _dev(k_scale, "k_scale"),
+                                     _dev(v_scale, "v_scale"), lead[-1], cap, dh)
+        self.ref = ctypes.byref(self.struct)
+
+    def layer(self, l):
+        if self.n_layers is None:
+            raise ValueError("one layer only")
+        return Kv8Cache(self.k[l], self.v[l], self.k_scale[l], self.v_scale[l], self.cap)
+
+
+def alloc_kv8_cache(n_kv_heads, cap, head_dim, device, n_layers=None) -> Kv8Cache:
+    """An empty 8-bit KV cache (zeros) of one layer or of n_layers."""
+    blocks = (cap + KV8_BLOCK - 1) // KV8_BLOCK
+    lead = (n_kv_heads,) if n_layers is None else (n_layers, n_kv_heads)
+    z = [torch.zeros(lead + s, dtype=torch.uint8, device=device)
+         for s in ((blocks, KV8_BLOCK, head_dim), (blocks, head_dim, KV8_BLOCK), (blocks,),
+                   (blocks,))]
+    z[2].fill_(127)
+    z[3].fill_(127)
+    return Kv8Cache(*z, cap)
+
+
+def _one_layer(cache):
+    if cache.n_layers is not None:
+        raise ValueError("the call takes one layer of the cache: cache.layer(l)")
+    return cache.ref
+
+
+def wf_kv8_append(k, v, cache, start_pos, stream=None):
+    """k, v [n][Hkv][D] (bf16 or fp32) into cache rows start_pos .. of every
+    head.  The last dimension is dense; the others may be strided (alike for
+    k and v, in multiples of 16 bytes), as in a transposed [Hkv][n][D]."""
+    n, hkv, dh = k.shape
+    if v.shape != k.shape or v.dtype != k.dtype or hkv != cache.n_kv_heads or \
+            dh != cache.head_dim:
+        raise ValueError("k and v must match each other and the cache")
+    ks, vs = k.stride(), v.stride()
+    if n == 0:
+        ks = vs = (0, 0, 1)
+    # (the stride of a dimension of one entry says nothing)
+    ks = (ks[0] if n > 1 else 0, ks[1] if hkv > 1 else 0, ks[2])
+    vs = (vs[0] if n > 1 else 0, vs[1] if hkv > 1 else 0, vs[2])
+    if ks != vs or ks[2] != 1:
+        raise ValueError("k and v must have the same strides, the last one 1")
+    if not (k.is_cuda and v.is_cuda):
+        raise ValueError("k and v must be device tensors")
+    _check(lib.wf_kv8_append(_dtype_code(k), _one_layer(cache), k.data_ptr(), v.data_ptr(), n,
+                             start_pos, ks[0], ks[1], _stream_at(k, stream)), "wf_kv8_append")
+
+
+def wf_kv8_only_prefill_workspace_bytes(dtype, n_tok, d_in, n_kv_heads, head_dim) -> int:
+    code = dtype if isinstance(dtype, int) else (
+        WF_F32 if dtype == torch.float32 else WF_BF16)
+    return int(lib.wf_kv8_only_prefill_workspace_bytes(code, n_tok, d_in, n_kv_heads, head_dim))
+
+
+def wf_kv8_only_prefill(x, w_k, w_v, cache, start_pos, rope_base, workspace=None, stream=None):
+    """wf_kv_only_prefill into an 8-bit cache: x [n][d_in]; w_k, w_v
+    [Hkv*D][d_in]."""
+    n_tok, d_in = x.shape
+    hkv, dh = cache.n_kv_heads, cache.head_dim
+    for w in (w_k, w_v):
+        if tuple(w.shape) != (hkv * dh, d_in):
+            raise ValueError("weights must be [n_kv_heads * head_dim][d_in]")
+    code = _weight_code(x, w_k, w_v)
+    if workspace is None:
+        workspace = alloc_workspace(wf_kv8_only_prefill_workspace_bytes(
+            code, n_tok, d_in, hkv, dh), x.device)
+    _check(lib.wf_kv8_only_prefill(code, _dev(x, "x"), _dev(w_k, "w_k"), _dev(w_v, "w_v"),
+                                   _one_layer(cache), n_tok, start_pos, d_in,
+                                   float(rope_base), _dev(workspace, "workspace"),
+                                   workspace.numel(), _stream_at(x, stream)), "wf_kv8_only_prefill")
+
+
+def wf_kv8_verify_attn_workspace_bytes(dtype, gamma, ctx_len, n_q_heads, n_kv_heads, head_dim,
+                                       num_splits=0) -> int:
+    code = dtype if isinstance(dtype, int) else (
+        WF_F32 if dtype == torch.float32 else WF_BF16)
+    return int(lib.wf_kv8_verify_attn_workspace_bytes(
+        code, gamma, ctx_len, n_q_heads, n_kv_heads, head_dim, num_splits))
+
+
+def _kv8_attn(q, cache, out, ctx_len, tree_mask, softmax_scale, num_splits, workspace, stream):
+    shape = q.shape
+    gamma, hq, dh = shape
+    if dh != cache.head_dim or out.shape != shape or out.dtype != q.dtype:
+        raise ValueError("q, out and the cache do not match")
+    code = _dtype_code(q)
+    if softmax_scale is None:
+        softmax_scale = dh ** -0.5
+    if workspace is None:
+        workspace = alloc_workspace(wf_kv8_verify_attn_workspace_bytes(
+            code, gamma, ctx_len, hq, cache.n_kv_heads, dh, num_splits), q.device)
+    args = (gamma, ctx_len, hq, softmax_scale, num_splits, _dev(workspace, "workspace"),
+            workspace.numel(), _stream_at(q, stream))
+    if tree_mask is None:
+        st = lib.wf_kv8_verify_attn(code, _dev(q, "q"), _one_layer(cache), _dev(out, "out"),
+                                    *args)
+        _check(st, "wf_kv8_verify_attn")
+    else:
+        st = lib.wf_kv8_verify_attn_tree(code, _dev(q, "q"), _one_layer(cache),
+                                         _dev(out, "out"), _dev(tree_mask, "tree_mask"), *args)
+        _check(st, "wf_kv8_verify_attn_tree")
+    return out
+
+
+def wf_kv8_verify_attn(q, cache, out, ctx_len, softmax_scale=None, num_splits=0,
+                       workspace=None, stream=None):
+    """wf_verify_attn over an 8-bit cache: q, out [gamma][Hq][D] (bf16 or
+    fp32), cache rows [0, ctx_len + gamma) valid."""
+    return _kv8_attn(q, cache, out, ctx_len, None, softmax_scale, num_splits, workspace, stream)
+
+
+def wf_kv8_verify_attn_tree(q, cache, out, ctx_len, tree_mask, softmax_scale=None,
+                            num_splits=0, workspace=None, stream=None):
+    """wf_verify_attn_tree over an 8-bit cache; tree_mask as there."""
+    if tree_mask.numel() != q.shape[0] or tree_mask.element_size() != 8:
+        raise ValueError("tree_mask must hold gamma 64-bit words")
+    return _kv8_attn(q, cache, out, ctx_len, tree_mask, softmax_scale, num_splits, workspace,
+                     stream)
+
+
+def wf_kv8_compact_path(cache, accept, path, ctx_len, stream=None):
+    """wf_kv_compact_path for an 8-bit cache (one layer or the whole stack):
+    accept (n at [0]) and path [gamma] int32 device tensors, as written by
+    wf_lmhead_accept_tree."""
+    layers, codes, scales = 1, 0, 0
+    if cache.n_layers is not None:
+        layers, codes, scales = cache.n_layers, cache.k.stride(0), cache.k_scale.stride(0)
+    if accept.dtype != torch.int32 or path.dtype != torch.int32:
+        raise TypeError("accept and path are int32")
+    _check(lib.wf_kv8_compact_path(cache.ref, _dev(accept, "accept"), _dev(path, "path"),
+                                   path.numel(), ctx_len, layers, codes, scales,
+                                   _stream_at(path, stream)), "wf_kv8_compact_path")
+
+
+class W4Weight:
+    """A 4-bit weight [rows][cols] (wf.h: e2m1 codes, one power-of-two scale
+    byte per 32 columns): codes [rows][cols / 2] uint8, low nibble first, and
+    scales [rows][cols / 32] uint8 (or float8_e8m0fnu)."""
+
+    def __init__(self, codes, scales):
+        rows, half = codes.shape
+        if half % 16 or tuple(scales.shape) != (rows, half // 16):
+            raise ValueError("codes [rows][cols / 2] and scales [rows][cols / 32] do not match")
+        if codes.element_size() != 1 or scales.element_size() != 1 or \
+                codes.device != scales.device:
+            raise ValueError("codes and scales hold bytes, on one device")
+        self.codes, self.scales, self.shape = codes, scales, (rows, 2 * half)
+        self.device = codes.device
+
+
+def wf_w4_quantize(w, stream=None) -> W4Weight:
+    """The 4-bit copy of a bf16 weight [rows][cols], cols % 32 == 0."""
+    if w.dtype != torch.bfloat16:
+        raise TypeError("4-bit weights are made from bf16")
+    rows, cols = w.shape
+    codes = torch.empty((rows, cols // 2), dtype=torch.uint8, device=w.device)
+    scales = torch.empty((rows, cols // 32), dtype=torch.uint8, device=w.device)
+    _check(lib.wf_w4_quantize(_dev(w, "w"), rows, cols, _dev(codes, "codes"),
+                              _dev(scales, "scales"), _stream_at(w, stream)), "wf_w4_quantize")
+    return W4Weight(codes, scales)
+
+
+def wf_linear_w4_workspace_bytes(n_rows, n_out, k_in) -> int:
+    return int(lib.wf_linear_w4_workspace_bytes(n_rows, n_out, k_in))
+
+
+def wf_linear_w4(x, weight, out, residual=None, workspace=None, stream=None):
+    """out = x W^T (+ residual): x [n][k_in] bf16 (n <= 64), weight a W4Weight
+    [n_out][k_in], residual [n][n_out] bf16, out [n][n_out] bf16 or fp32."""
+    n, k_in = x.shape
+    n_out, cols = weight.shape
+    if x.dtype != torch.bfloat16 or (residual is not None and residual.dtype != torch.bfloat16):
+        raise TypeError("x and residual are bf16")
+    if cols != k_in or tuple(out.shape) != (n, n_out) or \
+            (residual is not None and residual.shape != out.shape):
+        raise ValueError("x, weight, residual and out do not match")
+    if workspace is None:
+        need = wf_linear_w4_workspace_bytes(n, n_out, k_in)
+        workspace = alloc_workspace(need, x.device) if need else None
+    st = lib.wf_linear_w4(_dev(x, "x"), _dev(weight.codes, "codes"),
+                          _dev(weight.scales, "scales"), _dev(residual, "residual"),
+                          _dtype_code(out), _dev(out, "out"), n, n_out, k_in,
+                          _dev(workspace, "workspace"),
+                          workspace.numel() if workspace is not None else 0, _stream_at(x, stream))
+    _check(st, "wf_linear_w4")
     return out
 
 

@@ -9,17 +9,15 @@
 
 namespace {
 
-constexpr int kMaxGamma = 64;
-constexpr int kMaxQHeads = 256;
+using wf::aligned16;
+using wf::head_dim_ok;
+using wf::kMaxGamma;
+using wf::kMaxLayers;
+using wf::kMaxPrefillTokens;
+using wf::kMaxQHeads;
 constexpr int kMaxSplits = 1024;
-constexpr int kMaxPrefillTokens = 4096;
 constexpr int kMaxBacklog = 1 << 20;        // drafter catch-up, in 4096-token batches
-constexpr int kMaxLayers = 1024;
 constexpr int kMaxRouterHidden = 1 << 16;
-
-inline bool aligned16(const void *p) {
-    return (reinterpret_cast<uintptr_t>(p) & 15u) == 0;
-}
 
 inline bool dtype_ok(wf_dtype_t dt) { return dt == WF_F32 || dt == WF_BF16; }
 
@@ -28,8 +26,9 @@ inline bool is_bf16(wf_dtype_t dt) { return dt == WF_BF16 || dt == WF_BF16_TILED
 inline bool weight_dtype_ok(wf_dtype_t dt) { return dtype_ok(dt) || dt == WF_BF16_TILED; }
 inline wf_dtype_t storage(wf_dtype_t dt) { return is_bf16(dt) ? WF_BF16 : dt; }
 
-inline bool head_dim_ok(int dh) { return dh == 64 || dh == 128; }
+}  // namespace
 
+namespace wf {
 wf_status_t check_attn(wf_dtype_t dt, int gamma, int ctx_len, int n_q_heads,
                        int n_kv_heads, int head_dim, int num_splits) {
     if (!dtype_ok(dt))
@@ -48,7 +47,7 @@ wf_status_t check_attn(wf_dtype_t dt, int gamma, int ctx_len, int n_q_heads,
     return WF_OK;
 }
 
-}  // namespace
+}  // namespace wf
 
 extern "C" {
 
@@ -70,8 +69,8 @@ size_t wf_verify_attn_workspace_bytes(wf_dtype_t dt, int32_t gamma,
                                       int32_t ctx_len, int32_t n_q_heads,
                                       int32_t n_kv_heads, int32_t head_dim,
                                       int32_t num_splits) {
-    if (check_attn(dt, gamma, ctx_len, n_q_heads, n_kv_heads, head_dim,
-                   num_splits) != WF_OK)
+    if (wf::check_attn(dt, gamma, ctx_len, n_q_heads, n_kv_heads, head_dim,
+                       num_splits) != WF_OK)
         return 0;
     const wf::AttnPlan p = wf::plan_attn(dt, gamma, ctx_len, n_q_heads,
                                          n_kv_heads, head_dim, num_splits);
@@ -162,7 +161,9 @@ wf_status_t wf_verify_attn_tree(wf_dtype_t dt, const void *q,
                               workspace_bytes, stream);
 }
 
-namespace {
+}  // extern "C"
+
+namespace wf {
 wf_status_t check_prefill(wf_dtype_t dt, int n_tok, int start_pos, int cap,
                           int d_in, int n_kv_heads, int head_dim,
                           double rope_base) {
@@ -178,16 +179,18 @@ wf_status_t check_prefill(wf_dtype_t dt, int n_tok, int start_pos, int cap,
         return WF_ERR_UNSUPPORTED;
     if (is_bf16(dt) && d_in % 32 != 0)
         return WF_ERR_UNSUPPORTED;
-    if (is_bf16(dt) && n_tok > 0 && !wf::prefill_fits(n_tok, d_in, n_kv_heads, head_dim))
+    if (is_bf16(dt) && n_tok > 0 && !prefill_fits(n_tok, d_in, n_kv_heads, head_dim))
         return WF_ERR_UNSUPPORTED;
     return WF_OK;
 }
-}  // namespace
+}  // namespace wf
+
+extern "C" {
 
 size_t wf_kv_only_prefill_workspace_bytes(wf_dtype_t dt, int32_t n_tok,
                                           int32_t d_in, int32_t n_kv_heads,
                                           int32_t head_dim) {
-    if (check_prefill(dt, n_tok, 0, n_tok, d_in, n_kv_heads, head_dim, 1.0) != WF_OK)
+    if (wf::check_prefill(dt, n_tok, 0, n_tok, d_in, n_kv_heads, head_dim, 1.0) != WF_OK)
         return 0;
     return wf::prefill_workspace_bytes(storage(dt), n_tok, d_in, n_kv_heads, head_dim);
 }
@@ -199,7 +202,7 @@ wf_status_t wf_kv_only_prefill(wf_dtype_t dt, const void *x, const void *w_k,
                                int32_t head_dim, double rope_base,
                                void *workspace, size_t workspace_bytes,
                                void *stream) {
-    const wf_status_t st = check_prefill(dt, n_tok, start_pos, cap, d_in,
+    const wf_status_t st = wf::check_prefill(dt, n_tok, start_pos, cap, d_in,
                                          n_kv_heads, head_dim, rope_base);
     if (st != WF_OK)
         return st;
@@ -243,7 +246,7 @@ wf_status_t check_prefill_layers(wf_dtype_t dt, int n_tok, int cap, int d_in, in
 size_t wf_kv_only_prefill_layers_workspace_bytes(wf_dtype_t dt, int32_t n_tok, int32_t d_in,
                                                  int32_t n_kv_heads, int32_t head_dim,
                                                  int32_t n_layers) {
-    if (check_prefill(dt, n_tok, 0, n_tok, d_in, n_kv_heads, head_dim, 1.0) != WF_OK ||
+    if (wf::check_prefill(dt, n_tok, 0, n_tok, d_in, n_kv_heads, head_dim, 1.0) != WF_OK ||
         n_layers < 1 || n_layers > kMaxLayers ||
         (is_bf16(dt) && n_tok > 0 &&
          !wf::prefill_fits(n_tok, d_in, n_kv_heads, head_dim, n_layers)))
@@ -259,7 +262,7 @@ wf_status_t wf_kv_only_prefill_layers(wf_dtype_t dt, const void *x, const void *
                                       size_t x_layer_stride, size_t w_layer_stride,
                                       size_t cache_layer_stride, void *workspace,
                                       size_t workspace_bytes, void *stream) {
-    wf_status_t st = check_prefill(dt, n_tok, start_pos, cap, d_in, n_kv_heads, head_dim,
+    wf_status_t st = wf::check_prefill(dt, n_tok, start_pos, cap, d_in, n_kv_heads, head_dim,
                                    rope_base);
     if (st != WF_OK)
         return st;

@@ -1148,6 +1148,44 @@ size_t attn_workspace_bytes(const AttnPlan &p, int gamma, int n_q_heads, int hea
     return kCounterBytes + (size_t)p.splits * pairs * (2 * sizeof(float) + (size_t)head_dim * p.part_bytes);
 }
 
+// out = the partials of all splits merged: their rows (bf16 or fp32, as out),
+// (reference, sum) pairs, and the factor that takes a difference of
+// references to log2 units.
+wf_status_t launch_attn_merge(int head_dim, bool bf16, const void *ws_o, const float *ws_ml,
+                              void *out, int pairs, int splits, float sl2, hipStream_t stream) {
+    constexpr int kMergeWpb = 1;
+    if (splits <= (kWave / (head_dim / 4)) * kMergeBatch) {
+        dim3 g1((unsigned)cdiv(pairs, kMergeWpb)), b1(64 * kMergeWpb);
+        if (head_dim == 128) {
+            if (bf16)
+                attn_merge_one<128, true, kMergeWpb><<<g1, b1, 0, stream>>>(ws_o, ws_ml, out, pairs, splits, sl2);
+            else
+                attn_merge_one<128, false, kMergeWpb><<<g1, b1, 0, stream>>>(ws_o, ws_ml, out, pairs, splits, sl2);
+        } else {
+            if (bf16)
+                attn_merge_one<64, true, kMergeWpb><<<g1, b1, 0, stream>>>(ws_o, ws_ml, out, pairs, splits, sl2);
+            else
+                attn_merge_one<64, false, kMergeWpb><<<g1, b1, 0, stream>>>(ws_o, ws_ml, out, pairs, splits, sl2);
+        }
+        return hipGetLastError() == hipSuccess ? WF_OK : WF_ERR_HIP;
+    }
+    dim3 mgrid((unsigned)pairs), mblock(64);
+    if (head_dim == 128) {
+        if (bf16)
+            attn_merge<128, true><<<mgrid, mblock, 0, stream>>>(ws_o, ws_ml, out, pairs, splits, sl2);
+        else
+            attn_merge<128, false><<<mgrid, mblock, 0, stream>>>(ws_o, ws_ml, out, pairs, splits, sl2);
+    } else {
+        if (bf16)
+            attn_merge<64, true><<<mgrid, mblock, 0, stream>>>(ws_o, ws_ml, out, pairs, splits, sl2);
+        else
+            attn_merge<64, false><<<mgrid, mblock, 0, stream>>>(ws_o, ws_ml, out, pairs, splits, sl2);
+    }
+    if (hipGetLastError() != hipSuccess)
+        return WF_ERR_HIP;
+    return WF_OK;
+}
+
 wf_status_t launch_attn(wf_dtype_t dt, const void *q, const void *k_cache,
                         const void *v_cache, void *out, int gamma, int ctx_len,
                         int cap, int n_q_heads, int n_kv_heads, int head_dim,
@@ -1214,38 +1252,8 @@ wf_status_t launch_attn(wf_dtype_t dt, const void *q, const void *k_cache,
     if (hipGetLastError() != hipSuccess)
         return WF_ERR_HIP;
 
-    const bool ob = (dt == WF_BF16);
-    constexpr int kMergeWpb = 1;
-    if (p.splits <= (kWave / (head_dim / 4)) * kMergeBatch) {
-        dim3 g1((unsigned)cdiv((int)pairs, kMergeWpb)), b1(64 * kMergeWpb);
-        if (head_dim == 128) {
-            if (ob)
-                attn_merge_one<128, true, kMergeWpb><<<g1, b1, 0, stream>>>(a.ws_o, a.ws_ml, out, (int)pairs, p.splits, a.sl2);
-            else
-                attn_merge_one<128, false, kMergeWpb><<<g1, b1, 0, stream>>>(a.ws_o, a.ws_ml, out, (int)pairs, p.splits, a.sl2);
-        } else {
-            if (ob)
-                attn_merge_one<64, true, kMergeWpb><<<g1, b1, 0, stream>>>(a.ws_o, a.ws_ml, out, (int)pairs, p.splits, a.sl2);
-            else
-                attn_merge_one<64, false, kMergeWpb><<<g1, b1, 0, stream>>>(a.ws_o, a.ws_ml, out, (int)pairs, p.splits, a.sl2);
-        }
-        return hipGetLastError() == hipSuccess ? WF_OK : WF_ERR_HIP;
-    }
-    dim3 mgrid((unsigned)pairs), mblock(64);
-    if (head_dim == 128) {
-        if (ob)
-            attn_merge<128, true><<<mgrid, mblock, 0, stream>>>(a.ws_o, a.ws_ml, out, (int)pairs, p.splits, a.sl2);
-        else
-            attn_merge<128, false><<<mgrid, mblock, 0, stream>>>(a.ws_o, a.ws_ml, out, (int)pairs, p.splits, a.sl2);
-    } else {
-        if (ob)
-            attn_merge<64, true><<<mgrid, mblock, 0, stream>>>(a.ws_o, a.ws_ml, out, (int)pairs, p.splits, a.sl2);
-        else
-            attn_merge<64, false><<<mgrid, mblock, 0, stream>>>(a.ws_o, a.ws_ml, out, (int)pairs, p.splits, a.sl2);
-    }
-    if (hipGetLastError() != hipSuccess)
-        return WF_ERR_HIP;
-    return WF_OK;
+    return launch_attn_merge(head_dim, dt == WF_BF16, a.ws_o, a.ws_ml, out, (int)pairs, p.splits,
+                             a.sl2, stream);
 }
 
 }  // namespace wf

@@ -20,6 +20,14 @@ namespace wf {
 constexpr size_t kCounterBytes = (size_t)4 << 20;
 constexpr int kCounterSlots = static_cast<int>(kCounterBytes / sizeof(unsigned));
 
+// Limits and argument checks of the ABI files (api.hip, api_lowbit.hip).
+constexpr int kMaxGamma = 64;
+constexpr int kMaxQHeads = 256;
+constexpr int kMaxPrefillTokens = 4096;
+constexpr int kMaxLayers = 1024;
+inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool head_dim_ok(int dh) { return dh == 64 || dh == 128; }
+
 struct AttnPlan {
     int rows;            // G * gamma query rows per KV head
     int nb;              // 16-row blocks per wave (bf16 path)
@@ -32,6 +40,11 @@ struct AttnPlan {
     int part_bytes;      // bytes per partial-output element (bf16 path: 2)
 };
 
+// Shapes of a verify-attention and of a KV-only prefill call (api.hip).
+wf_status_t check_prefill(wf_dtype_t dt, int n_tok, int start_pos, int cap, int d_in,
+                          int n_kv_heads, int head_dim, double rope_base);
+wf_status_t check_attn(wf_dtype_t dt, int gamma, int ctx_len, int n_q_heads, int n_kv_heads,
+                       int head_dim, int num_splits);
 AttnPlan plan_attn(wf_dtype_t dt, int gamma, int ctx_len, int n_q_heads,
                    int n_kv_heads, int head_dim, int num_splits);
 size_t attn_workspace_bytes(const AttnPlan &p, int gamma, int n_q_heads,
@@ -48,6 +61,32 @@ wf_status_t launch_attn(wf_dtype_t dt, const void *q, const void *k_cache,
                         int cap, int n_q_heads, int n_kv_heads, int head_dim,
                         float softmax_scale, const uint64_t *tree_mask,
                         const AttnPlan &p, void *workspace, hipStream_t stream);
+
+wf_status_t launch_attn_merge(int head_dim, bool bf16, const void *ws_o, const float *ws_ml,
+                              void *out, int pairs, int splits, float sl2, hipStream_t stream);
+
+// 8-bit KV cache (kv8.hip, attn8.hip).
+inline int kv8_blocks(int cap) { return (cap + WF_KV8_BLOCK - 1) / WF_KV8_BLOCK; }
+wf_status_t launch_kv8_append(wf_dtype_t dt, const wf_kv8_cache_t &c, const void *k,
+                              const void *v, int n_tok, int start, size_t tok_stride,
+                              size_t head_stride, hipStream_t stream);
+wf_status_t launch_kv8_compact(const wf_kv8_cache_t &c, const int32_t *accept,
+                               const int32_t *path, int gamma, int ctx_len, int n_layers,
+                               size_t code_stride, size_t scale_stride, hipStream_t stream);
+AttnPlan plan_attn8(wf_dtype_t dt, int gamma, int ctx_len, int n_q_heads, int n_kv_heads,
+                    int head_dim, int num_splits);
+wf_status_t launch_attn8(wf_dtype_t dt, const void *q, const wf_kv8_cache_t &c, void *out,
+                         int gamma, int ctx_len, int n_q_heads, float softmax_scale,
+                         const uint64_t *tree_mask, const AttnPlan &p, void *workspace,
+                         hipStream_t stream);
+
+// 4-bit weights (w4.hip).
+size_t linear_w4_workspace_bytes(int rows, int n_out, int k_in);
+wf_status_t launch_linear_w4(const uint16_t *x, const uint8_t *codes, const uint8_t *scales,
+                             const uint16_t *res, bool f32_out, void *y, int rows, int n_out,
+                             int k_in, void *workspace, hipStream_t stream);
+wf_status_t launch_w4_quantize(const void *w, int rows, int cols, void *codes, uint8_t *scales,
+                               hipStream_t stream);
 
 size_t lmhead_workspace_bytes(int gamma, int vocab);
 // The neural routing policy folded into the LM-head pass (bf16 weights in

@@ -1,0 +1,187 @@
+"""4-bit weights on the GPU against plain 64-bit definitions: the quantiser
+exactly, the product within the roundings it makes."""
+import numpy as np
+import pytest
+import torch
+
+import lowbit_ref as R
+
+pytestmark = pytest.mark.gpu
+
+wf = pytest.importorskip("paper_2606_07710_amd")
+DEV = "cuda"
+
+
+def _normal(seed, *shape, std=1.0, dtype=torch.bfloat16):
+    g = torch.Generator()
+    g.manual_seed(seed)
+    return (torch.randn(shape, generator=g) * std).to(dtype)
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 32), (3, 64), (17, 96), (5, 1056), (130, 512)])
+def test_quantize(rows, cols):
+    w = _normal(rows, rows, cols, std=0.02)
+    w[0, :8] = torch.tensor([0.0, -0.0, 1e-30, 6.0, 5.0, -0.25, 3.5, 2.5])
+    got = wf.wf_w4_quantize(w.to(DEV))
+    torch.cuda.synchronize()
+    codes, scales = R.encode_e2m1(w.double().numpy())
+    np.testing.assert_array_equal(got.scales.cpu().numpy(), scales)
+    np.testing.assert_array_equal(got.codes.cpu().numpy(), codes)
+
+
+def test_quantize_borders():
+    """Every rounding border of the format, both signs, groups of zeros, out of
+    range and not finite."""
+    mid = [0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0]
+    row = torch.tensor(mid + [-m for m in mid] + [6.0] + [0.0] * 17)
+    w = torch.stack([row, row * (1 + 2.0 ** -7), row * (1 - 2.0 ** -7), row * 2.0 ** -118,
+                     torch.zeros(32), row * 2.0 ** 119, row * 2.0 ** 125, row, row])
+    w[7, 3], w[8, 4] = float("nan"), float("-inf")
+    w = w.to(torch.bfloat16)
+    got = wf.wf_w4_quantize(w.to(DEV))
+    torch.cuda.synchronize()
+    codes, scales = R.encode_e2m1(w.double().numpy())
+    np.testing.assert_array_equal(got.scales.cpu().numpy(), scales)
+    fine = scales[:, 0] != 255
+    assert fine.sum() == 7
+    np.testing.assert_array_equal(got.codes.cpu().numpy()[fine], codes[fine])
+
+
+def _weight(seed, n_out, k_in):
+    g = torch.Generator()
+    g.manual_seed(seed)
+    codes = torch.randint(0, 256, (n_out, k_in // 2), generator=g, dtype=torch.uint8)
+    scales = torch.randint(112, 128, (n_out, k_in // 32), generator=g, dtype=torch.uint8)
+    return codes, scales
+
+
+SHAPES = [
+    # rows, n_out, k_in
+    (1, 1, 32), (1, 16, 128), (1, 4096, 4096), (2, 17, 96), (3, 1000, 2880), (5, 33, 160),
+    (11, 2560, 9728), (16, 1024, 4096), (17, 130, 1024), (31, 48, 64), (32, 257, 2560),
+    (33, 4096, 512), (47, 100, 4096), (61, 3001, 2560), (64, 512, 12288), (64, 5, 32),
+    (48, 24576, 544), (12, 16384, 1056), (1, 40, 40960),
+]
+
+
+def _check(x, codes, scales, got, res=None, out="bf16"):
+    """fp32 sums of exact products: k_in terms and the waves' sums, off by
+    (k_in + 64) 2^-24 of sum |x w| at the worst; the residual's addition by
+    2^-24 and a bf16 result by 2^-8 of the value."""
+    w = torch.from_numpy(R.decode_e2m1(codes.numpy(), scales.numpy()))
+    ref = x.double() @ w.t()
+    mass = x.double().abs() @ w.abs().t()
+    if res is not None:
+        ref, mass = ref + res.double(), mass + res.double().abs()
+    tol = mass * (x.shape[1] + 64) * 2.0 ** -24
+    if out == "bf16":
+        tol = tol + (ref.abs() + tol) * 2.0 ** -8
+    err = (got.double().cpu() - ref).abs()
+    assert (err <= tol).all(), float((err / tol).max())
+
+
+@pytest.mark.parametrize("rows,n_out,k_in", SHAPES)
+@pytest.mark.parametrize("out,res", [("bf16", False), ("bf16", True), ("f32", False),
+                                     ("f32", True)])
+def test_linear(rows, n_out, k_in, out, res):
+    print("linear", rows, n_out, k_in, out, res, flush=True)
+    codes, scales = _weight(rows + n_out, n_out, k_in)
+    x = _normal(k_in, rows, k_in)
+    r = _normal(7, rows, n_out) if res else None
+    dt = torch.bfloat16 if out == "bf16" else torch.float32
+    pad = torch.full((rows * n_out + 64,), float("nan"), dtype=dt, device=DEV)
+    y = pad[:rows * n_out].view(rows, n_out)
+    w = wf.W4Weight(codes.to(DEV), scales.to(DEV))
+    ret = wf.wf_linear_w4(x.to(DEV), w, y, r.to(DEV) if res else None)
+    torch.cuda.synchronize()
+    assert ret is y
+    _check(x, codes, scales, y, r, out)
+    assert pad[rows * n_out:].isnan().all()          # nothing behind the output
+    again = torch.empty_like(y)
+    wf.wf_linear_w4(x.to(DEV), w, again, r.to(DEV) if res else None)
+    torch.cuda.synchronize()
+    assert torch.equal(again, y)
+
+
+def test_linear_residual_in_place_and_workspace_reuse():
+    """The residual may be the output; calls of several sizes share one
+    workspace, also from a captured graph."""
+    ws = wf.alloc_workspace(max([wf.wf_linear_w4_workspace_bytes(*s) for s in SHAPES] + [16]), DEV)
+    calls = []
+    for rows, n_out, k_in in SHAPES[2:14]:
+        codes, scales = _weight(rows, n_out, k_in)
+        calls.append((_normal(1, rows, k_in), codes, scales, _normal(2, rows, n_out),
+                      wf.W4Weight(codes.to(DEV), scales.to(DEV))))
+    ys = [c[3].to(DEV) for c in calls]
+    xs = [c[0].to(DEV) for c in calls]
+    first = [c[3].to(DEV) for c in calls]
+
+    def step():
+        for x, c, y, f in zip(xs, calls, ys, first):
+            y.copy_(f)
+            wf.wf_linear_w4(x, c[4], y, y, workspace=ws)
+
+    step()
+    torch.cuda.synchronize()
+    ref = [y.clone() for y in ys]
+    for c, y in zip(calls, ys):
+        _check(c[0], c[1], c[2], y, c[3])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(3):
+        for y in ys:
+            y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(ref, ys))
+        step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(ref, ys))
+    assert ws.numel() < (4 << 20) or not bool(ws[:4 << 20].any().item())
+
+
+def test_linear_extreme_scales_and_nan():
+    """Scales at both ends of the range, and the NaN scale: only its feature."""
+    codes, scales = _weight(1, 48, 256)
+    scales[3], scales[4], scales[5, 2] = 27, 240, 255
+    x = _normal(2, 5, 256)
+    y = torch.empty(5, 48, device=DEV)
+    wf.wf_linear_w4(x.to(DEV), wf.W4Weight(codes.to(DEV), scales.to(DEV)), y)
+    torch.cuda.synchronize()
+    assert y[:, 5].isnan().all()
+    keep = [i for i in range(48) if i != 5]
+    _check(x, codes[keep], scales[keep], y[:, keep], out="f32")
+
+
+def test_quantised_layer_of_its_own():
+    """Quantise, then multiply: the product of what the codes hold."""
+    w = _normal(1, 300, 768, std=0.02)
+    x = _normal(2, 9, 768)
+    w4 = wf.wf_w4_quantize(w.to(DEV))
+    y = torch.empty(9, 300, dtype=torch.bfloat16, device=DEV)
+    wf.wf_linear_w4(x.to(DEV), w4, y)
+    torch.cuda.synchronize()
+    _check(x, w4.codes.cpu(), w4.scales.cpu(), y)
+    # e2m1 holds a weight to half a step, at most a sixth of the group's largest
+    held = R.decode_e2m1(w4.codes.cpu().numpy(), w4.scales.cpu().numpy())
+    big = w.double().abs().view(300, 24, 32).amax(2).repeat_interleave(32, 1).numpy()
+    assert (np.abs(held - w.double().numpy()) <= big / 3).all()
+
+
+def test_logits_feed_the_acceptance():
+    """fp32 logits of a 4-bit LM head through the logits mode of the LM-head
+    call: the argmax of the plain product where it is clear."""
+    g, d, vocab = 16, 512, 5000
+    codes, scales = _weight(3, vocab, d)
+    h = _normal(4, g, d)
+    logits = torch.empty(g, vocab, device=DEV)
+    wf.wf_linear_w4(h.to(DEV), wf.W4Weight(codes.to(DEV), scales.to(DEV)), logits)
+    am = torch.empty(g, dtype=torch.int32, device=DEV)
+    ent, acc = torch.empty(g, device=DEV), torch.empty(3, dtype=torch.int32, device=DEV)
+    ref = h.double() @ torch.from_numpy(R.decode_e2m1(codes.numpy(), scales.numpy())).t()
+    draft = ref.argmax(1).to(torch.int32)[:g - 1].to(DEV)
+    wf.wf_lmhead_accept_entropy(None, None, logits, draft, 1.0, am, ent, acc)
+    torch.cuda.synchronize()
+    assert am.cpu().tolist() == ref.argmax(1).tolist()
+    assert acc[0].item() == g - 1
