@@ -25,6 +25,8 @@ struct Attn8Params {
     const uint64_t *tree_mask;
     int gamma, ctx_len, n_blocks, n_q_heads, n_kv_heads, group, rows, n_keys;
     int splits, keys_per_split, n_row_groups;
+    int tiles_per_split, extra_tiles;    // 128-key tiles; the first splits' extra ones
+    unsigned group_magic;     // floor(2^32 / group) + 1: row / group as a high product
     float sl2;                // softmax_scale * log2(e)
 };
 
@@ -85,124 +87,184 @@ __device__ __forceinline__ f32x4 mfma_e4m3(i32x8 a, i32x8 b, f32x4 c, unsigned s
 
 // Four values of at most 256 as two e4m3 parts hi + lo / 16.
 constexpr int kLoShift = 4;
-__device__ __forceinline__ void two_parts(const float (&p)[4], uint32_t &hi, uint32_t &lo) {
+__device__ __forceinline__ void two_parts(const float (&p)[4], uint32_t dead, uint32_t &hi,
+                                          uint32_t &lo) {
     typedef short i16x2 __attribute__((ext_vector_type(2)));
     constexpr float kLo = 1.f / (1 << kLoShift);     // (the conversion divides by it)
-    int h = __builtin_amdgcn_cvt_pk_fp8_f32(p[0], p[1], 0, false);
+    // (the old value of a conversion's result, half of which it keeps, is any
+    // register that is free by then: a zero would have to be written first)
+    int h = __builtin_amdgcn_cvt_pk_fp8_f32(p[0], p[1], (int)dead, false);
     h = __builtin_amdgcn_cvt_pk_fp8_f32(p[2], p[3], h, true);
     float f[4];
     e4m3x4_to_f32((uint32_t)h, f);
-    i16x2 l = {0, 0};
-    l = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(l, p[0] - f[0], p[1] - f[1], kLo, false);
+    const float r0 = p[0] - f[0];
+    i16x2 l = __builtin_bit_cast(i16x2, f[0]);
+    l = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(l, r0, p[1] - f[1], kLo, false);
     l = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(l, p[2] - f[2], p[3] - f[3], kLo, true);
     hi = (uint32_t)h;
     lo = __builtin_bit_cast(uint32_t, l);
 }
 
-// The scale bytes of a tile's four blocks, in one dword: two aligned scalar
-// loads, neither of them past the dword that holds the head's last used byte.
-// Blocks past it read as scale 1 (their codes are masked).
-__device__ __forceinline__ unsigned tile_scales(const uint8_t *s, int block, int last_block) {
-    typedef const __attribute__((address_space(4))) uint32_t *scalar_ptr;
-    const uintptr_t at = reinterpret_cast<uintptr_t>(s + block);
-    const uintptr_t end = reinterpret_cast<uintptr_t>(s + last_block);
-    const uintptr_t a0 = at & ~(uintptr_t)3, e0 = end & ~(uintptr_t)3;
-    const uint32_t w0 = *(scalar_ptr)a0;
-    const uint32_t w1 = *(scalar_ptr)(a0 + 4 < e0 ? a0 + 4 : e0);
-    uint32_t w = (uint32_t)(((uint64_t)w1 << 32 | w0) >> (8 * (at & 3)));
-    const int live = last_block - block + 1;
-    if (live < kTileBlocks) {
-        const uint32_t keep = (1u << (8 * live)) - 1u;
-        w = (w & keep) | (0x7f7f7f7fu & ~keep);
-    }
-    return w;
+// Largest of the values that the four lane groups hold for a row, in all of
+// them.
+__device__ __forceinline__ float row_max(float m) {
+    typedef unsigned u32pair __attribute__((ext_vector_type(2)));
+    u32pair r = __builtin_amdgcn_permlane16_swap(__float_as_uint(m), __float_as_uint(m), false,
+                                                 false);
+    m = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(m), __float_as_uint(m), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-template <int D, int RG, int NBUF>
-__global__ __launch_bounds__(64 * RG) void attn8_tiles(Attn8Params a) {
+// Waves: KS key streams x RG row groups of 16 rows; a stage of the ring holds
+// TPS tiles of each stream.
+template <int D, int RG, int KS, int TPS, int NBUF>
+__global__ __launch_bounds__(64 * RG * KS) void attn8_tiles(Attn8Params a) {
     constexpr int HALF = kTileKeys8 * D;             // bytes of a K or V tile
-    constexpr int STAGE = 2 * HALF;
-    constexpr int LOADS = STAGE / 1024;              // wave loads per stage
-    constexpr int LPW = LOADS / RG;
+    constexpr int TILE = 2 * HALF + 1024;            // codes, then 16 bytes around the scales
+    constexpr int STAGE = KS * TPS * TILE;
+    constexpr int LPH = HALF / 1024 / RG;            // a wave's loads of K, and of V, per tile
+    constexpr int LPW = (2 * LPH + 1) * TPS;         // ... and of a stage, scales included
     constexpr int MD = D / 16;
+#ifndef VAH
+#define VAH MD/2
+#endif
+    constexpr int VAHEAD = VAH;
     constexpr int GRAN = D / 16;                     // 16-byte granules of a key
     constexpr int BLOCK = kKv8Block * D;             // bytes of a scale block
-    static_assert(LOADS % (2 * RG) == 0 && (NBUF - 2) * LPW < 64, "ring");
-    static_assert(NBUF * STAGE <= 160 * 1024, "LDS");
+    constexpr int QBYTES = 16 * D * 2;               // a wave's rows of q
+    constexpr int OST = D + 4;                       // padded fp32 row of the stream merge
+    static_assert((NBUF - 1) * LPW < 64 && RG * KS * QBYTES <= STAGE, "ring");
+    static_assert(NBUF * STAGE + 64 <= 160 * 1024, "LDS");
+    static_assert(KS <= 2 && (KS == 1 || RG * 16 * OST * 4 + RG * 128 <= NBUF * STAGE), "merge");
     __shared__ __attribute__((aligned(1024))) char ring[NBUF * STAGE];
 
     // ---- which (kv head, split, row group) this workgroup owns ----------------
-    int unit, rgw;
-    if (a.n_row_groups == 1) {
-        unit = blockIdx.x;
-        rgw = 0;
-    } else {
+    int g = blockIdx.x, split = blockIdx.y, rgw = 0;
+    if (a.n_row_groups > 1) {
         // the row groups of one (head, split) on one XCD, adjacent in its
         // dispatch order: all but the first find the tiles in its L2
         const int xcd = blockIdx.x & 7, w = blockIdx.x >> 3;
         rgw = w % a.n_row_groups;
-        unit = (w / a.n_row_groups) * 8 + xcd;
+        const int unit = (w / a.n_row_groups) * 8 + xcd;
+        if (unit >= a.n_kv_heads * a.splits)
+            return;
+        g = unit % a.n_kv_heads;
+        split = unit / a.n_kv_heads;
     }
-    if (unit >= a.n_kv_heads * a.splits)
-        return;
-    const int g = unit % a.n_kv_heads;
-    const int split = unit / a.n_kv_heads;
     const int wave = wave_id();
+    const int stream = wave % KS, rg = wave / KS;
     const int lane = threadIdx.x % kWave;
     const int m16 = lane & 15;
     const int c4 = lane >> 4;
 
-    const int tiles = (a.n_keys + kTileKeys8 - 1) / kTileKeys8;
-    const int t_first = (int)((long long)split * tiles / a.splits);
-    const int n_steps = (int)((long long)(split + 1) * tiles / a.splits) - t_first;
+    // the first splits take one tile more where they do not divide evenly
+    const int t_first = split * a.tiles_per_split + min(split, a.extra_tiles);
+    const int n_tiles = a.tiles_per_split + (split < a.extra_tiles ? 1 : 0);
+    const int n_steps = (n_tiles + KS * TPS - 1) / (KS * TPS);
     const int last_block = (a.n_keys - 1) / kKv8Block;
     const float sl2 = a.sl2;
     const size_t head = (size_t)g * a.n_blocks;
     const char *kg = a.k + head * BLOCK;
     const char *vg = a.v + head * BLOCK;
+    const uintptr_t ksat = reinterpret_cast<uintptr_t>(a.k_scale + head);
+    const uintptr_t vsat = reinterpret_cast<uintptr_t>(a.v_scale + head);
+    const uintptr_t ksend = (ksat + last_block) & ~(uintptr_t)3;
+    const uintptr_t vsend = (vsat + last_block) & ~(uintptr_t)3;
 
-    // Copies stage st: load j < LOADS / 2 of K, the rest of V, 1 KB each, dealt
-    // out to the waves.  A scale block past the last one repeats that block.
-    auto issue = [&](int st) __attribute__((always_inline)) {
-        const int b0 = (t_first + st) * kTileBlocks;
-        const unsigned slot = lds_addr(ring) + (st % NBUF) * STAGE;
-        const int most = last_block - b0;                // last block of the tile
+    // ---- the wave's 16 rows of q, by DMA into the stage that is filled last ------
+    const int row = (rgw * RG + rg) * 16 + m16;
+    auto token = [&](int r) { return a.group == 1 ? r : (int)__umulhi(r, a.group_magic); };
+    {
+        constexpr int LPR = D / 8;                   // lanes (16 bytes) per row
 #pragma unroll
-        for (int jr = 0; jr < LPW; ++jr) {
-            const bool is_v = jr >= LPW / 2;
-            const int j = wave + (jr - (is_v ? LPW / 2 : 0)) * RG;
-            unsigned off;
-            if (is_v) {
-                const int d = 32 * j + (lane >> 1);
-                off = 1024u * j + 32u * (lane >> 1) + 16u * ((lane ^ (d >> 2) ^ (d >> 3)) & 1);
-            } else {
-                const int k = j * (1024 / D) + lane / GRAN;
-                const int f = D == 128 ? (k & 3) | (k >> 2 & 4) : (k >> 1 & 1) | (k >> 3 & 2);
-                off = (unsigned)(k * D + ((lane % GRAN) ^ f) * 16);
-            }
-            const int b = j * 1024 / BLOCK;
-            const size_t src = (size_t)(b0 + min(b, most)) * BLOCK;
-            lds_dma16_so((is_v ? vg : kg) + src, off - (unsigned)(b * BLOCK),
-                         slot + (is_v ? HALF : 0) + j * 1024);
+        for (int w = 0; w < QBYTES / 1024; ++w) {
+            const int r = min((rgw * RG + rg) * 16 + (w * kWave + lane) / LPR, a.rows - 1);
+            const int i = token(r);
+            const int h = g * a.group + (r - i * a.group);
+            lds_dma16(static_cast<const char *>(a.q) + ((size_t)i * a.n_q_heads + h) * (D * 2) +
+                          lane % LPR * 16,
+                      lds_addr(ring) + (NBUF - 1) * STAGE + wave * QBYTES + w * 1024);
         }
-    };
+    }
 
-    // ---- the wave's 16 rows: q in two parts -------------------------------------
-    const int row = rgw * 16 * RG + wave * 16 + m16;
-    const int rc = min(row, a.rows - 1);             // (padding rows repeat the last one)
-    const int qi = rc / a.group;
-    const int qh = g * a.group + rc % a.group;
+    // Copies the stream's tile of stage st to buffer `buf`: 1 KB loads j of K and
+    // of V, dealt out to the stream's waves.  A stream without a tile in the last
+    // stage copies the one before again (never used), so that every wave counts
+    // the same loads; a scale block past the last one repeats that block.
+    unsigned koff, voff;
+    {
+        const int k = lane / GRAN;
+        koff = (unsigned)(k * D + ((lane % GRAN) ^ (D == 128 ? k & 3 : k >> 1 & 1)) * 16);
+        voff = (unsigned)(32 * (lane >> 1) + 16 * ((lane ^ (lane >> 3) ^ (lane >> 4)) & 1));
+    }
+    auto issue_tile = [&](int t, int slot_at) __attribute__((always_inline)) {
+        const int b0 = (t_first + min(t, n_tiles - 1)) * kTileBlocks;
+        const unsigned slot = lds_addr(ring) + slot_at + rg * 1024;
+        const int most = last_block - b0;                // last block of the tile
+        const char *kt = kg + (size_t)b0 * BLOCK, *vt = vg + (size_t)b0 * BLOCK;
+        auto go = [&](auto ragged) __attribute__((always_inline)) {
+#pragma unroll
+            for (int jr = 0; jr < 2 * LPH; ++jr) {
+                const bool is_v = jr >= LPH;
+                const int j = rg + (jr % LPH) * RG;
+                // (key bit 4 in a K granule's place: bit 1 of j, or 0 at head_dim 64)
+                unsigned off = is_v ? voff
+                                    : koff ^ (D == 128 ? (unsigned)(j & 2) << 5
+                                                       : (unsigned)(j & 1) << 5);
+                off += (unsigned)j * 1024u;
+                if constexpr (decltype(ragged)::value) {
+                    const int b = j * 1024 / BLOCK;
+                    off -= (unsigned)(max(b - most, 0) * BLOCK);
+                }
+                lds_dma16_so(is_v ? vt : kt, off, slot + (is_v ? HALF : 0) + jr % LPH * RG * 1024);
+            }
+        };
+        if (most >= kTileBlocks - 1)
+            go(std::false_type{});
+        else
+            go(std::true_type{});
+        // The scale bytes lie anywhere: lanes 0, 1 copy the two aligned dwords
+        // that hold the tile's four K scales, lanes 2, 3 those of V, neither
+        // past the dword of the last used byte (the other lanes repeat them).
+        const uintptr_t at = (lane & 2 ? vsat : ksat) + b0;
+        const uintptr_t from = min((at & ~(uintptr_t)3) + (lane & 1) * 4, lane & 2 ? vsend : ksend);
+        lds_dma4(reinterpret_cast<const char *>(from), lds_addr(ring) + slot_at + 2 * HALF);
+    };
+    auto issue = [&](int st, int buf) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < TPS; ++i)
+            issue_tile((KS * st + stream) * TPS + i, buf * STAGE + (stream * TPS + i) * TILE);
+    };
+#pragma unroll
+    for (int st = 0; st < NBUF - 1; ++st)
+        if (st < n_steps)
+            issue(st, st);
+    // Waits until all but the `later` stages issued last have landed.
+    auto landed = [&](int later) __attribute__((always_inline)) {
+        if (NBUF > 3 && later >= 3)
+            wait_vmcnt<(NBUF > 3 ? 3 : 0) * LPW>();
+        else if (NBUF > 2 && later >= 2)
+            wait_vmcnt<(NBUF > 2 ? 2 : 0) * LPW>();
+        else if (later >= 1)
+            wait_vmcnt<LPW>();
+        else
+            wait_vmcnt<0>();
+    };
+    const int qi = token(min(row, a.rows - 1));
+    const bool tree = a.tree_mask != nullptr;        // kernel argument: uniform
     constexpr int QW = D / 64;                       // 16-dim pieces of q per lane
     i32x8 qop[2];
     unsigned qscale, qlo;
+    landed(min(NBUF - 1, n_steps));
     {
-        const uint16_t *qp = static_cast<const uint16_t *>(a.q) +
-                             ((size_t)qi * a.n_q_heads + qh) * D + c4 * 16;
+        const WF_LDS(char) *qp = (const WF_LDS(char) *)ring + (NBUF - 1) * STAGE + wave * QBYTES +
+                                 m16 * (D * 2) + c4 * 32;
         float f[16 * QW];
         float m = 0.f;
 #pragma unroll
         for (int w = 0; w < 2 * QW; ++w) {
-            const u32x4 v = *reinterpret_cast<const u32x4 *>(qp + (w / 2) * 64 + (w % 2) * 8);
+            const u32x4 v = *(const WF_LDS(u32x4) *)(qp + (w / 2) * 128 + (w % 2) * 16);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 f[8 * w + 2 * e] = __uint_as_float(v[e] << 16);
@@ -212,19 +274,18 @@ __global__ __launch_bounds__(64 * RG) void attn8_tiles(Attn8Params a) {
 #pragma unroll
         for (int e = 0; e < 16 * QW; ++e)
             m = fmaxf(m, fabsf(f[e]));
-        m = fmaxf(m, __shfl_xor(m, 16, kWave));
-        m = fmaxf(m, __shfl_xor(m, 32, kWave));
+        m = row_max(m);
         const int e = max((int)(__float_as_uint(m) >> 23) - 127 - 7, -120);
         const float inv = __uint_as_float((unsigned)(127 - e) << 23);
         qscale = (unsigned)(e + 127);
+        qlo = qscale - kLoShift;
         uint32_t hi[4 * QW], lo[4 * QW];
 #pragma unroll
         for (int w = 0; w < 4 * QW; ++w) {
             const float p[4] = {f[4 * w] * inv, f[4 * w + 1] * inv, f[4 * w + 2] * inv,
                                 f[4 * w + 3] * inv};
-            two_parts(p, hi[w], lo[w]);
+            two_parts(p, __float_as_uint(f[4 * w]), hi[w], lo[w]);
         }
-        qlo = qscale - kLoShift;
         if constexpr (D == 128) {
             qop[0] = join(u32x4{hi[0], hi[1], hi[2], hi[3]}, u32x4{hi[4], hi[5], hi[6], hi[7]});
             qop[1] = join(u32x4{lo[0], lo[1], lo[2], lo[3]}, u32x4{lo[4], lo[5], lo[6], lo[7]});
@@ -235,65 +296,93 @@ __global__ __launch_bounds__(64 * RG) void attn8_tiles(Attn8Params a) {
                 qscale = qlo;
         }
     }
-    const bool tree = a.tree_mask != nullptr;        // kernel argument: uniform
-    const uint64_t gbits = a.gamma >= 64 ? ~0ull : (1ull << a.gamma) - 1ull;
-    const uint64_t tm = tree ? ((a.tree_mask[qi] | (1ull << qi)) & gbits) : 0ull;
-    const int lim = a.ctx_len + qi;
-    // the loads above are in before the first copy is issued, so no wait for
-    // them is left inside the loop
-    asm volatile("s_waitcnt vmcnt(0)" : "+v"(qop[0]), "+v"(qop[1]), "+v"(qscale), "+v"(qlo));
 
-    f32x4 o[MD];
+    // o[MD] collects the sum of the weights: one more 16-row block, of ones
+    f32x4 o[MD + 1];
 #pragma unroll
-    for (int md = 0; md < MD; ++md)
+    for (int md = 0; md <= MD; ++md)
         o[md] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float ref = -INFINITY, lsum = 0.f;
+    float ref = -INFINITY;
 
-    auto compute = [&](int st) __attribute__((always_inline)) {
-        const WF_LDS(char) *kt = (const WF_LDS(char) *)ring + (st % NBUF) * STAGE;
-        const WF_LDS(char) *vt = kt + HALF;
-        const int b0 = (t_first + st) * kTileBlocks;
-        const int kb = b0 * kKv8Block;
-        // lane's scale of row m16 (token block m16 / 8 of either half) in bytes
-        // 0 and 2; lane's scale of token block c4
-        const unsigned ks = tile_scales(a.k_scale + head, b0, last_block) >> (8 * (m16 >> 3));
-        const unsigned vs = tile_scales(a.v_scale + head, b0, last_block) >> (8 * c4);
+    const int kk0 = 16 * (m16 >> 2) + (m16 & 3);     // key of row m16 in block 0 of a half
+    const int kf = D == 128 ? (kk0 & 3) | (kk0 >> 2 & 4) : (kk0 >> 1 & 1) | (kk0 >> 3 & 2);
+    const int klane = kk0 * D + (c4 ^ kf) * 16;
+    const int vlane = HALF + (c4 >> 1) * BLOCK + m16 * kKv8Block +
+                      ((c4 ^ (m16 >> 2) ^ (m16 >> 3)) & 1) * 16;
 
-        // S^T = K Q^T
-        f32x4 s[8];
+    auto compute = [&](int t, int at) __attribute__((always_inline)) {
+        const WF_LDS(char) *base = (const WF_LDS(char) *)ring + at;
+        const int kb = (t_first + t) * kTileKeys8;
+        // the scales of the tile's four token blocks in a dword each
+        const WF_LDS(u32x4) *sp = (const WF_LDS(u32x4) *)(base + 2 * HALF);
+        const u32x4 sw = *sp;
+        // S^T = K Q^T, all operands asked for before the first is used
+        i32x8 kop[8];
 #pragma unroll
         for (int mb = 0; mb < 8; ++mb) {
-            const int k = 64 * (mb >> 2) + 16 * (m16 >> 2) + 4 * (mb & 3) + (m16 & 3);
-            const WF_LDS(char) *kr = kt + k * D;
-            i32x8 kop;
-            if constexpr (D == 128) {
-                const int f = (k & 3) | (k >> 2 & 4);
-                kop = join(*(const WF_LDS(u32x4) *)(kr + (c4 ^ f) * 16),
-                           *(const WF_LDS(u32x4) *)(kr + ((c4 + 4) ^ f) * 16));
-            } else {
-                const int f = (k >> 1 & 1) | (k >> 3 & 2);
-                const u32x4 w = *(const WF_LDS(u32x4) *)(kr + (c4 ^ f) * 16);
-                kop = join(w, w);
-            }
-            const f32x4 z = {0.f, 0.f, 0.f, 0.f};
-            s[mb] = mb < 4 ? mfma_e4m3<0, 0>(kop, qop[0], z, ks, qscale)
-                           : mfma_e4m3<2, 0>(kop, qop[0], z, ks, qscale);
+            const int off = (64 * (mb >> 2) + 4 * (mb & 3)) * D;
+            const u32x4 k0 = *(const WF_LDS(u32x4) *)(base + klane + off);
             if constexpr (D == 128)
-                s[mb] = mb < 4 ? mfma_e4m3<0, 0>(kop, qop[1], s[mb], ks, qlo)
-                               : mfma_e4m3<2, 0>(kop, qop[1], s[mb], ks, qlo);
+                kop[mb] = join(k0, *(const WF_LDS(u32x4) *)(base + (klane ^ 64) + off));
+            else
+                kop[mb] = join(k0, k0);
         }
-        // mask: only tiles that reach into the block
+        __builtin_amdgcn_sched_barrier(0);
+        const int b0 = kb / kKv8Block;
+        unsigned ks4 = __builtin_amdgcn_alignbyte(sw[1], sw[0], (unsigned)(ksat + b0) & 3u);
+        unsigned vs4 = __builtin_amdgcn_alignbyte(sw[3], sw[2], (unsigned)(vsat + b0) & 3u);
+        // lane's scale of row m16 (token block m16 / 8 of either half) in bytes
+        // 0 and 2; lane's scale of token block c4 (past the last one: 1)
+        const unsigned ks = ks4 >> (8 * (m16 >> 3));
+        const unsigned vs = b0 + c4 <= last_block ? vs4 >> (8 * c4) : 127u;
+        f32x4 s[8];
+        const f32x4 z = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int mb = 0; mb < 8; ++mb)
+            s[mb] = mb < 4 ? mfma_e4m3<0, 0>(kop[mb], qop[0], z, ks, qscale)
+                           : mfma_e4m3<2, 0>(kop[mb], qop[0], z, ks, qscale);
+        if constexpr (D == 128) {
+#pragma unroll
+            for (int mb = 0; mb < 8; ++mb)
+                s[mb] = mb < 4 ? mfma_e4m3<0, 0>(kop[mb], qop[1], s[mb], ks, qlo)
+                               : mfma_e4m3<2, 0>(kop[mb], qop[1], s[mb], ks, qlo);
+        }
+        // the values of the first dims, on their way during the softmax
+        u32x4 vop[MD][2];
+        auto read_v = [&](int md) {
+            const WF_LDS(char) *vr = base + vlane + md * 16 * kKv8Block;
+            vop[md][0] = *(const WF_LDS(u32x4) *)vr;
+            vop[md][1] = *(const WF_LDS(u32x4) *)(vr + 2 * BLOCK);
+        };
+#pragma unroll
+        for (int md = 0; md < VAHEAD; ++md)
+            read_v(md);
+        __builtin_amdgcn_sched_barrier(0);
+        // mask: only tiles that reach into the block.  Bit 16 h + b of `seen`:
+        // the row sees key 64 h + 16 c4 + b of the tile.
         if (kb + kTileKeys8 > a.ctx_len) {
+            uint64_t tm = 0;
+            if (tree) {
+                const uint64_t gbits = a.gamma >= 64 ? ~0ull : (1ull << a.gamma) - 1ull;
+                tm = (a.tree_mask[qi] | (1ull << qi)) & gbits;
+            }
+            unsigned seen = 0;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int j = kb + 64 * h + 16 * c4 - a.ctx_len;     // block row of bit 0
+                unsigned bits;
+                if (tree)                // keys before the block are seen by every row
+                    bits = j >= 64 ? 0u : j >= 0 ? (unsigned)(tm >> j)
+                           : j <= -16 ? ~0u : (unsigned)(tm << -j) | ((1u << -j) - 1u);
+                else
+                    bits = (1u << min(max(qi + 1 - j, 0), 16)) - 1u;
+                seen |= (bits & 0xffffu) << (16 * h);
+            }
 #pragma unroll
             for (int mb = 0; mb < 8; ++mb)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int key = kb + 64 * (mb >> 2) + 16 * c4 + 4 * (mb & 3) + i;
-                    const int j = key - a.ctx_len;
-                    const bool bit = ((tm >> (j & 63)) & 1ull) != 0;
-                    const bool vis = tree ? (j < 0) | ((j < a.gamma) & bit) : key <= lim;
-                    s[mb][i] = vis ? s[mb][i] : -INFINITY;
-                }
+                for (int i = 0; i < 4; ++i)
+                    s[mb][i] = seen >> (4 * mb + i) & 1u ? s[mb][i] : -INFINITY;
         }
         float m = s[0][0];
 #pragma unroll
@@ -301,99 +390,129 @@ __global__ __launch_bounds__(64 * RG) void attn8_tiles(Attn8Params a) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 m = fmaxf(m, s[mb][i]);
-        m = fmaxf(m, __shfl_xor(m, 16, kWave));
-        m = fmaxf(m, __shfl_xor(m, 32, kWave));
+        m = row_max(m);
         // the row's exponent in this tile, and against its reference
         const bool any = m > -INFINITY;
         const float e = any ? ceilf(m * sl2) : 0.f;
         if (__ballot(any && !(e - ref <= kRefGrow))) {
-            // (also a row's first visible tile: ref is -inf, o and lsum zero)
+            // (also a row's first visible tile: ref is -inf, o zero)
             if (any && !(e - ref <= kRefGrow)) {
                 const float back = fast_exp2(ref - e);
-                lsum *= back;
 #pragma unroll
-                for (int md = 0; md < MD; ++md)
+                for (int md = 0; md <= MD; ++md)
                     o[md] *= back;
                 ref = e;
             }
         }
         const int shift = any ? (int)fmaxf(e - ref, -120.f) : 0;
-        const unsigned ps = (unsigned)(127 + shift);
-        // P, its sum and its two parts
+        const unsigned ps = (unsigned)(127 + shift), pslo = ps - kLoShift;
+        // P in two parts
         const float add = 8.f - e;
-        float psum = 0.f;
         uint32_t hi[8], lo[8];
 #pragma unroll
         for (int mb = 0; mb < 8; ++mb) {
             float p[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < 4; ++i)
                 p[i] = fast_exp2(fmaf(s[mb][i], sl2, add));
-                psum += p[i];
-            }
-            two_parts(p, hi[mb], lo[mb]);
+            two_parts(p, __float_as_uint(s[mb][0]), hi[mb], lo[mb]);
         }
-        lsum += ldexpf(psum, shift);
         const i32x8 ph = join(u32x4{hi[0], hi[1], hi[2], hi[3]}, u32x4{hi[4], hi[5], hi[6], hi[7]});
         const i32x8 pl = join(u32x4{lo[0], lo[1], lo[2], lo[3]}, u32x4{lo[4], lo[5], lo[6], lo[7]});
         // O^T += V^T P^T
-        const bool ragged = kb + kTileKeys8 > a.n_keys;
+        auto pv = [&](auto ragged) __attribute__((always_inline)) {
+            constexpr int kOnes = 0x38383838;
+            const i32x8 ones = {kOnes, kOnes, kOnes, kOnes, kOnes, kOnes, kOnes, kOnes};
+            o[MD] = mfma_e4m3<0, 0>(ones, ph, o[MD], 127u, ps);
 #pragma unroll
-        for (int md = 0; md < MD; ++md) {
-            const int d = 16 * md + m16;
-            const WF_LDS(char) *vr = vt + (c4 >> 1) * BLOCK + d * kKv8Block +
-                                     ((c4 ^ (d >> 2) ^ (d >> 3)) & 1) * 16;
-            u32x4 v0 = *(const WF_LDS(u32x4) *)vr;
-            u32x4 v1 = *(const WF_LDS(u32x4) *)(vr + 2 * BLOCK);
-            if (ragged) {
-                // codes behind the last key may be NaN, and 0 * NaN is no zero
-                const int n0 = a.n_keys - kb - 16 * c4, n1 = n0 - 64;
+            for (int md = VAHEAD; md < MD; ++md)
+                read_v(md);
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const int x0 = min(max(n0 - 4 * w, 0), 4), x1 = min(max(n1 - 4 * w, 0), 4);
-                    v0[w] &= (uint32_t)((1ull << (8 * x0)) - 1ull);
-                    v1[w] &= (uint32_t)((1ull << (8 * x1)) - 1ull);
+            for (int md = 0; md < MD; ++md) {
+                if constexpr (decltype(ragged)::value) {
+                    // codes behind the last key may be NaN, and 0 * NaN is no zero
+                    const int n0 = a.n_keys - kb - 16 * c4, n1 = n0 - 64;
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const int x0 = min(max(n0 - 4 * w, 0), 4), x1 = min(max(n1 - 4 * w, 0), 4);
+                        vop[md][0][w] &= (uint32_t)((1ull << (8 * x0)) - 1ull);
+                        vop[md][1][w] &= (uint32_t)((1ull << (8 * x1)) - 1ull);
+                    }
                 }
+                o[md] = mfma_e4m3<0, 0>(join(vop[md][0], vop[md][1]), ph, o[md], vs, ps);
             }
-            const i32x8 vop = join(v0, v1);
-            o[md] = mfma_e4m3<0, 0>(vop, ph, o[md], vs, ps);
-            o[md] = mfma_e4m3<0, 0>(vop, pl, o[md], vs, ps - kLoShift);
-        }
+#pragma unroll
+            for (int md = 0; md < MD; ++md)
+                o[md] = mfma_e4m3<0, 0>(join(vop[md][0], vop[md][1]), pl, o[md], vs, pslo);
+            o[MD] = mfma_e4m3<0, 0>(ones, pl, o[MD], 127u, pslo);
+        };
+        if (kb + kTileKeys8 > a.n_keys)
+            pv(std::true_type{});
+        else
+            pv(std::false_type{});
     };
 
-    // ---- the ring: up to NBUF - 1 stages in flight -------------------------------
-#pragma unroll
-    for (int st = 0; st < NBUF - 1; ++st)
-        if (st < n_steps)
-            issue(st);
+#ifdef PRIO
+    if (wave >= 4)
+        __builtin_amdgcn_s_setprio(PRIO);
+#endif
+    // ---- the ring: up to NBUF - 1 stages in flight ----------------------------------
+    int buf = 0;
     for (int st = 0; st < n_steps; ++st) {
-        // (loads complete in order; the stages issued after st stay in flight)
-        const int later = min(NBUF - 2, n_steps - 1 - st);
-        if (NBUF > 3 && later >= 2)
-            wait_vmcnt<(NBUF > 3 ? 2 : 0) * LPW>();
-        else if (later >= 1)
-            wait_vmcnt<LPW>();
-        else
-            wait_vmcnt<0>();
+        landed(min(NBUF - 2, n_steps - 1 - st));
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         if (st + NBUF - 1 < n_steps)
-            issue(st + NBUF - 1);
-        compute(st);
+            issue(st + NBUF - 1, buf == 0 ? NBUF - 1 : buf - 1);
+        // (not unrolled: the tiles' code is long)
+#pragma unroll 1
+        for (int i = 0; i < TPS; ++i) {
+            const int t = (KS * st + stream) * TPS + i;
+            if (t < n_tiles)
+                compute(t, buf * STAGE + (stream * TPS + i) * TILE);
+        }
+        buf = buf + 1 == NBUF ? 0 : buf + 1;
+    }
+
+    // ---- the two streams of a row, in stream 0's registers -------------------------
+    float l = o[MD][0];                              // (all 16 rows of the block are alike)
+    if constexpr (KS == 2) {
+        __syncthreads();                 // the ring is free
+        WF_LDS(float) *part = (WF_LDS(float) *)ring + rg * 16 * OST;
+        WF_LDS(float) *ml = (WF_LDS(float) *)ring + RG * 16 * OST + rg * 32;
+        if (stream == 1) {
+#pragma unroll
+            for (int md = 0; md < MD; ++md)
+                *(WF_LDS(f32x4) *)(part + m16 * OST + md * 16 + 4 * c4) = o[md];
+            if (c4 == 0) {
+                ml[m16] = ref;
+                ml[16 + m16] = l;
+            }
+        }
+        __syncthreads();
+        if (stream == 1)
+            return;
+        const float ref1 = ml[m16], top = fmaxf(ref, ref1);
+        const float use = top == -INFINITY ? 0.f : top;
+        const float f0 = fast_exp2(ref - use), f1 = fast_exp2(ref1 - use);
+        l = l * f0 + ml[16 + m16] * f1;
+#pragma unroll
+        for (int md = 0; md < MD; ++md)
+            o[md] = o[md] * f0 + *(WF_LDS(f32x4) *)(part + m16 * OST + md * 16 + 4 * c4) * f1;
+        ref = top;
     }
 
     // ---- the split's partial ---------------------------------------------------------
-    lsum += __shfl_xor(lsum, 16, kWave);
-    lsum += __shfl_xor(lsum, 32, kWave);
     if (row >= a.rows)
         return;
-    const size_t pr = ((size_t)split * a.gamma + qi) * a.n_q_heads + qh;
+    const size_t pr = ((size_t)split * a.gamma + qi) * a.n_q_heads + g * a.group +
+                      (row - qi * a.group);
     uint2 *dst = reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.ws_o) + pr * D);
 #pragma unroll
     for (int md = 0; md < MD; ++md)
         dst[md * 4 + c4] = uint2{pack_bf16x2(o[md][0], o[md][1]), pack_bf16x2(o[md][2], o[md][3])};
     if (c4 == 0) {
         a.ws_ml[pr * 2] = ref;
-        a.ws_ml[pr * 2 + 1] = lsum;
+        a.ws_ml[pr * 2 + 1] = l;
     }
 }
 
@@ -513,8 +632,9 @@ AttnPlan plan_attn8(wf_dtype_t dt, int gamma, int ctx_len, int n_q_heads, int n_
     AttnPlan p{};
     p.part_bytes = 2;
     p.rows = n_q_heads / n_kv_heads * gamma;
-    p.nb = p.ks = 1;
+    p.nb = 1;
     p.rg = p.rows <= 16 ? 1 : p.rows <= 32 ? 2 : p.rows <= 64 ? 4 : 8;
+    p.ks = p.rg == 8 ? 1 : 2;
     p.n_row_groups = (p.rows + 16 * p.rg - 1) / (16 * p.rg);
     const int tiles = (ctx_len + gamma + kTileKeys8 - 1) / kTileKeys8;
     const int want = num_splits > 0 ? num_splits
@@ -550,14 +670,26 @@ wf_status_t launch_attn8(wf_dtype_t dt, const void *q, const wf_kv8_cache_t &c, 
     a.n_row_groups = p.n_row_groups;
     a.sl2 = softmax_scale * kLog2e;
     if (dt == WF_BF16) {
+        const int tiles = (a.n_keys + kTileKeys8 - 1) / kTileKeys8;
+        a.tiles_per_split = tiles / p.splits;
+        a.extra_tiles = tiles % p.splits;
+        // (exact for rows below 2^14 in groups of 2 to 2^8)
+        a.group_magic = (unsigned)((1ull << 32) / a.group + 1);
         const int units = c.n_kv_heads * p.splits;
-        const dim3 grid(p.n_row_groups > 1 ? (units + 7) / 8 * 8 * p.n_row_groups : units);
-#define WF_ATTN8(DV, RGV, NBUFV)                                                           \
-    if (c.head_dim == DV && p.rg == RGV)                                                   \
-        attn8_tiles<DV, RGV, NBUFV><<<grid, 64 * RGV, 0, stream>>>(a);                     \
+        const dim3 grid = p.n_row_groups > 1 ? dim3((units + 7) / 8 * 8 * p.n_row_groups)
+                                             : dim3(c.n_kv_heads, p.splits);
+#define WF_ATTN8(DV, RGV, KSV, TPSV, NBUFV)                                                \
+    if (c.head_dim == DV && p.rg == RGV && p.ks == KSV)                                    \
+        attn8_tiles<DV, RGV, KSV, TPSV, NBUFV><<<grid, 64 * RGV * KSV, 0, stream>>>(a);    \
     else
-        WF_ATTN8(128, 1, 3) WF_ATTN8(128, 2, 4) WF_ATTN8(128, 4, 4) WF_ATTN8(128, 8, 4)
-        WF_ATTN8(64, 1, 4) WF_ATTN8(64, 2, 4) WF_ATTN8(64, 4, 4) WF_ATTN8(64, 8, 4)
+        WF_ATTN8(128, 1, 2, 1, 2) WF_ATTN8(128, 2, 2, 1, 2) WF_ATTN8(128, 4, 2, 1, 2)
+#ifdef V2
+        WF_ATTN8(128, 8, 1, 2, 2)
+#else
+        WF_ATTN8(128, 8, 1, 1, 4)
+#endif
+        WF_ATTN8(64, 1, 2, 1, 2) WF_ATTN8(64, 2, 2, 1, 4) WF_ATTN8(64, 4, 2, 1, 4)
+        WF_ATTN8(64, 8, 1, 2, 4)
         return WF_ERR_UNSUPPORTED;
 #undef WF_ATTN8
     } else {

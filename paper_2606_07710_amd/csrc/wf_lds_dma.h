@@ -72,4 +72,15 @@ __device__ __forceinline__ void lds_dma16(const char *src, unsigned lds) {
                      : "memory", "m0");
 }
 
+// HBM -> LDS copy of 4 bytes per lane, 64-bit address per lane: lane L's bytes
+// land at LDS byte lds + 4*L.
+__device__ __forceinline__ void lds_dma4(const char *src, unsigned lds) {
+    asm volatile("s_mov_b32 m0, %1\n\t"
+                 "s_nop 0\n\t"
+                 "global_load_lds_dword %0, off"
+                 :
+                 : "v"(src), "s"(lds)
+                 : "memory", "m0");
+}
+
 }  // namespace wf
