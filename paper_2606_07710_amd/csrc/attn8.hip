@@ -117,19 +117,16 @@ __device__ __forceinline__ float row_max(float m) {
 }
 
 // Waves: KS key streams x RG row groups of 16 rows; a stage of the ring holds
-// TPS tiles of each stream.
-template <int D, int RG, int KS, int TPS, int NBUF>
+// one tile of each stream.
+template <int D, int RG, int KS, int NBUF>
 __global__ __launch_bounds__(64 * RG * KS) void attn8_tiles(Attn8Params a) {
     constexpr int HALF = kTileKeys8 * D;             // bytes of a K or V tile
     constexpr int TILE = 2 * HALF + 1024;            // codes, then 16 bytes around the scales
-    constexpr int STAGE = KS * TPS * TILE;
+    constexpr int STAGE = KS * TILE;
     constexpr int LPH = HALF / 1024 / RG;            // a wave's loads of K, and of V, per tile
-    constexpr int LPW = (2 * LPH + 1) * TPS;         // ... and of a stage, scales included
+    constexpr int LPW = 2 * LPH + 1;                 // ... and of a stage, scales included
     constexpr int MD = D / 16;
-#ifndef VAH
-#define VAH MD/2
-#endif
-    constexpr int VAHEAD = VAH;
+    constexpr int VAHEAD = MD / 2;                   // values read before the softmax, in 16 dims
     constexpr int GRAN = D / 16;                     // 16-byte granules of a key
     constexpr int BLOCK = kKv8Block * D;             // bytes of a scale block
     constexpr int QBYTES = 16 * D * 2;               // a wave's rows of q
@@ -161,7 +158,7 @@ __global__ __launch_bounds__(64 * RG * KS) void attn8_tiles(Attn8Params a) {
     // the first splits take one tile more where they do not divide evenly
     const int t_first = split * a.tiles_per_split + min(split, a.extra_tiles);
     const int n_tiles = a.tiles_per_split + (split < a.extra_tiles ? 1 : 0);
-    const int n_steps = (n_tiles + KS * TPS - 1) / (KS * TPS);
+    const int n_steps = (n_tiles + KS - 1) / KS;
     const int last_block = (a.n_keys - 1) / kKv8Block;
     const float sl2 = a.sl2;
     const size_t head = (size_t)g * a.n_blocks;
@@ -232,9 +229,7 @@ __global__ __launch_bounds__(64 * RG * KS) void attn8_tiles(Attn8Params a) {
         lds_dma4(reinterpret_cast<const char *>(from), lds_addr(ring) + slot_at + 2 * HALF);
     };
     auto issue = [&](int st, int buf) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < TPS; ++i)
-            issue_tile((KS * st + stream) * TPS + i, buf * STAGE + (stream * TPS + i) * TILE);
+        issue_tile(KS * st + stream, buf * STAGE + stream * TILE);
     };
 #pragma unroll
     for (int st = 0; st < NBUF - 1; ++st)
@@ -452,24 +447,17 @@ __global__ __launch_bounds__(64 * RG * KS) void attn8_tiles(Attn8Params a) {
             pv(std::false_type{});
     };
 
-#ifdef PRIO
-    if (wave >= 4)
-        __builtin_amdgcn_s_setprio(PRIO);
-#endif
     // ---- the ring: up to NBUF - 1 stages in flight ----------------------------------
     int buf = 0;
+#pragma unroll 1
     for (int st = 0; st < n_steps; ++st) {
         landed(min(NBUF - 2, n_steps - 1 - st));
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         if (st + NBUF - 1 < n_steps)
             issue(st + NBUF - 1, buf == 0 ? NBUF - 1 : buf - 1);
-        // (not unrolled: the tiles' code is long)
-#pragma unroll 1
-        for (int i = 0; i < TPS; ++i) {
-            const int t = (KS * st + stream) * TPS + i;
-            if (t < n_tiles)
-                compute(t, buf * STAGE + (stream * TPS + i) * TILE);
-        }
+        const int t = KS * st + stream;
+        if (t < n_tiles)
+            compute(t, buf * STAGE + stream * TILE);
         buf = buf + 1 == NBUF ? 0 : buf + 1;
     }
 
@@ -623,8 +611,12 @@ __global__ __launch_bounds__(64) void attn8_rows(Attn8Params a) {
 
 }  // namespace
 
-// Split plan of a call.  bf16: 16 rows per wave and up to 8 waves, so that up
-// to 128 rows share a tile; one workgroup per CU, none without a tile.
+// Split plan of a call.  bf16: up to 64 rows share a workgroup's tiles, two key
+// streams of up to four 16-row waves, one workgroup per CU; of more rows each 64
+// take a workgroup of one stream, two per CU, which do not wait for each other's
+// barriers (128 rows, 64K keys: 51.4 us, 53.0 as one workgroup of eight waves; 244
+// rows, 8K keys: 18.9 and 21.5 us, though the tiles are then read from L2 twice as
+// often).  No workgroup is without a tile.
 AttnPlan plan_attn8(wf_dtype_t dt, int gamma, int ctx_len, int n_q_heads, int n_kv_heads,
                     int head_dim, int num_splits) {
     if (dt == WF_F32)
@@ -633,12 +625,13 @@ AttnPlan plan_attn8(wf_dtype_t dt, int gamma, int ctx_len, int n_q_heads, int n_
     p.part_bytes = 2;
     p.rows = n_q_heads / n_kv_heads * gamma;
     p.nb = 1;
-    p.rg = p.rows <= 16 ? 1 : p.rows <= 32 ? 2 : p.rows <= 64 ? 4 : 8;
-    p.ks = p.rg == 8 ? 1 : 2;
+    p.rg = p.rows <= 16 ? 1 : p.rows <= 32 ? 2 : 4;
+    p.ks = p.rows <= 64 ? 2 : 1;
     p.n_row_groups = (p.rows + 16 * p.rg - 1) / (16 * p.rg);
     const int tiles = (ctx_len + gamma + kTileKeys8 - 1) / kTileKeys8;
+    const int fill = p.ks == 2 ? 256 : 512;
     const int want = num_splits > 0 ? num_splits
-                                    : std::max(1, 256 / (n_kv_heads * p.n_row_groups));
+                                    : std::max(1, fill / (n_kv_heads * p.n_row_groups));
     p.splits = std::min(want, tiles);
     return p;
 }
@@ -678,18 +671,13 @@ wf_status_t launch_attn8(wf_dtype_t dt, const void *q, const wf_kv8_cache_t &c, 
         const int units = c.n_kv_heads * p.splits;
         const dim3 grid = p.n_row_groups > 1 ? dim3((units + 7) / 8 * 8 * p.n_row_groups)
                                              : dim3(c.n_kv_heads, p.splits);
-#define WF_ATTN8(DV, RGV, KSV, TPSV, NBUFV)                                                \
+#define WF_ATTN8(DV, RGV, KSV, NBUFV)                                                      \
     if (c.head_dim == DV && p.rg == RGV && p.ks == KSV)                                    \
-        attn8_tiles<DV, RGV, KSV, TPSV, NBUFV><<<grid, 64 * RGV * KSV, 0, stream>>>(a);    \
+        attn8_tiles<DV, RGV, KSV, NBUFV><<<grid, 64 * RGV * KSV, 0, stream>>>(a);          \
     else
-        WF_ATTN8(128, 1, 2, 1, 2) WF_ATTN8(128, 2, 2, 1, 2) WF_ATTN8(128, 4, 2, 1, 2)
-#ifdef V2
-        WF_ATTN8(128, 8, 1, 2, 2)
-#else
-        WF_ATTN8(128, 8, 1, 1, 4)
-#endif
-        WF_ATTN8(64, 1, 2, 1, 2) WF_ATTN8(64, 2, 2, 1, 4) WF_ATTN8(64, 4, 2, 1, 4)
-        WF_ATTN8(64, 8, 1, 2, 4)
+        WF_ATTN8(128, 1, 2, 2) WF_ATTN8(128, 2, 2, 2) WF_ATTN8(128, 4, 2, 2)
+        WF_ATTN8(128, 4, 1, 2)
+        WF_ATTN8(64, 1, 2, 2) WF_ATTN8(64, 2, 2, 4) WF_ATTN8(64, 4, 2, 4) WF_ATTN8(64, 4, 1, 4)
         return WF_ERR_UNSUPPORTED;
 #undef WF_ATTN8
     } else {
