@@ -55,7 +55,9 @@
  *   wf_kv8_verify_attn        verify attention over the 8-bit cache
  *   wf_kv8_verify_attn_tree   the same under a per-row ancestor mask
  *   wf_kv8_compact_path       moves an accepted path's rows together
- *   wf_w4_quantize            one-time 4-bit copy of a weight
+ *   wf_w4_quantize            the 4-bit form of a weight
+ *   wf_w4_pack                one-time copy of it into the tiles that the
+ *                             products stream
  *   wf_linear_w4              y = W x (+ residual) over a 4-bit weight
  *
  * Conventions shared by every call
@@ -702,37 +704,52 @@ wf_status_t wf_kv8_compact_path(const wf_kv8_cache_t *cache, const int32_t *acce
  * 4-bit weights.  Codes are OCP e2m1 (magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6;
  * bit 3 the sign), two to a byte with the lower column in the low nibble;
  * one scale byte s for each group of 32 consecutive columns of a row stands
- * for 2^(s - 127) (255: the group is NaN):
+ * for 2^(s - 127) (1 <= s <= 254; 255: the group is NaN):
  *   codes    [rows][cols / 2], scales [rows][cols / 32], cols % 32 == 0
  *   W[r][c]  = e2m1(codes[r][c / 2] nibble c % 2) * 2^(scales[r][c / 32] - 127)
- * the plain row-major form of such checkpoints, read as it is.
+ * the plain row-major form of such checkpoints.  The products stream a packed
+ * copy of it, made once per weight: tiles of 16 rows x 128 columns, 1088 bytes
+ * each (tile (b, c) at (b * ceil(cols/128) + c) * 1088), in which byte
+ * 16 * (m + 16 q) + i, i < 16, holds codes byte [16b + m][64c + 16q + i] and
+ * byte 1024 + m + 16 q the scale of [16b + m][4c + q] (m < 16, q < 4); rows and
+ * columns past the end are zeros under scale 127.  A tile is one operand load
+ * of a wave, contiguous (row-major, 64-byte pieces of 16 rows stream at 3.0 of
+ * the 4 TB/s and more that the tiles reach).
+ * Limits of every call: 1 <= rows <= 2^30; cols a positive multiple of 32, at
+ * most 2^20; fewer than 2^26 tiles.
  * ---------------------------------------------------------------------- */
 
-/* The 4-bit copy of the bf16 weight w [rows][cols]: per group, e is the
+/* The 4-bit form of the bf16 weight w [rows][cols]: per group, e is the
  * smallest integer with amax <= 6 * 2^e, at least -100 and at most 120 (0 for
- * a group of zeros), and each code e2m1(w * 2^-e) rounded to nearest, ties to
- * the even code.  A group with an element that is not finite gets scale 255.
- * w and codes 16-byte aligned; rows >= 1; cols a positive multiple of 32. */
+ * a group of zeros), the scale e + 127, and each code e2m1(w * 2^-e) rounded to
+ * nearest, ties to the even code.  A group with an element that is not finite
+ * gets scale 255.  w and codes 16-byte aligned. */
 wf_status_t wf_w4_quantize(const void *w, int32_t rows, int32_t cols, void *codes,
                            uint8_t *scales, void *stream);
+
+/* Bytes of a packed weight (0 for invalid arguments). */
+size_t wf_w4_packed_bytes(int32_t rows, int32_t cols);
+
+/* Writes the packed copy of a weight into `packed` (packed_bytes >=
+ * wf_w4_packed_bytes(rows, cols), else WF_ERR_WORKSPACE; it must not overlap
+ * codes or scales).  codes and packed 16-byte aligned. */
+wf_status_t wf_w4_pack(const void *codes, const uint8_t *scales, int32_t rows, int32_t cols,
+                       void *packed, size_t packed_bytes, void *stream);
 
 /* wf_linear_w4 -- y[r][o] = sum_i x[r][i] W[o][i] (+ res[r][o]) for a few
  * rows: the products are exact (bf16 by e2m1), the sums fp32 in a fixed order.
  *
  * x        [n_rows][k_in] bf16.
- * codes, scales  the 4-bit weight [n_out][k_in].
+ * packed   the packed 4-bit weight [n_out][k_in].
  * res      [n_rows][n_out] bf16, or NULL.  May be y itself when out_dt is
  *          WF_BF16.
  * y        [n_rows][n_out], out_dt WF_BF16 (rounded once) or WF_F32 (as the
  *          logits of wf_lmhead_accept_entropy and wf_lmhead_accept_tree).
- * Limits:  1 <= n_rows <= 64; 1 <= n_out <= 2^30; k_in a positive multiple of 32, at
- *          most 2^20; x, codes 16-byte aligned (rows of codes are 16-byte
- *          aligned then, k_in / 2 being a multiple of 16).
+ * Limits:  1 <= n_rows <= 64; the weight's; x and packed 16-byte aligned.
  * workspace >= wf_linear_w4_workspace_bytes(...) bytes (may be NULL when
  *          that is 0). */
-wf_status_t wf_linear_w4(const void *x, const void *codes, const uint8_t *scales,
-                         const void *res, wf_dtype_t out_dt, void *y, int32_t n_rows,
-                         int32_t n_out, int32_t k_in, void *workspace,
+wf_status_t wf_linear_w4(const void *x, const void *packed, const void *res, wf_dtype_t out_dt,
+                         void *y, int32_t n_rows, int32_t n_out, int32_t k_in, void *workspace,
                          size_t workspace_bytes, void *stream);
 size_t wf_linear_w4_workspace_bytes(int32_t n_rows, int32_t n_out, int32_t k_in);
 

@@ -36,7 +36,7 @@ EXPORTED_SYMBOLS = (
     "wf_kv8_code_bytes", "wf_kv8_scale_bytes", "wf_kv8_append", "wf_kv8_only_prefill",
     "wf_kv8_only_prefill_workspace_bytes", "wf_kv8_verify_attn", "wf_kv8_verify_attn_tree",
     "wf_kv8_verify_attn_workspace_bytes", "wf_kv8_compact_path", "wf_w4_quantize",
-    "wf_linear_w4", "wf_linear_w4_workspace_bytes",
+    "wf_w4_packed_bytes", "wf_w4_pack", "wf_linear_w4", "wf_linear_w4_workspace_bytes",
 )
 KV8_BLOCK = 32                       # WF_KV8_BLOCK
 NOALLOC_SCRATCH_BYTES = 32 << 20     # WF_NOALLOC_SCRATCH_BYTES
@@ -164,7 +164,11 @@ def _load():
     lib.wf_kv8_compact_path.restype = i32
     lib.wf_w4_quantize.argtypes = [p, i32, i32, p, p, p]
     lib.wf_w4_quantize.restype = i32
-    lib.wf_linear_w4.argtypes = [p, p, p, p, i32, p, i32, i32, i32, p, sz, p]
+    lib.wf_w4_packed_bytes.argtypes = [i32, i32]
+    lib.wf_w4_packed_bytes.restype = sz
+    lib.wf_w4_pack.argtypes = [p, p, i32, i32, p, sz, p]
+    lib.wf_w4_pack.restype = i32
+    lib.wf_linear_w4.argtypes = [p, p, p, i32, p, i32, i32, i32, p, sz, p]
     lib.wf_linear_w4.restype = i32
     lib.wf_linear_w4_workspace_bytes.argtypes = [i32, i32, i32]
     lib.wf_linear_w4_workspace_bytes.restype = sz
@@ -800,31 +804,40 @@ def wf_kv8_compact_path(cache, accept, path, ctx_len, stream=None):
 
 
 class W4Weight:
-    """A 4-bit weight [rows][cols] (wf.h: e2m1 codes, one power-of-two scale
-    byte per 32 columns): codes [rows][cols / 2] uint8, low nibble first, and
-    scales [rows][cols / 32] uint8 (or float8_e8m0fnu)."""
+    """A 4-bit weight [rows][cols] in the packed tiles that wf_linear_w4
+    streams (wf.h: e2m1 codes, one power-of-two scale byte per 32 columns),
+    made once from its row-major form: codes [rows][cols / 2] uint8, low
+    nibble first, and scales [rows][cols / 32] uint8 (or float8_e8m0fnu),
+    which are not kept."""
 
-    def __init__(self, codes, scales):
+    def __init__(self, codes, scales, stream=None):
         rows, half = codes.shape
         if half % 16 or tuple(scales.shape) != (rows, half // 16):
             raise ValueError("codes [rows][cols / 2] and scales [rows][cols / 32] do not match")
         if codes.element_size() != 1 or scales.element_size() != 1 or \
                 codes.device != scales.device:
             raise ValueError("codes and scales hold bytes, on one device")
-        self.codes, self.scales, self.shape = codes, scales, (rows, 2 * half)
-        self.device = codes.device
+        self.shape, self.device = (rows, 2 * half), codes.device
+        n = int(lib.wf_w4_packed_bytes(rows, 2 * half))
+        self.packed = torch.empty(n, dtype=torch.uint8, device=codes.device)
+        _check(lib.wf_w4_pack(_dev(codes, "codes"), _dev(scales, "scales"), rows, 2 * half,
+                              _dev(self.packed, "packed"), n, _stream_at(codes, stream)),
+               "wf_w4_pack")
 
 
-def wf_w4_quantize(w, stream=None) -> W4Weight:
-    """The 4-bit copy of a bf16 weight [rows][cols], cols % 32 == 0."""
+def wf_w4_quantize(w, stream=None):
+    """The 4-bit form (codes, scales) of a bf16 weight [rows][cols], cols % 32
+    == 0; W4Weight(codes, scales) packs it for the products."""
     if w.dtype != torch.bfloat16:
         raise TypeError("4-bit weights are made from bf16")
     rows, cols = w.shape
+    if cols % 32:
+        raise ValueError("the columns of a 4-bit weight come in groups of 32")
     codes = torch.empty((rows, cols // 2), dtype=torch.uint8, device=w.device)
     scales = torch.empty((rows, cols // 32), dtype=torch.uint8, device=w.device)
     _check(lib.wf_w4_quantize(_dev(w, "w"), rows, cols, _dev(codes, "codes"),
                               _dev(scales, "scales"), _stream_at(w, stream)), "wf_w4_quantize")
-    return W4Weight(codes, scales)
+    return codes, scales
 
 
 def wf_linear_w4_workspace_bytes(n_rows, n_out, k_in) -> int:
@@ -844,9 +857,8 @@ def wf_linear_w4(x, weight, out, residual=None, workspace=None, stream=None):
     if workspace is None:
         need = wf_linear_w4_workspace_bytes(n, n_out, k_in)
         workspace = alloc_workspace(need, x.device) if need else None
-    st = lib.wf_linear_w4(_dev(x, "x"), _dev(weight.codes, "codes"),
-                          _dev(weight.scales, "scales"), _dev(residual, "residual"),
-                          _dtype_code(out), _dev(out, "out"), n, n_out, k_in,
+    st = lib.wf_linear_w4(_dev(x, "x"), _dev(weight.packed, "packed"),
+                          _dev(residual, "residual"), _dtype_code(out), _dev(out, "out"), n, n_out, k_in,
                           _dev(workspace, "workspace"),
                           workspace.numel() if workspace is not None else 0, _stream_at(x, stream))
     _check(st, "wf_linear_w4")

@@ -197,18 +197,39 @@ wf_status_t wf_kv8_compact_path(const wf_kv8_cache_t *cache, const int32_t *acce
                                   static_cast<hipStream_t>(stream));
 }
 
+namespace {
+// a weight's shape: fewer than 2^26 tiles of 16 x 128 (the grid of the packing)
+bool w4_weight_ok(int rows, int cols) {
+    return rows >= 1 && rows <= (1 << 30) && cols >= 32 && cols % 32 == 0 &&
+           cols <= kMaxW4Inputs &&
+           (long long)((rows + 15) / 16) * ((cols + 127) / 128) < (1 << 26);
+}
+}  // namespace
+
 wf_status_t wf_w4_quantize(const void *w, int32_t rows, int32_t cols, void *codes,
                            uint8_t *scales, void *stream) {
-    if (!w || !codes || !scales || !aligned16(w) || !aligned16(codes) || rows < 1 || cols < 32 ||
-        cols % 32 || (long long)rows * (cols / 32) > (long long)INT32_MAX * 128)
+    if (!w || !codes || !scales || !aligned16(w) || !aligned16(codes) || !w4_weight_ok(rows, cols))
         return WF_ERR_INVALID_ARG;
     return wf::launch_w4_quantize(w, rows, cols, codes, scales, static_cast<hipStream_t>(stream));
 }
 
+size_t wf_w4_packed_bytes(int32_t rows, int32_t cols) {
+    return w4_weight_ok(rows, cols) ? wf::w4_packed_bytes(rows, cols) : 0;
+}
+
+wf_status_t wf_w4_pack(const void *codes, const uint8_t *scales, int32_t rows, int32_t cols,
+                       void *packed, size_t packed_bytes, void *stream) {
+    if (!codes || !scales || !packed || !aligned16(codes) || !aligned16(packed) ||
+        !w4_weight_ok(rows, cols))
+        return WF_ERR_INVALID_ARG;
+    if (packed_bytes < wf::w4_packed_bytes(rows, cols))
+        return WF_ERR_WORKSPACE;
+    return wf::launch_w4_pack(codes, scales, rows, cols, packed, static_cast<hipStream_t>(stream));
+}
+
 namespace {
 bool linear_w4_shape_ok(int n_rows, int n_out, int k_in) {
-    return n_rows >= 1 && n_rows <= kMaxW4Rows && n_out >= 1 && n_out <= (1 << 30) && k_in >= 32 && k_in % 32 == 0 &&
-           k_in <= kMaxW4Inputs;
+    return n_rows >= 1 && n_rows <= kMaxW4Rows && w4_weight_ok(n_out, k_in);
 }
 }  // namespace
 
@@ -218,18 +239,17 @@ size_t wf_linear_w4_workspace_bytes(int32_t n_rows, int32_t n_out, int32_t k_in)
                : 0;
 }
 
-wf_status_t wf_linear_w4(const void *x, const void *codes, const uint8_t *scales,
-                         const void *res, wf_dtype_t out_dt, void *y, int32_t n_rows,
-                         int32_t n_out, int32_t k_in, void *workspace, size_t workspace_bytes,
-                         void *stream) {
-    if (!dtype_ok(out_dt) || !x || !codes || !scales || !y || !aligned16(x) ||
-        !aligned16(codes) || !linear_w4_shape_ok(n_rows, n_out, k_in))
+wf_status_t wf_linear_w4(const void *x, const void *packed, const void *res, wf_dtype_t out_dt,
+                         void *y, int32_t n_rows, int32_t n_out, int32_t k_in, void *workspace,
+                         size_t workspace_bytes, void *stream) {
+    if (!dtype_ok(out_dt) || !x || !packed || !y || !aligned16(x) || !aligned16(packed) ||
+        !linear_w4_shape_ok(n_rows, n_out, k_in))
         return WF_ERR_INVALID_ARG;
     const size_t need = wf::linear_w4_workspace_bytes(n_rows, n_out, k_in);
     if (need && (!workspace || workspace_bytes < need || !aligned16(workspace)))
         return WF_ERR_WORKSPACE;
     return wf::launch_linear_w4(static_cast<const uint16_t *>(x),
-                                static_cast<const uint8_t *>(codes), scales,
+                                static_cast<const uint8_t *>(packed),
                                 static_cast<const uint16_t *>(res), out_dt == WF_F32, y, n_rows,
                                 n_out, k_in, workspace, static_cast<hipStream_t>(stream));
 }

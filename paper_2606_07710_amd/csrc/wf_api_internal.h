@@ -82,9 +82,12 @@ wf_status_t launch_attn8(wf_dtype_t dt, const void *q, const wf_kv8_cache_t &c, 
 
 // 4-bit weights (w4.hip).
 size_t linear_w4_workspace_bytes(int rows, int n_out, int k_in);
-wf_status_t launch_linear_w4(const uint16_t *x, const uint8_t *codes, const uint8_t *scales,
-                             const uint16_t *res, bool f32_out, void *y, int rows, int n_out,
-                             int k_in, void *workspace, hipStream_t stream);
+wf_status_t launch_linear_w4(const uint16_t *x, const uint8_t *w, const uint16_t *res,
+                             bool f32_out, void *y, int rows, int n_out, int k_in,
+                             void *workspace, hipStream_t stream);
+size_t w4_packed_bytes(int rows, int cols);
+wf_status_t launch_w4_pack(const void *codes, const uint8_t *scales, int rows, int cols,
+                           void *packed, hipStream_t stream);
 wf_status_t launch_w4_quantize(const void *w, int rows, int cols, void *codes, uint8_t *scales,
                                hipStream_t stream);
 

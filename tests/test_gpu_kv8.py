@@ -423,7 +423,7 @@ def test_round_in_a_graph_and_on_a_side_stream():
     x = _normal(1, g, d).to(DEV)
     wk, wv = (_normal(i, hkv * dh, d, std=0.05).to(DEV) for i in (2, 3))
     q, h = _normal(4, g, hq, dh).to(DEV), _normal(5, g, d).to(DEV)
-    w4 = wf.wf_w4_quantize(_normal(6, vocab, d, std=0.05).to(DEV))
+    w4 = wf.W4Weight(*wf.wf_w4_quantize(_normal(6, vocab, d, std=0.05).to(DEV)))
     tokens = torch.randint(0, vocab, (g,), generator=_rng(7)).to(torch.int32).to(DEV)
     logits = torch.empty(g, vocab, device=DEV)
     wf.wf_linear_w4(h, w4, logits)

@@ -25,8 +25,8 @@ def test_quantize(rows, cols):
     got = wf.wf_w4_quantize(w.to(DEV))
     torch.cuda.synchronize()
     codes, scales = R.encode_e2m1(w.double().numpy())
-    np.testing.assert_array_equal(got.scales.cpu().numpy(), scales)
-    np.testing.assert_array_equal(got.codes.cpu().numpy(), codes)
+    np.testing.assert_array_equal(got[1].cpu().numpy(), scales)
+    np.testing.assert_array_equal(got[0].cpu().numpy(), codes)
 
 
 def test_quantize_borders():
@@ -41,10 +41,26 @@ def test_quantize_borders():
     got = wf.wf_w4_quantize(w.to(DEV))
     torch.cuda.synchronize()
     codes, scales = R.encode_e2m1(w.double().numpy())
-    np.testing.assert_array_equal(got.scales.cpu().numpy(), scales)
+    np.testing.assert_array_equal(got[1].cpu().numpy(), scales)
     fine = scales[:, 0] != 255
     assert fine.sum() == 7
-    np.testing.assert_array_equal(got.codes.cpu().numpy()[fine], codes[fine])
+    np.testing.assert_array_equal(got[0].cpu().numpy()[fine], codes[fine])
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 32), (16, 128), (17, 160), (40, 2880)])
+def test_pack(rows, cols):
+    """Every byte of the packed tiles, padding included."""
+    codes, scales = _weight(rows, rows, cols)
+    got = wf.W4Weight(codes.to(DEV), scales.to(DEV)).packed
+    torch.cuda.synchronize()
+    nb, nc = (rows + 15) // 16, (cols + 127) // 128
+    c = np.zeros((nb * 16, nc * 4, 16), np.uint8)
+    c[:rows, :cols // 32] = codes.numpy().reshape(rows, cols // 32, 16)
+    s = np.full((nb * 16, nc * 4), 127, np.uint8)
+    s[:rows, :cols // 32] = scales.numpy()
+    c = c.reshape(nb, 16, nc, 4, 16).transpose(0, 2, 3, 1, 4).reshape(nb, nc, 1024)
+    s = s.reshape(nb, 16, nc, 4).transpose(0, 2, 3, 1).reshape(nb, nc, 64)
+    np.testing.assert_array_equal(got.cpu().numpy(), np.concatenate([c, s], 2).ravel())
 
 
 def _weight(seed, n_out, k_in):
@@ -158,13 +174,14 @@ def test_quantised_layer_of_its_own():
     """Quantise, then multiply: the product of what the codes hold."""
     w = _normal(1, 300, 768, std=0.02)
     x = _normal(2, 9, 768)
-    w4 = wf.wf_w4_quantize(w.to(DEV))
+    held4, scales4 = wf.wf_w4_quantize(w.to(DEV))
+    w4 = wf.W4Weight(held4, scales4)
     y = torch.empty(9, 300, dtype=torch.bfloat16, device=DEV)
     wf.wf_linear_w4(x.to(DEV), w4, y)
     torch.cuda.synchronize()
-    _check(x, w4.codes.cpu(), w4.scales.cpu(), y)
+    _check(x, held4.cpu(), scales4.cpu(), y)
     # e2m1 holds a weight to half a step, at most a sixth of the group's largest
-    held = R.decode_e2m1(w4.codes.cpu().numpy(), w4.scales.cpu().numpy())
+    held = R.decode_e2m1(held4.cpu().numpy(), scales4.cpu().numpy())
     big = w.double().abs().view(300, 24, 32).amax(2).repeat_interleave(32, 1).numpy()
     assert (np.abs(held - w.double().numpy()) <= big / 3).all()
 

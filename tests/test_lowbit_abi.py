@@ -142,18 +142,19 @@ def test_prefill_workspace_query():
 
 
 def _linear(**kw):
-    a = dict(x=FAKE, codes=FAKE, scales=FAKE, res=None, dt=1, y=FAKE, rows=16, n_out=4096,
-             k_in=4096, ws=FAKE, wsb=1 << 30)
+    a = dict(x=FAKE, packed=FAKE, res=None, dt=1, y=FAKE, rows=16, n_out=4096, k_in=4096,
+             ws=FAKE, wsb=1 << 30)
     a.update(kw)
-    return wf.lib.wf_linear_w4(a["x"], a["codes"], a["scales"], a["res"], a["dt"], a["y"],
-                               a["rows"], a["n_out"], a["k_in"], a["ws"], a["wsb"], None)
+    return wf.lib.wf_linear_w4(a["x"], a["packed"], a["res"], a["dt"], a["y"], a["rows"],
+                               a["n_out"], a["k_in"], a["ws"], a["wsb"], None)
 
 
 @pytest.mark.parametrize("kw,status", [
-    (dict(x=None), 1), (dict(codes=None), 1), (dict(scales=None), 1), (dict(y=None), 1),
-    (dict(x=ODD), 1), (dict(codes=ODD), 1), (dict(rows=0), 1), (dict(rows=65), 1),
+    (dict(x=None), 1), (dict(packed=None), 1), (dict(y=None), 1),
+    (dict(x=ODD), 1), (dict(packed=ODD), 1), (dict(rows=0), 1), (dict(rows=65), 1),
     (dict(n_out=0), 1), (dict(n_out=(1 << 30) + 1), 1), (dict(k_in=0), 1), (dict(k_in=48), 1),
     (dict(k_in=(1 << 20) + 32), 1), (dict(dt=2), 1), (dict(dt=9), 1),
+    (dict(n_out=1 << 30, k_in=1 << 20), 1),
 ])
 def test_linear_refuses(kw, status):
     assert _linear(**kw) == status
@@ -167,6 +168,25 @@ def test_linear_refuses(kw, status):
 ])
 def test_quantize_refuses(args, status):
     assert wf.lib.wf_w4_quantize(*args, None) == status
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(codes=None), 1), (dict(scales=None), 1), (dict(packed=None), 1), (dict(codes=ODD), 1),
+    (dict(packed=ODD), 1), (dict(rows=0), 1), (dict(cols=0), 1), (dict(cols=48), 1),
+    (dict(nbytes=2 * 1088 - 1), 3),
+])
+def test_pack_refuses(kw, status):
+    a = dict(codes=FAKE, scales=FAKE, rows=16, cols=160, packed=FAKE, nbytes=2 * 1088)
+    a.update(kw)
+    assert wf.lib.wf_w4_pack(a["codes"], a["scales"], a["rows"], a["cols"], a["packed"],
+                             a["nbytes"], None) == status
+
+
+def test_packed_sizes():
+    f = wf.lib.wf_w4_packed_bytes
+    assert f(1, 32) == 1088 and f(16, 128) == 1088 and f(17, 160) == 4 * 1088
+    assert f(151936, 2560) == 9496 * 20 * 1088
+    assert f(0, 32) == f(16, 0) == f(16, 48) == f(1 << 30, 1 << 20) == 0
 
 
 # ---- the Python layer -------------------------------------------------------------
@@ -209,6 +229,12 @@ def _kv8(hkv=2, cap=70, dh=64, layers=None, **kw):
              k_scale=_bytes(*lead, hkv, b), v_scale=_bytes(*lead, hkv, b))
     t.update(kw)
     return wf.Kv8Cache(t["k"], t["v"], t["k_scale"], t["v_scale"], cap)
+
+
+def _w4():
+    w = wf.W4Weight.__new__(wf.W4Weight)
+    w.packed, w.shape = _bytes(1088), (16, 64)
+    return w
 
 
 @pytest.mark.parametrize("kw", [
@@ -260,7 +286,7 @@ def test_python_takes_whole_numbers_only(ctx):
 def test_python_calls_reach_the_library():
     q, x = Fake(4, 8, 64), Fake(4, 64)
     path = Fake(4, dtype=torch.int32)
-    w = wf.W4Weight(_bytes(16, 32), _bytes(16, 2))
+    w = _w4()
     for call in (lambda: wf.wf_kv8_verify_attn(q, _kv8(), q, 5, workspace=_bytes(64),
                                                stream=FakeStream),
                  lambda: wf.wf_kv8_append(Fake(4, 2, 64), Fake(4, 2, 64), _kv8(), 0,
@@ -289,7 +315,7 @@ def test_python_weight_shapes(codes, scales):
     (Fake(4, 64), Fake(4, 16), Fake(4, 16, dtype=torch.float32)),
 ])
 def test_python_linear_refuses(x, out, res):
-    w = wf.W4Weight(_bytes(16, 32), _bytes(16, 2))
+    w = _w4()
     with pytest.raises((ValueError, TypeError)):
         wf.wf_linear_w4(x, w, out, res, stream=FakeStream)
 
