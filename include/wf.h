@@ -709,12 +709,12 @@ wf_status_t wf_kv8_compact_path(const wf_kv8_cache_t *cache, const int32_t *acce
  *   W[r][c]  = e2m1(codes[r][c / 2] nibble c % 2) * 2^(scales[r][c / 32] - 127)
  * the plain row-major form of such checkpoints.  The products stream a packed
  * copy of it, made once per weight: tiles of 16 rows x 128 columns, 1088 bytes
- * each (tile (b, c) at (b * ceil(cols/128) + c) * 1088), in which byte
- * 16 * (m + 16 q) + i, i < 16, holds codes byte [16b + m][64c + 16q + i] and
- * byte 1024 + m + 16 q the scale of [16b + m][4c + q] (m < 16, q < 4); rows and
- * columns past the end are zeros under scale 127.  A tile is one operand load
- * of a wave, contiguous (row-major, 64-byte pieces of 16 rows stream at 3.0 of
- * the 4 TB/s and more that the tiles reach).
+ * each (tile (b, c) at (b * ceil(cols/128) + c) * 1088), in which bytes
+ * 16 * (m + 16 q) + 4 k + i, i < 4, hold the codes bytes [16b + m][64c + 16k +
+ * 4q + i] and byte 1024 + 4 m + k the scale of [16b + m][4c + k] (m < 16; q, k <
+ * 4); rows and columns past the end are zeros under scale 127.  A tile is one
+ * operand load of a wave, contiguous (row-major, 64-byte pieces of 16 rows, the
+ * products reach 3.0 TB/s where the tiles reach 4.7).
  * Limits of every call: 1 <= rows <= 2^30; cols a positive multiple of 32, at
  * most 2^20; fewer than 2^26 tiles.
  * ---------------------------------------------------------------------- */

@@ -10,28 +10,28 @@
 // one the features (many: x is read from memory once per workgroup and from LDS
 // after that).
 #include "wf_api_internal.h"
+#include "wf_lds_dma.h"
 #include "wf_lowbit.h"
 
 namespace wf {
 
 namespace {
 
-#ifdef NT
-#define LOADW(p) __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p))
-#else
-#define LOADW(p) (*reinterpret_cast<const u32x4 *>(p))
-#endif
-#ifndef WIDE_FROM
-#define WIDE_FROM 6
-#endif
 constexpr int kW4Waves = 8;
 constexpr int kW4Group = 32;             // inputs per scale
 constexpr int kW4Chunk = 128;            // inputs per tile: 16 bytes of codes per lane
 constexpr int kW4Tile = 1024 + 64;       // 16 features x 128 inputs: codes, then scales
 
-// Scale byte -> the float that the conversion multiplies by (255: NaN).
-__device__ __forceinline__ float w4_scale(unsigned s) {
-    return s == 255u ? __uint_as_float(0x7fc00000u) : scale_value(s);
+// Scale byte kk of a lane's dword -> the float that the conversion multiplies
+// by: its exponent field (255 is then an infinity, which the conversion, like the
+// format, takes for NaN).
+__device__ __forceinline__ float w4_scale(unsigned s, int kk) {
+    return __uint_as_float((kk < 3 ? s << (23 - 8 * kk) : s >> 1) & 0x7f800000u);
+}
+
+// A lane's 16 bytes of a tile, which no other workgroup reads.
+__device__ __forceinline__ u32x4 load_codes(const uint8_t *p) {
+    return __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p));
 }
 
 // Eight codes (one dword, low nibble first) times their scale as an MFMA
@@ -45,29 +45,29 @@ __device__ __forceinline__ bf16x8 w4_expand(uint32_t w, float s) {
     return bf16x8{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
 }
 
-// The sum of `n` waves' partial blocks, the residual, and the store.
-template <bool F32OUT>
-__device__ __forceinline__ void store_y(void *y, const uint16_t *res, size_t at, float z) {
+// y[at] = z (+ the residual), in y's type.
+__device__ __forceinline__ void store_y(void *y, const uint16_t *res, size_t at, float z,
+                                        bool f32_out) {
     if (res)
         z += bf16_to_f32(res[at]);
-    if constexpr (F32OUT)
+    if (f32_out)
         static_cast<float *>(y)[at] = z;
     else
         static_cast<uint16_t *>(y)[at] = f32_to_bf16(z);
 }
 
-// Input split: workgroup b owns FB blocks of 16 features and the whole input,
-// its 8 waves take interleaved 128-input chunks, U of them loaded at once, and
-// their sums meet in LDS in wave order.  NB 16-row blocks of x.  Lane (m16, c4)
-// holds, for chunk c, the 32 inputs 128c + 32*c4 .. +31 (one scale group) of
-// feature m16 of each block and of x row m16; MFMA kk takes the kk-th eight of
-// them on both sides.
-template <int NB, int FB, bool F32OUT>
+// Up to 16 rows, input split: workgroup b owns FB blocks of 16 features and the
+// whole input, its 8 waves take interleaved 128-input chunks, U of them loaded
+// at once and the next U on their way meanwhile, and their sums meet in LDS in
+// wave order.  MFMA kk of chunk c takes the scale group 128c + 32kk ..: lane (m16,
+// c4) its inputs 8*c4 .. +7 of feature m16 of each block and of x row m16, so four
+// lanes read 64 contiguous bytes of x.
+template <int FB>
 __global__ __launch_bounds__(kW4Waves * kWave) void linear_w4(
     const uint16_t *__restrict__ x, const uint8_t *__restrict__ w, const uint16_t *res, void *y,
-    int rows, int n_out, int k_in) {
-    constexpr int U = FB * NB == 1 ? 4 : FB * NB <= 4 ? 2 : 1;
-    __shared__ float zs[kW4Waves][16][16 * NB + 1];
+    int rows, int n_out, int k_in, bool f32_out) {
+    constexpr int U = FB == 1 ? 4 : FB <= 4 ? 2 : 1;
+    __shared__ float zs[kW4Waves][16][17];
     const int f0 = 16 * FB * blockIdx.x;
     const int wave = wave_id();
     const int lane = threadIdx.x % kWave;
@@ -81,20 +81,15 @@ __global__ __launch_bounds__(kW4Waves * kWave) void linear_w4(
     for (int fb = 0; fb < FB; ++fb)
         wp[fb] = w + (size_t)min(FB * (int)blockIdx.x + fb, (n_out + 15) / 16 - 1) * n_c * kW4Tile;
     // rows past the end read the last one; they are not stored
-    const uint16_t *xp[NB];
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-        xp[nb] = x + (size_t)min(16 * nb + m16, rows - 1) * k_in;
-    f32x4 acc[FB][NB];
+    const uint16_t *xp = x + (size_t)min(m16, rows - 1) * k_in + c4 * 8;
+    f32x4 acc[FB];
 #pragma unroll
     for (int fb = 0; fb < FB; ++fb)
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-            acc[fb][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
+        acc[fb] = f32x4{0.f, 0.f, 0.f, 0.f};
     struct Batch {
         u32x4 w[U][FB];
         unsigned s[U][FB];
-        bf16x8 x[U][NB][4];
+        bf16x8 x[U][4];
     };
     auto load = [&](Batch &q, int cb) __attribute__((always_inline)) {
 #pragma unroll
@@ -103,16 +98,13 @@ __global__ __launch_bounds__(kW4Waves * kWave) void linear_w4(
 #pragma unroll
             for (int fb = 0; fb < FB; ++fb) {
                 const uint8_t *t = wp[fb] + (size_t)c * kW4Tile;
-                q.w[u][fb] = LOADW(t + lane * 16);
-                q.s[u][fb] = t[1024 + lane];
+                q.w[u][fb] = load_codes(t + lane * 16);
+                q.s[u][fb] = reinterpret_cast<const uint32_t *>(t + 1024)[m16];
             }
             // (inputs past the end: the row's last ones, against zero codes)
-            const int g = min(4 * c + c4, last_g);
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-                for (int kk = 0; kk < 4; ++kk)
-                    q.x[u][nb][kk] = load_bf16x8(xp[nb] + g * kW4Group + 8 * kk);
+            for (int kk = 0; kk < 4; ++kk)
+                q.x[u][kk] = load_bf16x8(xp + min(4 * c + kk, last_g) * kW4Group);
         }
     };
     auto multiply = [&](const Batch &q, int cb) __attribute__((always_inline)) {
@@ -122,18 +114,13 @@ __global__ __launch_bounds__(kW4Waves * kWave) void linear_w4(
                 break;
 #pragma unroll
             for (int fb = 0; fb < FB; ++fb) {
-                const float sf = w4_scale(q.s[u][fb]);
 #pragma unroll
-                for (int kk = 0; kk < 4; ++kk) {
-                    const bf16x8 wo = w4_expand(q.w[u][fb][kk], sf);
-#pragma unroll
-                    for (int nb = 0; nb < NB; ++nb)
-                        acc[fb][nb] = mfma16x16x32(wo, q.x[u][nb][kk], acc[fb][nb]);
-                }
+                for (int kk = 0; kk < 4; ++kk)
+                    acc[fb] = mfma16x16x32(w4_expand(q.w[u][fb][kk], w4_scale(q.s[u][fb], kk)),
+                                           q.x[u][kk], acc[fb]);
             }
         }
     };
-    // the next batch is on its way while one is multiplied
     constexpr int STEP = kW4Waves * U;
     Batch even, odd;
     load(even, wave);
@@ -151,47 +138,55 @@ __global__ __launch_bounds__(kW4Waves * kWave) void linear_w4(
         if (fb)
             __syncthreads();
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                zs[wave][4 * c4 + i][16 * nb + m16] = acc[fb][nb][i];
+        for (int i = 0; i < 4; ++i)
+            zs[wave][4 * c4 + i][m16] = acc[fb][i];
         __syncthreads();
-        for (int idx = threadIdx.x; idx < 16 * rows; idx += kW4Waves * kWave) {
-            const int u = idx % 16, r = idx / 16, f = f0 + 16 * fb + u;
-            if (f >= n_out)
-                continue;
+        const int u = threadIdx.x % 16, r = threadIdx.x / 16, f = f0 + 16 * fb + u;
+        if (r < rows && f < n_out) {                 // 512 threads: r up to 31
             float z = zs[0][u][r];
 #pragma unroll
-            for (int w = 1; w < kW4Waves; ++w)
-                z += zs[w][u][r];
-            store_y<F32OUT>(y, res, (size_t)r * n_out + f, z);
+            for (int ww = 1; ww < kW4Waves; ++ww)
+                z += zs[ww][u][r];
+            store_y(y, res, (size_t)r * n_out + f, z, f32_out);
         }
     }
 }
 
-// Feature split: a workgroup's 8 waves own up to FB blocks of 16 features each,
-// all rows, and walk the input together in chunks of 256, whose x is staged in
-// LDS (a wave reads it once for all its blocks) while the next chunk's codes and
-// x are on their way to registers.  Lanes and tiles as above.  The staged x is swizzled in 16-byte granules, g ^ (row & 7), so eight
-// rows' reads meet distinct banks.
-constexpr int kW4Wide = 256;
-
-template <int NB, int FB, bool F32OUT>
+// Feature split: the 8 waves of a workgroup are 8 / KW feature groups, each of
+// up to FB blocks of 16 features, of KW waves that share the input among them.
+// All walk the input (or slice blockIdx.y of it) together in chunks of KW tiles
+// of 128 inputs, one per wave, whose x, all rows, is staged in LDS, so a wave
+// reads it once for all its blocks; the next chunk's codes and x are on their way
+// to registers meanwhile.  KW > 1 is for few blocks: a wave of one block reads 4 KB of x per 1
+// KB of codes and 16 rows from LDS, so with 64 rows the waves ask it for more than
+// the 128 bytes a cycle it has; a quarter of the input and four times the blocks
+// ask for a quarter.  Lanes and tiles as above.  The staged x is swizzled in 16-
+// byte granules, g ^ (row & 7), so eight rows' reads meet distinct banks.  With
+// several slices each stores its fp32 sums, part[slice][row][16 * blocks], for
+// w4_sum.
+template <int NB, int FB, int KW>
 __global__ __launch_bounds__(kW4Waves * kWave) void linear_w4_wide(
     const uint16_t *__restrict__ x, const uint8_t *__restrict__ w, const uint16_t *res, void *y,
-    int rows, int n_out, int k_in) {
-    constexpr int GRAN = kW4Wide / 8;                // 16-byte granules of a row's chunk
-    __shared__ u32x4 xs[2][16 * NB * GRAN];
+    int rows, int n_out, int k_in, bool f32_out, float *part) {
+    constexpr int GRAN = 16 * KW;                    // 16-byte granules of a row's chunk
+    constexpr int XG = 16 * NB * GRAN;               // ... of the chunk, XT of them a thread's
+    constexpr int XT = (XG + kW4Waves * kWave - 1) / (kW4Waves * kWave);
+    constexpr int FG = kW4Waves / KW;
+    __shared__ u32x4 xs[2][XG];
+    static_assert(KW == 1 || sizeof(xs) >= FG * 1024 * NB, "the waves' sums meet in the chunks' place");
     const int wave = wave_id();
+    const int kw = wave % KW, fg = wave / KW;
     const int lane = threadIdx.x % kWave;
     const int m16 = lane & 15;
     const int c4 = lane >> 4;
-    const int n_t = (k_in + kW4Chunk - 1) / kW4Chunk, n_c = (n_t + 1) / 2;
-    // blocks dealt out evenly over all waves of the launch
+    const int n_t = (k_in + kW4Chunk - 1) / kW4Chunk, n_c = (n_t + KW - 1) / KW;
+    const int c_first = (int)blockIdx.y * n_c / (int)gridDim.y;
+    const int c_end = ((int)blockIdx.y + 1) * n_c / (int)gridDim.y;
+    // blocks dealt out evenly over all feature groups of the launch
     const int blocks = (n_out + 15) / 16;
-    const int waves = gridDim.x * kW4Waves, id = blockIdx.x * kW4Waves + wave;
-    const int b_first = (int)((long long)id * blocks / waves);
-    const int n_b = (int)((long long)(id + 1) * blocks / waves) - b_first;
+    const int groups = gridDim.x * FG, id = blockIdx.x * FG + fg;
+    const int b_first = (int)((long long)id * blocks / groups);
+    const int n_b = (int)((long long)(id + 1) * blocks / groups) - b_first;
 
     const uint8_t *wp[FB];
 #pragma unroll
@@ -204,84 +199,103 @@ __global__ __launch_bounds__(kW4Waves * kWave) void linear_w4_wide(
         for (int nb = 0; nb < NB; ++nb)
             acc[fb][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    struct Codes {
-        u32x4 w[FB][2];
-        unsigned s[FB][2];
+    struct Chunk {
+        u32x4 w[FB];
+        unsigned s[FB];
+        u32x4 x[XT];
     };
-    auto load_w = [&](Codes &c, int ch) __attribute__((always_inline)) {
+    Chunk ring[2];
+    // The chunk past the end is the last one again, never used: a branch around
+    // the loads would leave the compiler without a count of those in flight, and
+    // it would wait for all of them (2560 to 151936, one row: 41.8 us, 51.0 with
+    // the branch).  Of x a row past the end is the last row, a granule past the
+    // input's end the row's last, which meets zero codes.
+    auto load = [&](Chunk &q, int at) __attribute__((always_inline)) {
+        const int ch = min(at, c_end - 1);
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int fb = 0; fb < FB; ++fb) {
-                const uint8_t *t = wp[fb] + (size_t)min(2 * ch + h, n_t - 1) * kW4Tile;
-                c.w[fb][h] = LOADW(t + lane * 16);
-                c.s[fb][h] = t[1024 + lane];
-            }
-    };
-    // x of a chunk: NB granules per thread (row past the end: the last row; a
-    // granule past the input's end: the row's last, which meets zero codes)
-    u32x4 xr[NB];
-    auto load_x = [&](int ch) __attribute__((always_inline)) {
-#pragma unroll
-        for (int j = 0; j < NB; ++j) {
+        for (int j = 0; j < XT; ++j) {
             const int idx = threadIdx.x + j * kW4Waves * kWave;
             const int r = idx / GRAN, g = idx % GRAN;
             const int k = min(ch * GRAN + g, k_in / 8 - 1) * 8;
-            xr[j] = *reinterpret_cast<const u32x4 *>(x + (size_t)min(r, rows - 1) * k_in + k);
+            q.x[j] = *reinterpret_cast<const u32x4 *>(x + (size_t)min(r, rows - 1) * k_in + k);
+        }
+#pragma unroll
+        for (int fb = 0; fb < FB; ++fb) {
+            const uint8_t *t = wp[fb] + (size_t)min(KW * ch + kw, n_t - 1) * kW4Tile;
+            q.w[fb] = load_codes(t + lane * 16);
+            q.s[fb] = reinterpret_cast<const uint32_t *>(t + 1024)[m16];
         }
     };
-    auto stage_x = [&](int buf) __attribute__((always_inline)) {
+    auto stage_x = [&](const Chunk &q, int buf) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < NB; ++j) {
+        for (int j = 0; j < XT; ++j) {
             const int idx = threadIdx.x + j * kW4Waves * kWave;
             const int r = idx / GRAN, g = idx % GRAN;
-            xs[buf][r * GRAN + (g ^ (r & 7))] = xr[j];
+            if (XG % (kW4Waves * kWave) == 0 || idx < XG)
+                xs[buf][r * GRAN + (g ^ (r & 7))] = q.x[j];
         }
     };
     // every wave's LDS writes are done; loads in flight stay so
     auto barrier = [] { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
-
-    // One chunk: its codes are in `now`; the next one's go to `next`.
-    auto step = [&](const Codes &now, Codes &next, int ch) __attribute__((always_inline)) {
-        const int chn = min(ch + 1, n_c - 1);        // (the last chunk again: not used)
-        load_x(chn);
-        load_w(next, chn);
-        const u32x4 *xb = xs[ch & 1];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            if (2 * ch + h >= n_t)                   // uniform
-                break;
+    // One chunk, in ring[I] and LDS buffer I, while the next is loaded.
+    auto step = [&](auto it, int ch) __attribute__((always_inline)) {
+        constexpr int I = decltype(it)::value;
+        load(ring[1 - I], ch + 1);
+        const Chunk &now = ring[I];
+        const u32x4 *xb = xs[I];
+        if (KW * ch + kw < n_t) {                    // uniform
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk) {
                 bf16x8 xo[NB];
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
-                    const int r = 16 * nb + m16, g = 16 * h + 4 * c4 + kk;
+                    const int r = 16 * nb + m16, g = 16 * kw + 4 * kk + c4;
                     xo[nb] = __builtin_bit_cast(bf16x8, xb[r * GRAN + (g ^ (r & 7))]);
                 }
 #pragma unroll
                 for (int fb = 0; fb < FB; ++fb) {
-                    const bf16x8 wo = w4_expand(now.w[fb][h][kk], w4_scale(now.s[fb][h]));
+                    const bf16x8 wo = w4_expand(now.w[fb][kk], w4_scale(now.s[fb], kk));
 #pragma unroll
                     for (int nb = 0; nb < NB; ++nb)
                         acc[fb][nb] = mfma16x16x32(wo, xo[nb], acc[fb][nb]);
                 }
             }
         }
-        stage_x((ch + 1) & 1);
+        stage_x(ring[1 - I], 1 - I);
         barrier();
     };
-    Codes even, odd;
-    load_x(0);
-    load_w(even, 0);
-    stage_x(0);
+    load(ring[0], c_first);
+    stage_x(ring[0], 0);
     barrier();
-    for (int ch = 0; ch < n_c; ch += 2) {
-        step(even, odd, ch);
-        if (ch + 1 < n_c)
-            step(odd, even, ch + 1);
+    for (int ch = c_first; ch < c_end; ch += 2) {
+        step(ic<0>{}, ch);
+        if (ch + 1 < c_end)
+            step(ic<1>{}, ch + 1);
     }
     // lane (m16, c4) holds features 4*c4 .. +3 of row m16
+    if constexpr (KW > 1) {
+        // the sums of a feature group's waves, in wave order, block by block
+        f32x4 *meet = reinterpret_cast<f32x4 *>(xs) + fg * 64 * NB;
+#pragma unroll
+        for (int k = 1; k < KW; ++k)
+#pragma unroll
+            for (int fb = 0; fb < FB; ++fb) {
+                if (kw == k) {
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb)
+                        meet[64 * nb + lane] = acc[fb][nb];
+                }
+                __syncthreads();
+                if (kw == 0) {
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb)
+                        acc[fb][nb] += meet[64 * nb + lane];
+                }
+                __syncthreads();
+            }
+        if (kw != 0)
+            return;
+    }
 #pragma unroll
     for (int fb = 0; fb < FB; ++fb) {
         if (fb >= n_b)
@@ -291,12 +305,44 @@ __global__ __launch_bounds__(kW4Waves * kWave) void linear_w4_wide(
             const int r = 16 * nb + m16, f = 16 * (b_first + fb) + 4 * c4;
             if (r >= rows)
                 continue;
+            if (gridDim.y > 1) {
+                *reinterpret_cast<f32x4 *>(part + ((size_t)blockIdx.y * rows + r) * 16 * blocks +
+                                           f) = acc[fb][nb];
+                continue;
+            }
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 if (f + i < n_out)
-                    store_y<F32OUT>(y, res, (size_t)r * n_out + f + i, acc[fb][nb][i]);
+                    store_y(y, res, (size_t)r * n_out + f + i, acc[fb][nb][i], f32_out);
         }
     }
+}
+
+// y = the slices' sums in order (and the residual); 4 features per thread.
+constexpr int kW4MaxSlices = 8;
+
+__global__ __launch_bounds__(256) void w4_sum(const float *__restrict__ part, int slices,
+                                              const uint16_t *res, void *y, int rows, int n_out,
+                                              bool f32_out) {
+    const int quads = (n_out + 15) / 16 * 4;
+    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= (size_t)rows * quads)
+        return;
+    const int r = (int)(i / quads), f = (int)(i % quads) * 4;
+    f32x4 v[kW4MaxSlices];
+#pragma unroll
+    for (int k = 0; k < kW4MaxSlices; ++k)
+        if (k < slices)
+            v[k] = reinterpret_cast<const f32x4 *>(part)[((size_t)k * rows + r) * quads + f / 4];
+    f32x4 z = v[0];
+#pragma unroll
+    for (int k = 1; k < kW4MaxSlices; ++k)
+        if (k < slices)
+            z += v[k];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (f + j < n_out)
+            store_y(y, res, (size_t)r * n_out + f + j, z[j], f32_out);
 }
 
 // Nearest e2m1 code of |a| <= 6, ties to the even code.
@@ -345,27 +391,28 @@ __global__ __launch_bounds__(256) void w4_quantize(const uint16_t *__restrict__ 
     scales[i] = fine ? (uint8_t)(e + 127) : (uint8_t)255;
 }
 
-// Tile (block b, chunk c) of the packed weight: lane m16 + 16 * c4 of a wave
-// finds its 16 bytes of codes (feature 16b + m16, inputs 128c + 32*c4 .. +31) at
-// 16 * lane and their scale at 1024 + lane.  One wave per tile; features and
-// inputs past the end are zeros under scale 1.
+// Tile (block b, chunk c) of the packed weight: lane m + 16 q of a wave finds
+// its four dwords of codes at 16 * lane, dword kk the eight inputs 128c + 32kk +
+// 8q .. +7 of feature 16b + m, and the scales of the chunk's four groups, bytes
+// kk, at 1024 + 4m.  One wave per tile; features and inputs past the end are
+// zeros under scale 1.
 __global__ __launch_bounds__(kWave) void w4_pack(const uint8_t *__restrict__ codes,
                                                  const uint8_t *__restrict__ scales, int rows,
                                                  int groups, uint8_t *__restrict__ packed) {
-    const int lane = threadIdx.x, m16 = lane & 15, c4 = lane >> 4;
+    const int lane = threadIdx.x, m = lane & 15, q = lane >> 4;
     const int n_c = (groups + 3) / 4;
     const size_t tile = blockIdx.x;
-    const size_t f = tile / n_c * 16 + m16;
-    const int g = (int)(tile % n_c) * 4 + c4;
+    const size_t f = tile / n_c * 16 + m;
+    const int g0 = (int)(tile % n_c) * 4;
     u32x4 v = {0u, 0u, 0u, 0u};
-    uint8_t s = 127;
-    if (f < (size_t)rows && g < groups) {
-        v = reinterpret_cast<const u32x4 *>(codes)[f * groups + g];
-        s = scales[f * groups + g];
-    }
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk)
+        if (f < (size_t)rows && g0 + kk < groups)
+            v[kk] = reinterpret_cast<const uint32_t *>(codes)[(f * groups + g0 + kk) * 4 + q];
     uint8_t *t = packed + tile * kW4Tile;
     reinterpret_cast<u32x4 *>(t)[lane] = v;
-    t[1024 + lane] = s;
+    // (lane m + 16 q writes the scale of group q)
+    t[1024 + 4 * m + q] = f < (size_t)rows && g0 + q < groups ? scales[f * groups + g0 + q] : 127;
 }
 
 }  // namespace
@@ -383,50 +430,96 @@ wf_status_t launch_w4_pack(const void *codes, const uint8_t *scales, int rows, i
     return hipGetLastError() == hipSuccess ? WF_OK : WF_ERR_HIP;
 }
 
-size_t linear_w4_workspace_bytes(int rows, int n_out, int k_in) { return 0; }
+namespace {
+
+// How a product runs: fb blocks of 16 features per workgroup (input split) or
+// feature group (feature split, kw waves each), the launch's workgroups, and
+// slices of the input.
+struct W4Plan {
+    bool wide;
+    int fb, kw, groups, slices;
+};
+
+W4Plan plan_linear_w4(int rows, int n_out, int k_in) {
+    const int blocks = (n_out + 15) / 16;
+    W4Plan p{};
+    p.slices = 1;
+    // up to 16 rows and six blocks per CU: the input split, one workgroup per CU
+    // (4096 to 24576, 16 rows: 15.8 us, the feature split 19.6; 2560 to 151936:
+    // 110 and 51 us)
+    if (rows <= 16 && blocks <= 6 * 256) {
+        p.fb = blocks <= 4 * 256 ? (blocks + 255) / 256 : 6;
+        p.groups = (blocks + p.fb - 1) / p.fb;
+        return p;
+    }
+    // Of more rows the LDS reads of x bound a wave of few blocks: four waves to a
+    // feature group up to eight blocks per CU, two up to 20 (64 rows, 4096 to 24576:
+    // 33.5 us with one, 28.3 with two, 25.9 with four; 2560 to 40000: 30.3, 26.9 and
+    // 29.6).
+    p.wide = true;
+    p.kw = rows <= 16 ? 1 : blocks <= 8 * 256 ? 4 : blocks <= 20 * 256 ? 2 : 1;
+    const int fg = kW4Waves / p.kw;
+    // fewer than two blocks per CU: slices of at least two chunks, so a workgroup
+    // reads less of x (64 rows, 4096 to 4096: 13.6 us, 23.4 without)
+    const int chunks = (k_in + 128 * p.kw - 1) / (128 * p.kw);
+    if (blocks < 2 * 256)
+        p.slices = std::max(1, std::min({kW4MaxSlices, chunks / 2, 5 * fg * 256 / blocks}));
+    const int per = fg * (256 / p.slices);           // feature groups of one workgroup per CU
+    const int rounds = (blocks + 5 * per - 1) / (5 * per);
+    p.fb = (blocks + rounds * per - 1) / (rounds * per);
+    p.groups = std::min(rounds * (256 / p.slices), (blocks + fg - 1) / fg);
+    return p;
+}
+
+}  // namespace
+
+size_t linear_w4_workspace_bytes(int rows, int n_out, int k_in) {
+    const W4Plan p = plan_linear_w4(rows, n_out, k_in);
+    return p.slices == 1 ? 0
+                         : kCounterBytes + (size_t)p.slices * rows * ((n_out + 15) / 16 * 16) *
+                                               sizeof(float);
+}
 
 wf_status_t launch_linear_w4(const uint16_t *x, const uint8_t *w, const uint16_t *res,
                              bool f32_out, void *y, int rows, int n_out, int k_in,
                              void *workspace, hipStream_t stream) {
-    const int blocks = (n_out + 15) / 16;
+    const W4Plan p = plan_linear_w4(rows, n_out, k_in);
     const dim3 block(kW4Waves * kWave);
-    const int nb = (rows + 15) / 16;
-    if (blocks > WIDE_FROM * 256) {
-        const int per = kW4Waves * 256;              // waves of one workgroup per CU
-        const int rounds = (blocks + 5 * per - 1) / (5 * per);
-        const int fb = (blocks + rounds * per - 1) / (rounds * per);
-        const dim3 grid(rounds * 256);
-#define WF_W4(NBV, FBV)                                                                      \
-    if (nb == NBV && fb == FBV) {                                                            \
-        if (f32_out)                                                                         \
-            linear_w4_wide<NBV, FBV, true><<<grid, block, 0, stream>>>(                      \
-                x, w, res, y, rows, n_out, k_in);                                \
-        else                                                                                 \
-            linear_w4_wide<NBV, FBV, false><<<grid, block, 0, stream>>>(                     \
-                x, w, res, y, rows, n_out, k_in);                                \
-    } else
-#define WF_W4_ROW(NBV) WF_W4(NBV, 1) WF_W4(NBV, 2) WF_W4(NBV, 3) WF_W4(NBV, 4) WF_W4(NBV, 5)
-        WF_W4_ROW(1) WF_W4_ROW(2) WF_W4_ROW(3) WF_W4_ROW(4)
-        { return WF_ERR_UNSUPPORTED; }
-#undef WF_W4_ROW
+    if (!p.wide) {
+#define WF_W4(FBV)                                                                            \
+    if (p.fb == FBV)                                                                          \
+        linear_w4<FBV><<<p.groups, block, 0, stream>>>(x, w, res, y, rows, n_out, k_in,       \
+                                                       f32_out);                              \
+    else
+        WF_W4(1) WF_W4(2) WF_W4(3) WF_W4(4) WF_W4(6)
+        return WF_ERR_UNSUPPORTED;
 #undef WF_W4
         return hipGetLastError() == hipSuccess ? WF_OK : WF_ERR_HIP;
     }
-    // rounds of one workgroup per CU, and as few blocks each as that takes
-    const int fb = (blocks + 255) / 256 <= 4 ? (blocks + 255) / 256 : 6;
-    const dim3 grid((blocks + fb - 1) / fb);
-#define WF_W4(NBV, FBV)                                                                      \
-    if (nb == NBV && fb == FBV) {                                                            \
-        if (f32_out)                                                                         \
-            linear_w4<NBV, FBV, true><<<grid, block, 0, stream>>>(x, w, res, y, rows, n_out, k_in); \
-        else                                                                                 \
-            linear_w4<NBV, FBV, false><<<grid, block, 0, stream>>>(x, w, res, y, rows, n_out, k_in); \
-    } else
-#define WF_W4_ROW(NBV) WF_W4(NBV, 1) WF_W4(NBV, 2) WF_W4(NBV, 3) WF_W4(NBV, 4) WF_W4(NBV, 6)
-    WF_W4_ROW(1) WF_W4_ROW(2) WF_W4_ROW(3) WF_W4_ROW(4)
-    { return WF_ERR_UNSUPPORTED; }
+    float *part = p.slices > 1 ? reinterpret_cast<float *>(static_cast<char *>(workspace) +
+                                                           kCounterBytes)
+                               : nullptr;
+    const int nb = (rows + 15) / 16;
+    const dim3 grid(p.groups, p.slices);
+#define WF_W4(NBV, FBV, KWV)                                                                  \
+    if (nb == NBV && p.fb == FBV && p.kw == KWV)                                              \
+        linear_w4_wide<NBV, FBV, KWV><<<grid, block, 0, stream>>>(x, w, res, y, rows, n_out,  \
+                                                                  k_in, f32_out, part);       \
+    else
+#define WF_W4_ROW(NBV, KWV)                                                                   \
+    WF_W4(NBV, 1, KWV) WF_W4(NBV, 2, KWV) WF_W4(NBV, 3, KWV) WF_W4(NBV, 4, KWV)               \
+    WF_W4(NBV, 5, KWV)
+    WF_W4_ROW(1, 1) WF_W4_ROW(2, 1) WF_W4_ROW(3, 1) WF_W4_ROW(4, 1)
+    WF_W4_ROW(2, 2) WF_W4_ROW(3, 2) WF_W4_ROW(4, 2)
+    WF_W4_ROW(2, 4) WF_W4_ROW(3, 4) WF_W4_ROW(4, 4)
+    return WF_ERR_UNSUPPORTED;
 #undef WF_W4_ROW
 #undef WF_W4
+    if (p.slices > 1) {
+        const size_t quads = (size_t)rows * ((n_out + 15) / 16 * 4);
+        const unsigned wg = (unsigned)((quads + 255) / 256);
+        w4_sum<<<wg, 256, 0, stream>>>(part, p.slices, res, y, rows, n_out, f32_out);
+    }
     return hipGetLastError() == hipSuccess ? WF_OK : WF_ERR_HIP;
 }
 

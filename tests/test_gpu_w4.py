@@ -54,12 +54,13 @@ def test_pack(rows, cols):
     got = wf.W4Weight(codes.to(DEV), scales.to(DEV)).packed
     torch.cuda.synchronize()
     nb, nc = (rows + 15) // 16, (cols + 127) // 128
-    c = np.zeros((nb * 16, nc * 4, 16), np.uint8)
-    c[:rows, :cols // 32] = codes.numpy().reshape(rows, cols // 32, 16)
+    c = np.zeros((nb * 16, nc * 64), np.uint8)
+    c[:rows, :cols // 2] = codes.numpy()
     s = np.full((nb * 16, nc * 4), 127, np.uint8)
     s[:rows, :cols // 32] = scales.numpy()
-    c = c.reshape(nb, 16, nc, 4, 16).transpose(0, 2, 3, 1, 4).reshape(nb, nc, 1024)
-    s = s.reshape(nb, 16, nc, 4).transpose(0, 2, 3, 1).reshape(nb, nc, 64)
+    # [block][row][chunk][group][quarter][4 bytes] -> a lane's quarter of each group
+    c = c.reshape(nb, 16, nc, 4, 4, 4).transpose(0, 2, 4, 1, 3, 5).reshape(nb, nc, 1024)
+    s = s.reshape(nb, 16, nc, 4).transpose(0, 2, 1, 3).reshape(nb, nc, 64)
     np.testing.assert_array_equal(got.cpu().numpy(), np.concatenate([c, s], 2).ravel())
 
 
