@@ -7,6 +7,7 @@ and raises WfError on a non-OK status.  All computation runs in the HIP
 kernels of libwf.so; there is no fallback path.  If the library has not been
 built, importing this package raises ImportError.
 """
+import contextlib
 import ctypes
 import operator
 import os
@@ -289,16 +290,36 @@ def _stream(stream):
     return stream.cuda_stream if stream is not None else _raw_stream(_device())
 
 
-def _stream_at(t, stream):
-    """The stream of a call whose first tensor is t: without one given, the
-    current stream, which has to be one of t's device."""
-    if stream is not None:
-        return stream.cuda_stream
+def _current():
+    """The current device's index, and its current stream as a raw handle."""
     dev = _device()
-    at = getattr(t.device, "index", None)
-    if dev is not None and at is not None and at != dev:
-        raise ValueError("tensors must be on the current device")
-    return _raw_stream(dev)
+    if dev is None:
+        dev = torch.cuda.current_device()
+    return dev, _raw_stream(dev)
+
+
+def _at(stream):
+    """(device index, raw stream) of a low-bit call: its tensors lie on the
+    current device, the stream is the one given or that device's current one."""
+    dev, raw = _current()
+    return dev, raw if stream is None else stream.cuda_stream
+
+
+def _on(stream):
+    """Where a low-bit call allocates: on the stream that it launches on, so
+    that memory freed there before is not written too early."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+def _ptr(t, dev, name):
+    """Pointer of a dense tensor of device `dev` (None: null)."""
+    if t is None:
+        return None
+    if t.get_device() != dev:
+        raise ValueError(f"{name} must be a tensor on the current device")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
 
 
 def _check(status, what):
@@ -662,14 +683,18 @@ class Kv8Cache:
                 tuple(k_scale.shape) != lead + (b,) or tuple(v_scale.shape) != lead + (b,):
             raise ValueError("cache shapes do not match each other and cap")
         for t in (k, v, k_scale, v_scale):
-            if t.element_size() != 1 or t.device != k.device:
-                raise ValueError("cache tensors hold bytes, on one device")
+            if t.element_size() != 1:
+                raise ValueError("cache tensors hold bytes")
+        dev = k.get_device()
+        if dev < 0:
+            raise ValueError("the cache must be device memory")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.n_layers = lead[0] if len(lead) == 2 else None
         self.n_kv_heads, self.cap, self.head_dim, self.device = lead[-1], cap, dh, k.device
-        self.struct = Kv8CacheStruct(_dev(k, "k"), _dev(v, "v"), _dev(k_scale, "k_scale"),
-                                     _dev(v_scale, "v_scale"), lead[-1], cap, dh)
-        self.ref = ctypes.byref(self.struct)
+        self.struct = Kv8CacheStruct(_ptr(k, dev, "k"), _ptr(v, dev, "v"),
+                                     _ptr(k_scale, dev, "k_scale"),
+                                     _ptr(v_scale, dev, "v_scale"), lead[-1], cap, dh)
+        self.ref, self.dev = ctypes.byref(self.struct), dev
 
     def layer(self, l):
         if self.n_layers is None:
@@ -689,9 +714,11 @@ def alloc_kv8_cache(n_kv_heads, cap, head_dim, device, n_layers=None) -> Kv8Cach
     return Kv8Cache(*z, cap)
 
 
-def _one_layer(cache):
+def _one_layer(cache, dev):
     if cache.n_layers is not None:
         raise ValueError("the call takes one layer of the cache: cache.layer(l)")
+    if cache.dev != dev:
+        raise ValueError("the cache must be on the current device")
     return cache.ref
 
 
@@ -699,22 +726,25 @@ def wf_kv8_append(k, v, cache, start_pos, stream=None):
     """k, v [n][Hkv][D] (bf16 or fp32) into cache rows start_pos .. of every
     head.  The last dimension is dense; the others may be strided (alike for
     k and v, in multiples of 16 bytes), as in a transposed [Hkv][n][D]."""
-    n, hkv, dh = k.shape
-    if v.shape != k.shape or v.dtype != k.dtype or hkv != cache.n_kv_heads or \
+    dev, raw = _at(stream)
+    shape = k.shape
+    n, hkv, dh = shape
+    code = _dtype_code(k)
+    if v.shape != shape or v.dtype != k.dtype or hkv != cache.n_kv_heads or \
             dh != cache.head_dim:
         raise ValueError("k and v must match each other and the cache")
     ks, vs = k.stride(), v.stride()
-    if n == 0:
-        ks = vs = (0, 0, 1)
-    # (the stride of a dimension of one entry says nothing)
-    ks = (ks[0] if n > 1 else 0, ks[1] if hkv > 1 else 0, ks[2])
-    vs = (vs[0] if n > 1 else 0, vs[1] if hkv > 1 else 0, vs[2])
+    # (the stride of a dimension of one entry, or of nothing, says nothing)
+    if n <= 1 or hkv == 1:
+        live = (n > 1, hkv > 1 and n > 0, n > 0)
+        ks = tuple(s if on else i // 2 for i, (s, on) in enumerate(zip(ks, live)))
+        vs = tuple(s if on else i // 2 for i, (s, on) in enumerate(zip(vs, live)))
     if ks != vs or ks[2] != 1:
         raise ValueError("k and v must have the same strides, the last one 1")
-    if not (k.is_cuda and v.is_cuda):
-        raise ValueError("k and v must be device tensors")
-    _check(lib.wf_kv8_append(_dtype_code(k), _one_layer(cache), k.data_ptr(), v.data_ptr(), n,
-                             start_pos, ks[0], ks[1], _stream_at(k, stream)), "wf_kv8_append")
+    if k.get_device() != dev or v.get_device() != dev:
+        raise ValueError("k and v must be tensors on the current device")
+    _check(lib.wf_kv8_append(code, _one_layer(cache, dev), k.data_ptr(), v.data_ptr(), n,
+                             start_pos, ks[0], ks[1], raw), "wf_kv8_append")
 
 
 def wf_kv8_only_prefill_workspace_bytes(dtype, n_tok, d_in, n_kv_heads, head_dim) -> int:
@@ -726,19 +756,23 @@ def wf_kv8_only_prefill_workspace_bytes(dtype, n_tok, d_in, n_kv_heads, head_dim
 def wf_kv8_only_prefill(x, w_k, w_v, cache, start_pos, rope_base, workspace=None, stream=None):
     """wf_kv_only_prefill into an 8-bit cache: x [n][d_in]; w_k, w_v
     [Hkv*D][d_in]."""
+    dev, raw = _at(stream)
     n_tok, d_in = x.shape
     hkv, dh = cache.n_kv_heads, cache.head_dim
     for w in (w_k, w_v):
-        if tuple(w.shape) != (hkv * dh, d_in):
-            raise ValueError("weights must be [n_kv_heads * head_dim][d_in]")
+        if tuple(w.shape) != (hkv * dh, d_in) or w.dtype != x.dtype:
+            raise ValueError("weights must be [n_kv_heads * head_dim][d_in], of x's type")
     code = _weight_code(x, w_k, w_v)
     if workspace is None:
-        workspace = alloc_workspace(wf_kv8_only_prefill_workspace_bytes(
-            code, n_tok, d_in, hkv, dh), x.device)
-    _check(lib.wf_kv8_only_prefill(code, _dev(x, "x"), _dev(w_k, "w_k"), _dev(w_v, "w_v"),
-                                   _one_layer(cache), n_tok, start_pos, d_in,
-                                   float(rope_base), _dev(workspace, "workspace"),
-                                   workspace.numel(), _stream_at(x, stream)), "wf_kv8_only_prefill")
+        with _on(stream):
+            workspace = alloc_workspace(wf_kv8_only_prefill_workspace_bytes(
+                code, n_tok, d_in, hkv, dh), x.device)
+    wk, wv = (w.data if isinstance(w, TiledWeight) else w for w in (w_k, w_v))
+    _check(lib.wf_kv8_only_prefill(code, _ptr(x, dev, "x"), _ptr(wk, dev, "w_k"),
+                                   _ptr(wv, dev, "w_v"), _one_layer(cache, dev), n_tok,
+                                   start_pos, d_in, float(rope_base),
+                                   _ptr(workspace, dev, "workspace"), workspace.numel(), raw),
+           "wf_kv8_only_prefill")
 
 
 def wf_kv8_verify_attn_workspace_bytes(dtype, gamma, ctx_len, n_q_heads, n_kv_heads, head_dim,
@@ -750,6 +784,7 @@ def wf_kv8_verify_attn_workspace_bytes(dtype, gamma, ctx_len, n_q_heads, n_kv_he
 
 
 def _kv8_attn(q, cache, out, ctx_len, tree_mask, softmax_scale, num_splits, workspace, stream):
+    dev, raw = _at(stream)
     shape = q.shape
     gamma, hq, dh = shape
     if dh != cache.head_dim or out.shape != shape or out.dtype != q.dtype:
@@ -758,18 +793,17 @@ def _kv8_attn(q, cache, out, ctx_len, tree_mask, softmax_scale, num_splits, work
     if softmax_scale is None:
         softmax_scale = dh ** -0.5
     if workspace is None:
-        workspace = alloc_workspace(wf_kv8_verify_attn_workspace_bytes(
-            code, gamma, ctx_len, hq, cache.n_kv_heads, dh, num_splits), q.device)
-    args = (gamma, ctx_len, hq, softmax_scale, num_splits, _dev(workspace, "workspace"),
-            workspace.numel(), _stream_at(q, stream))
+        with _on(stream):
+            workspace = alloc_workspace(wf_kv8_verify_attn_workspace_bytes(
+                code, gamma, ctx_len, hq, cache.n_kv_heads, dh, num_splits), q.device)
+    head = (code, _ptr(q, dev, "q"), _one_layer(cache, dev), _ptr(out, dev, "out"))
+    tail = (gamma, ctx_len, hq, softmax_scale, num_splits, _ptr(workspace, dev, "workspace"),
+            workspace.numel(), raw)
     if tree_mask is None:
-        st = lib.wf_kv8_verify_attn(code, _dev(q, "q"), _one_layer(cache), _dev(out, "out"),
-                                    *args)
-        _check(st, "wf_kv8_verify_attn")
+        _check(lib.wf_kv8_verify_attn(*head, *tail), "wf_kv8_verify_attn")
     else:
-        st = lib.wf_kv8_verify_attn_tree(code, _dev(q, "q"), _one_layer(cache),
-                                         _dev(out, "out"), _dev(tree_mask, "tree_mask"), *args)
-        _check(st, "wf_kv8_verify_attn_tree")
+        _check(lib.wf_kv8_verify_attn_tree(*head, _ptr(tree_mask, dev, "tree_mask"), *tail),
+               "wf_kv8_verify_attn_tree")
     return out
 
 
@@ -793,14 +827,17 @@ def wf_kv8_compact_path(cache, accept, path, ctx_len, stream=None):
     """wf_kv_compact_path for an 8-bit cache (one layer or the whole stack):
     accept (n at [0]) and path [gamma] int32 device tensors, as written by
     wf_lmhead_accept_tree."""
+    dev, raw = _at(stream)
     layers, codes, scales = 1, 0, 0
     if cache.n_layers is not None:
         layers, codes, scales = cache.n_layers, cache.k.stride(0), cache.k_scale.stride(0)
     if accept.dtype != torch.int32 or path.dtype != torch.int32:
         raise TypeError("accept and path are int32")
-    _check(lib.wf_kv8_compact_path(cache.ref, _dev(accept, "accept"), _dev(path, "path"),
-                                   path.numel(), ctx_len, layers, codes, scales,
-                                   _stream_at(path, stream)), "wf_kv8_compact_path")
+    if cache.dev != dev:
+        raise ValueError("the cache must be on the current device")
+    _check(lib.wf_kv8_compact_path(cache.ref, _ptr(accept, dev, "accept"),
+                                   _ptr(path, dev, "path"), path.numel(), ctx_len, layers,
+                                   codes, scales, raw), "wf_kv8_compact_path")
 
 
 class W4Weight:
@@ -814,15 +851,16 @@ class W4Weight:
         rows, half = codes.shape
         if half % 16 or tuple(scales.shape) != (rows, half // 16):
             raise ValueError("codes [rows][cols / 2] and scales [rows][cols / 32] do not match")
-        if codes.element_size() != 1 or scales.element_size() != 1 or \
-                codes.device != scales.device:
-            raise ValueError("codes and scales hold bytes, on one device")
-        self.shape, self.device = (rows, 2 * half), codes.device
+        if codes.element_size() != 1 or scales.element_size() != 1:
+            raise ValueError("codes and scales hold bytes")
+        dev, raw = _at(stream)
         n = int(lib.wf_w4_packed_bytes(rows, 2 * half))
-        self.packed = torch.empty(n, dtype=torch.uint8, device=codes.device)
-        _check(lib.wf_w4_pack(_dev(codes, "codes"), _dev(scales, "scales"), rows, 2 * half,
-                              _dev(self.packed, "packed"), n, _stream_at(codes, stream)),
-               "wf_w4_pack")
+        self.shape, self.device, self.dev = (rows, 2 * half), codes.device, dev
+        src = _ptr(codes, dev, "codes"), _ptr(scales, dev, "scales")
+        with _on(stream):
+            self.packed = torch.empty(n, dtype=torch.uint8, device=codes.device)
+        self.ptr = self.packed.data_ptr()
+        _check(lib.wf_w4_pack(*src, rows, 2 * half, self.ptr, n, raw), "wf_w4_pack")
 
 
 def wf_w4_quantize(w, stream=None):
@@ -830,13 +868,16 @@ def wf_w4_quantize(w, stream=None):
     == 0; W4Weight(codes, scales) packs it for the products."""
     if w.dtype != torch.bfloat16:
         raise TypeError("4-bit weights are made from bf16")
+    dev, raw = _at(stream)
     rows, cols = w.shape
     if cols % 32:
         raise ValueError("the columns of a 4-bit weight come in groups of 32")
-    codes = torch.empty((rows, cols // 2), dtype=torch.uint8, device=w.device)
-    scales = torch.empty((rows, cols // 32), dtype=torch.uint8, device=w.device)
-    _check(lib.wf_w4_quantize(_dev(w, "w"), rows, cols, _dev(codes, "codes"),
-                              _dev(scales, "scales"), _stream_at(w, stream)), "wf_w4_quantize")
+    src = _ptr(w, dev, "w")
+    with _on(stream):
+        codes = torch.empty((rows, cols // 2), dtype=torch.uint8, device=w.device)
+        scales = torch.empty((rows, cols // 32), dtype=torch.uint8, device=w.device)
+    _check(lib.wf_w4_quantize(src, rows, cols, codes.data_ptr(), scales.data_ptr(), raw),
+           "wf_w4_quantize")
     return codes, scales
 
 
@@ -847,20 +888,24 @@ def wf_linear_w4_workspace_bytes(n_rows, n_out, k_in) -> int:
 def wf_linear_w4(x, weight, out, residual=None, workspace=None, stream=None):
     """out = x W^T (+ residual): x [n][k_in] bf16 (n <= 64), weight a W4Weight
     [n_out][k_in], residual [n][n_out] bf16, out [n][n_out] bf16 or fp32."""
+    dev, raw = _at(stream)
     n, k_in = x.shape
     n_out, cols = weight.shape
-    if x.dtype != torch.bfloat16 or (residual is not None and residual.dtype != torch.bfloat16):
-        raise TypeError("x and residual are bf16")
-    if cols != k_in or tuple(out.shape) != (n, n_out) or \
-            (residual is not None and residual.shape != out.shape):
-        raise ValueError("x, weight, residual and out do not match")
+    shape = out.shape
+    if cols != k_in or shape != (n, n_out) or weight.dev != dev:
+        raise ValueError("x, weight and out do not match")
+    if x.dtype != torch.bfloat16:
+        raise TypeError("x is bf16")
+    if residual is not None and (residual.shape != shape or residual.dtype != torch.bfloat16):
+        raise ValueError("residual must be bf16, in out's shape")
     if workspace is None:
         need = wf_linear_w4_workspace_bytes(n, n_out, k_in)
-        workspace = alloc_workspace(need, x.device) if need else None
-    st = lib.wf_linear_w4(_dev(x, "x"), _dev(weight.packed, "packed"),
-                          _dev(residual, "residual"), _dtype_code(out), _dev(out, "out"), n, n_out, k_in,
-                          _dev(workspace, "workspace"),
-                          workspace.numel() if workspace is not None else 0, _stream_at(x, stream))
+        with _on(stream):
+            workspace = alloc_workspace(need, x.device) if need else None
+    st = lib.wf_linear_w4(_ptr(x, dev, "x"), weight.ptr, _ptr(residual, dev, "residual"),
+                          _dtype_code(out), _ptr(out, dev, "out"), n, n_out, k_in,
+                          _ptr(workspace, dev, "workspace"),
+                          0 if workspace is None else workspace.numel(), raw)
     _check(st, "wf_linear_w4")
     return out
 

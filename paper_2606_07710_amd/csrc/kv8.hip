@@ -14,9 +14,10 @@ namespace wf {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256;            // of a compaction workgroup
 
-// Largest of the workgroup's values, in every thread.
+// Largest of the values of a workgroup of N threads, in every thread.
+template <int N>
 __device__ __forceinline__ float group_max(float v, float *part) {
     v = wave_max(v);
     if (threadIdx.x % kWave == 0)
@@ -24,7 +25,7 @@ __device__ __forceinline__ float group_max(float v, float *part) {
     __syncthreads();
     float m = part[0];
 #pragma unroll
-    for (int w = 1; w < kThreads / kWave; ++w)
+    for (int w = 1; w < N / kWave; ++w)
         m = fmaxf(m, part[w]);
     return m;
 }
@@ -47,108 +48,109 @@ struct AppendParams {
     int start, end, n_blocks, first_block;
 };
 
-// One block of one head, K or V.  The block's valid rows are staged as fp32:
-// new rows from the source, rows below `start` decoded from their codes.
+// One block of one head, K or V.  A thread owns 4 rows x 4 dims: it takes new
+// rows from the source and rows below `start` from their codes, and encodes
+// its 16 values as the four words that they are in the block (4 dims of a row
+// in K, 4 rows of a dim in V).  Everything is loaded before anything is used,
+// one trip to memory; V's words are put in order in LDS and leave as 16 bytes.
 template <int D, bool BF16>
-__global__ __launch_bounds__(kThreads) void kv8_append(AppendParams a) {
-    constexpr int LD = D + 1;            // columns of 32 rows in distinct banks
-    __shared__ float val[kKv8Block * LD];
-    __shared__ float part[kThreads / kWave];
+__global__ __launch_bounds__(2 * D) void kv8_append(AppendParams a) {
+    __shared__ float part[2 * D / kWave];
+    // a V block in pieces of 16 rows of a dim, one more after every four dims:
+    // the words of a wave fall into 32 banks, not one
+    __shared__ u32x4 turned[D / 4 * 9];
     const int b = a.first_block + blockIdx.x;
     const int g = blockIdx.y, kind = blockIdx.z;
     const int r0 = b * kKv8Block;
     const int first = max(a.start - r0, 0);              // first new row of the block
     const int last = min(a.end - r0, kKv8Block);         // end of its valid rows
     const size_t at = (size_t)g * a.n_blocks + b;
-    char *codes = a.codes[kind] + at * (kKv8Block * D);
+    uint32_t *codes = reinterpret_cast<uint32_t *>(a.codes[kind] + at * (kKv8Block * D));
     uint8_t *scale = a.scale[kind] + at;
-
-    float m = 0.f;
-    // new rows, 8 elements per thread
-    for (int c = threadIdx.x; c < (last - first) * (D / 8); c += kThreads) {
-        const int r = first + c / (D / 8), d = c % (D / 8) * 8;
-        const size_t off = (size_t)(r0 + r - a.start) * a.tok_stride + g * a.head_stride + d;
-        float f[8];
+    const int j = threadIdx.x % (D / 4), i0 = threadIdx.x / (D / 4) * 4;
+    auto word = [&](int u) {             // where the thread's word u lies in the block
+        return kind ? (4 * j + u) * (kKv8Block / 4) + i0 / 4 : (i0 + u) * (D / 4) + j;
+    };
+    const bool partly = first > 0 || last < kKv8Block;
+    uint32_t old[4] = {};
+    unsigned sb = 127;
+    if (partly) {
+        sb = *scale;
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            old[u] = codes[word(u)];
+    }
+    float f[4][4];                       // [row][dim]
+    using Raw = std::conditional_t<BF16, u32x2, f32x4>;
+    Raw raw[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        raw[u] = Raw{};
+        if (i0 + u >= first && i0 + u < last) {
+            const size_t off = (size_t)(r0 + i0 + u - a.start) * a.tok_stride +
+                               g * a.head_stride + 4 * j;
+            raw[u] = *reinterpret_cast<const Raw *>(
+                static_cast<const char *>(a.src[kind]) + off * (BF16 ? 2 : 4));
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
         if constexpr (BF16) {
-            const u32x4 v = *reinterpret_cast<const u32x4 *>(
-                static_cast<const uint16_t *>(a.src[kind]) + off);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                f[2 * i] = __uint_as_float(v[i] << 16);
-                f[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
-            }
+            f[u][0] = __uint_as_float(raw[u][0] << 16);
+            f[u][1] = __uint_as_float(raw[u][0] & 0xffff0000u);
+            f[u][2] = __uint_as_float(raw[u][1] << 16);
+            f[u][3] = __uint_as_float(raw[u][1] & 0xffff0000u);
         } else {
-            const f32x4 *p = reinterpret_cast<const f32x4 *>(
-                static_cast<const float *>(a.src[kind]) + off);
-            const f32x4 lo = p[0], hi = p[1];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                f[i] = lo[i];
-                f[4 + i] = hi[i];
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            m = fmaxf(m, finite_abs(f[i]));
-            val[r * LD + d + i] = f[i];
+            for (int d = 0; d < 4; ++d)
+                f[u][d] = raw[u][d];
         }
     }
-    // the open block's earlier rows, 4 codes per thread: 4 dims of a row (K),
-    // 4 rows of a dim (V)
     if (first > 0) {
-        const float s = scale_value(*scale);
-        for (int c = threadIdx.x; c < kKv8Block * D / 4; c += kThreads) {
-            const int hi = c / (kind ? kKv8Block / 4 : D / 4);
-            const int lo = c % (kind ? kKv8Block / 4 : D / 4) * 4;
-            if ((kind ? lo : hi) >= first)
-                continue;
-            float f[4];
-            e4m3x4_to_f32(reinterpret_cast<const uint32_t *>(codes)[c], f);
+        const float s = scale_value((uint8_t)sb);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int r = kind ? lo + i : hi, d = kind ? hi : lo + i;
-                if (r < first) {
-                    const float x = f[i] * s;
-                    m = fmaxf(m, finite_abs(x));
-                    val[r * LD + d] = x;
-                }
+        for (int u = 0; u < 4; ++u) {
+            float x[4];
+            e4m3x4_to_f32(old[u], x);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                if (kind && i0 + w < first)
+                    f[w][u] = x[w] * s;
+                if (!kind && i0 + u < first)
+                    f[u][w] = x[w] * s;
             }
         }
     }
-    m = group_max(m, part);              // (its barrier publishes the rows too)
+    float m = 0.f;
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+            m = fmaxf(m, finite_abs(f[u][d]));
+    m = group_max<2 * D>(m, part);
     const int e = e4m3_exponent(m);
     const float inv = __uint_as_float((unsigned)(127 - e) << 23);
-    for (int c = threadIdx.x; c < kKv8Block * D / 16; c += kThreads) {
-        float f[16];
-        u32x4 *dst = reinterpret_cast<u32x4 *>(codes) + c;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
         if (kind == 0) {
-            const int r = c / (D / 16), d = c % (D / 16) * 16;
-            if (r >= last)
-                continue;
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                f[i] = val[r * LD + d + i];
-            *dst = encode16(f, inv);
+            if (i0 + u < last)
+                codes[word(u)] = f32x4_to_e4m3(f[u][0] * inv, f[u][1] * inv, f[u][2] * inv,
+                                               f[u][3] * inv);
         } else {
-            const int d = c / 2, r = c % 2 * 16;
-            if (r >= last)
-                continue;
-            const bool whole = r + 16 <= last;
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                f[i] = whole || r + i < last ? val[(r + i) * LD + d] : 0.f;
-            u32x4 w = encode16(f, inv);
-            if (!whole) {
-                const u32x4 old = *dst;              // rows behind the last valid one
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int n = min(max(last - (r + 4 * i), 0), 4);
-                    const uint32_t mask = n == 4 ? ~0u : (1u << (8 * n)) - 1u;
-                    w[i] = (w[i] & mask) | (old[i] & ~mask);
-                }
-            }
-            *dst = w;
+            uint32_t w = f32x4_to_e4m3(f[0][u] * inv, f[1][u] * inv, f[2][u] * inv,
+                                       f[3][u] * inv);
+            // rows behind the last valid one keep their codes
+            const int n = min(max(last - i0, 0), 4);
+            const uint32_t mask = n == 4 ? ~0u : (1u << (8 * n)) - 1u;
+            reinterpret_cast<uint32_t *>(turned)[word(u) + 4 * j] =
+                (w & mask) | (old[u] & ~mask);
         }
+    }
+    if (kind) {
+        __syncthreads();
+        const int c = threadIdx.x;
+        if (c % 2 * 16 < last)
+            reinterpret_cast<u32x4 *>(codes)[c] = turned[c + c / 8];
     }
     if (threadIdx.x == 0)
         *scale = (uint8_t)(e + 127);
@@ -221,7 +223,7 @@ __global__ __launch_bounds__(kThreads) void kv8_compact(char *k, char *v, uint8_
                 m = fmaxf(m, finite_abs(f[u][i]));
             }
         }
-        m = group_max(m, part);
+        m = group_max<kThreads>(m, part);
         const int e = e4m3_exponent(m);
         const float inv = __uint_as_float((unsigned)(127 - e) << 23);
 #pragma unroll
@@ -271,13 +273,13 @@ wf_status_t launch_kv8_append(wf_dtype_t dt, const wf_kv8_cache_t &c, const void
     const int blocks = (start + n_tok - 1) / kKv8Block - a.first_block + 1;
     const dim3 grid(blocks, c.n_kv_heads, 2);
     if (c.head_dim == 128 && dt == WF_BF16)
-        kv8_append<128, true><<<grid, kThreads, 0, stream>>>(a);
+        kv8_append<128, true><<<grid, 2 * 128, 0, stream>>>(a);
     else if (c.head_dim == 128)
-        kv8_append<128, false><<<grid, kThreads, 0, stream>>>(a);
+        kv8_append<128, false><<<grid, 2 * 128, 0, stream>>>(a);
     else if (dt == WF_BF16)
-        kv8_append<64, true><<<grid, kThreads, 0, stream>>>(a);
+        kv8_append<64, true><<<grid, 2 * 64, 0, stream>>>(a);
     else
-        kv8_append<64, false><<<grid, kThreads, 0, stream>>>(a);
+        kv8_append<64, false><<<grid, 2 * 64, 0, stream>>>(a);
     return hipGetLastError() == hipSuccess ? WF_OK : WF_ERR_HIP;
 }
 

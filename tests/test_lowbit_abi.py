@@ -193,14 +193,17 @@ def test_packed_sizes():
 
 class Fake:
     """A stand-in for a device tensor whose pointer the C side refuses."""
-    is_cuda, device = True, "cuda"
+    device = "cuda"
 
-    def __init__(self, *shape, dtype=torch.bfloat16, stride=None, ptr=8):
-        self.shape, self.dtype, self.ptr = torch.Size(shape), dtype, ptr
+    def __init__(self, *shape, dtype=torch.bfloat16, stride=None, ptr=8, on=0):
+        self.shape, self.dtype, self.ptr, self.on = torch.Size(shape), dtype, ptr, on
         self.strides = stride or torch.empty(shape, device="meta").stride()
 
     def data_ptr(self):
         return self.ptr
+
+    def get_device(self):
+        return self.on
 
     def is_contiguous(self):
         return True
@@ -219,6 +222,11 @@ class FakeStream:
     cuda_stream = 0
 
 
+@pytest.fixture(autouse=True)
+def _device_zero(monkeypatch):
+    monkeypatch.setattr(wf, "_current", lambda: (0, 0))
+
+
 def _bytes(*shape, **kw):
     return Fake(*shape, dtype=torch.uint8, **kw)
 
@@ -231,9 +239,9 @@ def _kv8(hkv=2, cap=70, dh=64, layers=None, **kw):
     return wf.Kv8Cache(t["k"], t["v"], t["k_scale"], t["v_scale"], cap)
 
 
-def _w4():
+def _w4(dev=0):
     w = wf.W4Weight.__new__(wf.W4Weight)
-    w.packed, w.shape = _bytes(1088), (16, 64)
+    w.packed, w.shape, w.ptr, w.dev = _bytes(1088), (16, 64), 8, dev
     return w
 
 
@@ -272,6 +280,34 @@ def test_python_one_layer_calls_refuse_a_stack():
 def test_python_append_refuses(k, v):
     with pytest.raises(ValueError):
         wf.wf_kv8_append(k, v, _kv8(), 0, stream=FakeStream)
+
+
+def test_python_calls_refuse_other_devices():
+    """Every tensor lies on the current device, whatever stream is given."""
+    q, x, far = Fake(4, 8, 64), Fake(4, 64), dict(on=1)
+    ws, path = _bytes(64), Fake(4, dtype=torch.int32)
+    for call in (
+            lambda: wf.wf_kv8_verify_attn(Fake(4, 8, 64, **far), _kv8(), q, 5, workspace=ws),
+            lambda: wf.wf_kv8_verify_attn(q, _kv8(), Fake(4, 8, 64, **far), 5, workspace=ws),
+            lambda: wf.wf_kv8_verify_attn(q, _kv8(), q, 5, workspace=_bytes(64, on=-1)),
+            lambda: wf.wf_kv8_verify_attn(q, _far_cache(), q, 5, workspace=ws,
+                                          stream=FakeStream),
+            lambda: wf.wf_kv8_append(Fake(4, 2, 64, **far), Fake(4, 2, 64), _kv8(), 0),
+            lambda: wf.wf_kv8_append(Fake(4, 2, 64), Fake(4, 2, 64, on=-1), _kv8(), 0),
+            lambda: wf.wf_kv8_compact_path(_far_cache(), path, path, 0),
+            lambda: wf.wf_kv8_compact_path(_kv8(), Fake(4, dtype=torch.int32, on=1), path, 0),
+            lambda: wf.wf_linear_w4(Fake(4, 64, **far), _w4(), Fake(4, 16)),
+            lambda: wf.wf_linear_w4(x, _w4(dev=1), Fake(4, 16)),
+            lambda: wf.W4Weight(_bytes(16, 32, on=1), _bytes(16, 2)),
+            lambda: wf.wf_w4_quantize(Fake(16, 64, **far)),
+            lambda: _kv8(v=_bytes(2, 3, 64, 32, on=1)), lambda: _kv8(k=_bytes(2, 3, 32, 64, on=-1))):
+        with pytest.raises(ValueError):
+            call()
+
+
+def _far_cache():
+    far = [_bytes(*s, on=1) for s in ((2, 3, 32, 64), (2, 3, 64, 32), (2, 3), (2, 3))]
+    return wf.Kv8Cache(*far, 70)
 
 
 @pytest.mark.parametrize("ctx", [5.5, "5"])
