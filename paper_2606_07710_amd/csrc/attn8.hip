@@ -20,12 +20,13 @@ struct Attn8Params {
     const void *q;
     const char *k, *v;
     const uint8_t *k_scale, *v_scale;
-    void *ws_o;               // [splits][gamma*n_q_heads][head_dim], unnormalised
+    void *ws_o;               // [splits][gamma*n_q_heads][head_dim], unnormalised;
+                              // of one split: the output itself
     float *ws_ml;             // [splits][gamma*n_q_heads][2]: reference, sum
     const uint64_t *tree_mask;
     int gamma, ctx_len, n_blocks, n_q_heads, n_kv_heads, group, rows, n_keys;
-    int splits, keys_per_split, n_row_groups;
-    int tiles_per_split, extra_tiles;    // 128-key tiles; the first splits' extra ones
+    int splits, n_row_groups;
+    int tiles_per_split, extra_tiles;    // a split's tiles (fp32: steps); the first ones' extra
     unsigned group_magic;     // floor(2^32 / group) + 1: row / group as a high product
     float sl2;                // softmax_scale * log2(e)
 };
@@ -495,40 +496,65 @@ __global__ __launch_bounds__(64 * RG * KS) void attn8_tiles(Attn8Params a) {
     const size_t pr = ((size_t)split * a.gamma + qi) * a.n_q_heads + g * a.group +
                       (row - qi * a.group);
     uint2 *dst = reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.ws_o) + pr * D);
+    if (a.splits == 1) {                 // (every row sees itself: l > 0)
+        const float inv = 1.f / l;
+#pragma unroll
+        for (int md = 0; md < MD; ++md)
+            o[md] *= inv;
+    }
 #pragma unroll
     for (int md = 0; md < MD; ++md)
         dst[md * 4 + c4] = uint2{pack_bf16x2(o[md][0], o[md][1]), pack_bf16x2(o[md][2], o[md][3])};
-    if (c4 == 0) {
+    if (c4 == 0 && a.splits > 1) {
         a.ws_ml[pr * 2] = ref;
         a.ws_ml[pr * 2 + 1] = l;
     }
 }
 
 // ---------------------------------------------------------------------------
-// fp32 queries: one wave per (split, row, head), fp32 throughout.  64 keys at
-// a time, two scale blocks: lane t forms key t's score from its code row, then
-// lane d adds the weighted values of dim d (one or two per lane), whose codes
-// lie together in the transposed V blocks.
+// fp32 queries: a workgroup per (split, row, head), fp32 throughout.  Its eight
+// waves take 64 keys, two scale blocks, at a time, each with a softmax of its
+// own: lane t forms key t's score from its code row, then lane d adds the
+// weighted values of dim d (one or two per lane), whose codes lie together in
+// the transposed V blocks.  The waves meet once, in LDS.  A step is one trip to
+// memory: both blocks' codes and scales are asked for before any is used (one
+// wave of 64 keys, each operand loaded where it is needed: 8 rows, 8 heads,
+// 264 keys 6.8 us; now 3.7).  Bound by its launch at such sizes, by the
+// conversions and products in fp32 at 4K keys (8 rows, 32 heads: 25.5 us).
 // ---------------------------------------------------------------------------
+// Orders a wave's LDS accesses before and after it.
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+constexpr int kRowWaves = 8;
+constexpr int kRowKeys = kRowWaves * kWave;          // keys of a workgroup's step
+
 template <int D>
-__global__ __launch_bounds__(64) void attn8_rows(Attn8Params a) {
+__global__ __launch_bounds__(64 * kRowWaves) void attn8_rows(Attn8Params a) {
     constexpr int E = D / kWave;
     __shared__ float qs[D];
-    __shared__ float ps[kWave];
+    __shared__ float ps_all[kRowWaves][kWave];
+    __shared__ float acc_all[kRowWaves][D], ml[kRowWaves][2];
     const int split = blockIdx.x;
     const int pr = blockIdx.y;           // i * n_q_heads + h
     const int i = pr / a.n_q_heads, h = pr % a.n_q_heads;
     const int g = h / a.group;
-    const int lane = threadIdx.x;
-    for (int d = lane; d < D; d += kWave)
-        qs[d] = static_cast<const float *>(a.q)[(size_t)pr * D + d];
+    const int wave = wave_id(), lane = threadIdx.x % kWave;
+    float *ps = ps_all[wave];
+    if (threadIdx.x < D)
+        qs[threadIdx.x] = static_cast<const float *>(a.q)[(size_t)pr * D + threadIdx.x];
     __syncthreads();
 
-    const int k_begin = split * a.keys_per_split;
+    const int first = split * a.tiles_per_split + min(split, a.extra_tiles);
+    const int steps = a.tiles_per_split + (split < a.extra_tiles ? 1 : 0);
+    const int k_begin = first * kRowKeys;
     const bool tree = a.tree_mask != nullptr;
     const uint64_t gbits = a.gamma >= 64 ? ~0ull : (1ull << a.gamma) - 1ull;
     const uint64_t tm = tree ? ((a.tree_mask[i] | (1ull << i)) & gbits) : 0ull;
-    const int k_end = min(min(a.n_keys, k_begin + a.keys_per_split),
+    const int k_end = min(min(a.n_keys, k_begin + steps * kRowKeys),
                           tree ? a.n_keys : a.ctx_len + i + 1);
     const size_t head = (size_t)g * a.n_blocks;
 
@@ -536,33 +562,48 @@ __global__ __launch_bounds__(64) void attn8_rows(Attn8Params a) {
 #pragma unroll
     for (int e = 0; e < E; ++e)
         acc[e] = 0.f;
-    for (int kb = k_begin; kb < k_end; kb += kWave) {
+    for (int kb = k_begin + wave * kWave; kb < k_end; kb += kRowKeys) {
         const int j = kb + lane;
         const int jb = j - a.ctx_len;
         const bool vis = j < k_end && (!tree || jb < 0 || ((tm >> jb) & 1ull));
         const uint64_t seen = __ballot(vis);
-        float sc = -INFINITY;
-        if (vis) {
-            const size_t blk = head + j / kKv8Block;
-            const u32x4 *kr = reinterpret_cast<const u32x4 *>(
-                a.k + (blk * kKv8Block + j % kKv8Block) * D);
-            float dot = 0.f;
+        // the step's codes and scales at once (past the last key: that key's)
+        const int jr = min(j, k_end - 1);
+        const size_t kblk = head + jr / kKv8Block;
+        const u32x4 *kr = reinterpret_cast<const u32x4 *>(
+            a.k + (kblk * kKv8Block + jr % kKv8Block) * D);
+        u32x4 kw[D / 16], vw[2][E][2];
+        unsigned vs[2];
+        const unsigned ks = a.k_scale[kblk];
 #pragma unroll
-            for (int c = 0; c < D / 16; ++c) {
-                const u32x4 w = kr[c];
+        for (int b = 0; b < 2; ++b) {
+            const size_t blk = head + min(kb / kKv8Block + b, (k_end - 1) / kKv8Block);
+            vs[b] = a.v_scale[blk];
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    float f[4];
-                    e4m3x4_to_f32(w[u], f);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        dot = fmaf(qs[16 * c + 4 * u + e], f[e], dot);
-                }
+            for (int e = 0; e < E; ++e) {
+                const u32x4 *vr = reinterpret_cast<const u32x4 *>(
+                    a.v + (blk * D + lane + e * kWave) * kKv8Block);
+                vw[b][e][0] = vr[0];
+                vw[b][e][1] = vr[1];
             }
-            sc = dot * scale_value(a.k_scale[blk]);
         }
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c)
+            kw[c] = kr[c];
+        float dot = 0.f;
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                float f[4];
+                e4m3x4_to_f32(kw[c][u], f);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    dot = fmaf(qs[16 * c + 4 * u + e], f[e], dot);
+            }
         if (seen == 0)                   // uniform: nothing of this step counts
             continue;
+        const float sc = vis ? dot * scale_value((uint8_t)ks) : -INFINITY;
         const float mnew = fmaxf(m, wave_max(sc));
         const float alpha = (m == -INFINITY) ? 0.f : exp2f((m - mnew) * a.sl2);
         const float p = vis ? exp2f((sc - mnew) * a.sl2) : 0.f;
@@ -572,40 +613,60 @@ __global__ __launch_bounds__(64) void attn8_rows(Attn8Params a) {
 #pragma unroll
         for (int e = 0; e < E; ++e)
             acc[e] *= alpha;
-        __syncthreads();
+        wave_sync();
+#pragma unroll
         for (int b = 0; b < 2; ++b) {
             const unsigned live = (unsigned)(seen >> (32 * b));
-            if (live == 0)
-                continue;
-            const size_t blk = head + kb / kKv8Block + b;
-            const float s = scale_value(a.v_scale[blk]);
+            float sum[E] = {};
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const u32x4 *vr = reinterpret_cast<const u32x4 *>(
-                    a.v + (blk * D + lane + e * kWave) * kKv8Block);
-                const u32x4 w[2] = {vr[0], vr[1]};
-                float sum = 0.f;
+            for (int u = 0; u < 8; ++u) {
+                // codes that the row does not see may be NaN: zeros instead
+                const unsigned bytes =
+                    ((live >> (4 * u) & 15u) * 0x00204081u & 0x01010101u) * 255u;
 #pragma unroll
-                for (int u = 0; u < 8; ++u) {
+                for (int e = 0; e < E; ++e) {
                     float f[4];
-                    e4m3x4_to_f32(w[u / 4][u % 4], f);
+                    e4m3x4_to_f32(vw[b][e][u / 4][u % 4] & bytes, f);
 #pragma unroll
-                    for (int t = 0; t < 4; ++t)      // (a code no row sees may be a NaN)
-                        if ((live >> (4 * u + t)) & 1u)
-                            sum = fmaf(ps[32 * b + 4 * u + t], f[t], sum);
+                    for (int t = 0; t < 4; ++t)
+                        sum[e] = fmaf(ps[32 * b + 4 * u + t], f[t], sum[e]);
                 }
-                acc[e] = fmaf(sum, s, acc[e]);
             }
+            const float s = live ? scale_value((uint8_t)vs[b]) : 0.f;
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                acc[e] = fmaf(sum[e], s, acc[e]);
         }
-        __syncthreads();
+        wave_sync();
     }
-    const size_t prs = (size_t)split * a.gamma * a.n_q_heads + pr;
+    // the waves' parts under the largest reference; a wave without a key adds 0
 #pragma unroll
     for (int e = 0; e < E; ++e)
-        static_cast<float *>(a.ws_o)[prs * D + lane + e * kWave] = acc[e];
+        acc_all[wave][lane + e * kWave] = acc[e];
     if (lane == 0) {
-        a.ws_ml[prs * 2] = m * a.sl2;
-        a.ws_ml[prs * 2 + 1] = l;
+        ml[wave][0] = m;
+        ml[wave][1] = l;
+    }
+    __syncthreads();
+    if (threadIdx.x >= D)
+        return;
+    float top = ml[0][0];
+#pragma unroll
+    for (int w = 1; w < kRowWaves; ++w)
+        top = fmaxf(top, ml[w][0]);
+    float sum = 0.f, out = 0.f;
+#pragma unroll
+    for (int w = 0; w < kRowWaves; ++w) {
+        const float f = ml[w][0] == -INFINITY ? 0.f : exp2f((ml[w][0] - top) * a.sl2);
+        sum = fmaf(ml[w][1], f, sum);
+        out = fmaf(acc_all[w][threadIdx.x], f, out);
+    }
+    const size_t prs = (size_t)split * a.gamma * a.n_q_heads + pr;
+    // (of one split: every row sees itself, sum > 0)
+    static_cast<float *>(a.ws_o)[prs * D + threadIdx.x] = a.splits == 1 ? out / sum : out;
+    if (threadIdx.x == 0 && a.splits > 1) {
+        a.ws_ml[prs * 2] = top * a.sl2;
+        a.ws_ml[prs * 2 + 1] = sum;
     }
 }
 
@@ -616,12 +677,25 @@ __global__ __launch_bounds__(64) void attn8_rows(Attn8Params a) {
 // take a workgroup of one stream, two per CU, which do not wait for each other's
 // barriers (128 rows, 64K keys: 51.4 us, 53.0 as one workgroup of eight waves; 244
 // rows, 8K keys: 18.9 and 21.5 us, though the tiles are then read from L2 twice as
-// often).  No workgroup is without a tile.
+// often).  No workgroup is without a tile.  Where a tile is left for each, one
+// stream (32 rows, 1K keys: 8.9 -> 8.1 us; 64 rows: 10.9 -> 9.0).  Few tiles stay
+// one split, whose workgroup writes the output and spares the merge: up to two
+// steps (32 rows, 500 keys: 7.6 us, 7.9 as four splits), or one of 64 rows, whose
+// steps take twice as long (256 keys: 7.1 and 8.2 us; 516 keys in three: 12.3 and
+// 8.7).  fp32: splits only where the rows leave CUs idle (256 rows and heads,
+// 2K keys: 13.8 us, 17.3 as four; 32, 4K keys: 25.1 and 8.8 as eight).
 AttnPlan plan_attn8(wf_dtype_t dt, int gamma, int ctx_len, int n_q_heads, int n_kv_heads,
                     int head_dim, int num_splits) {
-    if (dt == WF_F32)
-        return plan_attn(WF_F32, gamma, ctx_len, n_q_heads, n_kv_heads, head_dim, num_splits);
     AttnPlan p{};
+    if (dt == WF_F32) {
+        const int steps = (ctx_len + gamma + kRowKeys - 1) / kRowKeys;
+        const int want = num_splits > 0 ? num_splits
+                         : steps <= 2   ? 1
+                                        : std::max(1, 256 / (gamma * n_q_heads));
+        p.part_bytes = 4;
+        p.splits = std::min(want, steps);
+        return p;
+    }
     p.part_bytes = 2;
     p.rows = n_q_heads / n_kv_heads * gamma;
     p.nb = 1;
@@ -633,6 +707,10 @@ AttnPlan plan_attn8(wf_dtype_t dt, int gamma, int ctx_len, int n_q_heads, int n_
     const int want = num_splits > 0 ? num_splits
                                     : std::max(1, fill / (n_kv_heads * p.n_row_groups));
     p.splits = std::min(want, tiles);
+    if (num_splits == 0 && tiles <= (p.rg == 4 ? 1 : 2) * p.ks)
+        p.splits = 1;
+    if (p.splits == tiles)
+        p.ks = 1;
     return p;
 }
 
@@ -649,6 +727,8 @@ wf_status_t launch_attn8(wf_dtype_t dt, const void *q, const wf_kv8_cache_t &c, 
     a.v_scale = c.v_scale;
     a.ws_ml = reinterpret_cast<float *>(static_cast<char *>(workspace) + kCounterBytes);
     a.ws_o = a.ws_ml + (size_t)p.splits * pairs * 2;
+    if (p.splits == 1)
+        a.ws_o = out;
     a.tree_mask = tree_mask;
     a.gamma = gamma;
     a.ctx_len = ctx_len;
@@ -659,13 +739,13 @@ wf_status_t launch_attn8(wf_dtype_t dt, const void *q, const wf_kv8_cache_t &c, 
     a.rows = p.rows;
     a.n_keys = ctx_len + gamma;
     a.splits = p.splits;
-    a.keys_per_split = p.keys_per_split;
     a.n_row_groups = p.n_row_groups;
     a.sl2 = softmax_scale * kLog2e;
+    const int unit = dt == WF_BF16 ? kTileKeys8 : kRowKeys;
+    const int tiles = (a.n_keys + unit - 1) / unit;
+    a.tiles_per_split = tiles / p.splits;
+    a.extra_tiles = tiles % p.splits;
     if (dt == WF_BF16) {
-        const int tiles = (a.n_keys + kTileKeys8 - 1) / kTileKeys8;
-        a.tiles_per_split = tiles / p.splits;
-        a.extra_tiles = tiles % p.splits;
         // (exact for rows below 2^14 in groups of 2 to 2^8)
         a.group_magic = (unsigned)((1ull << 32) / a.group + 1);
         const int units = c.n_kv_heads * p.splits;
@@ -676,19 +756,22 @@ wf_status_t launch_attn8(wf_dtype_t dt, const void *q, const wf_kv8_cache_t &c, 
         attn8_tiles<DV, RGV, KSV, NBUFV><<<grid, 64 * RGV * KSV, 0, stream>>>(a);          \
     else
         WF_ATTN8(128, 1, 2, 2) WF_ATTN8(128, 2, 2, 2) WF_ATTN8(128, 4, 2, 2)
-        WF_ATTN8(128, 4, 1, 2)
+        WF_ATTN8(128, 4, 1, 2) WF_ATTN8(128, 1, 1, 2) WF_ATTN8(128, 2, 1, 2)
+        WF_ATTN8(64, 1, 1, 2) WF_ATTN8(64, 2, 1, 2)
         WF_ATTN8(64, 1, 2, 2) WF_ATTN8(64, 2, 2, 4) WF_ATTN8(64, 4, 2, 4) WF_ATTN8(64, 4, 1, 4)
         return WF_ERR_UNSUPPORTED;
 #undef WF_ATTN8
     } else {
         const dim3 grid(p.splits, (unsigned)pairs);
         if (c.head_dim == 128)
-            attn8_rows<128><<<grid, 64, 0, stream>>>(a);
+            attn8_rows<128><<<grid, 64 * kRowWaves, 0, stream>>>(a);
         else
-            attn8_rows<64><<<grid, 64, 0, stream>>>(a);
+            attn8_rows<64><<<grid, 64 * kRowWaves, 0, stream>>>(a);
     }
     if (hipGetLastError() != hipSuccess)
         return WF_ERR_HIP;
+    if (p.splits == 1)
+        return WF_OK;
     // (the references are held in log2 units, so the merge's factor is 1)
     return launch_attn_merge(c.head_dim, dt == WF_BF16, a.ws_o, a.ws_ml, out, (int)pairs,
                              p.splits, 1.f, stream);

@@ -254,6 +254,11 @@ SHAPES = [
     (61, 2050, 32, 8, 64, 0), (16, 3000, 64, 8, 128, 3), (33, 95, 10, 2, 128, 1024),
     (64, 0, 32, 8, 128, 0), (4, 2999, 256, 2, 64, 0), (7, 640, 3, 3, 128, 2),
     (2, 255, 80, 5, 128, 1), (64, 64, 256, 1, 64, 0),
+    # (one split: the output is written at once; a tile per split: one key stream)
+    (8, 240, 32, 8, 128, 0), (16, 240, 32, 8, 128, 0), (4, 500, 8, 2, 64, 0),
+    (2, 500, 8, 2, 128, 0), (16, 100, 32, 8, 64, 0), (17, 900, 8, 4, 64, 0),
+    (8, 1200, 8, 2, 64, 0), (1, 4000, 32, 8, 128, 0), (3, 1400, 32, 8, 128, 2),
+    (5, 2700, 4, 4, 64, 4),
 ]
 
 
