@@ -29,6 +29,60 @@ __device__ __forceinline__ float w4_scale(unsigned s, int kk) {
     return __uint_as_float((kk < 3 ? s << (23 - 8 * kk) : s >> 1) & 0x7f800000u);
 }
 
+// A raw buffer's last word (data format 32, without which loads return nothing),
+// and the cache policy of bytes that are read once.
+constexpr int kRawBuffer = 4 << 15;
+constexpr int kNonTemporal = 2;
+
+// y[at] = z (+ the residual), in y's type.
+__device__ __forceinline__ void store_y(void *y, const uint16_t *res, size_t at, float z,
+                                        bool f32_out) {
+    if (res)
+        z += bf16_to_f32(res[at]);
+    if (f32_out)
+        static_cast<float *>(y)[at] = z;
+    else
+        static_cast<uint16_t *>(y)[at] = f32_to_bf16(z);
+}
+
+// Four features f .. f+3 of row r: in one store where `quads` says that rows keep
+// its alignment, a quarter of the requests (61 rows, 2560 to 151936: 68 -> 56 us).
+__device__ __forceinline__ void store_y4(void *y, const uint16_t *res, int r, int f, int n_out,
+                                         f32x4 z, bool f32_out, bool quads) {
+    const size_t at = (size_t)r * n_out + f;
+    if (quads) {                                     // uniform
+        if (f >= n_out)
+            return;
+        if (res) {
+            const u32x2 v = *reinterpret_cast<const u32x2 *>(res + at);
+            z[0] += __uint_as_float(v[0] << 16);
+            z[1] += __uint_as_float(v[0] & 0xffff0000u);
+            z[2] += __uint_as_float(v[1] << 16);
+            z[3] += __uint_as_float(v[1] & 0xffff0000u);
+        }
+        if (f32_out)
+            *reinterpret_cast<f32x4 *>(static_cast<float *>(y) + at) = z;
+        else
+            *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(y) + at) =
+                uint2{pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3])};
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (f + i < n_out)
+            store_y(y, res, at + i, z[i], f32_out);
+}
+
+// The rows of x as a buffer; the offset of 16 bytes of it, behind its end (so
+// that zeros are loaded) if `in` is false.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t x_buffer(const uint16_t *x, int rows, int k_in) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(x), 0, rows * k_in * 2,
+                                             kRawBuffer);
+}
+__device__ __forceinline__ u32x4 load_x16(__amdgpu_buffer_rsrc_t x, unsigned at, bool in) {
+    return __builtin_amdgcn_raw_buffer_load_b128(x, in ? at : 0x7ffffff0u, 0, 0);
+}
+
 // A lane's 16 bytes of a tile, which no other workgroup reads.
 __device__ __forceinline__ u32x4 load_codes(const uint8_t *p) {
     return __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p));
@@ -43,17 +97,6 @@ __device__ __forceinline__ bf16x8 w4_expand(uint32_t w, float s) {
     const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2);
     const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3);
     return bf16x8{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
-}
-
-// y[at] = z (+ the residual), in y's type.
-__device__ __forceinline__ void store_y(void *y, const uint16_t *res, size_t at, float z,
-                                        bool f32_out) {
-    if (res)
-        z += bf16_to_f32(res[at]);
-    if (f32_out)
-        static_cast<float *>(y)[at] = z;
-    else
-        static_cast<uint16_t *>(y)[at] = f32_to_bf16(z);
 }
 
 // Up to 16 rows, input split: workgroup b owns FB blocks of 16 features and the
@@ -80,8 +123,9 @@ __global__ __launch_bounds__(kW4Waves * kWave) void linear_w4(
 #pragma unroll
     for (int fb = 0; fb < FB; ++fb)
         wp[fb] = w + (size_t)min(FB * (int)blockIdx.x + fb, (n_out + 15) / 16 - 1) * n_c * kW4Tile;
-    // rows past the end read the last one; they are not stored
-    const uint16_t *xp = x + (size_t)min(m16, rows - 1) * k_in + c4 * 8;
+    // (rows and inputs past the end are zeros)
+    const __amdgpu_buffer_rsrc_t xp = x_buffer(x, rows, k_in);
+    const unsigned xo = (unsigned)(m16 * k_in + c4 * 8) * 2;
     f32x4 acc[FB];
 #pragma unroll
     for (int fb = 0; fb < FB; ++fb)
@@ -101,10 +145,10 @@ __global__ __launch_bounds__(kW4Waves * kWave) void linear_w4(
                 q.w[u][fb] = load_codes(t + lane * 16);
                 q.s[u][fb] = reinterpret_cast<const uint32_t *>(t + 1024)[m16];
             }
-            // (inputs past the end: the row's last ones, against zero codes)
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk)
-                q.x[u][kk] = load_bf16x8(xp + min(4 * c + kk, last_g) * kW4Group);
+                q.x[u][kk] = __builtin_bit_cast(
+                    bf16x8, load_x16(xp, xo + (4 * c + kk) * (kW4Group * 2), 4 * c + kk <= last_g));
         }
     };
     auto multiply = [&](const Batch &q, int cb) __attribute__((always_inline)) {
@@ -156,7 +200,7 @@ __global__ __launch_bounds__(kW4Waves * kWave) void linear_w4(
 // up to FB blocks of 16 features, of KW waves that share the input among them.
 // All walk the input (or slice blockIdx.y of it) together in chunks of KW tiles
 // of 128 inputs, one per wave, whose x, all rows, is staged in LDS, so a wave
-// reads it once for all its blocks; the next chunk's codes and x are on their way
+// reads it once for all its blocks; the next chunks' codes and x are on their way
 // to registers meanwhile.  KW > 1 is for few blocks: a wave of one block reads 4 KB of x per 1
 // KB of codes and 16 rows from LDS, so with 64 rows the waves ask it for more than
 // the 128 bytes a cycle it has; a quarter of the input and four times the blocks
@@ -167,13 +211,14 @@ __global__ __launch_bounds__(kW4Waves * kWave) void linear_w4(
 template <int NB, int FB, int KW>
 __global__ __launch_bounds__(kW4Waves * kWave) void linear_w4_wide(
     const uint16_t *__restrict__ x, const uint8_t *__restrict__ w, const uint16_t *res, void *y,
-    int rows, int n_out, int k_in, bool f32_out, float *part) {
+    int rows, int n_out, int k_in, bool f32_out, bool quads, float *part) {
     constexpr int GRAN = 16 * KW;                    // 16-byte granules of a row's chunk
     constexpr int XG = 16 * NB * GRAN;               // ... of the chunk, XT of them a thread's
     constexpr int XT = (XG + kW4Waves * kWave - 1) / (kW4Waves * kWave);
     constexpr int FG = kW4Waves / KW;
+    // chunks of codes held or on their way (three where the registers take them)
+    constexpr int R = NB == 1 || (KW == 4 && NB * FB >= 16) ? 2 : 3;
     __shared__ u32x4 xs[2][XG];
-    static_assert(KW == 1 || sizeof(xs) >= FG * 1024 * NB, "the waves' sums meet in the chunks' place");
     const int wave = wave_id();
     const int kw = wave % KW, fg = wave / KW;
     const int lane = threadIdx.x % kWave;
@@ -188,10 +233,15 @@ __global__ __launch_bounds__(kW4Waves * kWave) void linear_w4_wide(
     const int b_first = (int)((long long)id * blocks / groups);
     const int n_b = (int)((long long)(id + 1) * blocks / groups) - b_first;
 
-    const uint8_t *wp[FB];
+    // A block's tiles up to the slice's end, as a buffer: loads past them return
+    // zeros and cost no traffic.
+    __amdgpu_buffer_rsrc_t wp[FB];
+    const int w_bytes = min(KW * c_end, n_t) * kW4Tile;
 #pragma unroll
-    for (int fb = 0; fb < FB; ++fb)      // (without an fb-th block: its last one again)
-        wp[fb] = w + (size_t)min(b_first + min(fb, max(n_b - 1, 0)), blocks - 1) * n_t * kW4Tile;
+    for (int fb = 0; fb < FB; ++fb)      // (without an fb-th block: none)
+        wp[fb] = __builtin_amdgcn_make_buffer_rsrc(
+            const_cast<uint8_t *>(w) + (size_t)min(b_first + fb, blocks - 1) * n_t * kW4Tile, 0,
+            fb < n_b ? w_bytes : 0, kRawBuffer);
     f32x4 acc[FB][NB];
 #pragma unroll
     for (int fb = 0; fb < FB; ++fb)
@@ -199,121 +249,138 @@ __global__ __launch_bounds__(kW4Waves * kWave) void linear_w4_wide(
         for (int nb = 0; nb < NB; ++nb)
             acc[fb][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    struct Chunk {
+    // Codes are asked for two chunks ahead, or one, x one ahead (61 rows, 2560 to
+    // 151936: 67 us, 70 with codes one ahead; up to 16 rows one is better, 46 and
+    // 49 us).  No branch surrounds the loads: the compiler would lose count of
+    // those in flight and wait for all (one row: 42 us, 51 with a branch at the end
+    // of the input).
+    struct Codes {
         u32x4 w[FB];
         unsigned s[FB];
-        u32x4 x[XT];
     };
-    Chunk ring[2];
-    // The chunk past the end is the last one again, never used: a branch around
-    // the loads would leave the compiler without a count of those in flight, and
-    // it would wait for all of them (2560 to 151936, one row: 41.8 us, 51.0 with
-    // the branch).  Of x a row past the end is the last row, a granule past the
-    // input's end the row's last, which meets zero codes.
-    auto load = [&](Chunk &q, int at) __attribute__((always_inline)) {
-        const int ch = min(at, c_end - 1);
+    Codes ring[R];
+    u32x4 xr[XT];
+    auto load_w = [&](Codes &q, int ch) __attribute__((always_inline)) {
+        const unsigned at = (unsigned)(KW * ch + kw) * kW4Tile;
+#pragma unroll
+        for (int fb = 0; fb < FB; ++fb) {
+            q.w[fb] = __builtin_amdgcn_raw_buffer_load_b128(wp[fb], at + lane * 16, 0, kNonTemporal);
+            q.s[fb] = __builtin_amdgcn_raw_buffer_load_b32(wp[fb], at + 1024 + m16 * 4, 0, 0);
+        }
+    };
+    // (rows and inputs past the end are zeros)
+    const __amdgpu_buffer_rsrc_t xp = x_buffer(x, rows, k_in);
+    auto load_x = [&](int ch) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < XT; ++j) {
             const int idx = threadIdx.x + j * kW4Waves * kWave;
-            const int r = idx / GRAN, g = idx % GRAN;
-            const int k = min(ch * GRAN + g, k_in / 8 - 1) * 8;
-            q.x[j] = *reinterpret_cast<const u32x4 *>(x + (size_t)min(r, rows - 1) * k_in + k);
-        }
-#pragma unroll
-        for (int fb = 0; fb < FB; ++fb) {
-            const uint8_t *t = wp[fb] + (size_t)min(KW * ch + kw, n_t - 1) * kW4Tile;
-            q.w[fb] = load_codes(t + lane * 16);
-            q.s[fb] = reinterpret_cast<const uint32_t *>(t + 1024)[m16];
+            const int r = idx / GRAN, g = ch * GRAN + idx % GRAN;
+            xr[j] = load_x16(xp, (unsigned)(r * k_in * 2 + g * 16), g < k_in / 8);
         }
     };
-    auto stage_x = [&](const Chunk &q, int buf) __attribute__((always_inline)) {
+    auto stage_x = [&](int buf) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < XT; ++j) {
             const int idx = threadIdx.x + j * kW4Waves * kWave;
             const int r = idx / GRAN, g = idx % GRAN;
             if (XG % (kW4Waves * kWave) == 0 || idx < XG)
-                xs[buf][r * GRAN + (g ^ (r & 7))] = q.x[j];
+                xs[buf][r * GRAN + (g ^ (r & 7))] = xr[j];
         }
     };
     // every wave's LDS writes are done; loads in flight stay so
     auto barrier = [] { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
-    // One chunk, in ring[I] and LDS buffer I, while the next is loaded.
+    // One chunk, its codes in ring[I].
     auto step = [&](auto it, int ch) __attribute__((always_inline)) {
         constexpr int I = decltype(it)::value;
-        load(ring[1 - I], ch + 1);
-        const Chunk &now = ring[I];
-        const u32x4 *xb = xs[I];
-        if (KW * ch + kw < n_t) {                    // uniform
+        load_x(ch + 1);
+        __builtin_amdgcn_sched_barrier(0);           // (x first: its wait leaves the codes be)
+        load_w(ring[(I + R - 1) % R], ch + R - 1);
+        __builtin_amdgcn_sched_barrier(0);
+        const Codes &now = ring[I];
+        const int buf = (ch - c_first) & 1;
+        const u32x4 *xb = xs[buf];
 #pragma unroll
-            for (int kk = 0; kk < 4; ++kk) {
-                bf16x8 xo[NB];
+        for (int kk = 0; kk < 4; ++kk) {
+            bf16x8 xo[NB];
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb) {
-                    const int r = 16 * nb + m16, g = 16 * kw + 4 * kk + c4;
-                    xo[nb] = __builtin_bit_cast(bf16x8, xb[r * GRAN + (g ^ (r & 7))]);
-                }
-#pragma unroll
-                for (int fb = 0; fb < FB; ++fb) {
-                    const bf16x8 wo = w4_expand(now.w[fb][kk], w4_scale(now.s[fb], kk));
-#pragma unroll
-                    for (int nb = 0; nb < NB; ++nb)
-                        acc[fb][nb] = mfma16x16x32(wo, xo[nb], acc[fb][nb]);
-                }
+            for (int nb = 0; nb < NB; ++nb) {
+                const int r = 16 * nb + m16, g = 16 * kw + 4 * kk + c4;
+                xo[nb] = __builtin_bit_cast(bf16x8, xb[r * GRAN + (g ^ (r & 7))]);
             }
-        }
-        stage_x(ring[1 - I], 1 - I);
-        barrier();
-    };
-    load(ring[0], c_first);
-    stage_x(ring[0], 0);
-    barrier();
-    for (int ch = c_first; ch < c_end; ch += 2) {
-        step(ic<0>{}, ch);
-        if (ch + 1 < c_end)
-            step(ic<1>{}, ch + 1);
-    }
-    // lane (m16, c4) holds features 4*c4 .. +3 of row m16
-    if constexpr (KW > 1) {
-        // the sums of a feature group's waves, in wave order, block by block
-        f32x4 *meet = reinterpret_cast<f32x4 *>(xs) + fg * 64 * NB;
-#pragma unroll
-        for (int k = 1; k < KW; ++k)
 #pragma unroll
             for (int fb = 0; fb < FB; ++fb) {
-                if (kw == k) {
+                const bf16x8 wo = w4_expand(now.w[fb][kk], w4_scale(now.s[fb], kk));
 #pragma unroll
-                    for (int nb = 0; nb < NB; ++nb)
-                        meet[64 * nb + lane] = acc[fb][nb];
-                }
-                __syncthreads();
-                if (kw == 0) {
-#pragma unroll
-                    for (int nb = 0; nb < NB; ++nb)
-                        acc[fb][nb] += meet[64 * nb + lane];
-                }
-                __syncthreads();
+                for (int nb = 0; nb < NB; ++nb)
+                    acc[fb][nb] = mfma16x16x32(wo, xo[nb], acc[fb][nb]);
             }
-        if (kw != 0)
-            return;
+        }
+        stage_x(1 - buf);
+        barrier();
+    };
+    load_x(c_first);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < R - 1; ++i)
+        load_w(ring[i], c_first + i);
+    __builtin_amdgcn_sched_barrier(0);
+    stage_x(0);
+    barrier();
+    int ch = c_first;
+    for (; ch + R <= c_end; ch += R) {
+        step(ic<0>{}, ch);
+        step(ic<1>{}, ch + 1);
+        if constexpr (R > 2)
+            step(ic<R - 1>{}, ch + 2);
     }
+    if (ch < c_end)
+        step(ic<0>{}, ch);
+    if (R > 2 && ch + 1 < c_end)
+        step(ic<1>{}, ch + 1);
+    // lane (m16, c4) holds features 4*c4 .. +3 of row m16
+    auto put = [&](int fb, int nb, f32x4 z) __attribute__((always_inline)) {
+        const int r = 16 * nb + m16, f = 16 * (b_first + fb) + 4 * c4;
+        if (r >= rows || fb >= n_b)
+            return;
+        if (gridDim.y > 1)
+            *reinterpret_cast<f32x4 *>(part + ((size_t)blockIdx.y * rows + r) * 16 * blocks + f) =
+                z;
+        else
+            store_y4(y, res, r, f, n_out, z, f32_out, quads);
+    };
+    if constexpr (KW == 1) {
 #pragma unroll
-    for (int fb = 0; fb < FB; ++fb) {
-        if (fb >= n_b)
-            break;
+        for (int fb = 0; fb < FB; ++fb)
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-            const int r = 16 * nb + m16, f = 16 * (b_first + fb) + 4 * c4;
-            if (r >= rows)
-                continue;
-            if (gridDim.y > 1) {
-                *reinterpret_cast<f32x4 *>(part + ((size_t)blockIdx.y * rows + r) * 16 * blocks +
-                                           f) = acc[fb][nb];
-                continue;
+            for (int nb = 0; nb < NB; ++nb)
+                put(fb, nb, acc[fb][nb]);
+    } else {
+        // The sums of a feature group's waves meet in the chunks' place, P blocks
+        // at a time; each wave adds up, in wave order, and stores every KW-th
+        // piece of 16 rows.
+        constexpr int P = KW < FB ? KW : FB;
+        static_assert(sizeof(xs) >= kW4Waves * P * NB * 1024, "room");
+        f32x4 *meet = reinterpret_cast<f32x4 *>(xs) + fg * (KW * P * NB * kWave);
+#pragma unroll
+        for (int f0 = 0; f0 < FB; f0 += P) {
+            if (f0)
+                __syncthreads();
+#pragma unroll
+            for (int t = 0; t < P * NB; ++t)
+                if (f0 + t / NB < FB)
+                    meet[(kw * P * NB + t) * kWave + lane] = acc[f0 + t / NB][t % NB];
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < (P * NB + KW - 1) / KW; ++i) {
+                const int t = i * KW + kw;
+                if (P * NB % KW && t >= P * NB)
+                    continue;
+                f32x4 z = meet[t * kWave + lane];
+#pragma unroll
+                for (int k = 1; k < KW; ++k)
+                    z += meet[(k * P * NB + t) * kWave + lane];
+                put(f0 + t / NB, t % NB, z);
             }
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (f + i < n_out)
-                    store_y(y, res, (size_t)r * n_out + f + i, acc[fb][nb][i], f32_out);
         }
     }
 }
@@ -323,26 +390,23 @@ constexpr int kW4MaxSlices = 8;
 
 __global__ __launch_bounds__(256) void w4_sum(const float *__restrict__ part, int slices,
                                               const uint16_t *res, void *y, int rows, int n_out,
-                                              bool f32_out) {
-    const int quads = (n_out + 15) / 16 * 4;
+                                              bool f32_out, bool quads) {
+    const int row_quads = (n_out + 15) / 16 * 4;
     const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= (size_t)rows * quads)
+    if (i >= (size_t)rows * row_quads)
         return;
-    const int r = (int)(i / quads), f = (int)(i % quads) * 4;
+    const int r = (int)(i / row_quads), f = (int)(i % row_quads) * 4;
     f32x4 v[kW4MaxSlices];
 #pragma unroll
     for (int k = 0; k < kW4MaxSlices; ++k)
         if (k < slices)
-            v[k] = reinterpret_cast<const f32x4 *>(part)[((size_t)k * rows + r) * quads + f / 4];
+            v[k] = reinterpret_cast<const f32x4 *>(part)[((size_t)k * rows + r) * row_quads + f / 4];
     f32x4 z = v[0];
 #pragma unroll
     for (int k = 1; k < kW4MaxSlices; ++k)
         if (k < slices)
             z += v[k];
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-        if (f + j < n_out)
-            store_y(y, res, (size_t)r * n_out + f + j, z[j], f32_out);
+    store_y4(y, res, r, f, n_out, z, f32_out, quads);
 }
 
 // Nearest e2m1 code of |a| <= 6, ties to the even code.
@@ -446,7 +510,7 @@ W4Plan plan_linear_w4(int rows, int n_out, int k_in) {
     p.slices = 1;
     // up to 16 rows and six blocks per CU: the input split, one workgroup per CU
     // (4096 to 24576, 16 rows: 15.8 us, the feature split 19.6; 2560 to 151936:
-    // 110 and 51 us)
+    // 110 and 46 us)
     if (rows <= 16 && blocks <= 6 * 256) {
         p.fb = blocks <= 4 * 256 ? (blocks + 255) / 256 : 6;
         p.groups = (blocks + p.fb - 1) / p.fb;
@@ -454,13 +518,14 @@ W4Plan plan_linear_w4(int rows, int n_out, int k_in) {
     }
     // Of more rows the LDS reads of x bound a wave of few blocks: four waves to a
     // feature group up to eight blocks per CU, two up to 20 (64 rows, 4096 to 24576:
-    // 33.5 us with one, 28.3 with two, 25.9 with four; 2560 to 40000: 30.3, 26.9 and
-    // 29.6).
+    // 33.5 us with one, 28.3 with two, 25.9 with four, now 22.5; 2560 to 40000: 30.3,
+    // 26.9 and 29.6, now 22.4).
     p.wide = true;
     p.kw = rows <= 16 ? 1 : blocks <= 8 * 256 ? 4 : blocks <= 20 * 256 ? 2 : 1;
     const int fg = kW4Waves / p.kw;
     // fewer than two blocks per CU: slices of at least two chunks, so a workgroup
-    // reads less of x (64 rows, 4096 to 4096: 13.6 us, 23.4 without)
+    // reads less of x (64 rows, 4096 to 4096: 13.6 us, 23.4 without, now 13.0; the
+    // last workgroup to arrive adding the slices up instead of w4_sum: 16.8)
     const int chunks = (k_in + 128 * p.kw - 1) / (128 * p.kw);
     if (blocks < 2 * 256)
         p.slices = std::max(1, std::min({kW4MaxSlices, chunks / 2, 5 * fg * 256 / blocks}));
@@ -472,6 +537,8 @@ W4Plan plan_linear_w4(int rows, int n_out, int k_in) {
 }
 
 }  // namespace
+
+static bool aligned(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
 size_t linear_w4_workspace_bytes(int rows, int n_out, int k_in) {
     const W4Plan p = plan_linear_w4(rows, n_out, k_in);
@@ -500,25 +567,26 @@ wf_status_t launch_linear_w4(const uint16_t *x, const uint8_t *w, const uint16_t
                                                            kCounterBytes)
                                : nullptr;
     const int nb = (rows + 15) / 16;
+    const bool quads = n_out % 4 == 0 && aligned(y, 16) && aligned(res, 8);
     const dim3 grid(p.groups, p.slices);
 #define WF_W4(NBV, FBV, KWV)                                                                  \
     if (nb == NBV && p.fb == FBV && p.kw == KWV)                                              \
         linear_w4_wide<NBV, FBV, KWV><<<grid, block, 0, stream>>>(x, w, res, y, rows, n_out,  \
-                                                                  k_in, f32_out, part);       \
+                                                                  k_in, f32_out, quads, part);\
     else
-#define WF_W4_ROW(NBV, KWV)                                                                   \
-    WF_W4(NBV, 1, KWV) WF_W4(NBV, 2, KWV) WF_W4(NBV, 3, KWV) WF_W4(NBV, 4, KWV)               \
-    WF_W4(NBV, 5, KWV)
-    WF_W4_ROW(1, 1) WF_W4_ROW(2, 1) WF_W4_ROW(3, 1) WF_W4_ROW(4, 1)
-    WF_W4_ROW(2, 2) WF_W4_ROW(3, 2) WF_W4_ROW(4, 2)
+#define WF_W4_MANY(NBV, KWV) WF_W4(NBV, 3, KWV) WF_W4(NBV, 4, KWV) WF_W4(NBV, 5, KWV)
+#define WF_W4_ROW(NBV, KWV) WF_W4(NBV, 1, KWV) WF_W4(NBV, 2, KWV) WF_W4_MANY(NBV, KWV)
+    WF_W4_ROW(1, 1) WF_W4_MANY(2, 1) WF_W4_MANY(3, 1) WF_W4_MANY(4, 1)
+    WF_W4_MANY(2, 2) WF_W4_MANY(3, 2) WF_W4_MANY(4, 2)
     WF_W4_ROW(2, 4) WF_W4_ROW(3, 4) WF_W4_ROW(4, 4)
     return WF_ERR_UNSUPPORTED;
 #undef WF_W4_ROW
+#undef WF_W4_MANY
 #undef WF_W4
     if (p.slices > 1) {
-        const size_t quads = (size_t)rows * ((n_out + 15) / 16 * 4);
-        const unsigned wg = (unsigned)((quads + 255) / 256);
-        w4_sum<<<wg, 256, 0, stream>>>(part, p.slices, res, y, rows, n_out, f32_out);
+        const size_t n = (size_t)rows * ((n_out + 15) / 16 * 4);
+        const unsigned wg = (unsigned)((n + 255) / 256);
+        w4_sum<<<wg, 256, 0, stream>>>(part, p.slices, res, y, rows, n_out, f32_out, quads);
     }
     return hipGetLastError() == hipSuccess ? WF_OK : WF_ERR_HIP;
 }

@@ -120,6 +120,63 @@ def test_linear(rows, n_out, k_in, out, res):
     assert torch.equal(again, y)
 
 
+# Many features: the feature split of up to 16 rows, two waves and one to a
+# feature group, several rounds of workgroups, blocks that do not divide evenly.
+@pytest.mark.parametrize("rows,n_out,k_in", [
+    (5, 30000, 96), (12, 82000, 64), (16, 200000, 32), (33, 40000, 160), (17, 66004, 96),
+    (50, 36002, 288), (61, 90001, 64), (20, 140000, 32), (64, 170000, 32),
+])
+def test_linear_many_features(rows, n_out, k_in):
+    print("many features", rows, n_out, k_in, flush=True)
+    codes, scales = _weight(rows + n_out, n_out, k_in)
+    x = _normal(k_in, rows, k_in)
+    y = torch.full((rows, n_out), float("nan"), device=DEV)
+    wf.wf_linear_w4(x.to(DEV), wf.W4Weight(codes.to(DEV), scales.to(DEV)), y)
+    torch.cuda.synchronize()
+    _check(x, codes, scales, y, out="f32")
+
+
+@pytest.mark.parametrize("rows,n_out,k_in", [(3, 40, 64), (20, 1000, 512), (40, 33000, 64)])
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+def test_linear_odd_addresses(rows, n_out, k_in, out):
+    """Output and residual that start at any element."""
+    print("odd addresses", rows, n_out, k_in, out, flush=True)
+    codes, scales = _weight(n_out, n_out, k_in)
+    x, r = _normal(1, rows, k_in), _normal(2, rows, n_out)
+    dt = torch.bfloat16 if out == "bf16" else torch.float32
+    w = wf.W4Weight(codes.to(DEV), scales.to(DEV))
+    for at in (1, 2, 3):
+        buf = torch.full((rows * n_out + 8,), float("nan"), dtype=dt, device=DEV)
+        rb = torch.empty(rows * n_out + 8, dtype=torch.bfloat16, device=DEV)
+        y, rd = (t[at:at + rows * n_out].view(rows, n_out) for t in (buf, rb))
+        rd.copy_(r)
+        wf.wf_linear_w4(x.to(DEV), w, y, rd)
+        torch.cuda.synchronize()
+        _check(x, codes, scales, y, r, out)
+        assert buf[:at].isnan().all() and buf[at + rows * n_out:].isnan().all()
+
+
+@pytest.mark.parametrize("rows,n_out,k_in", [(3, 40, 96), (20, 300, 160), (18, 33000, 64),
+                                             (5, 30000, 32)])
+def test_linear_infinite_inputs(rows, n_out, k_in):
+    """An infinity, also among the last inputs: infinities of the weight's sign
+    in its row, and nothing in the others."""
+    print("infinite inputs", rows, n_out, k_in, flush=True)
+    codes, scales = _weight(n_out, n_out, k_in)
+    codes = codes | 0x11                             # (no zero weight)
+    x = _normal(1, rows, k_in)
+    x[0, 1], x[1, k_in - 1], x[2, k_in - 2] = float("inf"), float("-inf"), float("nan")
+    y = torch.empty(rows, n_out, device=DEV)
+    wf.wf_linear_w4(x.to(DEV), wf.W4Weight(codes.to(DEV), scales.to(DEV)), y)
+    torch.cuda.synchronize()
+    w = torch.from_numpy(R.decode_e2m1(codes.numpy(), scales.numpy()))
+    y = y.cpu()
+    assert torch.equal(y[0].double(), float("inf") * w[:, 1].sign())
+    assert torch.equal(y[1].double(), float("-inf") * w[:, -1].sign())
+    assert y[2].isnan().all()
+    _check(x[3:], codes, scales, y[3:], out="f32")
+
+
 def test_linear_residual_in_place_and_workspace_reuse():
     """The residual may be the output; calls of several sizes share one
     workspace, also from a captured graph."""
