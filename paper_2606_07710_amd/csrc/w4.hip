@@ -386,7 +386,7 @@ __global__ __launch_bounds__(kW4Waves * kWave) void linear_w4_wide(
 }
 
 // y = the slices' sums in order (and the residual); 4 features per thread.
-constexpr int kW4MaxSlices = 8;
+constexpr int kW4MaxSlices = 4;
 
 __global__ __launch_bounds__(256) void w4_sum(const float *__restrict__ part, int slices,
                                               const uint16_t *res, void *y, int rows, int n_out,
@@ -508,10 +508,15 @@ W4Plan plan_linear_w4(int rows, int n_out, int k_in) {
     const int blocks = (n_out + 15) / 16;
     W4Plan p{};
     p.slices = 1;
-    // up to 16 rows and six blocks per CU: the input split, one workgroup per CU
+    // Up to 16 rows and six blocks per CU: the input split, one workgroup per CU
     // (4096 to 24576, 16 rows: 15.8 us, the feature split 19.6; 2560 to 151936:
     // 110 and 46 us)
-    if (rows <= 16 && blocks <= 6 * 256) {
+    // But each workgroup reads all of x, so where that is much and the features few,
+    // slices of the feature split (16 rows, 12288 to 4096: 15.1 us, 12.8 in four
+    // slices; 25600 to 5120: 33 and 21; 8192 to 4096: 10.6 and 10.9; 8 rows, 12288
+    // to 4096: 11.2 and 12.6).
+    const bool much_x = blocks < 2 * 256 && rows * k_in > 144 * 1024;
+    if (rows <= 16 && blocks <= 6 * 256 && !much_x) {
         p.fb = blocks <= 4 * 256 ? (blocks + 255) / 256 : 6;
         p.groups = (blocks + p.fb - 1) / p.fb;
         return p;
@@ -521,11 +526,12 @@ W4Plan plan_linear_w4(int rows, int n_out, int k_in) {
     // 33.5 us with one, 28.3 with two, 25.9 with four, now 22.5; 2560 to 40000: 30.3,
     // 26.9 and 29.6, now 22.4).
     p.wide = true;
-    p.kw = rows <= 16 ? 1 : blocks <= 8 * 256 ? 4 : blocks <= 20 * 256 ? 2 : 1;
+    p.kw = rows <= 16 && !much_x ? 1 : blocks <= 8 * 256 ? 4 : blocks <= 20 * 256 ? 2 : 1;
     const int fg = kW4Waves / p.kw;
     // fewer than two blocks per CU: slices of at least two chunks, so a workgroup
     // reads less of x (64 rows, 4096 to 4096: 13.6 us, 23.4 without, now 13.0; the
-    // last workgroup to arrive adding the slices up instead of w4_sum: 16.8)
+    // last workgroup to arrive adding the slices up instead of w4_sum: 16.8), at most
+    // four (12288 to 4096: 18.8 us, 20.2 with eight, 22.5 with two)
     const int chunks = (k_in + 128 * p.kw - 1) / (128 * p.kw);
     if (blocks < 2 * 256)
         p.slices = std::max(1, std::min({kW4MaxSlices, chunks / 2, 5 * fg * 256 / blocks}));
@@ -574,13 +580,17 @@ wf_status_t launch_linear_w4(const uint16_t *x, const uint8_t *w, const uint16_t
         linear_w4_wide<NBV, FBV, KWV><<<grid, block, 0, stream>>>(x, w, res, y, rows, n_out,  \
                                                                   k_in, f32_out, quads, part);\
     else
-#define WF_W4_MANY(NBV, KWV) WF_W4(NBV, 3, KWV) WF_W4(NBV, 4, KWV) WF_W4(NBV, 5, KWV)
-#define WF_W4_ROW(NBV, KWV) WF_W4(NBV, 1, KWV) WF_W4(NBV, 2, KWV) WF_W4_MANY(NBV, KWV)
-    WF_W4_ROW(1, 1) WF_W4_MANY(2, 1) WF_W4_MANY(3, 1) WF_W4_MANY(4, 1)
+#define WF_W4_FEW(NBV, KWV) WF_W4(NBV, 1, KWV) WF_W4(NBV, 2, KWV)
+#define WF_W4_SOME(NBV, KWV) WF_W4(NBV, 3, KWV) WF_W4(NBV, 4, KWV)
+#define WF_W4_MANY(NBV, KWV) WF_W4_SOME(NBV, KWV) WF_W4(NBV, 5, KWV)
+    // (what the plan can ask for)
+    WF_W4_FEW(1, 1) WF_W4_MANY(1, 1) WF_W4_MANY(2, 1) WF_W4_MANY(3, 1) WF_W4_MANY(4, 1)
     WF_W4_MANY(2, 2) WF_W4_MANY(3, 2) WF_W4_MANY(4, 2)
-    WF_W4_ROW(2, 4) WF_W4_ROW(3, 4) WF_W4_ROW(4, 4)
+    WF_W4_FEW(1, 4) WF_W4_FEW(2, 4) WF_W4_FEW(3, 4) WF_W4_FEW(4, 4)
+    WF_W4_SOME(1, 4) WF_W4_SOME(2, 4) WF_W4_SOME(3, 4) WF_W4_SOME(4, 4)
     return WF_ERR_UNSUPPORTED;
-#undef WF_W4_ROW
+#undef WF_W4_FEW
+#undef WF_W4_SOME
 #undef WF_W4_MANY
 #undef WF_W4
     if (p.slices > 1) {

@@ -78,6 +78,8 @@ SHAPES = [
     (11, 2560, 9728), (16, 1024, 4096), (17, 130, 1024), (31, 48, 64), (32, 257, 2560),
     (33, 4096, 512), (47, 100, 4096), (61, 3001, 2560), (64, 512, 12288), (64, 5, 32),
     (48, 24576, 544), (12, 16384, 1056), (1, 40, 40960),
+    # (few features and much x: slices)
+    (16, 300, 12352), (13, 1001, 12000), (4, 17, 40992),
 ]
 
 
@@ -156,7 +158,7 @@ def test_linear_odd_addresses(rows, n_out, k_in, out):
         assert buf[:at].isnan().all() and buf[at + rows * n_out:].isnan().all()
 
 
-@pytest.mark.parametrize("rows,n_out,k_in", [(3, 40, 96), (20, 300, 160), (18, 33000, 64),
+@pytest.mark.parametrize("rows,n_out,k_in", [(3, 40, 96), (20, 300, 160), (18, 33000, 64), (16, 40, 10016),
                                              (5, 30000, 32)])
 def test_linear_infinite_inputs(rows, n_out, k_in):
     """An infinity, also among the last inputs: infinities of the weight's sign
