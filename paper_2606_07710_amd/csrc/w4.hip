@@ -109,7 +109,7 @@ template <int FB>
 __global__ __launch_bounds__(kW4Waves * kWave) void linear_w4(
     const uint16_t *__restrict__ x, const uint8_t *__restrict__ w, const uint16_t *res, void *y,
     int rows, int n_out, int k_in, bool f32_out) {
-    constexpr int U = FB == 1 ? 4 : FB <= 4 ? 2 : 1;
+    constexpr int U = FB == 1 ? 4 : 2;
     __shared__ float zs[kW4Waves][16][17];
     const int f0 = 16 * FB * blockIdx.x;
     const int wave = wave_id();
@@ -200,7 +200,7 @@ __global__ __launch_bounds__(kW4Waves * kWave) void linear_w4(
 // up to FB blocks of 16 features, of KW waves that share the input among them.
 // All walk the input (or slice blockIdx.y of it) together in chunks of KW tiles
 // of 128 inputs, one per wave, whose x, all rows, is staged in LDS, so a wave
-// reads it once for all its blocks; the next chunks' codes and x are on their way
+// reads it once for all its blocks; the next chunk's codes and x are on their way
 // to registers meanwhile.  KW > 1 is for few blocks: a wave of one block reads 4 KB of x per 1
 // KB of codes and 16 rows from LDS, so with 64 rows the waves ask it for more than
 // the 128 bytes a cycle it has; a quarter of the input and four times the blocks
@@ -216,9 +216,9 @@ __global__ __launch_bounds__(kW4Waves * kWave) void linear_w4_wide(
     constexpr int XG = 16 * NB * GRAN;               // ... of the chunk, XT of them a thread's
     constexpr int XT = (XG + kW4Waves * kWave - 1) / (kW4Waves * kWave);
     constexpr int FG = kW4Waves / KW;
-    // chunks of codes held or on their way (three where the registers take them)
-    constexpr int R = NB == 1 || (KW == 4 && NB * FB >= 16) ? 2 : 3;
-    __shared__ u32x4 xs[2][XG];
+    // (with room for all threads' granules: under a condition the loads would move
+    // behind the codes' to the stores, 1 row, 4096 to 128256: 55 us, 47 without)
+    __shared__ u32x4 xs[2][XT * kW4Waves * kWave];
     const int wave = wave_id();
     const int kw = wave % KW, fg = wave / KW;
     const int lane = threadIdx.x % kWave;
@@ -249,16 +249,14 @@ __global__ __launch_bounds__(kW4Waves * kWave) void linear_w4_wide(
         for (int nb = 0; nb < NB; ++nb)
             acc[fb][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    // Codes are asked for two chunks ahead, or one, x one ahead (61 rows, 2560 to
-    // 151936: 67 us, 70 with codes one ahead; up to 16 rows one is better, 46 and
-    // 49 us).  No branch surrounds the loads: the compiler would lose count of
-    // those in flight and wait for all (one row: 42 us, 51 with a branch at the end
-    // of the input).
+    // No branch surrounds the loads: the compiler would lose count of those in
+    // flight and wait for all (one row, 2560 to 151936: 42 us, 51 with a branch at
+    // the end of the input).
     struct Codes {
         u32x4 w[FB];
         unsigned s[FB];
     };
-    Codes ring[R];
+    Codes ring[2];
     u32x4 xr[XT];
     auto load_w = [&](Codes &q, int ch) __attribute__((always_inline)) {
         const unsigned at = (unsigned)(KW * ch + kw) * kW4Tile;
@@ -283,22 +281,20 @@ __global__ __launch_bounds__(kW4Waves * kWave) void linear_w4_wide(
         for (int j = 0; j < XT; ++j) {
             const int idx = threadIdx.x + j * kW4Waves * kWave;
             const int r = idx / GRAN, g = idx % GRAN;
-            if (XG % (kW4Waves * kWave) == 0 || idx < XG)
-                xs[buf][r * GRAN + (g ^ (r & 7))] = xr[j];
+            xs[buf][r * GRAN + (g ^ (r & 7))] = xr[j];
         }
     };
     // every wave's LDS writes are done; loads in flight stay so
     auto barrier = [] { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
-    // One chunk, its codes in ring[I].
+    // One chunk, its codes in ring[I], its x in buffer I.
     auto step = [&](auto it, int ch) __attribute__((always_inline)) {
         constexpr int I = decltype(it)::value;
         load_x(ch + 1);
         __builtin_amdgcn_sched_barrier(0);           // (x first: its wait leaves the codes be)
-        load_w(ring[(I + R - 1) % R], ch + R - 1);
+        load_w(ring[1 - I], ch + 1);
         __builtin_amdgcn_sched_barrier(0);
         const Codes &now = ring[I];
-        const int buf = (ch - c_first) & 1;
-        const u32x4 *xb = xs[buf];
+        const u32x4 *xb = xs[I];
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) {
             bf16x8 xo[NB];
@@ -315,28 +311,22 @@ __global__ __launch_bounds__(kW4Waves * kWave) void linear_w4_wide(
                     acc[fb][nb] = mfma16x16x32(wo, xo[nb], acc[fb][nb]);
             }
         }
-        stage_x(1 - buf);
+        stage_x(1 - I);
         barrier();
     };
     load_x(c_first);
     __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int i = 0; i < R - 1; ++i)
-        load_w(ring[i], c_first + i);
+    load_w(ring[0], c_first);
     __builtin_amdgcn_sched_barrier(0);
     stage_x(0);
     barrier();
     int ch = c_first;
-    for (; ch + R <= c_end; ch += R) {
+    for (; ch + 1 < c_end; ch += 2) {
         step(ic<0>{}, ch);
         step(ic<1>{}, ch + 1);
-        if constexpr (R > 2)
-            step(ic<R - 1>{}, ch + 2);
     }
     if (ch < c_end)
         step(ic<0>{}, ch);
-    if (R > 2 && ch + 1 < c_end)
-        step(ic<1>{}, ch + 1);
     // lane (m16, c4) holds features 4*c4 .. +3 of row m16
     auto put = [&](int fb, int nb, f32x4 z) __attribute__((always_inline)) {
         const int r = 16 * nb + m16, f = 16 * (b_first + fb) + 4 * c4;
@@ -508,25 +498,30 @@ W4Plan plan_linear_w4(int rows, int n_out, int k_in) {
     const int blocks = (n_out + 15) / 16;
     W4Plan p{};
     p.slices = 1;
-    // Up to 16 rows and six blocks per CU: the input split, one workgroup per CU
-    // (4096 to 24576, 16 rows: 15.8 us, the feature split 19.6; 2560 to 151936:
-    // 110 and 46 us)
-    // But each workgroup reads all of x, so where that is much and the features few,
-    // slices of the feature split (16 rows, 12288 to 4096: 15.1 us, 12.8 in four
-    // slices; 25600 to 5120: 33 and 21; 8192 to 4096: 10.6 and 10.9; 8 rows, 12288
-    // to 4096: 11.2 and 12.6).
+    // Up to 16 rows and three blocks per CU: the input split, one workgroup per CU
+    // (one row, 4096 to 8192: 6.3 us, the feature split 7.4; 16 rows, 4096 to 16384:
+    // 12.1 and 11.1).  But each workgroup reads all of x, so where that is much and
+    // the features few, slices of the feature split (16 rows, 12288 to 4096: 15.1
+    // us, 12.4 in four slices; 25600 to 5120: 33 and 21; 8192 to 4096: 10.6 and
+    // 10.9; 8 rows, 12288 to 4096: 11.2 and 12.6).
     const bool much_x = blocks < 2 * 256 && rows * k_in > 144 * 1024;
-    if (rows <= 16 && blocks <= 6 * 256 && !much_x) {
-        p.fb = blocks <= 4 * 256 ? (blocks + 255) / 256 : 6;
+    if (rows <= 16 && blocks <= 3 * 256 && !much_x) {
+        p.fb = (blocks + 255) / 256;
         p.groups = (blocks + p.fb - 1) / p.fb;
         return p;
     }
-    // Of more rows the LDS reads of x bound a wave of few blocks: four waves to a
-    // feature group up to eight blocks per CU, two up to 20 (64 rows, 4096 to 24576:
-    // 33.5 us with one, 28.3 with two, 25.9 with four, now 22.5; 2560 to 40000: 30.3,
-    // 26.9 and 29.6, now 22.4).
+    // As many waves to a feature group as leave each up to five blocks: more loads
+    // in flight (one row, 4096 to 32000: 23.0 us with one, 19.7 with two, 15.2 with
+    // four; 16 rows, 4096 to 16384: 12.1 with four, 11.1 with eight; to 64000: 37,
+    // 26.7 and 28.0).  Of more than 16 rows the LDS reads of x weigh against it: four
+    // up to eight blocks per CU, two up to 20 (64 rows, 4096 to 24576: 33.5 us with
+    // one, 28.3 with two, 25.9 with four, now 21.6; 2560 to 40000: 30.3, 26.9 and
+    // 29.6, now 21.5).
     p.wide = true;
-    p.kw = rows <= 16 && !much_x ? 1 : blocks <= 8 * 256 ? 4 : blocks <= 20 * 256 ? 2 : 1;
+    if (rows <= 16)
+        p.kw = much_x ? 4 : blocks <= 5 * 256 ? 8 : blocks <= 10 * 256 ? 4 : blocks <= 20 * 256 ? 2 : 1;
+    else
+        p.kw = blocks <= 8 * 256 ? 4 : blocks <= 20 * 256 ? 2 : 1;
     const int fg = kW4Waves / p.kw;
     // fewer than two blocks per CU: slices of at least two chunks, so a workgroup
     // reads less of x (64 rows, 4096 to 4096: 13.6 us, 23.4 without, now 13.0; the
@@ -564,7 +559,7 @@ wf_status_t launch_linear_w4(const uint16_t *x, const uint8_t *w, const uint16_t
         linear_w4<FBV><<<p.groups, block, 0, stream>>>(x, w, res, y, rows, n_out, k_in,       \
                                                        f32_out);                              \
     else
-        WF_W4(1) WF_W4(2) WF_W4(3) WF_W4(4) WF_W4(6)
+        WF_W4(1) WF_W4(2) WF_W4(3)
         return WF_ERR_UNSUPPORTED;
 #undef WF_W4
         return hipGetLastError() == hipSuccess ? WF_OK : WF_ERR_HIP;
@@ -584,10 +579,11 @@ wf_status_t launch_linear_w4(const uint16_t *x, const uint8_t *w, const uint16_t
 #define WF_W4_SOME(NBV, KWV) WF_W4(NBV, 3, KWV) WF_W4(NBV, 4, KWV)
 #define WF_W4_MANY(NBV, KWV) WF_W4_SOME(NBV, KWV) WF_W4(NBV, 5, KWV)
     // (what the plan can ask for)
-    WF_W4_FEW(1, 1) WF_W4_MANY(1, 1) WF_W4_MANY(2, 1) WF_W4_MANY(3, 1) WF_W4_MANY(4, 1)
-    WF_W4_MANY(2, 2) WF_W4_MANY(3, 2) WF_W4_MANY(4, 2)
+    WF_W4_MANY(1, 1) WF_W4_MANY(2, 1) WF_W4_MANY(3, 1) WF_W4_MANY(4, 1)
+    WF_W4_MANY(1, 2) WF_W4_MANY(2, 2) WF_W4_MANY(3, 2) WF_W4_MANY(4, 2)
     WF_W4_FEW(1, 4) WF_W4_FEW(2, 4) WF_W4_FEW(3, 4) WF_W4_FEW(4, 4)
-    WF_W4_SOME(1, 4) WF_W4_SOME(2, 4) WF_W4_SOME(3, 4) WF_W4_SOME(4, 4)
+    WF_W4_MANY(1, 4) WF_W4_SOME(2, 4) WF_W4_SOME(3, 4) WF_W4_SOME(4, 4)
+    WF_W4(1, 4, 8) WF_W4(1, 5, 8)
     return WF_ERR_UNSUPPORTED;
 #undef WF_W4_FEW
 #undef WF_W4_SOME

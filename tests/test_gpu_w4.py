@@ -122,11 +122,12 @@ def test_linear(rows, n_out, k_in, out, res):
     assert torch.equal(again, y)
 
 
-# Many features: the feature split of up to 16 rows, two waves and one to a
-# feature group, several rounds of workgroups, blocks that do not divide evenly.
+# Many features: the feature split of up to 16 rows, from eight waves to a feature
+# group to one, several rounds of workgroups, blocks that do not divide evenly.
 @pytest.mark.parametrize("rows,n_out,k_in", [
     (5, 30000, 96), (12, 82000, 64), (16, 200000, 32), (33, 40000, 160), (17, 66004, 96),
     (50, 36002, 288), (61, 90001, 64), (20, 140000, 32), (64, 170000, 32),
+    (7, 20400, 1312), (16, 45000, 544), (2, 70000, 96), (10, 100000, 64), (13, 24000, 2080),
 ])
 def test_linear_many_features(rows, n_out, k_in):
     print("many features", rows, n_out, k_in, flush=True)
