@@ -5,8 +5,13 @@
 //
 // A workgroup owns one block of one head, K or V (append), or the up to three
 // blocks that a path can touch (compaction), so a block's scale needs no
-// exchange between workgroups.  K blocks are [32][D], V blocks [D][32]: the
-// rows are staged in LDS and leave in 16-byte pieces of either order.
+// exchange between workgroups.  K blocks are [32][D], V blocks [D][32].
+//
+// Bound by: few tokens, the launch and one trip to memory (16 tokens, 8 heads:
+// 3.8 us of 1.7 that an empty launch takes); many, the bytes (8190 tokens, 50
+// MB: 12.0 us, 4.2 TB/s, where a large copy reaches 5.0).  Compaction: the
+// launch and two dependent trips, the path before the rows it picks from LDS
+// (one layer 4.7 us, 36 layers 6.0).
 #include "wf_api_internal.h"
 #include "wf_lowbit.h"
 
@@ -53,6 +58,8 @@ struct AppendParams {
 // its 16 values as the four words that they are in the block (4 dims of a row
 // in K, 4 rows of a dim in V).  Everything is loaded before anything is used,
 // one trip to memory; V's words are put in order in LDS and leave as 16 bytes.
+// (Rows staged as fp32 in LDS, new ones, old ones and the scale loaded one
+// after the other: 4.15 us for 16 tokens, 13.4 for 8190.)
 template <int D, bool BF16>
 __global__ __launch_bounds__(2 * D) void kv8_append(AppendParams a) {
     __shared__ float part[2 * D / kWave];
