@@ -302,7 +302,11 @@ def _at(stream):
     """(device index, raw stream) of a low-bit call: its tensors lie on the
     current device, the stream is the one given or that device's current one."""
     dev, raw = _current()
-    return dev, raw if stream is None else stream.cuda_stream
+    if stream is None:
+        return dev, raw
+    if getattr(stream, "device_index", dev) != dev:
+        raise ValueError("the stream must be one of the current device")
+    return dev, stream.cuda_stream
 
 
 def _on(stream):
@@ -855,12 +859,11 @@ class W4Weight:
             raise ValueError("codes and scales hold bytes")
         dev, raw = _at(stream)
         n = int(lib.wf_w4_packed_bytes(rows, 2 * half))
-        self.shape, self.device, self.dev = (rows, 2 * half), codes.device, dev
+        self.shape, self.device = (rows, 2 * half), codes.device
         src = _ptr(codes, dev, "codes"), _ptr(scales, dev, "scales")
         with _on(stream):
             self.packed = torch.empty(n, dtype=torch.uint8, device=codes.device)
-        self.ptr = self.packed.data_ptr()
-        _check(lib.wf_w4_pack(*src, rows, 2 * half, self.ptr, n, raw), "wf_w4_pack")
+        _check(lib.wf_w4_pack(*src, rows, 2 * half, self.packed.data_ptr(), n, raw), "wf_w4_pack")
 
 
 def wf_w4_quantize(w, stream=None):
@@ -892,7 +895,8 @@ def wf_linear_w4(x, weight, out, residual=None, workspace=None, stream=None):
     n, k_in = x.shape
     n_out, cols = weight.shape
     shape = out.shape
-    if cols != k_in or shape != (n, n_out) or weight.dev != dev:
+    packed = weight.packed
+    if cols != k_in or shape != (n, n_out) or packed.get_device() != dev:
         raise ValueError("x, weight and out do not match")
     if x.dtype != torch.bfloat16:
         raise TypeError("x is bf16")
@@ -902,7 +906,7 @@ def wf_linear_w4(x, weight, out, residual=None, workspace=None, stream=None):
         need = wf_linear_w4_workspace_bytes(n, n_out, k_in)
         with _on(stream):
             workspace = alloc_workspace(need, x.device) if need else None
-    st = lib.wf_linear_w4(_ptr(x, dev, "x"), weight.ptr, _ptr(residual, dev, "residual"),
+    st = lib.wf_linear_w4(_ptr(x, dev, "x"), packed.data_ptr(), _ptr(residual, dev, "residual"),
                           _dtype_code(out), _ptr(out, dev, "out"), n, n_out, k_in,
                           _ptr(workspace, dev, "workspace"),
                           0 if workspace is None else workspace.numel(), raw)

@@ -345,6 +345,29 @@ def test_attention_is_the_same_for_any_bytes_behind():
         assert torch.equal(o.view(torch.int16), outs[0].view(torch.int16))
 
 
+@pytest.mark.parametrize("dt,dh,gamma,ctx", [("f32", 64, 5, 900), ("f32", 128, 3, 20),
+                                             ("bf16", 64, 7, 83), ("bf16", 128, 16, 40),
+                                             ("bf16", 128, 40, 300)])
+def test_attention_short_is_the_same_for_any_bytes_behind(dt, dh, gamma, ctx):
+    print("bytes behind", dt, dh, gamma, ctx, flush=True)
+    hq, hkv = 8, 2
+    q = _normal(1, gamma, hq, dh, dtype=DT[dt]).to(DEV)
+    outs = []
+    for fill in (0, 0x7f, 0xff):
+        c = _filled(2, hkv, ctx + gamma + 200, dh, rows=ctx + gamma)
+        n, b = ctx + gamma, (ctx + gamma + 31) // 32
+        r = R.Cache(c)
+        r.codes[:, :, n:] = fill
+        r.scales[:, :, b:] = fill
+        _load(c, r)
+        outs.append(torch.empty_like(q))
+        wf.wf_kv8_verify_attn(q, c, outs[-1], ctx)
+    torch.cuda.synchronize()
+    assert outs[0].isfinite().all()
+    for o in outs[1:]:
+        assert torch.equal(o, outs[0])
+
+
 def test_attention_nan_stays_in_its_row():
     """A NaN in one row's query is in that row's output alone."""
     gamma, ctx, hq, hkv, dh = 16, 300, 32, 8, 128

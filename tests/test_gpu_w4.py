@@ -1,5 +1,7 @@
 """4-bit weights on the GPU against plain 64-bit definitions: the quantiser
 exactly, the product within the roundings it makes."""
+import copy
+
 import numpy as np
 import pytest
 import torch
@@ -229,6 +231,38 @@ def test_linear_extreme_scales_and_nan():
     assert y[:, 5].isnan().all()
     keep = [i for i in range(48) if i != 5]
     _check(x, codes[keep], scales[keep], y[:, keep], out="f32")
+
+
+def test_weight_copies_stand_alone():
+    """A deep copy of a packed weight holds its own memory."""
+    codes, scales = _weight(3, 48, 256)
+    x = _normal(2, 5, 256).to(DEV)
+    w = wf.W4Weight(codes.to(DEV), scales.to(DEV))
+    mine = copy.deepcopy(w)
+    w.packed.zero_()
+    del w
+    y = torch.empty(5, 48, device=DEV)
+    wf.wf_linear_w4(x, mine, y)
+    torch.cuda.synchronize()
+    _check(x.cpu(), codes, scales, y, out="f32")
+
+
+def test_weight_on_a_side_stream():
+    """Quantised, packed and used on a stream of its own, workspaces included."""
+    side = torch.cuda.Stream()
+    w16 = _normal(4, 130, 12352).to(DEV)
+    x = _normal(5, 16, 12352).to(DEV)
+    codes, scales = wf.wf_w4_quantize(w16)
+    here = torch.empty(16, 130, device=DEV)
+    wf.wf_linear_w4(x, wf.W4Weight(codes, scales), here)
+    side.wait_stream(torch.cuda.current_stream())
+    for _ in range(3):
+        there = torch.zeros(16, 130, device=DEV)
+        side.wait_stream(torch.cuda.current_stream())
+        w = wf.W4Weight(*wf.wf_w4_quantize(w16, stream=side), stream=side)
+        wf.wf_linear_w4(x, w, there, stream=side)
+        side.synchronize()
+        assert torch.equal(there, here)
 
 
 def test_quantised_layer_of_its_own():

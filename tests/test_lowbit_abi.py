@@ -241,7 +241,7 @@ def _kv8(hkv=2, cap=70, dh=64, layers=None, **kw):
 
 def _w4(dev=0):
     w = wf.W4Weight.__new__(wf.W4Weight)
-    w.packed, w.shape, w.ptr, w.dev = _bytes(1088), (16, 64), 8, dev
+    w.packed, w.shape = _bytes(1088, on=dev), (16, 64)
     return w
 
 
@@ -303,6 +303,15 @@ def test_python_calls_refuse_other_devices():
             lambda: _kv8(v=_bytes(2, 3, 64, 32, on=1)), lambda: _kv8(k=_bytes(2, 3, 32, 64, on=-1))):
         with pytest.raises(ValueError):
             call()
+
+
+def test_python_calls_refuse_other_devices_streams():
+    class Far:
+        cuda_stream, device_index = 0, 1
+    with pytest.raises(ValueError):
+        wf.wf_kv8_append(Fake(4, 2, 64), Fake(4, 2, 64), _kv8(), 0, stream=Far)
+    with pytest.raises(ValueError):
+        wf.wf_linear_w4(Fake(4, 64), _w4(), Fake(4, 16), stream=Far)
 
 
 def _far_cache():
