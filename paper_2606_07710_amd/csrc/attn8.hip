@@ -118,8 +118,8 @@ __device__ __forceinline__ float row_max(float m) {
 }
 
 // Waves: KS key streams x RG row groups of 16 rows; a stage of the ring holds
-// one tile of each stream.
-template <int D, int RG, int KS, int NBUF>
+// one tile of each stream.  MANY: several workgroups for the rows of a split.
+template <int D, int RG, int KS, int NBUF, bool MANY>
 __global__ __launch_bounds__(64 * RG * KS) void attn8_tiles(Attn8Params a) {
     constexpr int HALF = kTileKeys8 * D;             // bytes of a K or V tile
     constexpr int TILE = 2 * HALF + 1024;            // codes, then 16 bytes around the scales
@@ -139,7 +139,7 @@ __global__ __launch_bounds__(64 * RG * KS) void attn8_tiles(Attn8Params a) {
 
     // ---- which (kv head, split, row group) this workgroup owns ----------------
     int g = blockIdx.x, split = blockIdx.y, rgw = 0;
-    if (a.n_row_groups > 1) {
+    if constexpr (MANY) {
         // the row groups of one (head, split) on one XCD, adjacent in its
         // dispatch order: all but the first find the tiles in its L2
         const int xcd = blockIdx.x & 7, w = blockIdx.x >> 3;
@@ -495,16 +495,37 @@ __global__ __launch_bounds__(64 * RG * KS) void attn8_tiles(Attn8Params a) {
         return;
     const size_t pr = ((size_t)split * a.gamma + qi) * a.n_q_heads + g * a.group +
                       (row - qi * a.group);
-    uint2 *dst = reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.ws_o) + pr * D);
     if (a.splits == 1) {                 // (every row sees itself: l > 0)
         const float inv = 1.f / l;
 #pragma unroll
         for (int md = 0; md < MD; ++md)
             o[md] *= inv;
     }
+    // Lane groups 2i and 2i + 1 hold 4 dims each of every 16; they trade, so that
+    // the first has 8 of the even 16s and the second 8 of the odd ones: 16-byte
+    // stores, 64 bytes of a row together (32 rows, 1K keys: 8.0 -> 7.85 us).  Many
+    // rows' partials go past the L2, from which the merge, on another XCD, would
+    // have to fetch them while the next call's are written in their place (244
+    // rows, 8K keys, one workspace: 21.0 -> 19.2 us; several: 18.4 either way; 64
+    // rows, 32K keys: 22.5 and 22.7, so not for those).
+    u32x4 *dst = reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(a.ws_o) + pr * D);
 #pragma unroll
-    for (int md = 0; md < MD; ++md)
-        dst[md * 4 + c4] = uint2{pack_bf16x2(o[md][0], o[md][1]), pack_bf16x2(o[md][2], o[md][3])};
+    for (int md = 0; md < MD; md += 2) {
+        u32x4 v;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const auto r = __builtin_amdgcn_permlane16_swap(
+                pack_bf16x2(o[md][2 * i], o[md][2 * i + 1]),
+                pack_bf16x2(o[md + 1][2 * i], o[md + 1][2 * i + 1]), false, false);
+            v[i] = r[0];
+            v[2 + i] = r[1];
+        }
+        u32x4 *to = dst + (md + (c4 & 1)) * 2 + (c4 >> 1);
+        if constexpr (MANY)
+            __builtin_nontemporal_store(v, to);
+        else
+            *to = v;
+    }
     if (c4 == 0 && a.splits > 1) {
         a.ws_ml[pr * 2] = ref;
         a.ws_ml[pr * 2 + 1] = l;
@@ -749,16 +770,19 @@ wf_status_t launch_attn8(wf_dtype_t dt, const void *q, const wf_kv8_cache_t &c, 
         // (exact for rows below 2^14 in groups of 2 to 2^8)
         a.group_magic = (unsigned)((1ull << 32) / a.group + 1);
         const int units = c.n_kv_heads * p.splits;
-        const dim3 grid = p.n_row_groups > 1 ? dim3((units + 7) / 8 * 8 * p.n_row_groups)
+        const bool many = p.n_row_groups > 1;
+        const dim3 grid = many ? dim3((units + 7) / 8 * 8 * p.n_row_groups)
                                              : dim3(c.n_kv_heads, p.splits);
-#define WF_ATTN8(DV, RGV, KSV, NBUFV)                                                      \
-    if (c.head_dim == DV && p.rg == RGV && p.ks == KSV)                                    \
-        attn8_tiles<DV, RGV, KSV, NBUFV><<<grid, 64 * RGV * KSV, 0, stream>>>(a);          \
+#define WF_ATTN8(DV, RGV, KSV, NBUFV, MANYV)                                               \
+    if (c.head_dim == DV && p.rg == RGV && p.ks == KSV && many == MANYV)                   \
+        attn8_tiles<DV, RGV, KSV, NBUFV, MANYV><<<grid, 64 * RGV * KSV, 0, stream>>>(a);   \
     else
-        WF_ATTN8(128, 1, 2, 2) WF_ATTN8(128, 2, 2, 2) WF_ATTN8(128, 4, 2, 2)
-        WF_ATTN8(128, 4, 1, 2) WF_ATTN8(128, 1, 1, 2) WF_ATTN8(128, 2, 1, 2)
-        WF_ATTN8(64, 1, 1, 2) WF_ATTN8(64, 2, 1, 2)
-        WF_ATTN8(64, 1, 2, 2) WF_ATTN8(64, 2, 2, 4) WF_ATTN8(64, 4, 2, 4) WF_ATTN8(64, 4, 1, 4)
+        WF_ATTN8(128, 1, 2, 2, false) WF_ATTN8(128, 2, 2, 2, false) WF_ATTN8(128, 4, 2, 2, false)
+        WF_ATTN8(128, 1, 1, 2, false) WF_ATTN8(128, 2, 1, 2, false) WF_ATTN8(128, 4, 1, 2, false)
+        WF_ATTN8(128, 4, 1, 2, true)
+        WF_ATTN8(64, 1, 2, 2, false) WF_ATTN8(64, 2, 2, 4, false) WF_ATTN8(64, 4, 2, 4, false)
+        WF_ATTN8(64, 1, 1, 2, false) WF_ATTN8(64, 2, 1, 2, false) WF_ATTN8(64, 4, 1, 4, false)
+        WF_ATTN8(64, 4, 1, 4, true)
         return WF_ERR_UNSUPPORTED;
 #undef WF_ATTN8
     } else {
