@@ -698,13 +698,15 @@ __global__ __launch_bounds__(64 * kRowWaves) void attn8_rows(Attn8Params a) {
 // take a workgroup of one stream, two per CU, which do not wait for each other's
 // barriers (128 rows, 64K keys: 51.4 us, 53.0 as one workgroup of eight waves; 244
 // rows, 8K keys: 18.9 and 21.5 us, though the tiles are then read from L2 twice as
-// often).  No workgroup is without a tile.  Where a tile is left for each, one
-// stream (32 rows, 1K keys: 8.9 -> 8.1 us; 64 rows: 10.9 -> 9.0).  Few tiles stay
-// one split, whose workgroup writes the output and spares the merge: up to two
-// steps (32 rows, 500 keys: 7.6 us, 7.9 as four splits), or one of 64 rows, whose
-// steps take twice as long (256 keys: 7.1 and 8.2 us; 516 keys in three: 12.3 and
-// 8.7).  fp32: splits only where the rows leave CUs idle (256 rows and heads,
-// 2K keys: 13.8 us, 17.3 as four; 32, 4K keys: 25.1 and 8.8 as eight).
+// often).  No workgroup is without a tile.  Where each has few, one stream, whose
+// first stage is there sooner and which has nothing to join at its end (32 rows,
+// 1K keys: 8.9 -> 8.1 us, 8K 13.3 -> 12.6, but 32K 22.4 -> 22.7; 64 rows, 1K keys:
+// 10.9 -> 9.0, 8K 15.3 -> 13.7, 32K 25.9 -> 23.7, 64K 38.4 both ways, 128K 59.6 ->
+// 67.8).  The fewest stay one split, whose workgroup writes the output and spares
+// the merge: up to two steps (32 rows, 500 keys: 7.6 us, 7.9 as four splits), or one
+// of 64 rows, whose steps take twice as long (256 keys: 7.1 and 8.2 us; 516 keys in
+// three: 12.3 and 8.7).  fp32: splits only where the rows leave CUs idle (256 rows
+// and heads, 2K keys: 13.8 us, 17.3 as four; 32, 4K keys: 25.1 and 8.8 as eight).
 AttnPlan plan_attn8(wf_dtype_t dt, int gamma, int ctx_len, int n_q_heads, int n_kv_heads,
                     int head_dim, int num_splits) {
     AttnPlan p{};
@@ -730,7 +732,8 @@ AttnPlan plan_attn8(wf_dtype_t dt, int gamma, int ctx_len, int n_q_heads, int n_
     p.splits = std::min(want, tiles);
     if (num_splits == 0 && tiles <= (p.rg == 4 ? 1 : 2) * p.ks)
         p.splits = 1;
-    if (p.splits == tiles)
+    const int each = (tiles + p.splits - 1) / p.splits;
+    if (p.splits == 1 ? each == 1 : each <= (p.rg == 4 ? 12 : 3))
         p.ks = 1;
     return p;
 }

@@ -259,6 +259,9 @@ SHAPES = [
     (2, 500, 8, 2, 128, 0), (16, 100, 32, 8, 64, 0), (17, 900, 8, 4, 64, 0),
     (8, 1200, 8, 2, 64, 0), (1, 4000, 32, 8, 128, 0), (3, 1400, 32, 8, 128, 2),
     (5, 2700, 4, 4, 64, 4),
+    # (few tiles each: one key stream; more: two)
+    (16, 2500, 4, 1, 128, 3), (16, 2500, 4, 1, 128, 1), (16, 4600, 4, 1, 64, 2),
+    (8, 1500, 4, 1, 128, 4), (8, 1500, 4, 1, 64, 3), (3, 1500, 8, 2, 128, 6),
 ]
 
 
