@@ -67,6 +67,12 @@ struct Attn8Params {
 // g ^ ((k & 3) | (k >> 4 & 1) << 2) (head_dim 64: two keys share 128 bytes, g ^
 // ((k >> 1 & 1) | (k >> 4 & 1) << 1)), V half h of dim d at
 // h ^ (d >> 2 & 1) ^ (d >> 3 & 1).
+//
+// Bound, up to 64 rows, by the cache's bytes, the first tile and the merge (16
+// rows, 32K keys of 8 heads, 67 MB: 17.5 us and the merge's 4.6; cold 23.7 in
+// all); above by the two waves per SIMD that its registers allow: products, vector
+// work and LDS reads of a tile take about half of its time (1024 rows and heads, 64K
+// keys: 50 us, 15 of products and 16 of vector work).
 // ---------------------------------------------------------------------------
 constexpr int kTileKeys8 = 128;
 constexpr int kTileBlocks = kTileKeys8 / kKv8Block;
