@@ -371,6 +371,28 @@ def test_attention_short_is_the_same_for_any_bytes_behind(dt, dh, gamma, ctx):
         assert torch.equal(o, outs[0])
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("gamma,ctx,hq,hkv,dh", [
+    (5, 300, 24, 8, 128), (1, 40, 3, 3, 64), (7, 2000, 10, 2, 64), (9, 1500, 80, 8, 128),
+])
+def test_attention_writes_its_output_and_workspace_only(dt, gamma, ctx, hq, hkv, dh):
+    print("bounds", dt, gamma, ctx, hq, hkv, dh, flush=True)
+    c = _filled(4, hkv, ctx + gamma, dh)
+    held = [t.clone() for t in (c.k, c.v, c.k_scale, c.v_scale)]
+    q = _normal(1, gamma, hq, dh, dtype=DT[dt]).to(DEV)
+    n, need = q.numel(), wf.wf_kv8_verify_attn_workspace_bytes(DT[dt], gamma, ctx, hq, hkv, dh)
+    buf = torch.full((n + 512,), 7.0, dtype=DT[dt], device=DEV)
+    room = torch.full((need + 4096,), 0x5a, dtype=torch.uint8, device=DEV)
+    room[:need] = 0
+    out = buf[256:256 + n].view(gamma, hq, dh)
+    wf.wf_kv8_verify_attn(q, c, out, ctx, workspace=room[:need])
+    torch.cuda.synchronize()
+    assert (buf[:256] == 7).all() and (buf[256 + n:] == 7).all() and out.isfinite().all()
+    assert (room[need:] == 0x5a).all() and not room[:4 << 20].any()
+    for a, b in zip(held, (c.k, c.v, c.k_scale, c.v_scale)):
+        assert torch.equal(a, b)
+
+
 def test_attention_nan_stays_in_its_row():
     """A NaN in one row's query is in that row's output alone."""
     gamma, ctx, hq, hkv, dh = 16, 300, 32, 8, 128

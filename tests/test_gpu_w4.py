@@ -233,6 +233,24 @@ def test_linear_extreme_scales_and_nan():
     _check(x, codes[keep], scales[keep], y[:, keep], out="f32")
 
 
+@pytest.mark.parametrize("rows,n_out,k_in", [(17, 130, 1024), (61, 500, 4096), (16, 33, 12000),
+                                             (33, 200, 2080)])
+def test_linear_writes_its_output_and_workspace_only(rows, n_out, k_in):
+    print("bounds", rows, n_out, k_in, flush=True)
+    codes, scales = _weight(5, n_out, k_in)
+    x = _normal(6, rows, k_in)
+    w = wf.W4Weight(codes.to(DEV), scales.to(DEV))
+    need = wf.wf_linear_w4_workspace_bytes(rows, n_out, k_in)
+    room = torch.full((need + 4096,), 0x5a, dtype=torch.uint8, device=DEV)
+    buf = torch.full((rows * n_out + 32,), 7.0, device=DEV)
+    y = buf[16:16 + rows * n_out].view(rows, n_out)
+    wf.wf_linear_w4(x.to(DEV), w, y, workspace=room[:need])
+    torch.cuda.synchronize()
+    assert (room[need:] == 0x5a).all() and (room[:4 << 20] == 0x5a).all()
+    assert (buf[:16] == 7).all() and (buf[16 + rows * n_out:] == 7).all()
+    _check(x, codes, scales, y, out="f32")
+
+
 def test_weight_copies_stand_alone():
     """A deep copy of a packed weight holds its own memory."""
     codes, scales = _weight(3, 48, 256)
