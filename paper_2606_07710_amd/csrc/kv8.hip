@@ -9,7 +9,7 @@
 //
 // Bound by: few tokens, the launch and one trip to memory (16 tokens, 8 heads:
 // 3.8 us of 1.7 that an empty launch takes); many, the bytes (8190 tokens, 50
-// MB: 12.0 us, 4.2 TB/s, where a large copy reaches 5.0).  Compaction: the
+// MB: 11.6 us, 4.4 TB/s, where a large copy reaches 5.0).  Compaction: the
 // launch and two dependent trips, the path before the rows it picks from LDS
 // (one layer 4.7 us, 36 layers 6.0).
 #include "wf_api_internal.h"
@@ -58,7 +58,9 @@ struct AppendParams {
 // its 16 values as the four words that they are in the block (4 dims of a row
 // in K, 4 rows of a dim in V).  Everything is loaded before anything is used,
 // one trip to memory; V's words are put in order in LDS and leave as 16 bytes.
-// (Rows staged as fp32 in LDS, new ones, old ones and the scale loaded one
+// The codes go past the L2, where no later call of another XCD would look for
+// them (8190 tokens: 12.8 -> 11.6 us, out of HBM 14.4 -> 12.6; an attention right
+// behind takes as long as before).  (Rows staged as fp32 in LDS, new ones, old ones and the scale loaded one
 // after the other: 4.15 us for 16 tokens, 13.4 for 8190.)
 template <int D, bool BF16>
 __global__ __launch_bounds__(2 * D) void kv8_append(AppendParams a) {
@@ -141,8 +143,9 @@ __global__ __launch_bounds__(2 * D) void kv8_append(AppendParams a) {
     for (int u = 0; u < 4; ++u) {
         if (kind == 0) {
             if (i0 + u < last)
-                codes[word(u)] = f32x4_to_e4m3(f[u][0] * inv, f[u][1] * inv, f[u][2] * inv,
-                                               f[u][3] * inv);
+                __builtin_nontemporal_store(f32x4_to_e4m3(f[u][0] * inv, f[u][1] * inv,
+                                                          f[u][2] * inv, f[u][3] * inv),
+                                            codes + word(u));
         } else {
             uint32_t w = f32x4_to_e4m3(f[0][u] * inv, f[1][u] * inv, f[2][u] * inv,
                                        f[3][u] * inv);
@@ -157,7 +160,7 @@ __global__ __launch_bounds__(2 * D) void kv8_append(AppendParams a) {
         __syncthreads();
         const int c = threadIdx.x;
         if (c % 2 * 16 < last)
-            reinterpret_cast<u32x4 *>(codes)[c] = turned[c + c / 8];
+            __builtin_nontemporal_store(turned[c + c / 8], reinterpret_cast<u32x4 *>(codes) + c);
     }
     if (threadIdx.x == 0)
         *scale = (uint8_t)(e + 127);
