@@ -290,13 +290,15 @@ __global__ __launch_bounds__(kW4Waves * kWave) void linear_w4_wide(
     };
     // every wave's LDS writes are done; loads in flight stay so
     auto barrier = [] { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
-    // One chunk, its codes in ring[I], its x in buffer I.
-    auto step = [&](auto it, int ch) __attribute__((always_inline)) {
+    // One chunk, its codes in ring[I], its x in buffer I; `more`: another follows.
+    auto step = [&](auto it, auto more, int ch) __attribute__((always_inline)) {
         constexpr int I = decltype(it)::value;
-        load_x(ch + 1);
-        __builtin_amdgcn_sched_barrier(0);           // (x first: its wait leaves the codes be)
-        load_w(ring[1 - I], ch + 1);
-        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (decltype(more)::value) {
+            load_x(ch + 1);
+            __builtin_amdgcn_sched_barrier(0);       // (x first: its wait leaves the codes be)
+            load_w(ring[1 - I], ch + 1);
+            __builtin_amdgcn_sched_barrier(0);
+        }
         const Codes &now = ring[I];
         const u32x4 *xb = xs[I];
 #pragma unroll
@@ -315,8 +317,10 @@ __global__ __launch_bounds__(kW4Waves * kWave) void linear_w4_wide(
                     acc[fb][nb] = mfma16x16x32(wo, xo[nb], acc[fb][nb]);
             }
         }
-        stage_x(1 - I);
-        barrier();
+        if constexpr (decltype(more)::value) {
+            stage_x(1 - I);
+            barrier();
+        }
     };
     load_x(c_first);
     __builtin_amdgcn_sched_barrier(0);
@@ -324,13 +328,19 @@ __global__ __launch_bounds__(kW4Waves * kWave) void linear_w4_wide(
     __builtin_amdgcn_sched_barrier(0);
     stage_x(0);
     barrier();
+    constexpr std::true_type more;
+    constexpr std::false_type last;
     int ch = c_first;
-    for (; ch + 1 < c_end; ch += 2) {
-        step(ic<0>{}, ch);
-        step(ic<1>{}, ch + 1);
+    for (; ch + 2 < c_end; ch += 2) {
+        step(ic<0>{}, more, ch);
+        step(ic<1>{}, more, ch + 1);
     }
-    if (ch < c_end)
-        step(ic<0>{}, ch);
+    if (ch + 1 < c_end) {
+        step(ic<0>{}, more, ch);
+        step(ic<1>{}, last, ch + 1);
+    } else {
+        step(ic<0>{}, last, ch);
+    }
     // lane (m16, c4) holds features 4*c4 .. +3 of row m16
     auto put = [&](int fb, int nb, f32x4 z) __attribute__((always_inline)) {
         const int r = 16 * nb + m16, f = 16 * (b_first + fb) + 4 * c4;
@@ -357,8 +367,7 @@ __global__ __launch_bounds__(kW4Waves * kWave) void linear_w4_wide(
         f32x4 *meet = reinterpret_cast<f32x4 *>(xs) + fg * (KW * P * NB * kWave);
 #pragma unroll
         for (int f0 = 0; f0 < FB; f0 += P) {
-            if (f0)
-                __syncthreads();
+            __syncthreads();             // (the chunks, or the sums before, are done with)
 #pragma unroll
             for (int t = 0; t < P * NB; ++t)
                 if (f0 + t / NB < FB)
@@ -519,8 +528,8 @@ W4Plan plan_linear_w4(int rows, int n_out, int k_in) {
     // four; 16 rows, 4096 to 16384: 12.1 with four, 11.1 with eight; to 64000: 37,
     // 26.7 and 28.0).  Of more than 16 rows the LDS reads of x weigh against it: four
     // up to eight blocks per CU, two up to 20 (64 rows, 4096 to 24576: 33.5 us with
-    // one, 28.3 with two, 25.9 with four, now 21.6; 2560 to 40000: 30.3, 26.9 and
-    // 29.6, now 21.5).
+    // one, 28.3 with two, 25.9 with four, now 20.4; 2560 to 40000: 30.3, 26.9 and
+    // 29.6, now 20.8).
     p.wide = true;
     if (rows <= 16)
         p.kw = much_x ? 4 : blocks <= 5 * 256 ? 8 : blocks <= 10 * 256 ? 4 : blocks <= 20 * 256 ? 2 : 1;
@@ -528,9 +537,9 @@ W4Plan plan_linear_w4(int rows, int n_out, int k_in) {
         p.kw = blocks <= 8 * 256 ? 4 : blocks <= 20 * 256 ? 2 : 1;
     const int fg = kW4Waves / p.kw;
     // fewer than two blocks per CU: slices of at least two chunks, so a workgroup
-    // reads less of x (64 rows, 4096 to 4096: 13.6 us, 23.4 without, now 13.0; the
+    // reads less of x (64 rows, 4096 to 4096: 13.6 us, 23.4 without, now 11.5; the
     // last workgroup to arrive adding the slices up instead of w4_sum: 16.8), at most
-    // four (12288 to 4096: 18.8 us, 20.2 with eight, 22.5 with two)
+    // four (12288 to 4096: 18.8 us, now 17.3, 20.2 with eight, 22.5 with two)
     const int chunks = (k_in + 128 * p.kw - 1) / (128 * p.kw);
     if (blocks < 2 * 256)
         p.slices = std::max(1, std::min({kW4MaxSlices, chunks / 2, 5 * fg * 256 / blocks}));
