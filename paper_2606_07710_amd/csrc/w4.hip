@@ -209,7 +209,7 @@ __global__ __launch_bounds__(kW4Waves * kWave) void linear_w4(
 // ask for a quarter.  Lanes and tiles as above.  The staged x is swizzled in 16-
 // byte granules, g ^ (row & 7), so eight rows' reads meet distinct banks.  With
 // several slices each stores its fp32 sums, part[slice][row][16 * blocks], for
-// w4_sum.  Bound by HBM up to 16 rows (4096 to 24576: 13.4 us, 4.1 TB/s; 4096 to
+// w4_sum.  Bound by HBM up to 16 rows (4096 to 24576: 13.2 us, 4.1 TB/s; 4096 to
 // 128256: 46.9, 6.0) and with many features (61 rows, 2560 to 151936: 55 us, 44 MB
 // of them logits stored at the end), else by x: LDS, and L2 once per workgroup.
 template <int NB, int FB, int KW>
@@ -220,6 +220,10 @@ __global__ __launch_bounds__(kW4Waves * kWave) void linear_w4_wide(
     constexpr int XG = 16 * NB * GRAN;               // ... of the chunk, XT of them a thread's
     constexpr int XT = (XG + kW4Waves * kWave - 1) / (kW4Waves * kWave);
     constexpr int FG = kW4Waves / KW;
+    // x two chunks ahead where the registers take it easily (16 rows, 12288 to 4096:
+    // 12.55 -> 12.0 us; one row, 4096 to 24576: 12.85 -> 12.3; 64 rows, two blocks,
+    // 5120 to 16384: 20.0 -> 20.4, so not there)
+    constexpr bool X2 = NB * FB < 8;
     // (with room for all threads' granules: under a condition the loads would move
     // behind the codes' to the stores, 1 row, 4096 to 128256: 55 us, 47 without)
     __shared__ u32x4 xs[2][XT * kW4Waves * kWave];
@@ -261,7 +265,7 @@ __global__ __launch_bounds__(kW4Waves * kWave) void linear_w4_wide(
         unsigned s[FB];
     };
     Codes ring[2];
-    u32x4 xr[XT];
+    u32x4 xr[X2 ? 2 : 1][XT];
     auto load_w = [&](Codes &q, int ch) __attribute__((always_inline)) {
         const unsigned at = (unsigned)(KW * ch + kw) * kW4Tile;
 #pragma unroll
@@ -272,20 +276,21 @@ __global__ __launch_bounds__(kW4Waves * kWave) void linear_w4_wide(
     };
     // (rows and inputs past the end are zeros)
     const __amdgpu_buffer_rsrc_t xp = x_buffer(x, rows, k_in);
-    auto load_x = [&](int ch) __attribute__((always_inline)) {
+    auto load_x = [&](u32x4 (&to)[XT], int ch) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < XT; ++j) {
             const int idx = threadIdx.x + j * kW4Waves * kWave;
             const int r = idx / GRAN, g = ch * GRAN + idx % GRAN;
-            xr[j] = load_x16(xp, (unsigned)(r * k_in * 2 + g * 16), g < k_in / 8);
+            to[j] = load_x16(xp, (unsigned)(r * k_in * 2 + g * 16),
+                             g < k_in / 8 && (!X2 || ch < c_end));
         }
     };
-    auto stage_x = [&](int buf) __attribute__((always_inline)) {
+    auto stage_x = [&](const u32x4 (&from)[XT], int buf) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < XT; ++j) {
             const int idx = threadIdx.x + j * kW4Waves * kWave;
             const int r = idx / GRAN, g = idx % GRAN;
-            xs[buf][r * GRAN + (g ^ (r & 7))] = xr[j];
+            xs[buf][r * GRAN + (g ^ (r & 7))] = from[j];
         }
     };
     // every wave's LDS writes are done; loads in flight stay so
@@ -294,7 +299,7 @@ __global__ __launch_bounds__(kW4Waves * kWave) void linear_w4_wide(
     auto step = [&](auto it, auto more, int ch) __attribute__((always_inline)) {
         constexpr int I = decltype(it)::value;
         if constexpr (decltype(more)::value) {
-            load_x(ch + 1);
+            load_x(xr[X2 ? I : 0], X2 ? ch + 2 : ch + 1);
             __builtin_amdgcn_sched_barrier(0);       // (x first: its wait leaves the codes be)
             load_w(ring[1 - I], ch + 1);
             __builtin_amdgcn_sched_barrier(0);
@@ -318,15 +323,17 @@ __global__ __launch_bounds__(kW4Waves * kWave) void linear_w4_wide(
             }
         }
         if constexpr (decltype(more)::value) {
-            stage_x(1 - I);
+            stage_x(xr[X2 ? 1 - I : 0], 1 - I);
             barrier();
         }
     };
-    load_x(c_first);
+    load_x(xr[0], c_first);
     __builtin_amdgcn_sched_barrier(0);
     load_w(ring[0], c_first);
+    if constexpr (X2)
+        load_x(xr[1], c_first + 1);
     __builtin_amdgcn_sched_barrier(0);
-    stage_x(0);
+    stage_x(xr[0], 0);
     barrier();
     constexpr std::true_type more;
     constexpr std::false_type last;
