@@ -8,7 +8,7 @@
 // exchange between workgroups.  K blocks are [32][D], V blocks [D][32].
 //
 // Bound by: few tokens, the launch and one trip to memory (16 tokens, 8 heads:
-// 3.8 us of 1.7 that an empty launch takes); many, the bytes (8190 tokens, 50
+// 3.8 us, 1.7 of it what an empty launch takes); many, the bytes (8190 tokens, 50
 // MB: 11.6 us, 4.4 TB/s, where a large copy reaches 5.0).  Compaction: the
 // launch and two dependent trips, the path before the rows it picks from LDS
 // (one layer 4.7 us, 36 layers 6.0).
