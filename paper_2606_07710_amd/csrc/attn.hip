@@ -903,8 +903,23 @@ typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 constexpr int kMergeBatch = 16;          // float4 loads in flight per lane
 constexpr int kMaxSplits = 1024;
 
-// BF16: partials and output in bf16 (else fp32).
-template <int DH, bool BF16>
+// Four elements of a partial row.  Each is read once: non-temporal, where the
+// call is a bf16 one.
+template <bool PART16, bool OUT16>
+__device__ __forceinline__ f32x4 load_partial(const void *ws_o, size_t idx) {
+    if constexpr (PART16) {
+        const u32x2 pt = __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(ws_o) + idx);
+        return f32x4{bf16_to_f32((uint16_t)pt.x), bf16_to_f32((uint16_t)(pt.x >> 16)),
+                     bf16_to_f32((uint16_t)pt.y), bf16_to_f32((uint16_t)(pt.y >> 16))};
+    } else if constexpr (OUT16) {
+        return __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(ws_o) + idx);
+    } else {
+        return reinterpret_cast<const f32x4 *>(ws_o)[idx];
+    }
+}
+
+// PART16, OUT16: partials, output in bf16 (else fp32).
+template <int DH, bool PART16, bool OUT16>
 __global__ __launch_bounds__(64) void attn_merge(const void *__restrict__ ws_o,
                                                  const float *__restrict__ ws_ml,
                                                  void *out, int pairs, int splits,
@@ -924,15 +939,7 @@ __global__ __launch_bounds__(64) void attn_merge(const void *__restrict__ ws_o,
         for (int b = 0; b < B; ++b) {
             const size_t idx = (size_t)min(s0 + G * b, splits - 1) * sstride +
                                (size_t)pr * Q + d4;
-            if constexpr (BF16) {
-                // (each partial is read once: non-temporal)
-            const u32x2 pt = __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(ws_o) + idx);
-            const uint2 pk = {pt.x, pt.y};
-                v[b] = f32x4{bf16_to_f32((uint16_t)pk.x), bf16_to_f32((uint16_t)(pk.x >> 16)),
-                             bf16_to_f32((uint16_t)pk.y), bf16_to_f32((uint16_t)(pk.y >> 16))};
-            } else {
-                v[b] = reinterpret_cast<const f32x4 *>(ws_o)[idx];
-            }
+            v[b] = load_partial<PART16, OUT16>(ws_o, idx);
         }
     };
     f32x4 v[B];
@@ -978,7 +985,7 @@ __global__ __launch_bounds__(64) void attn_merge(const void *__restrict__ ws_o,
     if (grp == 0) {
         const size_t oi = (size_t)pr * DH + 4 * d4;
         const f32x4 r = acc * inv;
-        if (BF16) {
+        if (OUT16) {
             uint2 pk = {pack_bf16x2(r[0], r[1]), pack_bf16x2(r[2], r[3])};
             *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(out) + oi) = pk;
         } else {
@@ -995,7 +1002,7 @@ __global__ __launch_bounds__(64) void attn_merge(const void *__restrict__ ws_o,
 // maxima meet in a butterfly over the G groups, each lane weighs its own
 // splits in ascending order, and the weighted columns and sums meet in a
 // second fixed butterfly (every lane of a column ends with the same bits).
-template <int DH, bool BF16, int WPB>
+template <int DH, bool PART16, bool OUT16, int WPB>
 __global__ __launch_bounds__(64 * WPB) void attn_merge_one(const void *__restrict__ ws_o,
                                                            const float *__restrict__ ws_ml,
                                                            void *out, int pairs, int splits,
@@ -1016,15 +1023,7 @@ __global__ __launch_bounds__(64 * WPB) void attn_merge_one(const void *__restric
     for (int b = 0; b < B; ++b) {
         const int sp = min(grp + G * b, splits - 1);
         const size_t idx = (size_t)sp * sstride + (size_t)pr * Q + d4;
-        if constexpr (BF16) {
-            // (each partial is read once: non-temporal)
-            const u32x2 pt = __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(ws_o) + idx);
-            const uint2 pk = {pt.x, pt.y};
-            v[b] = f32x4{bf16_to_f32((uint16_t)pk.x), bf16_to_f32((uint16_t)(pk.x >> 16)),
-                         bf16_to_f32((uint16_t)pk.y), bf16_to_f32((uint16_t)(pk.y >> 16))};
-        } else {
-            v[b] = reinterpret_cast<const f32x4 *>(ws_o)[idx];
-        }
+        v[b] = load_partial<PART16, OUT16>(ws_o, idx);
         ml[b] = reinterpret_cast<const float2 *>(ws_ml)[(size_t)sp * pairs + pr];
     }
     float mx = -INFINITY;
@@ -1058,7 +1057,7 @@ __global__ __launch_bounds__(64 * WPB) void attn_merge_one(const void *__restric
     if (grp == 0) {
         const size_t oi = (size_t)pr * DH + 4 * d4;
         const f32x4 r = acc * (1.f / lsum);
-        if constexpr (BF16) {
+        if constexpr (OUT16) {
             *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(out) + oi) =
                 uint2{pack_bf16x2(r[0], r[1]), pack_bf16x2(r[2], r[3])};
         } else {
@@ -1148,42 +1147,29 @@ size_t attn_workspace_bytes(const AttnPlan &p, int gamma, int n_q_heads, int hea
     return kCounterBytes + (size_t)p.splits * pairs * (2 * sizeof(float) + (size_t)head_dim * p.part_bytes);
 }
 
-// out = the partials of all splits merged: their rows (bf16 or fp32, as out),
-// (reference, sum) pairs, and the factor that takes a difference of
-// references to log2 units.
-wf_status_t launch_attn_merge(int head_dim, bool bf16, const void *ws_o, const float *ws_ml,
-                              void *out, int pairs, int splits, float sl2, hipStream_t stream) {
+// out = the partials of all splits merged: their rows (bf16 or fp32), the
+// output's type, (reference, sum) pairs, and the factor that takes a difference
+// of references to log2 units.
+wf_status_t launch_attn_merge(int head_dim, bool part16, bool out16, const void *ws_o,
+                              const float *ws_ml, void *out, int pairs, int splits, float sl2,
+                              hipStream_t stream) {
     constexpr int kMergeWpb = 1;
-    if (splits <= (kWave / (head_dim / 4)) * kMergeBatch) {
-        dim3 g1((unsigned)cdiv(pairs, kMergeWpb)), b1(64 * kMergeWpb);
-        if (head_dim == 128) {
-            if (bf16)
-                attn_merge_one<128, true, kMergeWpb><<<g1, b1, 0, stream>>>(ws_o, ws_ml, out, pairs, splits, sl2);
-            else
-                attn_merge_one<128, false, kMergeWpb><<<g1, b1, 0, stream>>>(ws_o, ws_ml, out, pairs, splits, sl2);
-        } else {
-            if (bf16)
-                attn_merge_one<64, true, kMergeWpb><<<g1, b1, 0, stream>>>(ws_o, ws_ml, out, pairs, splits, sl2);
-            else
-                attn_merge_one<64, false, kMergeWpb><<<g1, b1, 0, stream>>>(ws_o, ws_ml, out, pairs, splits, sl2);
-        }
-        return hipGetLastError() == hipSuccess ? WF_OK : WF_ERR_HIP;
-    }
-    dim3 mgrid((unsigned)pairs), mblock(64);
-    if (head_dim == 128) {
-        if (bf16)
-            attn_merge<128, true><<<mgrid, mblock, 0, stream>>>(ws_o, ws_ml, out, pairs, splits, sl2);
-        else
-            attn_merge<128, false><<<mgrid, mblock, 0, stream>>>(ws_o, ws_ml, out, pairs, splits, sl2);
-    } else {
-        if (bf16)
-            attn_merge<64, true><<<mgrid, mblock, 0, stream>>>(ws_o, ws_ml, out, pairs, splits, sl2);
-        else
-            attn_merge<64, false><<<mgrid, mblock, 0, stream>>>(ws_o, ws_ml, out, pairs, splits, sl2);
-    }
-    if (hipGetLastError() != hipSuccess)
-        return WF_ERR_HIP;
-    return WF_OK;
+    const bool one = splits <= (kWave / (head_dim / 4)) * kMergeBatch;
+    const dim3 g1((unsigned)cdiv(pairs, kMergeWpb)), b1(64 * kMergeWpb);
+#define WF_MERGE(DHV, PV, OV)                                                                  \
+    if (head_dim == DHV && part16 == PV && out16 == OV) {                                      \
+        if (one)                                                                               \
+            attn_merge_one<DHV, PV, OV, kMergeWpb><<<g1, b1, 0, stream>>>(ws_o, ws_ml, out,    \
+                                                                          pairs, splits, sl2); \
+        else                                                                                   \
+            attn_merge<DHV, PV, OV><<<dim3((unsigned)pairs), dim3(64), 0, stream>>>(           \
+                ws_o, ws_ml, out, pairs, splits, sl2);                                         \
+    } else
+    WF_MERGE(128, true, true) WF_MERGE(128, false, true) WF_MERGE(128, false, false)
+    WF_MERGE(64, true, true) WF_MERGE(64, false, true) WF_MERGE(64, false, false)
+    { return WF_ERR_UNSUPPORTED; }
+#undef WF_MERGE
+    return hipGetLastError() == hipSuccess ? WF_OK : WF_ERR_HIP;
 }
 
 wf_status_t launch_attn(wf_dtype_t dt, const void *q, const void *k_cache,
@@ -1252,8 +1238,8 @@ wf_status_t launch_attn(wf_dtype_t dt, const void *q, const void *k_cache,
     if (hipGetLastError() != hipSuccess)
         return WF_ERR_HIP;
 
-    return launch_attn_merge(head_dim, dt == WF_BF16, a.ws_o, a.ws_ml, out, (int)pairs, p.splits,
-                             a.sl2, stream);
+    return launch_attn_merge(head_dim, dt == WF_BF16, dt == WF_BF16, a.ws_o, a.ws_ml, out,
+                             (int)pairs, p.splits, a.sl2, stream);
 }
 
 }  // namespace wf

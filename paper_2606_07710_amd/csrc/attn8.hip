@@ -20,7 +20,7 @@ struct Attn8Params {
     const void *q;
     const char *k, *v;
     const uint8_t *k_scale, *v_scale;
-    void *ws_o;               // [splits][gamma*n_q_heads][head_dim], unnormalised;
+    void *ws_o;               // [splits][gamma*n_q_heads][head_dim] fp32, unnormalised;
                               // of one split: the output itself
     float *ws_ml;             // [splits][gamma*n_q_heads][2]: reference, sum
     const uint64_t *tree_mask;
@@ -501,19 +501,33 @@ __global__ __launch_bounds__(64 * RG * KS) void attn8_tiles(Attn8Params a) {
         return;
     const size_t pr = ((size_t)split * a.gamma + qi) * a.n_q_heads + g * a.group +
                       (row - qi * a.group);
-    if (a.splits == 1) {                 // (every row sees itself: l > 0)
-        const float inv = 1.f / l;
+    // Partial rows stay fp32: rounded to bf16 they would bring the merged row as
+    // large an error again as its own rounding (from 64 bits 0.0024 of the output,
+    // 0.0017 as it is; 16 rows, 8K keys: 13.7 us, 13.9 as it is).  More than 32 rows'
+    // go past the L2, from which the merge, on another XCD, would have to fetch them
+    // while the next call's are written in their place (one workspace: 64 rows, 8K
+    // keys 15.1 us, 13.9 past it; 244 rows 26.3 and 22.2; 32 rows, 1K keys 8.5 and 8.7,
+    // so not for those).
+    if (a.splits > 1) {
+        f32x4 *dst = reinterpret_cast<f32x4 *>(static_cast<float *>(a.ws_o) + pr * D) + c4;
 #pragma unroll
-        for (int md = 0; md < MD; ++md)
-            o[md] *= inv;
+        for (int md = 0; md < MD; ++md) {
+            if constexpr (RG == 4)
+                __builtin_nontemporal_store(o[md], dst + 4 * md);
+            else
+                dst[4 * md] = o[md];
+        }
+        if (c4 == 0) {
+            a.ws_ml[pr * 2] = ref;
+            a.ws_ml[pr * 2 + 1] = l;
+        }
+        return;
     }
-    // Lane groups 2i and 2i + 1 hold 4 dims each of every 16; they trade, so that
-    // the first has 8 of the even 16s and the second 8 of the odd ones: 16-byte
-    // stores, 64 bytes of a row together (32 rows, 1K keys: 8.0 -> 7.85 us).  Many
-    // rows' partials go past the L2, from which the merge, on another XCD, would
-    // have to fetch them while the next call's are written in their place (244
-    // rows, 8K keys, one workspace: 21.0 -> 19.2 us; several: 18.4 either way; 64
-    // rows, 32K keys: 22.5 and 22.7, so not for those).
+    // One split: the output (every row sees itself: l > 0).  Lane groups 2i and
+    // 2i + 1 hold 4 dims each of every 16; they trade, so that the first has 8 of the
+    // even 16s and the second 8 of the odd ones: 16-byte stores, 64 bytes of a row
+    // together.
+    const float inv = 1.f / l;
     u32x4 *dst = reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(a.ws_o) + pr * D);
 #pragma unroll
     for (int md = 0; md < MD; md += 2) {
@@ -521,20 +535,12 @@ __global__ __launch_bounds__(64 * RG * KS) void attn8_tiles(Attn8Params a) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const auto r = __builtin_amdgcn_permlane16_swap(
-                pack_bf16x2(o[md][2 * i], o[md][2 * i + 1]),
-                pack_bf16x2(o[md + 1][2 * i], o[md + 1][2 * i + 1]), false, false);
+                pack_bf16x2(o[md][2 * i] * inv, o[md][2 * i + 1] * inv),
+                pack_bf16x2(o[md + 1][2 * i] * inv, o[md + 1][2 * i + 1] * inv), false, false);
             v[i] = r[0];
             v[2 + i] = r[1];
         }
-        u32x4 *to = dst + (md + (c4 & 1)) * 2 + (c4 >> 1);
-        if constexpr (MANY)
-            __builtin_nontemporal_store(v, to);
-        else
-            *to = v;
-    }
-    if (c4 == 0 && a.splits > 1) {
-        a.ws_ml[pr * 2] = ref;
-        a.ws_ml[pr * 2 + 1] = l;
+        dst[(md + (c4 & 1)) * 2 + (c4 >> 1)] = v;
     }
 }
 
@@ -716,16 +722,15 @@ __global__ __launch_bounds__(64 * kRowWaves) void attn8_rows(Attn8Params a) {
 AttnPlan plan_attn8(wf_dtype_t dt, int gamma, int ctx_len, int n_q_heads, int n_kv_heads,
                     int head_dim, int num_splits) {
     AttnPlan p{};
+    p.part_bytes = 4;
     if (dt == WF_F32) {
         const int steps = (ctx_len + gamma + kRowKeys - 1) / kRowKeys;
         const int want = num_splits > 0 ? num_splits
                          : steps <= 2   ? 1
                                         : std::max(1, 256 / (gamma * n_q_heads));
-        p.part_bytes = 4;
         p.splits = std::min(want, steps);
         return p;
     }
-    p.part_bytes = 2;
     p.rows = n_q_heads / n_kv_heads * gamma;
     p.nb = 1;
     p.rg = p.rows <= 16 ? 1 : p.rows <= 32 ? 2 : 4;
@@ -806,7 +811,7 @@ wf_status_t launch_attn8(wf_dtype_t dt, const void *q, const wf_kv8_cache_t &c, 
     if (p.splits == 1)
         return WF_OK;
     // (the references are held in log2 units, so the merge's factor is 1)
-    return launch_attn_merge(c.head_dim, dt == WF_BF16, a.ws_o, a.ws_ml, out, (int)pairs,
+    return launch_attn_merge(c.head_dim, false, dt == WF_BF16, a.ws_o, a.ws_ml, out, (int)pairs,
                              p.splits, 1.f, stream);
 }
 

@@ -37,7 +37,7 @@ struct AttnPlan {
     int n_row_groups;    // workgroup row groups of 16*nb*rg rows
     int splits;          // key splits per KV head
     int keys_per_split;  // multiple of the 32-key tile
-    int part_bytes;      // bytes per partial-output element (bf16 path: 2)
+    int part_bytes;      // bytes per partial-output element (bf16 cache, bf16 queries: 2)
 };
 
 // Shapes of a verify-attention and of a KV-only prefill call (api.hip).
@@ -62,8 +62,9 @@ wf_status_t launch_attn(wf_dtype_t dt, const void *q, const void *k_cache,
                         float softmax_scale, const uint64_t *tree_mask,
                         const AttnPlan &p, void *workspace, hipStream_t stream);
 
-wf_status_t launch_attn_merge(int head_dim, bool bf16, const void *ws_o, const float *ws_ml,
-                              void *out, int pairs, int splits, float sl2, hipStream_t stream);
+wf_status_t launch_attn_merge(int head_dim, bool part16, bool out16, const void *ws_o,
+                              const float *ws_ml, void *out, int pairs, int splits, float sl2,
+                              hipStream_t stream);
 
 // 8-bit KV cache (kv8.hip, attn8.hip).
 inline int kv8_blocks(int cap) { return (cap + WF_KV8_BLOCK - 1) / WF_KV8_BLOCK; }

@@ -541,3 +541,78 @@ def test_round_in_a_graph_and_on_a_side_stream():
         step()
         torch.cuda.synchronize()
     assert not bool(ws[:4 << 20].any().item())
+
+
+# ---- against 64 bits at the lengths the call is for -----------------------------------------
+
+def _appended(seed, hkv, rows, dh, std=1.28):
+    """A cache of `rows` appended rows, a few channels of K larger."""
+    c = wf.alloc_kv8_cache(hkv, rows + 13, dh, DEV)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    k, v = (torch.empty(rows, hkv, dh, device=DEV).normal_(0.0, std, generator=g)
+            for _ in range(2))
+    k[:, :, ::16] *= 4.0
+    wf.wf_kv8_append(k, v, c, 0)
+    return c
+
+
+def _rms(x):
+    return float(np.sqrt(np.mean(np.square(x))))
+
+
+@pytest.mark.parametrize("gamma,ctx,hq,hkv,dh,splits,tree", [
+    (8, 1003, 32, 8, 128, 0, False), (61, 8192, 32, 8, 128, 0, True),
+    (16, 32768, 32, 8, 128, 0, False), (16, 65536, 64, 8, 128, 0, False),
+    (1, 30000, 32, 8, 128, 0, False), (16, 9000, 16, 8, 64, 0, False),
+    (16, 9000, 16, 8, 128, 1, False), (16, 9000, 4, 4, 64, 70, False),
+    (64, 5000, 8, 2, 64, 24, True),
+])
+def test_attention_rms_error(gamma, ctx, hq, hkv, dh, splits, tree):
+    """The error's root mean square, where roundings average out.  The row is
+    rounded to bf16 once (the rounding of the 64-bit result itself is what it
+    costs), each weight is off by a value spread over at most 2^-9 of itself, in
+    numerator and denominator (2^-9 / sqrt(3) of sqrt(sum p^2 (v - out)^2), the signs
+    being independent), or over 2^-21 of the row's largest, and the scores by (d + 3)
+    2^-24 of a sum of magnitudes, of either sign; a tenth is for the spread of the
+    mean itself."""
+    print("rms", gamma, ctx, hq, hkv, dh, splits, tree, flush=True)
+    n = ctx + gamma
+    c = _appended(gamma + ctx, hkv, n, dh)
+    q = _normal(11, gamma, hq, dh, std=1.28)
+    out = torch.full((gamma, hq, dh), float("nan"), dtype=q.dtype, device=DEV)
+    masks = None
+    if tree:
+        masks = [int(m) for m in W.ancestor_masks(W.draft_tree(seed=3))]
+        masks = (masks + [1] * gamma)[:gamma]
+        m = torch.tensor([x - (1 << 64) if x >> 63 else x for x in masks], dtype=torch.int64,
+                         device=DEV)
+        wf.wf_kv8_verify_attn_tree(q.to(DEV), c, out, ctx, m, num_splits=splits)
+    else:
+        wf.wf_kv8_verify_attn(q.to(DEV), c, out, ctx, num_splits=splits)
+    got = out.double().cpu().numpy()
+    vis, grp = _visible(gamma, ctx, masks), hq // hkv
+    err, limit = [], []
+    for g in (0, hkv - 1):               # the first and the last KV head
+        kk = R.E4M3[c.k[g].cpu().numpy()] * R.pow2(c.k_scale[g].cpu())[:, None, None]
+        vv = R.E4M3[c.v[g].cpu().numpy()] * R.pow2(c.v_scale[g].cpu())[:, None, None]
+        kk = kk.reshape(-1, dh)[:n]
+        vv = vv.swapaxes(1, 2).reshape(-1, dh)[:n]
+        for h in (g * grp, (g + 1) * grp - 1):
+            qh = q[:, h].double().numpy()
+            z = np.where(vis, qh @ kk.T * dh ** -0.5, -np.inf)
+            p = np.exp(z - z.max(1, keepdims=True))
+            p /= p.sum(1, keepdims=True)
+            ref = p @ vv
+            half = torch.from_numpy(ref).to(torch.bfloat16).double().numpy() - ref
+            delta = (dh + 3) * 2.0 ** -24 * (np.abs(qh) @ np.abs(kk).T * dh ** -0.5 * vis).max()
+            def around(w):               # sum w (v - out)^2
+                return w @ np.square(vv) - 2 * ref * (w @ vv) + \
+                    np.square(ref) * w.sum(1, keepdims=True)
+            spread = (2.0 ** -9 / 3 ** 0.5 + 2 * delta) ** 2 * around(np.square(p)) + \
+                (2.0 ** -21 / 3 ** 0.5 * p.max(1, keepdims=True)) ** 2 * around(vis.astype(float))
+            err.append(got[:, h] - ref)
+            limit.append(np.square(half) + spread)
+    err, limit = np.stack(err), float(np.sqrt(np.mean(np.stack(limit))))
+    print("rms error", _rms(err), "limit", limit, flush=True)
+    assert _rms(err) <= 1.1 * limit
