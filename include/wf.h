@@ -637,7 +637,9 @@ wf_status_t wf_kv8_append(wf_dtype_t dt, const wf_kv8_cache_t *cache, const void
  * formed as there (rounded to dt's storage) in the workspace and then
  * appended.  Arguments and limits of both (dt: WF_F32, WF_BF16 or
  * WF_BF16_TILED).
- * workspace >= wf_kv8_only_prefill_workspace_bytes(...) bytes. */
+ * workspace >= wf_kv8_only_prefill_workspace_bytes(...) bytes (WF_F32: the
+ * rows alone, which the append leaves at zero where another call's zero block
+ * may lie). */
 wf_status_t wf_kv8_only_prefill(wf_dtype_t dt, const void *x, const void *w_k,
                                 const void *w_v, const wf_kv8_cache_t *cache,
                                 int32_t n_tok, int32_t start_pos, int32_t d_in,

@@ -30,8 +30,8 @@ inline wf_dtype_t storage(wf_dtype_t dt) { return dt == WF_BF16_TILED ? WF_BF16 
 inline size_t elem_bytes(wf_dtype_t dt) { return dt == WF_F32 ? 4 : 2; }
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// Workspace of the 8-bit prefill: the prefill's own (its zero block first),
-// then the K rows and the V rows, [n_kv_heads][n_tok][head_dim] each; this is
+// Workspace of the 8-bit prefill: the prefill's own (bf16: the zero block; fp32:
+// nothing), then the K rows and the V rows, [n_kv_heads][n_tok][head_dim] each; this is
 // where the K rows start.
 size_t kv8_prefill_rows_at(wf_dtype_t dt, int n_tok, int d_in, const wf_kv8_cache_t &c) {
     return align256(wf::prefill_workspace_bytes(storage(dt), n_tok, d_in, c.n_kv_heads,
@@ -95,7 +95,7 @@ wf_status_t wf_kv8_append(wf_dtype_t dt, const wf_kv8_cache_t *cache, const void
     if (!k || !v || !aligned16(k) || !aligned16(v) || tok_stride % unit || head_stride % unit)
         return WF_ERR_INVALID_ARG;
     return wf::launch_kv8_append(dt, *cache, k, v, n_tok, start_pos, tok_stride, head_stride,
-                                 static_cast<hipStream_t>(stream));
+                                 nullptr, static_cast<hipStream_t>(stream));
 }
 
 size_t wf_kv8_only_prefill_workspace_bytes(wf_dtype_t dt, int32_t n_tok, int32_t d_in,
@@ -143,8 +143,12 @@ wf_status_t wf_kv8_only_prefill(wf_dtype_t dt, const void *x, const void *w_k, c
                             workspace, s);
     if (st != WF_OK)
         return st;
+    // The fp32 prefill has no zero block, so its rows lie where other calls have
+    // theirs: the append leaves zeros there.
+    const char *zero_end =
+        dt == WF_F32 ? static_cast<const char *>(workspace) + wf::kCounterBytes : nullptr;
     return wf::launch_kv8_append(storage(dt), *cache, kr, vr, n_tok, start_pos, dh,
-                                 (size_t)n_tok * dh, s);
+                                 (size_t)n_tok * dh, zero_end, s);
 }
 
 size_t wf_kv8_verify_attn_workspace_bytes(wf_dtype_t dt, int32_t gamma, int32_t ctx_len,

@@ -51,6 +51,7 @@ struct AppendParams {
     uint8_t *scale[2];
     size_t tok_stride, head_stride;      // source strides in elements
     int start, end, n_blocks, first_block;
+    const char *zero_end;    // CLEAR: source rows before it are zeroed once read
 };
 
 // One block of one head, K or V.  A thread owns 4 rows x 4 dims: it takes new
@@ -61,8 +62,10 @@ struct AppendParams {
 // The codes go past the L2, where no later call of another XCD would look for
 // them (8190 tokens: 12.8 -> 11.6 us, out of HBM 14.4 -> 12.6; an attention right
 // behind takes as long as before).  (Rows staged as fp32 in LDS, new ones, old ones and the scale loaded one
-// after the other: 4.15 us for 16 tokens, 13.4 for 8190.)
-template <int D, bool BF16>
+// after the other: 4.15 us for 16 tokens, 13.4 for 8190.)  CLEAR: the source is a
+// workspace whose zero block has to be zero again; each element is read by one
+// thread, which stores the zero.
+template <int D, bool BF16, bool CLEAR>
 __global__ __launch_bounds__(2 * D) void kv8_append(AppendParams a) {
     __shared__ float part[2 * D / kWave];
     // a V block in pieces of 16 rows of a dim, one more after every four dims:
@@ -98,8 +101,10 @@ __global__ __launch_bounds__(2 * D) void kv8_append(AppendParams a) {
         if (i0 + u >= first && i0 + u < last) {
             const size_t off = (size_t)(r0 + i0 + u - a.start) * a.tok_stride +
                                g * a.head_stride + 4 * j;
-            raw[u] = *reinterpret_cast<const Raw *>(
-                static_cast<const char *>(a.src[kind]) + off * (BF16 ? 2 : 4));
+            const char *from = static_cast<const char *>(a.src[kind]) + off * (BF16 ? 2 : 4);
+            raw[u] = *reinterpret_cast<const Raw *>(from);
+            if (CLEAR && from < a.zero_end)
+                *reinterpret_cast<Raw *>(const_cast<char *>(from)) = Raw{};
         }
     }
 #pragma unroll
@@ -266,7 +271,7 @@ __global__ __launch_bounds__(kThreads) void kv8_compact(char *k, char *v, uint8_
 
 wf_status_t launch_kv8_append(wf_dtype_t dt, const wf_kv8_cache_t &c, const void *k,
                               const void *v, int n_tok, int start, size_t tok_stride,
-                              size_t head_stride, hipStream_t stream) {
+                              size_t head_stride, const void *zero_end, hipStream_t stream) {
     AppendParams a{};
     a.src[0] = k;
     a.src[1] = v;
@@ -281,15 +286,17 @@ wf_status_t launch_kv8_append(wf_dtype_t dt, const wf_kv8_cache_t &c, const void
     a.n_blocks = kv8_blocks(c.cap);
     a.first_block = start / kKv8Block;
     const int blocks = (start + n_tok - 1) / kKv8Block - a.first_block + 1;
+    a.zero_end = static_cast<const char *>(zero_end);
     const dim3 grid(blocks, c.n_kv_heads, 2);
-    if (c.head_dim == 128 && dt == WF_BF16)
-        kv8_append<128, true><<<grid, 2 * 128, 0, stream>>>(a);
-    else if (c.head_dim == 128)
-        kv8_append<128, false><<<grid, 2 * 128, 0, stream>>>(a);
-    else if (dt == WF_BF16)
-        kv8_append<64, true><<<grid, 2 * 64, 0, stream>>>(a);
+#define WF_APPEND(DV, BV, CV)                                                          \
+    if (c.head_dim == DV && (dt == WF_BF16) == BV && (zero_end != nullptr) == CV)      \
+        kv8_append<DV, BV, CV><<<grid, 2 * DV, 0, stream>>>(a);                        \
     else
-        kv8_append<64, false><<<grid, 2 * 64, 0, stream>>>(a);
+    WF_APPEND(128, true, false) WF_APPEND(64, true, false)
+    WF_APPEND(128, false, false) WF_APPEND(64, false, false)
+    WF_APPEND(128, false, true) WF_APPEND(64, false, true)
+    return WF_ERR_UNSUPPORTED;
+#undef WF_APPEND
     return hipGetLastError() == hipSuccess ? WF_OK : WF_ERR_HIP;
 }
 

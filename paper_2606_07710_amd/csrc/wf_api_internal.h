@@ -68,9 +68,10 @@ wf_status_t launch_attn_merge(int head_dim, bool part16, bool out16, const void 
 
 // 8-bit KV cache (kv8.hip, attn8.hip).
 inline int kv8_blocks(int cap) { return (cap + WF_KV8_BLOCK - 1) / WF_KV8_BLOCK; }
+// zero_end: null, or (fp32) the end of the bytes of k and v that are left at zero
 wf_status_t launch_kv8_append(wf_dtype_t dt, const wf_kv8_cache_t &c, const void *k,
                               const void *v, int n_tok, int start, size_t tok_stride,
-                              size_t head_stride, hipStream_t stream);
+                              size_t head_stride, const void *zero_end, hipStream_t stream);
 wf_status_t launch_kv8_compact(const wf_kv8_cache_t &c, const int32_t *accept,
                                const int32_t *path, int gamma, int ctx_len, int n_layers,
                                size_t code_stride, size_t scale_stride, hipStream_t stream);

@@ -460,6 +460,56 @@ def test_prefill_is_prefill_then_append(dt, n, start, hkv, dh, tiled):
     R.Cache(a).check(b)
 
 
+@pytest.mark.parametrize("n,start,hkv,dh", [
+    (9, 50, 2, 64), (1, 31, 1, 128), (45, 0, 8, 128), (900, 33, 8, 128),
+])
+def test_f32_prefill_leaves_the_zero_block(n, start, hkv, dh):
+    """An fp32 prefill, its rows shorter or longer than the zero block, and an
+    LM-head call share one workspace, in a captured graph too."""
+    print("zero block", n, start, hkv, dh, flush=True)
+    d, g, vocab = 256, 8, 5000
+    x = _normal(1, n, d, dtype=torch.float32).to(DEV)
+    wk, wv = (_normal(i, hkv * dh, d, std=0.05, dtype=torch.float32).to(DEV) for i in (2, 3))
+    logits = _normal(4, g, vocab, dtype=torch.float32).to(DEV)
+    draft = logits.argmax(1).to(torch.int32)[:g - 1].contiguous()
+    need = wf.wf_kv8_only_prefill_workspace_bytes(torch.float32, n, d, hkv, dh)
+    ws = wf.alloc_workspace(max(need, wf.wf_lmhead_workspace_bytes(g, vocab)), DEV)
+    a, b = (_filled(9, hkv, start + n, dh, rows=start) for _ in range(2))
+    am, ent = torch.empty(g, dtype=torch.int32, device=DEV), torch.empty(g, device=DEV)
+    acc = torch.empty(3, dtype=torch.int32, device=DEV)
+
+    def step(cache):
+        wf.wf_kv8_only_prefill(x, wk, wv, cache, start, 1e6, workspace=ws)
+        wf.wf_lmhead_accept_entropy(None, None, logits, draft, 1.0, am, ent, acc, workspace=ws)
+
+    def checked():
+        torch.cuda.synchronize()
+        assert not bool(ws[:4 << 20].any().item())
+        assert am.tolist() == logits.argmax(1).tolist() and acc[0].item() == g - 1
+        am.zero_()
+        acc.zero_()
+
+    wf.wf_kv8_only_prefill(x, wk, wv, a, start, 1e6)     # (a workspace of its own)
+    step(b)
+    checked()
+    R.Cache(a).check(b)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(b)
+    for _ in range(3):
+        graph.replay()
+        checked()
+        step(b)
+        checked()
+    # nothing behind the rows is written
+    room = torch.full((need + 4096,), 0x5a, dtype=torch.uint8, device=DEV)
+    wf.wf_kv8_only_prefill(x, wk, wv, b, start, 1e6, workspace=room[:need])
+    torch.cuda.synchronize()
+    assert (room[need:] == 0x5a).all()
+    assert not room[:min(n * hkv * dh * 4, 4 << 20)].any()
+    R.Cache(a).check(b)
+
+
 def test_round_in_a_graph_and_on_a_side_stream():
     """A tree round on the 8-bit cache (prefill of the block, attention, tree
     acceptance, compaction) captured once and replayed between eager runs, its
