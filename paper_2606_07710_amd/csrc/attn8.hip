@@ -77,6 +77,7 @@ struct Attn8Params {
 constexpr int kTileKeys8 = 128;
 constexpr int kTileBlocks = kTileKeys8 / kKv8Block;
 constexpr float kRefGrow = 64.f;         // log2 growth that moves a row's reference
+constexpr float kFarScore = 0x1p22f;     // |S sl2| whose fp32 spacing a weight would feel
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
@@ -92,7 +93,8 @@ __device__ __forceinline__ f32x4 mfma_e4m3(i32x8 a, i32x8 b, f32x4 c, unsigned s
                                                             (int)sb);
 }
 
-// Four values of at most 256 as two e4m3 parts hi + lo / 16.
+// Four values of at most 256 (279 where S sl2 is near kFarScore and rounded by 1/8) as
+// two e4m3 parts hi + lo / 16.
 constexpr int kLoShift = 4;
 __device__ __forceinline__ void two_parts(const float (&p)[4], uint32_t dead, uint32_t &hi,
                                           uint32_t &lo) {
@@ -396,7 +398,9 @@ __global__ __launch_bounds__(64 * RG * KS) void attn8_tiles(Attn8Params a) {
         // the row's exponent in this tile, and against its reference
         const bool any = m > -INFINITY;
         const float e = any ? ceilf(m * sl2) : 0.f;
-        if (__ballot(any && !(e - ref <= kRefGrow))) {
+        const bool far = fabsf(e) >= kFarScore;
+        float add = 8.f - e;
+        if (__ballot(far || (any && !(e - ref <= kRefGrow)))) {
             // (also a row's first visible tile: ref is -inf, o zero)
             if (any && !(e - ref <= kRefGrow)) {
                 const float back = fast_exp2(ref - e);
@@ -405,11 +409,21 @@ __global__ __launch_bounds__(64 * RG * KS) void attn8_tiles(Attn8Params a) {
                     o[md] *= back;
                 ref = e;
             }
+            // m sl2 is rounded, a score's product below is not: from 2^24 on that
+            // could put a weight at 2^9, past e4m3.  Such scores are taken from
+            // their largest first, whose weight is then 2^8 exactly.
+            if (far) {
+#pragma unroll
+                for (int mb = 0; mb < 8; ++mb)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        s[mb][i] -= m;
+                add = 8.f;
+            }
         }
         const int shift = any ? (int)fmaxf(e - ref, -120.f) : 0;
         const unsigned ps = (unsigned)(127 + shift), pslo = ps - kLoShift;
         // P in two parts
-        const float add = 8.f - e;
         uint32_t hi[8], lo[8];
 #pragma unroll
         for (int mb = 0; mb < 8; ++mb) {

@@ -326,6 +326,44 @@ def test_attention_scores(dt, kind):
     _check_attention(dt, q, c, ctx, scale=scale)
 
 
+@pytest.mark.parametrize("gamma,ctx,hq,hkv,dh,splits", [
+    (16, 100, 16, 4, 128, 0), (16, 1500, 16, 2, 64, 0), (64, 1500, 4, 1, 128, 3),
+    (4, 900, 64, 8, 128, 1), (16, 3000, 4, 1, 128, 5), (8, 700, 8, 2, 64, 1),
+])
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("low,high", [(20, 30), (30, 90)])
+def test_attention_far_scores(dt, low, high, gamma, ctx, hq, hkv, dh, splits):
+    """Scores of 2^20 to 2^90, where fp32 has no fraction left: q has one element
+    that is not zero, so that every score is exact and keys that share the largest
+    one share the weight.  What is left are the weights' two parts (2^-9, alike
+    for all of a row's ties) and the output's rounding (bf16), and the fp32 sums."""
+    print("far scores", dt, low, high, gamma, ctx, hq, hkv, dh, splits, flush=True)
+    n, g = ctx + gamma, _rng(gamma + ctx + low)
+    k = torch.randint(-15, 9, (n, hkv, dh), generator=g).float()
+    k[torch.rand(n, hkv, dh, generator=g) < 0.02] = 15.0         # (held exactly)
+    k[0] = 15.0
+    v = _normal(1, n, hkv, dh)
+    c = wf.alloc_kv8_cache(hkv, n, dh, DEV)
+    wf.wf_kv8_append(k.to(torch.bfloat16).to(DEV), v.to(DEV), c, 0)
+    at = torch.randint(0, dh, (gamma, hq, 1), generator=g)
+    size = (1 + torch.rand(gamma, hq, 1, generator=g)) * \
+        2.0 ** torch.randint(low, high, (gamma, hq, 1), generator=g)
+    sign = torch.where(torch.rand(gamma, hq, 1, generator=g) < 0.3, -1.0, 1.0)
+    q = torch.zeros(gamma, hq, dh).scatter_(2, at, size * sign).to(DT[dt])
+    out = torch.full(q.shape, float("nan"), dtype=q.dtype, device=DEV)
+    wf.wf_kv8_verify_attn(q.to(DEV), c, out, ctx, num_splits=splits)
+    torch.cuda.synchronize()
+    held = R.Cache(c).values()
+    assert (held[0, :, :n] == k.transpose(0, 1).double().numpy()).all()
+    ref, mass, _ = R.attention(q.double().numpy(), held[0][:, :n], held[1][:, :n],
+                               _visible(gamma, ctx), dh ** -0.5)
+    tol = mass * 2 * (n / 32 + 80) * 2.0 ** -24
+    if dt == "bf16":
+        tol = tol + mass * 2.0 ** -9 + np.abs(ref) * 2.0 ** -8
+    err = np.abs(out.double().cpu().numpy() - ref)
+    assert (err <= tol).all(), (np.isnan(err).sum(), float(np.nanmax(err / tol)))
+
+
 def test_attention_is_the_same_for_any_bytes_behind():
     """Codes of rows behind the block and scales of blocks behind it change no
     bit, and outputs repeat bit for bit."""
