@@ -659,6 +659,8 @@ size_t wf_kv8_only_prefill_workspace_bytes(wf_dtype_t dt, int32_t n_tok, int32_t
  *          in two e4m3 parts that together hold them to 2^-9 of themselves
  *          (or 2^-21 of the row's largest), accumulated in fp32 over the whole
  *          row, splits included, and rounded once.  WF_F32: fp32 throughout.
+ *          The sums stand before their division: values of which (ctx_len +
+ *          gamma) 2^16 max|v| reaches 2^128 may give infinities.
  * softmax_scale, num_splits and the workspace as there, with this call's
  * own workspace query; block rows a row does not see have to hold finite
  * values, as for wf_verify_attn_tree.

@@ -43,10 +43,12 @@ struct Attn8Params {
 //   P = 2^(S sl2 - E + 8), E = ceil of the row's largest S sl2 in the tile
 //   O^T += V^T P^T  per 16 dims two instructions over all 128 keys: A = the
 //                  transposed V codes with the token blocks' scales, B = P^T as
-//                  hi + lo with the scale 2^(E - R)
+//                  hi + lo with the scale 2^(E - R - 8)
 // The running softmax keeps one integer reference R per row, and a tile's
 // weights are put under it by the scale operand, not by rescaling O: only a
-// tile more than 2^64 above R moves it.
+// tile more than 2^16 above R moves it.  So no sum passes n_keys 2^16 max|v|: values
+// up to 2^111 / n_keys cannot overflow (with 2^64, and weights of 256, it was 2^56 /
+// n_keys; the times are the same).
 //
 // Two parts of e4m3 hold 8 significant bits, as bf16 does, the second one 16
 // times as large as it counts so that small values keep theirs: values of at
@@ -76,7 +78,7 @@ struct Attn8Params {
 // ---------------------------------------------------------------------------
 constexpr int kTileKeys8 = 128;
 constexpr int kTileBlocks = kTileKeys8 / kKv8Block;
-constexpr float kRefGrow = 64.f;         // log2 growth that moves a row's reference
+constexpr float kRefGrow = 16.f;         // log2 growth that moves a row's reference
 constexpr float kFarScore = 0x1p22f;     // |S sl2| whose fp32 spacing a weight would feel
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
@@ -421,8 +423,8 @@ __global__ __launch_bounds__(64 * RG * KS) void attn8_tiles(Attn8Params a) {
                 add = 8.f;
             }
         }
-        const int shift = any ? (int)fmaxf(e - ref, -120.f) : 0;
-        const unsigned ps = (unsigned)(127 + shift), pslo = ps - kLoShift;
+        const int shift = any ? (int)fmaxf(e - ref, -114.f) : 0;
+        const unsigned ps = (unsigned)(127 - 8 + shift), pslo = ps - kLoShift;
         // P in two parts
         uint32_t hi[8], lo[8];
 #pragma unroll

@@ -364,6 +364,30 @@ def test_attention_far_scores(dt, low, high, gamma, ctx, hq, hkv, dh, splits):
     assert (err <= tol).all(), (np.isnan(err).sum(), float(np.nanmax(err / tol)))
 
 
+@pytest.mark.parametrize("gamma,ctx,hq,hkv,dh,splits", [
+    (5, 900, 8, 2, 128, 0), (16, 1500, 16, 2, 64, 1), (4, 2000, 4, 1, 128, 2),
+    (64, 1500, 4, 1, 128, 3),
+])
+@pytest.mark.parametrize("grow", [15, 40, 63, 200])
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_attention_large_values(dt, grow, gamma, ctx, hq, hkv, dh, splits):
+    """Values of 2^98 under scores that grow by 2^grow from tile to tile (or fall):
+    no sum passes n 2^16 max|v| < 2^128."""
+    print("large values", dt, grow, gamma, ctx, hq, hkv, dh, splits, flush=True)
+    n = ctx + gamma
+    q = torch.ones(gamma, hq, dh, dtype=DT[dt]) * (1 + _normal(2, gamma, hq, 1).abs() / 64)
+    # k a multiple of ones: scores of log2 size step * tile
+    step = grow / (dh ** 0.5 * 1.4427)
+    tile = torch.arange(n) // 128
+    k = (tile * step)[:, None, None] * torch.ones(1, hkv, dh) + _normal(3, n, hkv, dh) / 32
+    k[:, -1] = k[:, -1].flip(0)                      # (the last head's fall)
+    v = (_normal(4, n, hkv, dh).float().clamp(-3.9, 3.9) * 2.0 ** 98).to(torch.bfloat16)
+    c = wf.alloc_kv8_cache(hkv, n + 3, dh, DEV)
+    wf.wf_kv8_append(k.to(torch.bfloat16).to(DEV), v.to(DEV), c, 0)
+    out = _check_attention(dt, q.to(DT[dt]), c, ctx, splits=splits)
+    assert out.isfinite().all()
+
+
 def test_attention_is_the_same_for_any_bytes_behind():
     """Codes of rows behind the block and scales of blocks behind it change no
     bit, and outputs repeat bit for bit."""
