@@ -315,6 +315,15 @@ def _on(stream):
     return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
+def _hold(stream, *tensors):
+    """Keeps the memory of tensors that the caller may drop at once from being
+    given out again before `stream`, on which a low-bit call reads them, gets
+    there (their own allocations follow the stream they were made on)."""
+    if stream is not None:
+        for t in tensors:
+            t.record_stream(stream)
+
+
 def _ptr(t, dev, name):
     """Pointer of a dense tensor of device `dev` (None: null)."""
     if t is None:
@@ -849,7 +858,7 @@ class W4Weight:
     streams (wf.h: e2m1 codes, one power-of-two scale byte per 32 columns),
     made once from its row-major form: codes [rows][cols / 2] uint8, low
     nibble first, and scales [rows][cols / 32] uint8 (or float8_e8m0fnu),
-    which are not kept."""
+    which are not kept and may be dropped at once."""
 
     def __init__(self, codes, scales, stream=None):
         rows, half = codes.shape
@@ -864,6 +873,7 @@ class W4Weight:
         with _on(stream):
             self.packed = torch.empty(n, dtype=torch.uint8, device=codes.device)
         _check(lib.wf_w4_pack(*src, rows, 2 * half, self.packed.data_ptr(), n, raw), "wf_w4_pack")
+        _hold(stream, codes, scales)
 
 
 def wf_w4_quantize(w, stream=None):
@@ -881,6 +891,7 @@ def wf_w4_quantize(w, stream=None):
         scales = torch.empty((rows, cols // 32), dtype=torch.uint8, device=w.device)
     _check(lib.wf_w4_quantize(src, rows, cols, codes.data_ptr(), scales.data_ptr(), raw),
            "wf_w4_quantize")
+    _hold(stream, w)
     return codes, scales
 
 

@@ -283,6 +283,32 @@ def test_weight_on_a_side_stream():
         assert torch.equal(there, here)
 
 
+def test_weight_from_temporaries_on_a_side_stream():
+    """Sources that nothing holds any more while a side stream, busy with other
+    work, has still to read them, and whose memory is asked for again."""
+    codes, scales = _weight(3, 512, 4096)
+    w16 = _normal(4, 512, 4096)
+    x = _normal(5, 3, 4096).to(DEV)
+    side = torch.cuda.Stream()
+    busy = torch.ones(4096, 4096, device=DEV)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(20):
+            busy = busy @ busy * 2.0 ** -12
+    w = wf.W4Weight(codes.to(DEV), scales.to(DEV), stream=side)
+    again = [torch.full(t.shape, 255, dtype=torch.uint8, device=DEV) for t in (codes, scales)]
+    got = wf.wf_w4_quantize(w16.to(DEV), stream=side)
+    again.append(torch.full((512, 4096), float("nan"), dtype=torch.bfloat16, device=DEV))
+    torch.cuda.synchronize()
+    y = torch.empty(3, 512, device=DEV)
+    wf.wf_linear_w4(x, w, y)
+    want = wf.wf_w4_quantize(w16.to(DEV))
+    torch.cuda.synchronize()
+    _check(x.cpu(), codes, scales, y, out="f32")
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    del again
+
+
 def test_quantised_layer_of_its_own():
     """Quantise, then multiply: the product of what the codes hold."""
     w = _normal(1, 300, 768, std=0.02)

@@ -1,5 +1,6 @@
 """What the 8-bit cache and 4-bit weight calls refuse, on the CPU: no call
 here reaches the GPU (pointers are never dereferenced by the checks)."""
+import contextlib
 import ctypes
 
 import numpy as np
@@ -363,6 +364,36 @@ def test_python_linear_refuses(x, out, res):
     w = _w4()
     with pytest.raises((ValueError, TypeError)):
         wf.wf_linear_w4(x, w, out, res, stream=FakeStream)
+
+
+def test_python_weights_hold_what_a_side_stream_still_reads(monkeypatch):
+    """codes, scales and w may be temporaries: memory that another stream still
+    reads must not be given out again."""
+    order = []
+
+    class Held(Fake):
+        device = "cpu"
+
+        def record_stream(self, stream):
+            order.append((self, stream))
+
+    def launch(*args):
+        order.append("launch")
+        return 0
+    monkeypatch.setattr(wf.lib, "wf_w4_pack", launch)
+    monkeypatch.setattr(wf.lib, "wf_w4_quantize", launch)
+    monkeypatch.setattr(wf, "_on", lambda stream: contextlib.nullcontext())
+    codes, scales = Held(16, 32, dtype=torch.uint8), Held(16, 2, dtype=torch.uint8)
+    wf.W4Weight(codes, scales, stream=FakeStream)
+    assert order == ["launch", (codes, FakeStream), (scales, FakeStream)]
+    order.clear()
+    w = Held(16, 64)
+    wf.wf_w4_quantize(w, stream=FakeStream)
+    assert order == ["launch", (w, FakeStream)]
+    order.clear()
+    wf.W4Weight(codes, scales)           # (their own stream: nothing to hold)
+    wf.wf_w4_quantize(w)
+    assert order == ["launch", "launch"]
 
 
 # ---- the reference itself -----------------------------------------------------------
