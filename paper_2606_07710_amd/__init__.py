@@ -40,6 +40,10 @@ EXPORTED_SYMBOLS = (
     "wf_w4_packed_bytes", "wf_w4_pack", "wf_linear_w4", "wf_linear_w4_workspace_bytes",
 )
 KV8_BLOCK = 32                       # WF_KV8_BLOCK
+# what the low-bit calls take as e4m3 elements, power-of-two scales, e2m1 pairs
+E4M3_BYTES = (torch.uint8, torch.float8_e4m3fn)
+E8M0_BYTES = (torch.uint8, torch.float8_e8m0fnu)
+E2M1_BYTES = (torch.uint8, torch.float4_e2m1fn_x2)
 NOALLOC_SCRATCH_BYTES = 32 << 20     # WF_NOALLOC_SCRATCH_BYTES
 WF_DRAFTER_AR, WF_DRAFTER_DIFFUSION = 0, 1
 
@@ -695,9 +699,10 @@ class Kv8Cache:
         if b != blocks or rows != KV8_BLOCK or tuple(v.shape) != lead + (b, dh, rows) or \
                 tuple(k_scale.shape) != lead + (b,) or tuple(v_scale.shape) != lead + (b,):
             raise ValueError("cache shapes do not match each other and cap")
-        for t in (k, v, k_scale, v_scale):
-            if t.element_size() != 1:
-                raise ValueError("cache tensors hold bytes")
+        if k.dtype not in E4M3_BYTES or v.dtype not in E4M3_BYTES:
+            raise ValueError("k and v are uint8 or float8_e4m3fn")
+        if k_scale.dtype not in E8M0_BYTES or v_scale.dtype not in E8M0_BYTES:
+            raise ValueError("scales are uint8 or float8_e8m0fnu")
         dev = k.get_device()
         if dev < 0:
             raise ValueError("the cache must be device memory")
@@ -830,8 +835,8 @@ def wf_kv8_verify_attn(q, cache, out, ctx_len, softmax_scale=None, num_splits=0,
 def wf_kv8_verify_attn_tree(q, cache, out, ctx_len, tree_mask, softmax_scale=None,
                             num_splits=0, workspace=None, stream=None):
     """wf_verify_attn_tree over an 8-bit cache; tree_mask as there."""
-    if tree_mask.numel() != q.shape[0] or tree_mask.element_size() != 8:
-        raise ValueError("tree_mask must hold gamma 64-bit words")
+    if tree_mask.numel() != q.shape[0] or tree_mask.dtype not in (torch.int64, torch.uint64):
+        raise ValueError("tree_mask must hold gamma 64-bit words (int64 or uint64)")
     return _kv8_attn(q, cache, out, ctx_len, tree_mask, softmax_scale, num_splits, workspace,
                      stream)
 
@@ -856,16 +861,17 @@ def wf_kv8_compact_path(cache, accept, path, ctx_len, stream=None):
 class W4Weight:
     """A 4-bit weight [rows][cols] in the packed tiles that wf_linear_w4
     streams (wf.h: e2m1 codes, one power-of-two scale byte per 32 columns),
-    made once from its row-major form: codes [rows][cols / 2] uint8, low
-    nibble first, and scales [rows][cols / 32] uint8 (or float8_e8m0fnu),
+    made once from its row-major form: codes [rows][cols / 2] uint8 (or
+    float4_e2m1fn_x2), low nibble first, and scales [rows][cols / 32] uint8 (or float8_e8m0fnu),
     which are not kept and may be dropped at once."""
 
     def __init__(self, codes, scales, stream=None):
         rows, half = codes.shape
         if half % 16 or tuple(scales.shape) != (rows, half // 16):
             raise ValueError("codes [rows][cols / 2] and scales [rows][cols / 32] do not match")
-        if codes.element_size() != 1 or scales.element_size() != 1:
-            raise ValueError("codes and scales hold bytes")
+        if codes.dtype not in E2M1_BYTES or scales.dtype not in E8M0_BYTES:
+            raise ValueError("codes are uint8 (or float4_e2m1fn_x2), scales uint8 (or "
+                             "float8_e8m0fnu)")
         dev, raw = _at(stream)
         n = int(lib.wf_w4_packed_bytes(rows, 2 * half))
         self.shape, self.device = (rows, 2 * half), codes.device

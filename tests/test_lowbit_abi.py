@@ -366,6 +366,47 @@ def test_python_linear_refuses(x, out, res):
         wf.wf_linear_w4(x, w, out, res, stream=FakeStream)
 
 
+@pytest.mark.parametrize("dtype", [torch.float64, torch.complex64, torch.int32])
+def test_python_tree_masks_are_whole_words(dtype):
+    q = Fake(4, 8, 64)
+    with pytest.raises(ValueError):
+        wf.wf_kv8_verify_attn_tree(q, _kv8(), q, 5, Fake(4, dtype=dtype), workspace=_bytes(64),
+                                   stream=FakeStream)
+
+
+@pytest.mark.parametrize("dtype", [torch.int64, torch.uint64])
+def test_python_tree_masks_reach_the_library(dtype):
+    q = Fake(4, 8, 64)
+    with pytest.raises(wf.WfError):
+        wf.wf_kv8_verify_attn_tree(q, _kv8(), q, 5, Fake(4, dtype=dtype), workspace=_bytes(64),
+                                   stream=FakeStream)
+
+
+@pytest.mark.parametrize("name,shape,good", [
+    ("k", (2, 3, 32, 64), "e4m3fn"), ("v", (2, 3, 64, 32), "e4m3fn"),
+    ("k_scale", (2, 3), "e8m0fnu"), ("v_scale", (2, 3), "e8m0fnu"),
+])
+def test_python_cache_types(name, shape, good):
+    """Bytes, or the format that they are in; no other one-byte type."""
+    for dtype in (torch.int8, torch.bool, torch.float8_e5m2, torch.float8_e4m3fnuz,
+                  torch.float8_e8m0fnu, torch.float8_e4m3fn, torch.uint8):
+        t = Fake(*shape, dtype=dtype)
+        if dtype == torch.uint8 or good in str(dtype).split("_")[-1:]:
+            assert getattr(_kv8(**{name: t}), name) is t
+        else:
+            with pytest.raises(ValueError):
+                _kv8(**{name: t})
+
+
+@pytest.mark.parametrize("codes,scales", [
+    (torch.int8, torch.uint8), (torch.float8_e4m3fn, torch.uint8), (torch.bool, torch.uint8),
+    (torch.uint8, torch.int8), (torch.uint8, torch.float8_e4m3fn),
+])
+def test_python_weight_types(codes, scales):
+    with pytest.raises(ValueError):
+        wf.W4Weight(Fake(16, 32, dtype=codes), Fake(16, 2, dtype=scales))
+
+
 def test_python_weights_hold_what_a_side_stream_still_reads(monkeypatch):
     """codes, scales and w may be temporaries: memory that another stream still
     reads must not be given out again."""
