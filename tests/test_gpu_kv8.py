@@ -673,6 +673,69 @@ def _rms(x):
     return float(np.sqrt(np.mean(np.square(x))))
 
 
+def _check_rms(q, c, ctx, masks=None, splits=0, scale=None):
+    """bf16 attention against 64 bits on the first and the last KV head, each
+    element and the root mean square, where roundings average out.
+
+    The row is rounded to bf16 once (in the mean square: what the 64-bit result's
+    own rounding costs).  Each weight is off by a value spread over at most 2^-9 of
+    itself, in numerator and denominator (mean square: 2^-9 / sqrt(3) of sqrt(sum p^2
+    (v - out)^2), the signs being independent), or over 2^-21 of the row's largest;
+    each element of q likewise by 2^-21 of its row's largest (it is exact above that:
+    8 bits), which moves a score by that times sum |k|, in the mean square times
+    sqrt(sum k^2); besides the scores by (d + 3) 2^-24 of a sum of magnitudes, of
+    either sign, and the sums as in _bound.  A tenth is for the spread of the mean
+    itself."""
+    gamma, hq, dh = q.shape
+    n, hkv = ctx + gamma, c.n_kv_heads
+    s = dh ** -0.5 if scale is None else scale
+    out = torch.full((gamma, hq, dh), float("nan"), dtype=q.dtype, device=DEV)
+    if masks is not None:
+        m = torch.tensor([x - (1 << 64) if x >> 63 else x for x in masks], dtype=torch.int64,
+                         device=DEV)
+        wf.wf_kv8_verify_attn_tree(q.to(DEV), c, out, ctx, m, scale, num_splits=splits)
+    else:
+        wf.wf_kv8_verify_attn(q.to(DEV), c, out, ctx, scale, num_splits=splits)
+    got = out.double().cpu().numpy()
+    vis, grp = _visible(gamma, ctx, masks), hq // hkv
+    err, limit, worst = [], [], 0.0
+    for g in {0, hkv - 1}:
+        kk = R.E4M3[c.k[g].cpu().numpy()] * R.pow2(c.k_scale[g].cpu())[:, None, None]
+        vv = R.E4M3[c.v[g].cpu().numpy()] * R.pow2(c.v_scale[g].cpu())[:, None, None]
+        kk = kk.reshape(-1, dh)[:n]
+        vv = vv.swapaxes(1, 2).reshape(-1, dh)[:n]
+        for h in {g * grp, (g + 1) * grp - 1}:
+            qh = q[:, h].double().numpy()
+            z = np.where(vis, qh @ kk.T * s, -np.inf)
+            p = np.exp(z - z.max(1, keepdims=True))
+            p /= p.sum(1, keepdims=True)
+            ref, mass = p @ vv, p @ np.abs(vv)
+            half = torch.from_numpy(ref).to(torch.bfloat16).double().numpy() - ref
+            dots = (np.abs(qh) @ np.abs(kk).T * vis).max(1)
+            dq = 2.0 ** -21 * np.abs(qh).max(1) * s
+            live = vis.astype(float)
+            tol = _bound("bf16", None, ref, mass, dots, s, n, dh) + \
+                2 * mass * (dq * np.abs(kk).sum(1).max())[:, None] + \
+                2.0 ** -20 * p.max(1, keepdims=True) * (live @ np.abs(vv))
+            worst = max(worst, float((np.abs(got[:, h] - ref) / tol).max()))
+
+            def around(w):               # sum w (v - out)^2
+                return w @ np.square(vv) - 2 * ref * (w @ vv) + \
+                    np.square(ref) * w.sum(1, keepdims=True)
+            score = (dh + 3) * 2.0 ** -24 * dots.max() * s
+            qoff = (dq[:, None] / 3 ** 0.5) ** 2 * np.square(kk).sum(1)[None]
+            p2 = np.square(p)
+            spread = (2.0 ** -9 / 3 ** 0.5 + 2 * score) ** 2 * around(p2) + \
+                around(p2 * qoff) + (2.0 ** -21 / 3 ** 0.5 * p.max(1, keepdims=True)) ** 2 * \
+                around(live)
+            err.append(got[:, h] - ref)
+            limit.append(np.square(half) + spread)
+    err, limit = np.stack(err), float(np.sqrt(np.mean(np.stack(limit))))
+    print("rms error", _rms(err), "limit", limit, "worst", worst, flush=True)
+    assert worst <= 1.0
+    assert _rms(err) <= 1.1 * limit
+
+
 @pytest.mark.parametrize("gamma,ctx,hq,hkv,dh,splits,tree", [
     (8, 1003, 32, 8, 128, 0, False), (61, 8192, 32, 8, 128, 0, True),
     (16, 32768, 32, 8, 128, 0, False), (16, 65536, 64, 8, 128, 0, False),
@@ -681,50 +744,28 @@ def _rms(x):
     (64, 5000, 8, 2, 64, 24, True),
 ])
 def test_attention_rms_error(gamma, ctx, hq, hkv, dh, splits, tree):
-    """The error's root mean square, where roundings average out.  The row is
-    rounded to bf16 once (the rounding of the 64-bit result itself is what it
-    costs), each weight is off by a value spread over at most 2^-9 of itself, in
-    numerator and denominator (2^-9 / sqrt(3) of sqrt(sum p^2 (v - out)^2), the signs
-    being independent), or over 2^-21 of the row's largest, and the scores by (d + 3)
-    2^-24 of a sum of magnitudes, of either sign; a tenth is for the spread of the
-    mean itself."""
     print("rms", gamma, ctx, hq, hkv, dh, splits, tree, flush=True)
-    n = ctx + gamma
-    c = _appended(gamma + ctx, hkv, n, dh)
-    q = _normal(11, gamma, hq, dh, std=1.28)
-    out = torch.full((gamma, hq, dh), float("nan"), dtype=q.dtype, device=DEV)
+    c = _appended(gamma + ctx, hkv, ctx + gamma, dh)
     masks = None
     if tree:
         masks = [int(m) for m in W.ancestor_masks(W.draft_tree(seed=3))]
         masks = (masks + [1] * gamma)[:gamma]
-        m = torch.tensor([x - (1 << 64) if x >> 63 else x for x in masks], dtype=torch.int64,
-                         device=DEV)
-        wf.wf_kv8_verify_attn_tree(q.to(DEV), c, out, ctx, m, num_splits=splits)
-    else:
-        wf.wf_kv8_verify_attn(q.to(DEV), c, out, ctx, num_splits=splits)
-    got = out.double().cpu().numpy()
-    vis, grp = _visible(gamma, ctx, masks), hq // hkv
-    err, limit = [], []
-    for g in (0, hkv - 1):               # the first and the last KV head
-        kk = R.E4M3[c.k[g].cpu().numpy()] * R.pow2(c.k_scale[g].cpu())[:, None, None]
-        vv = R.E4M3[c.v[g].cpu().numpy()] * R.pow2(c.v_scale[g].cpu())[:, None, None]
-        kk = kk.reshape(-1, dh)[:n]
-        vv = vv.swapaxes(1, 2).reshape(-1, dh)[:n]
-        for h in (g * grp, (g + 1) * grp - 1):
-            qh = q[:, h].double().numpy()
-            z = np.where(vis, qh @ kk.T * dh ** -0.5, -np.inf)
-            p = np.exp(z - z.max(1, keepdims=True))
-            p /= p.sum(1, keepdims=True)
-            ref = p @ vv
-            half = torch.from_numpy(ref).to(torch.bfloat16).double().numpy() - ref
-            delta = (dh + 3) * 2.0 ** -24 * (np.abs(qh) @ np.abs(kk).T * dh ** -0.5 * vis).max()
-            def around(w):               # sum w (v - out)^2
-                return w @ np.square(vv) - 2 * ref * (w @ vv) + \
-                    np.square(ref) * w.sum(1, keepdims=True)
-            spread = (2.0 ** -9 / 3 ** 0.5 + 2 * delta) ** 2 * around(np.square(p)) + \
-                (2.0 ** -21 / 3 ** 0.5 * p.max(1, keepdims=True)) ** 2 * around(vis.astype(float))
-            err.append(got[:, h] - ref)
-            limit.append(np.square(half) + spread)
-    err, limit = np.stack(err), float(np.sqrt(np.mean(np.stack(limit))))
-    print("rms error", _rms(err), "limit", limit, flush=True)
-    assert _rms(err) <= 1.1 * limit
+    _check_rms(_normal(11, gamma, hq, dh, std=1.28), c, ctx, masks, splits)
+
+
+@pytest.mark.parametrize("gamma,ctx,hq,hkv,dh", [
+    (16, 2000, 16, 4, 128), (16, 2000, 16, 4, 64), (1, 500, 8, 2, 128), (61, 3000, 32, 8, 128),
+])
+@pytest.mark.parametrize("far", [6, 10, 12])
+def test_attention_small_elements_of_q(far, gamma, ctx, hq, hkv, dh):
+    """Elements of q 2^far below the row's largest, which meets zeros of K: the
+    scores come from the small ones."""
+    print("small q", far, gamma, ctx, hq, hkv, dh, flush=True)
+    n = ctx + gamma
+    c = wf.alloc_kv8_cache(hkv, n, dh, DEV)
+    k, v = (_normal(60 + i, n, hkv, dh) for i in (0, 1))
+    k[:, :, 5] = 0
+    wf.wf_kv8_append(k.to(DEV), v.to(DEV), c, 0)
+    q = _normal(62, gamma, hq, dh).clamp(-2, 2)
+    q[:, :, 5] = 3.0 * 2.0 ** far
+    _check_rms(q, c, ctx, scale=2 * dh ** -0.5)
