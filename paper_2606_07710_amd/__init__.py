@@ -688,7 +688,8 @@ class Kv8Cache:
     cap      rows per head; blocks = ceil(cap / 32)
 
     The calls on one layer take a cache without L; layer(l) is one layer of a
-    stack (a view of its memory)."""
+    stack (a view of its memory).  The tensors stay the ones it was made of (the
+    calls hold their addresses); a deep copy has its own."""
 
     def __init__(self, k, v, k_scale, v_scale, cap):
         cap = operator.index(cap)
@@ -706,13 +707,21 @@ class Kv8Cache:
         dev = k.get_device()
         if dev < 0:
             raise ValueError("the cache must be device memory")
-        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self._tensors = k, v, k_scale, v_scale
         self.n_layers = lead[0] if len(lead) == 2 else None
         self.n_kv_heads, self.cap, self.head_dim, self.device = lead[-1], cap, dh, k.device
         self.struct = Kv8CacheStruct(_ptr(k, dev, "k"), _ptr(v, dev, "v"),
                                      _ptr(k_scale, dev, "k_scale"),
                                      _ptr(v_scale, dev, "v_scale"), lead[-1], cap, dh)
         self.ref, self.dev = ctypes.byref(self.struct), dev
+
+    k = property(lambda self: self._tensors[0])
+    v = property(lambda self: self._tensors[1])
+    k_scale = property(lambda self: self._tensors[2])
+    v_scale = property(lambda self: self._tensors[3])
+
+    def __reduce__(self):
+        return Kv8Cache, (*self._tensors, self.cap)
 
     def layer(self, l):
         if self.n_layers is None:

@@ -1,6 +1,8 @@
 """The 8-bit KV cache on the GPU against plain 64-bit definitions: append and
 path compaction exactly (codes and scales), attention within bounds derived
 from the roundings it makes, and a verification round that uses all of them."""
+import copy
+
 import numpy as np
 import pytest
 import torch
@@ -453,6 +455,22 @@ def test_attention_writes_its_output_and_workspace_only(dt, gamma, ctx, hq, hkv,
     assert (room[need:] == 0x5a).all() and not room[:4 << 20].any()
     for a, b in zip(held, (c.k, c.v, c.k_scale, c.v_scale)):
         assert torch.equal(a, b)
+
+
+def test_cache_copies_stand_alone():
+    """A deep copy of a cache (a sequence that branches) is written and read apart
+    from its source."""
+    c = _filled(3, 2, 70, 64, rows=40)
+    held, mine = R.Cache(c), copy.deepcopy(c)
+    ref = R.Cache(mine)
+    k, v = (_normal(i, 9, 2, 64) for i in (1, 2))
+    ref.write(np.stack([t.transpose(0, 1).double().numpy() for t in (k, v)]), 40)
+    wf.wf_kv8_append(k.to(DEV), v.to(DEV), mine, 40)
+    torch.cuda.synchronize()
+    held.check(c)
+    ref.check(mine)
+    del c
+    _check_attention("bf16", _normal(4, 9, 8, 64), mine, 40)
 
 
 def test_attention_nan_stays_in_its_row():

@@ -1,6 +1,7 @@
 """What the 8-bit cache and 4-bit weight calls refuse, on the CPU: no call
 here reaches the GPU (pointers are never dereferenced by the checks)."""
 import contextlib
+import copy
 import ctypes
 
 import numpy as np
@@ -262,6 +263,21 @@ def test_python_cache_takes_whole_capacities_only():
     with pytest.raises(TypeError):
         ok = _kv8()
         wf.Kv8Cache(ok.k, ok.v, ok.k_scale, ok.v_scale, 70.0)
+
+
+def test_python_cache_keeps_its_tensors():
+    """The calls hold the tensors' addresses: others cannot take their place, and a
+    deep copy holds those of its own."""
+    c = _kv8(layers=3)
+    for name in ("k", "v", "k_scale", "v_scale"):
+        with pytest.raises(AttributeError):
+            setattr(c, name, getattr(c, name))
+    for t, at in zip((c.k, c.v, c.k_scale, c.v_scale), (16, 32, 48, 64)):
+        t.ptr = at
+    mine = copy.deepcopy(c)
+    assert mine.k is not c.k and (mine.n_layers, mine.cap, mine.head_dim) == (3, 70, 64)
+    assert [getattr(mine.struct, n) for n in ("k", "v", "k_scale", "v_scale")] == [16, 32, 48, 64]
+    assert copy.copy(c).k is c.k and c.struct.k == 8
 
 
 def test_python_one_layer_calls_refuse_a_stack():
