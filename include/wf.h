@@ -748,7 +748,8 @@ wf_status_t wf_w4_pack(const void *codes, const uint8_t *scales, int32_t rows, i
  * res      [n_rows][n_out] bf16, or NULL.  May be y itself when out_dt is
  *          WF_BF16.
  * y        [n_rows][n_out], out_dt WF_BF16 (rounded once) or WF_F32 (as the
- *          logits of wf_lmhead_accept_entropy and wf_lmhead_accept_tree).
+ *          logits of wf_lmhead_accept_entropy and wf_lmhead_accept_tree).  Must
+ *          not overlap x.
  * Limits:  1 <= n_rows <= 64; the weight's; x and packed 16-byte aligned.
  * workspace >= wf_linear_w4_workspace_bytes(...) bytes (may be NULL when
  *          that is 0). */
