@@ -105,8 +105,9 @@ __device__ __forceinline__ bf16x8 w4_expand(uint32_t w, float s) {
 // wave order.  MFMA kk of chunk c takes the scale group 128c + 32kk ..: lane (m16,
 // c4) its inputs 8*c4 .. +7 of feature m16 of each block and of x row m16, so four
 // lanes read 64 contiguous bytes of x.  Bound by its launch and one or two trips to
-// memory (one row, 4096 to 4096: 3.7 us, of which an empty launch takes 1.7), or by
-// the bytes in flight (12288 to 4096: 9.7 us, 2.8 TB/s).
+// memory (one row, 4096 to 4096: 4.5 us out of HBM, 3.7 out of the last-level cache, of
+// which an empty launch takes 1.7), or by the bytes in flight (12288 to 4096: 9.8 us,
+// 2.7 TB/s).
 template <int FB>
 __global__ __launch_bounds__(kW4Waves * kWave) void linear_w4(
     const uint16_t *__restrict__ x, const uint8_t *__restrict__ w, const uint16_t *res, void *y,
@@ -209,9 +210,9 @@ __global__ __launch_bounds__(kW4Waves * kWave) void linear_w4(
 // ask for a quarter.  Lanes and tiles as above.  The staged x is swizzled in 16-
 // byte granules, g ^ (row & 7), so eight rows' reads meet distinct banks.  With
 // several slices each stores its fp32 sums, part[slice][row][16 * blocks], for
-// w4_sum.  Bound by HBM up to 16 rows (4096 to 24576: 13.2 us, 4.1 TB/s; 4096 to
-// 128256: 46.9, 6.0) and with many features (61 rows, 2560 to 151936: 55 us, 44 MB
-// of them logits stored at the end), else by x: LDS, and L2 once per workgroup.
+// w4_sum.  Bound by HBM up to 16 rows (16 rows, 4096 to 24576: 13.5 us, 4.0 TB/s; 4096
+// to 128256, fp32 out: 50, 5.7) and with many features (61 rows, 2560 to 151936: 55 us,
+// 37 MB of them logits stored at the end), else by x: LDS, and L2 once per workgroup.
 template <int NB, int FB, int KW>
 __global__ __launch_bounds__(kW4Waves * kWave) void linear_w4_wide(
     const uint16_t *__restrict__ x, const uint8_t *__restrict__ w, const uint16_t *res, void *y,
@@ -519,34 +520,33 @@ W4Plan plan_linear_w4(int rows, int n_out, int k_in) {
     W4Plan p{};
     p.slices = 1;
     // Up to 16 rows and three blocks per CU: the input split, one workgroup per CU
-    // (one row, 4096 to 8192: 6.3 us, the feature split 7.4; 16 rows, 4096 to 16384:
-    // 12.1 and 11.1).  But each workgroup reads all of x, so where that is much and
-    // the features few, slices of the feature split (16 rows, 12288 to 4096: 15.1
-    // us, 12.4 in four slices; 25600 to 5120: 33 and 21; 8192 to 4096: 10.6 and
-    // 10.9; 8 rows, 12288 to 4096: 11.2 and 12.6).
+    // (one row, 4096 to 8192: 6.5 us, the feature split 7.6; to 12288: 8.3 and 9.4; 8
+    // rows, 8192 to 8192: 12.2 and 13.5; 16 rows, 4096 to 12288: 10.3 and 10.0, to
+    // 8192: 8.4 and 7.8).  But each workgroup reads all of x, so where that is much and
+    // the features few, slices of the feature split (16 rows, 12288 to 4096: 15.6 us,
+    // 12.5 in four slices; 25600 to 5120: 33.8 and 20.8; 8192 to 4096: 11.1 and 11.2; 8
+    // rows, 12288 to 4096: 12.0 and 12.4).
     const bool much_x = blocks < 2 * 256 && rows * k_in > 144 * 1024;
     if (rows <= 16 && blocks <= 3 * 256 && !much_x) {
         p.fb = (blocks + 255) / 256;
         p.groups = (blocks + p.fb - 1) / p.fb;
         return p;
     }
-    // As many waves to a feature group as leave each up to five blocks: more loads
-    // in flight (one row, 4096 to 32000: 23.0 us with one, 19.7 with two, 15.2 with
-    // four; 16 rows, 4096 to 16384: 12.1 with four, 11.1 with eight; to 64000: 37,
-    // 26.7 and 28.0).  Of more than 16 rows the LDS reads of x weigh against it: four
-    // up to eight blocks per CU, two up to 20 (64 rows, 4096 to 24576: 33.5 us with
-    // one, 28.3 with two, 25.9 with four, now 20.4; 2560 to 40000: 30.3, 26.9 and
-    // 29.6, now 20.8).
+    // As many waves to a feature group as leave each up to five blocks, at most four:
+    // more loads in flight (us with one, two, four waves.  To 24576, from 4096: one row
+    // -, 14.0, 12.1; 64 rows 28.2, 23.2, 21.5.  To 40000: one row, from 4096, -, 19.4,
+    // 19.2; 64 rows, from 2560, 24.3, 21.8, 21.8, from 4096 -, 31.7, 30.3.  16 rows, 4096
+    // to 64000: 28.0, 28.1, 29.3; to 100000: 39.3, 42.5, -; 64 rows, 2560 to 60000: 28.3,
+    // 28.1, -; to 90000: 37.0, 43.2, -).  Eight lose to four from the first (16 rows, 4096
+    // to 16384: 11.0 and 10.8; one row, 2560 to 19456: 9.1 and 8.1).
     p.wide = true;
-    if (rows <= 16)
-        p.kw = much_x ? 4 : blocks <= 5 * 256 ? 8 : blocks <= 10 * 256 ? 4 : blocks <= 20 * 256 ? 2 : 1;
-    else
-        p.kw = blocks <= 8 * 256 ? 4 : blocks <= 20 * 256 ? 2 : 1;
+    p.kw = blocks <= 10 * 256 ? 4 : blocks <= 20 * 256 ? 2 : 1;
     const int fg = kW4Waves / p.kw;
     // fewer than two blocks per CU: slices of at least two chunks, so a workgroup
-    // reads less of x (64 rows, 4096 to 4096: 13.6 us, 23.4 without, now 11.5; the
-    // last workgroup to arrive adding the slices up instead of w4_sum: 16.8), at most
-    // four (12288 to 4096: 18.8 us, now 17.3, 20.2 with eight, 22.5 with two)
+    // reads less of x, at most four (64 rows, 4096 to 4096: 13.3 us without, 12.5 with
+    // two or four, 16.1 with eight; 12288 to 4096: 32.3, 22.3 with two, 19.0 with four,
+    // 20.8 with eight).  (The last workgroup to arrive adding the slices up instead of
+    // w4_sum took 16.8 us where the second launch took 13.)
     const int chunks = (k_in + 128 * p.kw - 1) / (128 * p.kw);
     if (blocks < 2 * 256)
         p.slices = std::max(1, std::min({kW4MaxSlices, chunks / 2, 5 * fg * 256 / blocks}));
@@ -596,17 +596,14 @@ wf_status_t launch_linear_w4(const uint16_t *x, const uint8_t *w, const uint16_t
                                                                   k_in, f32_out, quads, part);\
     else
 #define WF_W4_FEW(NBV, KWV) WF_W4(NBV, 1, KWV) WF_W4(NBV, 2, KWV)
-#define WF_W4_SOME(NBV, KWV) WF_W4(NBV, 3, KWV) WF_W4(NBV, 4, KWV)
-#define WF_W4_MANY(NBV, KWV) WF_W4_SOME(NBV, KWV) WF_W4(NBV, 5, KWV)
+#define WF_W4_MANY(NBV, KWV) WF_W4(NBV, 3, KWV) WF_W4(NBV, 4, KWV) WF_W4(NBV, 5, KWV)
     // (what the plan can ask for)
     WF_W4_MANY(1, 1) WF_W4_MANY(2, 1) WF_W4_MANY(3, 1) WF_W4_MANY(4, 1)
     WF_W4_MANY(1, 2) WF_W4_MANY(2, 2) WF_W4_MANY(3, 2) WF_W4_MANY(4, 2)
     WF_W4_FEW(1, 4) WF_W4_FEW(2, 4) WF_W4_FEW(3, 4) WF_W4_FEW(4, 4)
-    WF_W4_MANY(1, 4) WF_W4_SOME(2, 4) WF_W4_SOME(3, 4) WF_W4_SOME(4, 4)
-    WF_W4(1, 4, 8) WF_W4(1, 5, 8)
+    WF_W4_MANY(1, 4) WF_W4_MANY(2, 4) WF_W4_MANY(3, 4) WF_W4_MANY(4, 4)
     return WF_ERR_UNSUPPORTED;
 #undef WF_W4_FEW
-#undef WF_W4_SOME
 #undef WF_W4_MANY
 #undef WF_W4
     if (p.slices > 1) {

@@ -141,6 +141,20 @@ def test_linear_many_features(rows, n_out, k_in):
     _check(x, codes, scales, y, out="f32")
 
 
+# At the lines between four, two and one wave to a feature group, on both sides, for
+# each number of 16-row blocks.
+@pytest.mark.parametrize("n_out", [12289, 20480, 40950, 40970, 81920, 81921])
+@pytest.mark.parametrize("rows,k_in", [(1, 1056), (16, 544), (20, 544), (47, 288), (64, 1312)])
+def test_linear_wave_counts(rows, k_in, n_out):
+    print("wave counts", rows, n_out, k_in, flush=True)
+    codes, scales = _weight(rows + n_out, n_out, k_in)
+    x, r = _normal(k_in, rows, k_in), _normal(3, rows, n_out)
+    y = torch.full((rows, n_out), float("nan"), dtype=torch.bfloat16, device=DEV)
+    wf.wf_linear_w4(x.to(DEV), wf.W4Weight(codes.to(DEV), scales.to(DEV)), y, r.to(DEV))
+    torch.cuda.synchronize()
+    _check(x, codes, scales, y, r)
+
+
 @pytest.mark.parametrize("rows,n_out,k_in", [(3, 40, 64), (20, 1000, 512), (40, 33000, 64)])
 @pytest.mark.parametrize("out", ["bf16", "f32"])
 def test_linear_odd_addresses(rows, n_out, k_in, out):
