@@ -71,10 +71,10 @@ struct Attn8Params {
 // h ^ (d >> 2 & 1) ^ (d >> 3 & 1).
 //
 // Bound, up to 64 rows, by the cache's bytes, the first tile and the merge (16
-// rows, 32K keys of 8 heads, 67 MB: 17.5 us and the merge's 4.6; cold 23.7 in
+// rows, 32K keys of 8 heads, 67 MB: 17 us and the merge's 5; out of HBM 24.6 in
 // all); above by the two waves per SIMD that its registers allow: products, vector
 // work and LDS reads of a tile take about half of its time (1024 rows and heads, 64K
-// keys: 50 us, 15 of products and 16 of vector work).
+// keys: 54 us out of HBM, 15 of products and 16 of vector work).
 // ---------------------------------------------------------------------------
 constexpr int kTileKeys8 = 128;
 constexpr int kTileBlocks = kTileKeys8 / kKv8Block;
@@ -721,20 +721,20 @@ __global__ __launch_bounds__(64 * kRowWaves) void attn8_rows(Attn8Params a) {
 
 }  // namespace
 
-// Split plan of a call.  bf16: up to 64 rows share a workgroup's tiles, two key
-// streams of up to four 16-row waves, one workgroup per CU; of more rows each 64
-// take a workgroup of one stream, two per CU, which do not wait for each other's
-// barriers (128 rows, 64K keys: 51.4 us, 53.0 as one workgroup of eight waves; 244
-// rows, 8K keys: 18.9 and 21.5 us, though the tiles are then read from L2 twice as
-// often).  No workgroup is without a tile.  Where each has few, one stream, whose
-// first stage is there sooner and which has nothing to join at its end (32 rows,
-// 1K keys: 8.9 -> 8.1 us, 8K 13.3 -> 12.6, but 32K 22.4 -> 22.7; 64 rows, 1K keys:
-// 10.9 -> 9.0, 8K 15.3 -> 13.7, 32K 25.9 -> 23.7, 64K 38.4 both ways, 128K 59.6 ->
-// 67.8).  The fewest stay one split, whose workgroup writes the output and spares
-// the merge: up to two steps (32 rows, 500 keys: 7.6 us, 7.9 as four splits), or one
-// of 64 rows, whose steps take twice as long (256 keys: 7.1 and 8.2 us; 516 keys in
-// three: 12.3 and 8.7).  fp32: splits only where the rows leave CUs idle (256 rows
-// and heads, 2K keys: 13.8 us, 17.3 as four; 32, 4K keys: 25.1 and 8.8 as eight).
+// Split plan of a call (figures: three caches in turn, one workspace, in a graph).
+// bf16: up to 64 rows share a workgroup's tiles, two key streams of up to four 16-row
+// waves, one workgroup per CU; of more rows each 64 take a workgroup of one stream, two
+// per CU, which do not wait for each other's barriers (244 rows, 8K keys: 21.7 us, 23.8
+// with 128 rows to a workgroup of eight waves; 128 rows, 8K 16.9 and 18.0, 64K 59 both
+// ways).  No workgroup is without a tile.  Where each has few, one stream, whose first
+// stage is there sooner and which has nothing to join at its end (one stream and two,
+// us: 32 rows, 1K keys 8.4 and 9.3, 8K 12.8 and 13.2, 32K 21.1 and 19.7; 64 rows, 1K 9.5
+// and 11.4, 8K 13.8 and 15.6, 32K 22.9 and 23.4, 64K 39.9 and 39.7, 128K 69.2 and 64.7).
+// The fewest stay one split, whose workgroup writes the output and spares the merge: up
+// to two steps (32 rows, 500 keys: 7.6 us, 8.2 as four splits), or one of 64 rows,
+// whose steps take twice as long (256 keys: 6.9 us, 8.8 as two; 516 keys: 12.1 as one,
+// 9.4 as five).  fp32: splits only where the rows leave CUs idle (256 rows and heads,
+// 2K keys: 16.9 us, 18.6 as four; 32, 4K keys: 27.9 and 9.6 as eight).
 AttnPlan plan_attn8(wf_dtype_t dt, int gamma, int ctx_len, int n_q_heads, int n_kv_heads,
                     int head_dim, int num_splits) {
     AttnPlan p{};

@@ -537,8 +537,9 @@ W4Plan plan_linear_w4(int rows, int n_out, int k_in) {
     // -, 14.0, 12.1; 64 rows 28.2, 23.2, 21.5.  To 40000: one row, from 4096, -, 19.4,
     // 19.2; 64 rows, from 2560, 24.3, 21.8, 21.8, from 4096 -, 31.7, 30.3.  16 rows, 4096
     // to 64000: 28.0, 28.1, 29.3; to 100000: 39.3, 42.5, -; 64 rows, 2560 to 60000: 28.3,
-    // 28.1, -; to 90000: 37.0, 43.2, -).  Eight lose to four from the first (16 rows, 4096
-    // to 16384: 11.0 and 10.8; one row, 2560 to 19456: 9.1 and 8.1).
+    // 28.1, -; to 90000: 37.0, 43.2, -).  Eight gain on four nowhere but for one row of
+    // long input (16 rows, 4096 to 16384: 11.0 and 10.8; one row, 2560 to 19456: 9.1 and
+    // 8.1, 12288 to 16384: 22.2 and 22.7).
     p.wide = true;
     p.kw = blocks <= 10 * 256 ? 4 : blocks <= 20 * 256 ? 2 : 1;
     const int fg = kW4Waves / p.kw;
