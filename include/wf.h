@@ -60,6 +60,19 @@
  *                             products stream
  *   wf_linear_w4              y = W x (+ residual) over a 4-bit weight
  *
+ * and the round of many requests at once, whose K/V rows lie in the pages of
+ * a shared pool:
+ *
+ *   wf_paged_append           the new tokens' K (rotated) and V into their
+ *                             pages, the pages' bounds, and rotated q
+ *   wf_paged_verify_attn      verify attention of every request's rows over
+ *                             its pages, block-causal or under tree masks
+ *   wf_paged_select           per row and KV head, the pages whose bounds
+ *                             promise the largest scores
+ *   wf_paged_sparse_attn      attention over the selected pages only
+ *   wf_token_logprobs         log probability, rank and alternatives of the
+ *                             drafted tokens, with the entropy
+ *
  * Conventions shared by every call
  *   - Every tensor pointer is DEVICE memory owned by the caller, 16-byte
  *     aligned, densely packed in the layout stated.  The library never
@@ -757,6 +770,177 @@ wf_status_t wf_linear_w4(const void *x, const void *packed, const void *res, wf_
                          void *y, int32_t n_rows, int32_t n_out, int32_t k_in, void *workspace,
                          size_t workspace_bytes, void *stream);
 size_t wf_linear_w4_workspace_bytes(int32_t n_rows, int32_t n_out, int32_t k_in);
+
+/* ------------------------------------------------------------------------
+ * A paged KV cache and a batch of requests (Sec. 3.2's round, for many
+ * requests at once).  A layer's cache is a pool of pages:
+ *
+ *   k, v    [n_pages][n_kv_heads][page_size][head_dim], post-RoPE keys
+ *   bounds  [n_pages][n_kv_heads][2][head_dim], the smallest and the largest
+ *           key of the page in every dimension (NaN where one of them is
+ *           NaN), in the cache's type; NULL where no call needs it
+ *
+ * and a batch is a ragged list of n_seqs sequences, its arrays in device
+ * memory, so that a captured graph replays with other lengths and pages:
+ *
+ *   row_start   [n_seqs + 1] int32, not decreasing: sequence b owns the rows
+ *               row_start[b] .. row_start[b+1] - 1 of the call's tensors
+ *               (none: an idle sequence).  Rows before the first and behind
+ *               the last sequence are neither read nor written.
+ *   ctx_len     [n_seqs] int32: its row i sits at position ctx_len[b] + i
+ *   page_table  [n_seqs][max_pages] int32: position p lies in row p %
+ *               page_size of the page page_table[b][p / page_size].  Entries
+ *               outside [0, n_pages) name no page: nothing is stored there
+ *               and no row sees keys there.
+ *   max_rows    the most rows that a sequence has in an attention or
+ *               selection call, at most 64 (the append takes any number)
+ *
+ * A sequence whose numbers break these rules (row_start decreasing or outside
+ * [0, n_rows], more than max_rows rows, a negative context, positions past
+ * max_pages * page_size) is skipped: nothing of it is read or written.
+ * Limits: 1 <= n_seqs <= 1024; page_size in {16, 32, 64, 128}; 1 <= max_pages,
+ * max_pages * page_size <= 2^26; 1 <= n_pages; 0 <= n_rows <= 2^20 (0 is a
+ * no-op); head_dim in {64, 128}; WF_F32 or WF_BF16, one type for the cache and
+ * the call's tensors.  Two sequences must not share a page that a call
+ * writes.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+    void *k, *v, *bounds;
+    int32_t n_pages, page_size, n_kv_heads, head_dim;
+} wf_paged_cache_t;
+
+typedef struct {
+    const int32_t *page_table, *row_start, *ctx_len;
+    int32_t n_seqs, max_pages, max_rows;
+} wf_paged_batch_t;
+
+/* wf_paged_append -- the batch's new K/V rows into their pages, the rotation
+ * on the way: with pos = positions[r], or the row's position ctx_len[b] + i
+ * where positions is NULL (a draft tree's rows are rotated by their depth),
+ *
+ *   K page row <- RoPE(k[r], pos),  V page row <- v[r],
+ *   q_out[r] = RoPE(q[r], pos)
+ *
+ * RoPE as in wf_kv_only_prefill (rotate-half, angles in fp64).  Where the
+ * cache has bounds, those of every page that received a row become the
+ * bounds of its rows up to the sequence's newest position, as stored; older
+ * contents count for nothing, so rows taken back by a rollback leave no trace.
+ * k, v   n_rows rows of [n_kv_heads][head_dim], kv_row_stride ELEMENTS apart;
+ * q      n_rows rows of [n_q_heads][head_dim], q_row_stride apart, or NULL
+ *        (q_out is then not written); q_out [n_rows][n_q_heads][head_dim],
+ *        which may be q itself where q is dense.  Strides in multiples of 16
+ *        bytes, at least one row.  positions [n_rows] int32, not negative.
+ * Limits: n_q_heads % n_kv_heads == 0, n_q_heads <= 256 (with q);
+ *        rope_base > 0 and finite. */
+wf_status_t wf_paged_append(wf_dtype_t dt, const wf_paged_cache_t *cache,
+                            const wf_paged_batch_t *batch, const void *k,
+                            const void *v, size_t kv_row_stride, const void *q,
+                            size_t q_row_stride, void *q_out, int32_t n_q_heads,
+                            const int32_t *positions, double rope_base,
+                            int32_t n_rows, void *stream);
+
+/* wf_paged_verify_attn -- wf_verify_attn for every sequence of the batch over
+ * its pages: row i of sequence b attends to the positions 0 .. ctx_len[b]+i,
+ * or, with tree_mask ([n_rows] uint64, each row's mask as in
+ * wf_verify_attn_tree, bit j for the sequence's row j), to the ctx_len[b]
+ * cached positions, to itself and to the block rows of its mask.  q, out
+ * [n_rows][n_q_heads][head_dim].  The batch's rows must be in the pages
+ * (wf_paged_append); positions behind them are not read.  Values of block
+ * rows that a row does not see have to be finite.  A row that sees no key
+ * (pages missing) gets zeros.  Limits as for wf_verify_attn; n_rows *
+ * n_q_heads <= 2^22.
+ * workspace >= wf_paged_verify_attn_workspace_bytes(...) bytes. */
+wf_status_t wf_paged_verify_attn(wf_dtype_t dt, const void *q,
+                                 const wf_paged_cache_t *cache,
+                                 const wf_paged_batch_t *batch, void *out,
+                                 const uint64_t *tree_mask, int32_t n_rows,
+                                 int32_t n_q_heads, float softmax_scale,
+                                 void *workspace, size_t workspace_bytes,
+                                 void *stream);
+size_t wf_paged_verify_attn_workspace_bytes(wf_dtype_t dt, int32_t n_rows,
+                                            int32_t n_seqs, int32_t max_rows,
+                                            int32_t n_q_heads,
+                                            int32_t n_kv_heads,
+                                            int32_t head_dim);
+
+/* wf_paged_select -- the pages that each row's attention is worth reading.
+ * For row r at position p, the pages 0 .. p / page_size - n_recent are the old
+ * ones, the n_recent pages up to its own the recent ones (fewer near the
+ * start).  An old page's score for KV head g is the largest score that a key
+ * within its bounds could have with a query head of the group,
+ *
+ *   s = max_h sum_d q_d (q_d >= 0 ? hi[d] : lo[d]),  q_d = q[r][h][d],
+ *
+ * formed in fp64.  sel[r][g] receives the n_sel - n_recent old pages of the
+ * largest scores (the lower page among equals; a NaN score before all others;
+ * pages without an entry in the table never) and the recent ones, as logical
+ * page numbers in ascending order, then -1.  Every old page is complete and
+ * visible to its row, so the selection is causal for chains, blocks and trees.
+ * q [n_rows][n_q_heads][head_dim]; sel [n_rows][n_kv_heads][n_sel] int32.
+ * Limits: 1 <= n_recent <= n_sel <= 1024; max_pages <= 65536; n_rows *
+ * n_kv_heads <= 2^19; the cache's bounds; n_q_heads as for wf_verify_attn.
+ * workspace >= wf_paged_select_workspace_bytes(...) bytes. */
+wf_status_t wf_paged_select(wf_dtype_t dt, const void *q,
+                            const wf_paged_cache_t *cache,
+                            const wf_paged_batch_t *batch, int32_t *sel,
+                            int32_t n_sel, int32_t n_recent, int32_t n_rows,
+                            int32_t n_q_heads, void *workspace,
+                            size_t workspace_bytes, void *stream);
+size_t wf_paged_select_workspace_bytes(int32_t n_rows, int32_t n_kv_heads,
+                                       int32_t max_pages);
+
+/* wf_paged_sparse_attn -- wf_paged_verify_attn with the keys of row r and KV
+ * head g restricted to the pages sel[r][g][0 .. n_sel) (logical page numbers
+ * in any order, as wf_paged_select writes them; entries that are negative, or
+ * past the row's own page, are passed over; a page listed twice counts twice).
+ * Limits: 1 <= n_sel <= 1024; the rest as there.
+ * workspace >= wf_paged_sparse_attn_workspace_bytes(...) bytes. */
+wf_status_t wf_paged_sparse_attn(wf_dtype_t dt, const void *q,
+                                 const wf_paged_cache_t *cache,
+                                 const wf_paged_batch_t *batch,
+                                 const int32_t *sel, int32_t n_sel, void *out,
+                                 const uint64_t *tree_mask, int32_t n_rows,
+                                 int32_t n_q_heads, float softmax_scale,
+                                 void *workspace, size_t workspace_bytes,
+                                 void *stream);
+size_t wf_paged_sparse_attn_workspace_bytes(wf_dtype_t dt, int32_t n_rows,
+                                            int32_t n_q_heads,
+                                            int32_t n_kv_heads,
+                                            int32_t head_dim,
+                                            int32_t page_size, int32_t n_sel);
+
+/* ------------------------------------------------------------------------
+ * wf_token_logprobs -- what the target says of given tokens (Sec. 3.2's
+ * candidates, or a prompt's): for every row of logits z, p = softmax(z),
+ *
+ *   logprob_out[r]  = log p(t), t = tokens[r]
+ *   rank_out[r]     = number of tokens that come before t when they are
+ *                     ordered by logit, the lower index first among equals
+ *   entropy_out[r]  = -sum p log p, in nats
+ *   top_ids, top_logprobs [n_rows][n_top]: the first n_top tokens of that
+ *                     order and their log probabilities
+ *
+ * logits [n_rows] rows of vocab values of type dt (WF_F32 or WF_BF16),
+ * row_stride ELEMENTS apart (any stride >= vocab, any alignment of the
+ * element type).  A logit of -inf has probability 0 and adds nothing to the
+ * entropy; a row with a NaN, with +inf or with nothing above -inf has NaN for
+ * its log probabilities and entropy; NaN comes first in the order.
+ * A token outside [0, vocab) (padding) gets 0 and rank -1.
+ * entropy_out, rank_out may be NULL; tokens may be NULL with logprob_out and
+ * rank_out; top_ids and top_logprobs are NULL exactly when n_top is 0.
+ * Limits: 0 <= n_rows <= 2^20; 1 <= vocab <= 2^30; 0 <= n_top <= 64,
+ * n_top <= vocab.  Sums are fp32 of at most a few thousand terms each, joined
+ * in a fixed order.
+ * workspace >= wf_token_logprobs_workspace_bytes(...) bytes. */
+wf_status_t wf_token_logprobs(wf_dtype_t dt, const void *logits,
+                              size_t row_stride, const int32_t *tokens,
+                              int32_t n_rows, int32_t vocab, int32_t n_top,
+                              float *logprob_out, float *entropy_out,
+                              int32_t *rank_out, int32_t *top_ids,
+                              float *top_logprobs, void *workspace,
+                              size_t workspace_bytes, void *stream);
+size_t wf_token_logprobs_workspace_bytes(wf_dtype_t dt, int32_t n_rows,
+                                         int32_t vocab, int32_t n_top);
 
 /* ------------------------------------------------------------------------
  * wf_read_probe -- measurement support, not a step of the method: reads

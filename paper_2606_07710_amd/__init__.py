@@ -38,6 +38,10 @@ EXPORTED_SYMBOLS = (
     "wf_kv8_only_prefill_workspace_bytes", "wf_kv8_verify_attn", "wf_kv8_verify_attn_tree",
     "wf_kv8_verify_attn_workspace_bytes", "wf_kv8_compact_path", "wf_w4_quantize",
     "wf_w4_packed_bytes", "wf_w4_pack", "wf_linear_w4", "wf_linear_w4_workspace_bytes",
+    "wf_paged_append", "wf_paged_verify_attn", "wf_paged_verify_attn_workspace_bytes",
+    "wf_paged_select", "wf_paged_select_workspace_bytes", "wf_paged_sparse_attn",
+    "wf_paged_sparse_attn_workspace_bytes", "wf_token_logprobs",
+    "wf_token_logprobs_workspace_bytes",
 )
 KV8_BLOCK = 32                       # WF_KV8_BLOCK
 # what the low-bit calls take as e4m3 elements, power-of-two scales, e2m1 pairs
@@ -68,6 +72,21 @@ class Kv8CacheStruct(ctypes.Structure):
                 ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
                 ("n_kv_heads", ctypes.c_int32), ("cap", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32)]
+
+
+class PagedCacheStruct(ctypes.Structure):
+    """wf_paged_cache_t: device pointers of one layer's pool of pages and its
+    shape."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("bounds", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
+
+
+class PagedBatchStruct(ctypes.Structure):
+    """wf_paged_batch_t: device pointers of a batch's lists and their sizes."""
+    _fields_ = [("page_table", ctypes.c_void_p), ("row_start", ctypes.c_void_p),
+                ("ctx_len", ctypes.c_void_p), ("n_seqs", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("max_rows", ctypes.c_int32)]
 
 
 class SwitchState(ctypes.Structure):
@@ -177,6 +196,24 @@ def _load():
     lib.wf_linear_w4.restype = i32
     lib.wf_linear_w4_workspace_bytes.argtypes = [i32, i32, i32]
     lib.wf_linear_w4_workspace_bytes.restype = sz
+    lib.wf_paged_append.argtypes = [i32, p, p, p, p, sz, p, sz, p, i32, p, f64, i32, p]
+    lib.wf_paged_append.restype = i32
+    lib.wf_paged_verify_attn.argtypes = [i32, p, p, p, p, p, i32, i32, f32, p, sz, p]
+    lib.wf_paged_verify_attn.restype = i32
+    lib.wf_paged_verify_attn_workspace_bytes.argtypes = [i32] * 7
+    lib.wf_paged_verify_attn_workspace_bytes.restype = sz
+    lib.wf_paged_select.argtypes = [i32, p, p, p, p, i32, i32, i32, i32, p, sz, p]
+    lib.wf_paged_select.restype = i32
+    lib.wf_paged_select_workspace_bytes.argtypes = [i32] * 3
+    lib.wf_paged_select_workspace_bytes.restype = sz
+    lib.wf_paged_sparse_attn.argtypes = [i32, p, p, p, p, i32, p, p, i32, i32, f32, p, sz, p]
+    lib.wf_paged_sparse_attn.restype = i32
+    lib.wf_paged_sparse_attn_workspace_bytes.argtypes = [i32] * 7
+    lib.wf_paged_sparse_attn_workspace_bytes.restype = sz
+    lib.wf_token_logprobs.argtypes = [i32, p, sz, p, i32, i32, i32, p, p, p, p, p, p, sz, p]
+    lib.wf_token_logprobs.restype = i32
+    lib.wf_token_logprobs_workspace_bytes.argtypes = [i32] * 4
+    lib.wf_token_logprobs_workspace_bytes.restype = sz
     lib.wf_read_probe.argtypes = [p, sz, p, sz, i32, p]
     lib.wf_read_probe.restype = i32
     lib.wf_read_probe_series.argtypes = [p, sz, sz, i32, i32, p, sz, i32, i32, p]
@@ -938,6 +975,272 @@ def wf_linear_w4(x, weight, out, residual=None, workspace=None, stream=None):
                           0 if workspace is None else workspace.numel(), raw)
     _check(st, "wf_linear_w4")
     return out
+
+
+class PagedCache:
+    """One layer's paged K/V cache (wf.h): a pool of pages that the sequences of
+    a batch share.
+
+    k, v     [n_pages][Hkv][page][D] bf16 or fp32, page 16, 32, 64 or 128
+    bounds   [n_pages][Hkv][2][D] of the same type, each page's smallest and
+             largest key per dimension (kept by wf_paged_append, read by
+             wf_paged_select), or None
+
+    The tensors stay the ones it was made of (the calls hold their addresses); a
+    deep copy has its own."""
+
+    def __init__(self, k, v, bounds=None):
+        shape = tuple(k.shape)
+        if len(shape) != 4 or tuple(v.shape) != shape or v.dtype != k.dtype:
+            raise ValueError("k and v must be [n_pages][Hkv][page][D], of one type")
+        n, hkv, page, dh = shape
+        if bounds is not None and (tuple(bounds.shape) != (n, hkv, 2, dh)
+                                   or bounds.dtype != k.dtype):
+            raise ValueError("bounds must be [n_pages][Hkv][2][D], of k's type")
+        dev = k.get_device()
+        if dev < 0:
+            raise ValueError("the cache must be device memory")
+        self._tensors = k, v, bounds
+        self.code, self.dtype, self.device, self.dev = _dtype_code(k), k.dtype, k.device, dev
+        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = shape
+        self.struct = PagedCacheStruct(_ptr(k, dev, "k"), _ptr(v, dev, "v"),
+                                       _ptr(bounds, dev, "bounds"), n, page, hkv, dh)
+        self.ref = ctypes.byref(self.struct)
+
+    k = property(lambda self: self._tensors[0])
+    v = property(lambda self: self._tensors[1])
+    bounds = property(lambda self: self._tensors[2])
+
+    def __reduce__(self):
+        return PagedCache, self._tensors
+
+
+def alloc_paged_cache(n_pages, page_size, n_kv_heads, head_dim, dtype, device,
+                      bounds=True) -> PagedCache:
+    """An empty paged cache (zeros) of one layer."""
+    k, v = (torch.zeros((n_pages, n_kv_heads, page_size, head_dim), dtype=dtype, device=device)
+            for _ in range(2))
+    b = torch.zeros((n_pages, n_kv_heads, 2, head_dim), dtype=dtype,
+                    device=device) if bounds else None
+    return PagedCache(k, v, b)
+
+
+class PagedBatch:
+    """A ragged batch over paged caches (wf.h): int32 device tensors page_table
+    [n_seqs][max_pages], row_start [n_seqs + 1] and ctx_len [n_seqs], which the
+    caller may refill between calls (and between a captured graph's replays), and
+    the most rows that a sequence has in an attention or selection call."""
+
+    def __init__(self, page_table, row_start, ctx_len, max_rows=64):
+        n, max_pages = page_table.shape
+        if tuple(row_start.shape) != (n + 1,) or tuple(ctx_len.shape) != (n,):
+            raise ValueError("page_table [n][max_pages], row_start [n + 1], ctx_len [n]")
+        for t in (page_table, row_start, ctx_len):
+            if t.dtype != torch.int32:
+                raise TypeError("page_table, row_start and ctx_len are int32")
+        dev = page_table.get_device()
+        if dev < 0:
+            raise ValueError("the batch's lists must be device memory")
+        self._tensors = page_table, row_start, ctx_len
+        self.n_seqs, self.max_pages, self.dev = n, max_pages, dev
+        self.max_rows = operator.index(max_rows)
+        self.struct = PagedBatchStruct(_ptr(page_table, dev, "page_table"),
+                                       _ptr(row_start, dev, "row_start"),
+                                       _ptr(ctx_len, dev, "ctx_len"), n, max_pages,
+                                       self.max_rows)
+        self.ref = ctypes.byref(self.struct)
+
+    page_table = property(lambda self: self._tensors[0])
+    row_start = property(lambda self: self._tensors[1])
+    ctx_len = property(lambda self: self._tensors[2])
+
+    def __reduce__(self):
+        return PagedBatch, (*self._tensors, self.max_rows)
+
+
+def _paged(cache, batch, dev):
+    if cache.dev != dev or batch.dev != dev:
+        raise ValueError("the cache and the batch must be on the current device")
+    return cache.ref, batch.ref
+
+
+def _row_stride(t, name):
+    """The distance of t's rows [n][heads][D] in elements; the rest is dense."""
+    n, heads, dh = t.shape
+    s = t.stride()
+    if t.numel() and ((dh > 1 and s[2] != 1) or (heads > 1 and s[1] != dh)):
+        raise ValueError(f"the heads of a row of {name} must lie side by side")
+    return s[0] if n > 1 else heads * dh
+
+
+def wf_paged_append(k, v, cache, batch, rope_base, q=None, q_out=None, positions=None,
+                    stream=None):
+    """k, v [n][Hkv][D], not yet rotated, into the batch's pages, K rotated;
+    with q [n][Hq][D], q_out [n][Hq][D] receives it rotated.  A row's heads lie
+    side by side, rows may be strided (alike for k and v), as in views of one
+    fused projection.  positions [n] int32: what to rotate by, where that is not
+    the row's position (draft trees)."""
+    dev, raw = _at(stream)
+    shape = tuple(k.shape)
+    n, hkv, dh = shape
+    if tuple(v.shape) != shape or k.dtype != cache.dtype or v.dtype != cache.dtype or \
+            hkv != cache.n_kv_heads or dh != cache.head_dim:
+        raise ValueError("k and v must match each other and the cache")
+    stride = _row_stride(k, "k")
+    if _row_stride(v, "v") != stride:
+        raise ValueError("k and v must have the same strides")
+    qs, hq, qp = 0, 0, None
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out come together")
+    if q is not None:
+        hq = q.shape[1]
+        if tuple(q.shape) != (n, hq, dh) or tuple(q_out.shape) != (n, hq, dh) or \
+                q.dtype != cache.dtype or q_out.dtype != cache.dtype:
+            raise ValueError("q and q_out must be [n][Hq][D], of the cache's type")
+        qs, qp = _row_stride(q, "q"), q.data_ptr()
+    for t in (k, v) if q is None else (k, v, q):
+        if t.get_device() != dev:
+            raise ValueError("k, v and q must be tensors on the current device")
+    if positions is not None and (tuple(positions.shape) != (n,)
+                                  or positions.dtype != torch.int32):
+        raise ValueError("positions must be [n] int32")
+    _check(lib.wf_paged_append(cache.code, *_paged(cache, batch, dev), k.data_ptr(), v.data_ptr(),
+                               stride, qp, qs, _ptr(q_out, dev, "q_out"), hq,
+                               _ptr(positions, dev, "positions"), rope_base, n, raw),
+           "wf_paged_append")
+
+
+def _code_of(dtype):
+    return dtype if isinstance(dtype, int) else (WF_F32 if dtype == torch.float32 else WF_BF16)
+
+
+def wf_paged_verify_attn_workspace_bytes(dtype, n_rows, n_seqs, max_rows, n_q_heads, n_kv_heads,
+                                         head_dim) -> int:
+    return int(lib.wf_paged_verify_attn_workspace_bytes(_code_of(dtype), n_rows, n_seqs, max_rows,
+                                                        n_q_heads, n_kv_heads, head_dim))
+
+
+def _tree_ptr(tree_mask, n, dev):
+    if tree_mask is None:
+        return None
+    if tree_mask.numel() != n or tree_mask.dtype not in (torch.int64, torch.uint64):
+        raise ValueError("tree_mask must hold a 64-bit word (int64 or uint64) for every row")
+    return _ptr(tree_mask, dev, "tree_mask")
+
+
+def wf_paged_verify_attn(q, cache, batch, out, tree_mask=None, softmax_scale=None,
+                         workspace=None, stream=None):
+    """Attention of the batch's rows over their pages: q, out [n][Hq][D] of the
+    cache's type; tree_mask [n] 64-bit words, or None for chains and blocks.
+    Rows that belong to no sequence are left as they were."""
+    dev, raw = _at(stream)
+    shape = tuple(q.shape)
+    n, hq, dh = shape
+    if dh != cache.head_dim or tuple(out.shape) != shape or q.dtype != cache.dtype or \
+            out.dtype != cache.dtype:
+        raise ValueError("q, out and the cache do not match")
+    if workspace is None:
+        with _on(stream):
+            workspace = alloc_workspace(wf_paged_verify_attn_workspace_bytes(
+                cache.code, n, batch.n_seqs, batch.max_rows, hq, cache.n_kv_heads, dh), q.device)
+    _check(lib.wf_paged_verify_attn(
+        cache.code, _ptr(q, dev, "q"), *_paged(cache, batch, dev), _ptr(out, dev, "out"),
+        _tree_ptr(tree_mask, n, dev), n, hq, dh ** -0.5 if softmax_scale is None else softmax_scale,
+        _ptr(workspace, dev, "workspace"), workspace.numel(), raw), "wf_paged_verify_attn")
+    return out
+
+
+def wf_paged_select_workspace_bytes(n_rows, n_kv_heads, max_pages) -> int:
+    return int(lib.wf_paged_select_workspace_bytes(n_rows, n_kv_heads, max_pages))
+
+
+def wf_paged_select(q, cache, batch, sel, n_recent, workspace=None, stream=None):
+    """sel [n][Hkv][n_sel] int32 receives, for every row and KV head, the
+    n_sel - n_recent old pages whose bounds promise the largest scores and the
+    n_recent newest ones, ascending, then -1."""
+    dev, raw = _at(stream)
+    n, hq, dh = q.shape
+    if dh != cache.head_dim or q.dtype != cache.dtype or sel.dim() != 3 or \
+            tuple(sel.shape[:2]) != (n, cache.n_kv_heads) or sel.dtype != torch.int32:
+        raise ValueError("q [n][Hq][D] of the cache's type, sel [n][Hkv][n_sel] int32")
+    if workspace is None:
+        with _on(stream):
+            workspace = alloc_workspace(wf_paged_select_workspace_bytes(
+                n, cache.n_kv_heads, batch.max_pages), q.device)
+    _check(lib.wf_paged_select(cache.code, _ptr(q, dev, "q"), *_paged(cache, batch, dev),
+                               _ptr(sel, dev, "sel"), sel.shape[2], n_recent, n, hq,
+                               _ptr(workspace, dev, "workspace"), workspace.numel(), raw),
+           "wf_paged_select")
+    return sel
+
+
+def wf_paged_sparse_attn_workspace_bytes(dtype, n_rows, n_q_heads, n_kv_heads, head_dim,
+                                         page_size, n_sel) -> int:
+    return int(lib.wf_paged_sparse_attn_workspace_bytes(_code_of(dtype), n_rows, n_q_heads,
+                                                        n_kv_heads, head_dim, page_size, n_sel))
+
+
+def wf_paged_sparse_attn(q, cache, batch, sel, out, tree_mask=None, softmax_scale=None,
+                         workspace=None, stream=None):
+    """wf_paged_verify_attn over the pages sel [n][Hkv][n_sel] (int32 logical
+    page numbers, as wf_paged_select writes them)."""
+    dev, raw = _at(stream)
+    shape = tuple(q.shape)
+    n, hq, dh = shape
+    if dh != cache.head_dim or tuple(out.shape) != shape or q.dtype != cache.dtype or \
+            out.dtype != cache.dtype:
+        raise ValueError("q, out and the cache do not match")
+    if sel.dim() != 3 or tuple(sel.shape[:2]) != (n, cache.n_kv_heads) or \
+            sel.dtype != torch.int32:
+        raise ValueError("sel must be [n][Hkv][n_sel] int32")
+    if workspace is None:
+        with _on(stream):
+            workspace = alloc_workspace(wf_paged_sparse_attn_workspace_bytes(
+                cache.code, n, hq, cache.n_kv_heads, dh, cache.page_size, sel.shape[2]), q.device)
+    _check(lib.wf_paged_sparse_attn(
+        cache.code, _ptr(q, dev, "q"), *_paged(cache, batch, dev), _ptr(sel, dev, "sel"),
+        sel.shape[2], _ptr(out, dev, "out"), _tree_ptr(tree_mask, n, dev), n, hq,
+        dh ** -0.5 if softmax_scale is None else softmax_scale, _ptr(workspace, dev, "workspace"),
+        workspace.numel(), raw), "wf_paged_sparse_attn")
+    return out
+
+
+def wf_token_logprobs_workspace_bytes(dtype, n_rows, vocab, n_top) -> int:
+    return int(lib.wf_token_logprobs_workspace_bytes(_code_of(dtype), n_rows, vocab, n_top))
+
+
+def wf_token_logprobs(logits, tokens, logprob, entropy=None, rank=None, top_ids=None,
+                      top_logprobs=None, workspace=None, stream=None):
+    """logits [n][vocab] fp32 or bf16 (rows may be strided), tokens [n] int32
+    -> logprob [n] fp32, entropy [n] fp32, rank [n] int32, and the n_top best
+    tokens of every row, top_ids [n][n_top] int32 and top_logprobs [n][n_top]
+    fp32, each where it is given; tokens and logprob may be None together."""
+    dev, raw = _at(stream)
+    n, vocab = logits.shape
+    code = _dtype_code(logits)
+    ls = logits.stride()
+    if logits.get_device() != dev or (vocab > 1 and ls[1] != 1):
+        raise ValueError("logits must be rows of consecutive values on the current device")
+    stride = ls[0] if n > 1 else vocab
+    top = 0 if top_ids is None else top_ids.shape[-1]
+    for t, dt, want in ((tokens, torch.int32, (n,)), (logprob, torch.float32, (n,)),
+                        (entropy, torch.float32, (n,)), (rank, torch.int32, (n,)),
+                        (top_ids, torch.int32, (n, top)),
+                        (top_logprobs, torch.float32, (n, top))):
+        if t is not None and (tuple(t.shape) != want or t.dtype != dt):
+            raise ValueError("tokens, rank [n] and top_ids [n][n_top] are int32, logprob, "
+                             "entropy [n] and top_logprobs [n][n_top] fp32")
+    if top == 0 and n and (top_ids is not None or top_logprobs is not None):
+        raise ValueError("leave top_ids and top_logprobs out where no alternatives are wanted")
+    if workspace is None:
+        with _on(stream):
+            workspace = alloc_workspace(wf_token_logprobs_workspace_bytes(code, n, vocab, top),
+                                        logits.device)
+    _check(lib.wf_token_logprobs(
+        code, logits.data_ptr(), stride, _ptr(tokens, dev, "tokens"), n, vocab, top,
+        _ptr(logprob, dev, "logprob"), _ptr(entropy, dev, "entropy"), _ptr(rank, dev, "rank"),
+        _ptr(top_ids, dev, "top_ids"), _ptr(top_logprobs, dev, "top_logprobs"),
+        _ptr(workspace, dev, "workspace"), workspace.numel(), raw), "wf_token_logprobs")
 
 
 def wf_read_probe(src, sink, workgroups, stream=None):

@@ -1,0 +1,537 @@
+// paged.hip -- the paged cache of a batch of requests: the append, which
+// rotates K and q on the way and keeps the pages' bounds, and the selection of
+// the pages that a row's attention is worth reading.
+#include <cmath>
+
+#include "wf_paged.h"
+
+namespace wf {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMaxHalfDim = 64;
+
+template <typename T>
+struct Elem;
+template <>
+struct Elem<uint16_t> {
+    static constexpr int kVec = 8;                   // elements of 16 bytes
+    static __device__ __forceinline__ void unpack(u32x4 w, float (&f)[8]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f[2 * i] = __uint_as_float(w[i] << 16);
+            f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    }
+    static __device__ __forceinline__ u32x4 pack(const float (&f)[8]) {
+        return u32x4{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]),
+                     pack_bf16x2(f[6], f[7])};
+    }
+};
+template <>
+struct Elem<float> {
+    static constexpr int kVec = 4;
+    static __device__ __forceinline__ void unpack(u32x4 w, float (&f)[4]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            f[i] = __uint_as_float(w[i]);
+    }
+    static __device__ __forceinline__ u32x4 pack(const float (&f)[4]) {
+        return u32x4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]),
+                     __float_as_uint(f[3])};
+    }
+};
+
+// Smaller and larger of two values, NaN if either is one.
+__device__ __forceinline__ float nan_min(float a, float b) { return (a < b || a != a) ? a : b; }
+__device__ __forceinline__ float nan_max(float a, float b) { return (a > b || a != a) ? a : b; }
+
+// ---------------------------------------------------------------------------
+// Append.  A workgroup takes one page that the batch writes and one KV head's
+// K and V rows in it, or the group of query heads that reads that head: rows
+// move in 16-byte pieces, a thread holding both halves of its rotation pairs.
+//   k' = R(pos) k: (lo, hi) -> (lo cos - hi sin, hi cos + lo sin), the angle
+//   pos * theta_i in turns, reduced to half a turn in fp64 (an fp32 product
+//   would be off by a part in a hundred of a radian at 64K positions), sine and
+//   cosine in fp32.
+// The bounds are taken anew from all of the page's valid rows, older ones
+// included, so they never depend on what the page held before.
+// ---------------------------------------------------------------------------
+struct AppendParams {
+    PagedView v;
+    double turns[kMaxHalfDim];     // theta_i / 2 pi
+    const void *k_in, *v_in, *q_in;
+    void *k, *vc, *bounds, *q_out;
+    const int32_t *positions;
+    size_t kv_stride, q_stride;    // elements
+    int group, n_q_heads;
+};
+
+template <typename T, int DH>
+__global__ __launch_bounds__(kThreads) void paged_append(AppendParams a) {
+    using E = Elem<T>;
+    constexpr int V = E::kVec;
+    constexpr int LPR = DH / 2 / V;                  // threads per row
+    constexpr int ROWS = kThreads / LPR;             // rows at a time
+    const int page = 1 << a.v.page_shift;
+    const int any_rows = a.v.n_rows;
+    long long first, total;
+    const int b = paged_find<kThreads>(
+        a.v.n_seqs, blockIdx.x,
+        [&](int s) {
+            const Seq q = paged_seq(a.v, s, any_rows);
+            return q.rows ? ((q.ctx + q.rows - 1) >> a.v.page_shift) - (q.ctx >> a.v.page_shift) + 1
+                          : 0;
+        },
+        &first, &total);
+    if (b < 0)
+        return;
+    const Seq s = paged_seq(a.v, b, any_rows);
+    const int lp = (s.ctx >> a.v.page_shift) + (int)(blockIdx.x - first);
+    const int p0 = lp << a.v.page_shift;
+    // page rows [from, to) are new, [0, from) older
+    const int from = max(s.ctx - p0, 0), to = min(s.ctx + s.rows - p0, page);
+    const int row0 = s.r0 + p0 - s.ctx;              // the call's row of page row 0
+    const int c = threadIdx.x % LPR, rt = threadIdx.x / LPR;
+
+    float cs[V], sn[V];
+    auto angle = [&](int r) {
+        const int pos = a.positions ? a.positions[r] : s.ctx + (r - s.r0);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const double t = (double)pos * a.turns[c * V + e];
+            sincospif(2.f * (float)(t - rint(t)), &sn[e], &cs[e]);
+        }
+    };
+    auto rotate = [&](const T *src, u32x4 &lo, u32x4 &hi, float (&fl)[V], float (&fh)[V]) {
+        float x[V], y[V];
+        E::unpack(*reinterpret_cast<const u32x4 *>(src + c * V), x);
+        E::unpack(*reinterpret_cast<const u32x4 *>(src + DH / 2 + c * V), y);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            fl[e] = x[e] * cs[e] - y[e] * sn[e];
+            fh[e] = y[e] * cs[e] + x[e] * sn[e];
+        }
+        lo = E::pack(fl);
+        hi = E::pack(fh);
+    };
+
+    if ((int)blockIdx.y >= a.v.n_kv_heads) {
+        // ---- the query heads of a group ----
+        const int h0 = ((int)blockIdx.y - a.v.n_kv_heads) * a.group;
+        for (int base = from; base < to; base += ROWS) {
+            const int nr = min(to - base, ROWS);
+            int have = -1;
+            for (int p = rt; p < nr * a.group; p += ROWS) {
+                const int r = row0 + base + p % nr, h = h0 + p / nr;
+                if (r != have)
+                    angle(r);
+                have = r;
+                u32x4 lo, hi;
+                float fl[V], fh[V];
+                rotate(static_cast<const T *>(a.q_in) + r * a.q_stride + (size_t)h * DH, lo, hi,
+                       fl, fh);
+                T *dst = static_cast<T *>(a.q_out) + ((size_t)r * a.n_q_heads + h) * DH;
+                *reinterpret_cast<u32x4 *>(dst + c * V) = lo;
+                *reinterpret_cast<u32x4 *>(dst + DH / 2 + c * V) = hi;
+            }
+        }
+        return;
+    }
+
+    // ---- one KV head ----
+    const int id = paged_page(a.v, b, lp);
+    if (id < 0)
+        return;
+    const int g = blockIdx.y;
+    const size_t head = (size_t)id * a.v.n_kv_heads + g;
+    T *kp = static_cast<T *>(a.k) + (head << a.v.page_shift) * DH;
+    T *vp = static_cast<T *>(a.vc) + (head << a.v.page_shift) * DH;
+    float mn[2 * V], mx[2 * V];
+#pragma unroll
+    for (int e = 0; e < 2 * V; ++e) {
+        mn[e] = INFINITY;
+        mx[e] = -INFINITY;
+    }
+    auto count = [&](u32x4 lo, u32x4 hi) {
+        float x[V], y[V];
+        E::unpack(lo, x);
+        E::unpack(hi, y);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            mn[e] = nan_min(mn[e], x[e]);
+            mx[e] = nan_max(mx[e], x[e]);
+            mn[V + e] = nan_min(mn[V + e], y[e]);
+            mx[V + e] = nan_max(mx[V + e], y[e]);
+        }
+    };
+    for (int r = from + rt; r < to; r += ROWS) {
+        const size_t src = (size_t)(row0 + r) * a.kv_stride + (size_t)g * DH;
+        const T *vs = static_cast<const T *>(a.v_in) + src;
+        const u32x4 v0 = *reinterpret_cast<const u32x4 *>(vs + c * V);
+        const u32x4 v1 = *reinterpret_cast<const u32x4 *>(vs + DH / 2 + c * V);
+        angle(row0 + r);
+        u32x4 lo, hi;
+        float fl[V], fh[V];
+        rotate(static_cast<const T *>(a.k_in) + src, lo, hi, fl, fh);
+        T *kd = kp + (size_t)r * DH, *vd = vp + (size_t)r * DH;
+        *reinterpret_cast<u32x4 *>(kd + c * V) = lo;
+        *reinterpret_cast<u32x4 *>(kd + DH / 2 + c * V) = hi;
+        *reinterpret_cast<u32x4 *>(vd + c * V) = v0;
+        *reinterpret_cast<u32x4 *>(vd + DH / 2 + c * V) = v1;
+        if (a.bounds)
+            count(lo, hi);
+    }
+    if (!a.bounds)
+        return;
+    for (int r = rt; r < from; r += ROWS) {
+        const T *kd = kp + (size_t)r * DH;
+        count(*reinterpret_cast<const u32x4 *>(kd + c * V),
+              *reinterpret_cast<const u32x4 *>(kd + DH / 2 + c * V));
+    }
+    // over the rows of a wave, then over the waves
+#pragma unroll
+    for (int off = LPR; off < kWave; off <<= 1)
+#pragma unroll
+        for (int e = 0; e < 2 * V; ++e) {
+            mn[e] = nan_min(mn[e], __shfl_xor(mn[e], off, kWave));
+            mx[e] = nan_max(mx[e], __shfl_xor(mx[e], off, kWave));
+        }
+    constexpr int WAVES = kThreads / kWave;
+    __shared__ float red[WAVES][2][DH];
+    if (threadIdx.x % kWave < LPR) {
+        const int w = threadIdx.x / kWave;
+#pragma unroll
+        for (int e = 0; e < 2 * V; ++e) {
+            const int d = (e < V ? 0 : DH / 2) + c * V + e % V;
+            red[w][0][d] = mn[e];
+            red[w][1][d] = mx[e];
+        }
+    }
+    __syncthreads();
+    if (threadIdx.x < 2 * DH) {
+        const int which = threadIdx.x / DH, d = threadIdx.x % DH;
+        float x = red[0][which][d];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w)
+            x = which ? nan_max(x, red[w][1][d]) : nan_min(x, red[w][0][d]);
+        T *dst = static_cast<T *>(a.bounds) + (head * 2 + which) * DH + d;
+        if constexpr (sizeof(T) == 2)
+            *dst = f32_to_bf16(x);                   // exact: x is a stored value
+        else
+            *dst = x;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Selection.  The workgroups of one (row, KV head) share its old pages, at
+// least kScorePages each: DH / V lanes to a page, V dimensions each,
+//   s = max_h sum_d q_d (q_d >= 0 ? hi_d : lo_d)
+// in fp64 (bf16 products are exact and their sums all but exact there, so the
+// order of the pages does not hang on the order of the sums), and stores the
+// scores as 64-bit keys of the same order.  The last workgroup of the (row,
+// head) finds the n_top-th largest key digit by digit and lists the pages at
+// or above it in page order.
+// ---------------------------------------------------------------------------
+constexpr int kScorePages = 64;
+constexpr int kLdsKeys = 2048;
+
+struct SelectParams {
+    PagedView v;
+    const void *q, *bounds;
+    int32_t *sel;
+    uint64_t *keys;                // [n_rows * n_kv_heads][max_pages]
+    unsigned *arrived;             // [n_rows * n_kv_heads], in the zero block
+    int n_sel, n_recent, group, n_q_heads;
+};
+
+// A key of a score: larger scores have larger keys, NaN the largest; 0 is kept
+// for pages without an entry.
+__device__ __forceinline__ uint64_t score_key(double s) {
+    if (s != s)
+        return ~0ull;
+    const uint64_t u = __builtin_bit_cast(uint64_t, s + 0.0);
+    return (u >> 63) ? ~u : u | (1ull << 63);
+}
+
+template <typename T, int DH>
+__global__ __launch_bounds__(kThreads) void paged_select(SelectParams a) {
+    using E = Elem<T>;
+    constexpr int V = E::kVec;
+    constexpr int LPP = DH / V;                      // lanes per page
+    constexpr int WAVES = kThreads / kWave;
+    __shared__ int seq_of_row;
+    const int unit = blockIdx.x;
+    const int r = unit / a.v.n_kv_heads, g = unit % a.v.n_kv_heads;
+    if (threadIdx.x == 0)
+        seq_of_row = -1;
+    __syncthreads();
+    for (int s = threadIdx.x; s < a.v.n_seqs; s += kThreads) {
+        const Seq q = paged_seq(a.v, s, a.v.max_rows);
+        if (r >= q.r0 && r < q.r0 + q.rows)
+            seq_of_row = s;
+    }
+    __syncthreads();
+    const int b = uniform(seq_of_row);
+    if (b < 0)
+        return;
+    const Seq s = paged_seq(a.v, b, a.v.max_rows);
+    const int newest = (s.ctx + r - s.r0) >> a.v.page_shift;
+    const int n_old = max(newest + 1 - a.n_recent, 0);
+    const int n_top = a.n_sel - a.n_recent;
+    const int wave = wave_id(), lane = threadIdx.x % kWave;
+    uint64_t *keys = a.keys + (size_t)unit * a.v.max_pages;
+    const bool choose = n_old > n_top && n_top > 0;
+
+    // the workgroups of a (row, head) that have pages to score
+    const int chunks =
+        choose ? min((n_old + kScorePages - 1) / kScorePages, (int)gridDim.y) : 1;
+    if ((int)blockIdx.y >= chunks)
+        return;
+    if (choose) {
+        constexpr int PPW = kWave / LPP;             // pages at a time of a wave
+        const int lp = lane % LPP;
+        for (int p0 = (blockIdx.y * WAVES + wave) * PPW; p0 < n_old; p0 += chunks * WAVES * PPW) {
+            const int p = p0 + lane / LPP;
+            const int id = p < n_old ? paged_page(a.v, b, p) : -1;
+            float lo[V], hi[V];
+            if (id >= 0) {
+                const T *src = static_cast<const T *>(a.bounds) +
+                               ((size_t)id * a.v.n_kv_heads + g) * 2 * DH + lp * V;
+                E::unpack(*reinterpret_cast<const u32x4 *>(src), lo);
+                E::unpack(*reinterpret_cast<const u32x4 *>(src + DH), hi);
+            } else {
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    lo[e] = hi[e] = 0.f;
+            }
+            double best = -INFINITY;
+            bool nan = false;
+            for (int h = 0; h < a.group; ++h) {
+                float q[V];
+                E::unpack(*reinterpret_cast<const u32x4 *>(
+                              static_cast<const T *>(a.q) +
+                              ((size_t)r * a.n_q_heads + g * a.group + h) * DH + lp * V),
+                          q);
+                double acc = 0.0;
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    acc = fma((double)q[e], (double)(q[e] >= 0.f ? hi[e] : lo[e]), acc);
+#pragma unroll
+                for (int off = 1; off < LPP; off <<= 1)
+                    acc += __shfl_xor(acc, off, kWave);
+                nan |= acc != acc;
+                best = acc > best ? acc : best;
+            }
+            if (lp == 0 && p < n_old)
+                keys[p] = id < 0 ? 0ull : score_key(nan ? (double)NAN : best);
+        }
+        if (!arrive_last(a.arrived + unit, chunks))
+            return;
+        if (threadIdx.x == 0)
+            a.arrived[unit] = 0;
+    }
+
+    // ---- the smallest selected key ----
+    __shared__ uint64_t lds_keys[kLdsKeys];
+    __shared__ int hist[256];
+    __shared__ int wave_count[2][WAVES];
+    __shared__ int digit, above;
+    uint64_t least = 1;                              // all pages with an entry
+    int equal_quota = n_old;                         // of the pages at `least`
+    const bool in_lds = choose && n_old <= kLdsKeys;
+    if (in_lds) {
+        for (int i = threadIdx.x; i < n_old; i += kThreads)
+            lds_keys[i] = keys[i];
+        __syncthreads();
+    }
+    auto key = [&](int i) -> uint64_t {
+        if (!choose)
+            return n_top > 0 && paged_page(a.v, b, i) >= 0 ? 1ull : 0ull;
+        return in_lds ? lds_keys[i] : keys[i];
+    };
+    if (choose) {
+        uint64_t prefix = 0;
+        int need = n_top;
+        int shift = 56;
+        for (;; shift -= 8) {
+            for (int i = threadIdx.x; i < 256; i += kThreads)
+                hist[i] = 0;
+            __syncthreads();
+            for (int i = threadIdx.x; i < n_old; i += kThreads) {
+                const uint64_t k = key(i);
+                if (shift == 56 || (k >> (shift + 8)) == (prefix >> (shift + 8)))
+                    atomicAdd(&hist[(k >> shift) & 255], 1);
+            }
+            __syncthreads();
+            // the digit of the need-th largest key: bins from the top on
+            if (wave == 0) {
+                int mine[4], sum = 0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    mine[j] = hist[255 - (4 * lane + j)];
+                    sum += mine[j];
+                }
+                int incl = sum;
+#pragma unroll
+                for (int off = 1; off < kWave; off <<= 1) {
+                    const int o = __shfl_up(incl, off, kWave);
+                    incl += lane >= off ? o : 0;
+                }
+                int before = incl - sum;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (before < need && need <= before + mine[j]) {
+                        digit = 255 - (4 * lane + j);
+                        above = before;
+                    }
+                    before += mine[j];
+                }
+            }
+            __syncthreads();
+            need -= above;
+            prefix |= (uint64_t)digit << shift;
+            const bool whole = hist[digit] == need;
+            if (shift == 0 || whole)
+                break;
+            __syncthreads();
+        }
+        // every key from `prefix` on: all of them where the last bin was taken
+        // whole, else the first `need` of those equal to it
+        least = prefix;
+        equal_quota = shift == 0 ? need : n_old;
+        if (least == 0)                              // fewer pages than n_top have entries
+            least = 1, equal_quota = n_old;
+    }
+
+    // ---- list them in page order: a run of pages per wave ----
+    const int run = (n_old + WAVES * kWave - 1) / (WAVES * kWave) * kWave;
+    const int i0 = wave * run, i1 = min(i0 + run, n_old);
+    auto tally = [&](int i, bool &gt, bool &eq) {
+        const uint64_t k = i < i1 ? key(i) : 0ull;
+        gt = k > least;
+        eq = k == least;
+    };
+    int n_gt = 0, n_eq = 0;
+    for (int i = i0; i < i1; i += kWave) {
+        bool gt, eq;
+        tally(i + lane, gt, eq);
+        n_gt += __popcll(__ballot(gt));
+        n_eq += __popcll(__ballot(eq));
+    }
+    if (lane == 0) {
+        wave_count[0][wave] = n_gt;
+        wave_count[1][wave] = n_eq;
+    }
+    __syncthreads();
+    int at = 0, eq_seen = 0, all_gt = 0, all_eq = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        const int gt = wave_count[0][w], eq = wave_count[1][w];
+        if (w < wave) {
+            at += gt + min(eq, max(equal_quota - eq_seen, 0));
+            eq_seen += eq;
+        }
+        all_gt += gt;
+        all_eq += eq;
+    }
+    const int listed = all_gt + min(all_eq, equal_quota);
+    int32_t *out = a.sel + (size_t)unit * a.n_sel;
+    const uint64_t below = (1ull << lane) - 1ull;
+    for (int i = i0; i < i1; i += kWave) {
+        bool gt, eq;
+        tally(i + lane, gt, eq);
+        const uint64_t em = __ballot(eq);
+        const bool take = gt || (eq && eq_seen + __popcll(em & below) < equal_quota);
+        const uint64_t tm = __ballot(take);
+        if (take)
+            out[at + __popcll(tm & below)] = i + lane;
+        at += __popcll(tm);
+        eq_seen += __popcll(em);
+    }
+    // the recent pages, and -1 behind them
+    const int recent = newest + 1 - n_old;
+    for (int i = listed + threadIdx.x; i < a.n_sel; i += kThreads)
+        out[i] = i - listed < recent ? n_old + i - listed : -1;
+}
+
+}  // namespace
+
+wf_status_t launch_paged_append(wf_dtype_t dt, const wf_paged_cache_t &c,
+                                const wf_paged_batch_t &b, const void *k, const void *v,
+                                size_t kv_stride, const void *q, size_t q_stride, void *q_out,
+                                int n_q_heads, const int32_t *positions, double rope_base,
+                                int n_rows, hipStream_t stream) {
+    AppendParams a{};
+    a.v = paged_view(c, b, n_rows);
+    for (int i = 0; i < c.head_dim / 2; ++i)
+        a.turns[i] = std::pow(rope_base, -2.0 * i / c.head_dim) / 6.283185307179586;
+    a.k_in = k;
+    a.v_in = v;
+    a.q_in = q;
+    a.k = c.k;
+    a.vc = c.v;
+    a.bounds = c.bounds;
+    a.q_out = q_out;
+    a.positions = positions;
+    a.kv_stride = kv_stride;
+    a.q_stride = q_stride;
+    a.n_q_heads = n_q_heads;
+    a.group = q ? n_q_heads / c.n_kv_heads : 0;
+    // at most this many pages receive rows: a sequence's rows reach one page
+    // more than they fill
+    const int pages = (int)std::min<long long>(
+        n_rows, n_rows / c.page_size + 2ll * std::min(b.n_seqs, n_rows));
+    const dim3 grid(pages, c.n_kv_heads * (q ? 2 : 1));
+    const dim3 block(kThreads);
+    if (dt == WF_BF16) {
+        if (c.head_dim == 128)
+            hipLaunchKernelGGL((paged_append<uint16_t, 128>), grid, block, 0, stream, a);
+        else
+            hipLaunchKernelGGL((paged_append<uint16_t, 64>), grid, block, 0, stream, a);
+    } else if (c.head_dim == 128)
+        hipLaunchKernelGGL((paged_append<float, 128>), grid, block, 0, stream, a);
+    else
+        hipLaunchKernelGGL((paged_append<float, 64>), grid, block, 0, stream, a);
+    return hipGetLastError() == hipSuccess ? WF_OK : WF_ERR_HIP;
+}
+
+size_t paged_select_workspace_bytes(int n_rows, int n_kv_heads, int max_pages) {
+    const size_t units = std::max<size_t>((size_t)n_rows * n_kv_heads, 1);
+    return kCounterBytes + units * max_pages * sizeof(uint64_t);
+}
+
+wf_status_t launch_paged_select(wf_dtype_t dt, const void *q, const wf_paged_cache_t &c,
+                                const wf_paged_batch_t &b, int32_t *sel, int n_sel, int n_recent,
+                                int n_rows, int n_q_heads, void *workspace, hipStream_t stream) {
+    SelectParams a{};
+    a.v = paged_view(c, b, n_rows);
+    a.q = q;
+    a.bounds = c.bounds;
+    a.sel = sel;
+    a.arrived = static_cast<unsigned *>(workspace);
+    a.keys = reinterpret_cast<uint64_t *>(static_cast<char *>(workspace) + kCounterBytes);
+    a.n_sel = n_sel;
+    a.n_recent = n_recent;
+    a.group = n_q_heads / c.n_kv_heads;
+    a.n_q_heads = n_q_heads;
+    // (the table may be far wider than the sequences are long: no more
+    // workgroups than fill the chip a few times)
+    const int units = n_rows * c.n_kv_heads;
+    const int chunks = (b.max_pages + kScorePages - 1) / kScorePages;
+    const dim3 grid(units, std::min(chunks, std::max(2048 / units, 1)));
+    const dim3 block(kThreads);
+    if (dt == WF_BF16) {
+        if (c.head_dim == 128)
+            hipLaunchKernelGGL((paged_select<uint16_t, 128>), grid, block, 0, stream, a);
+        else
+            hipLaunchKernelGGL((paged_select<uint16_t, 64>), grid, block, 0, stream, a);
+    } else if (c.head_dim == 128)
+        hipLaunchKernelGGL((paged_select<float, 128>), grid, block, 0, stream, a);
+    else
+        hipLaunchKernelGGL((paged_select<float, 64>), grid, block, 0, stream, a);
+    return hipGetLastError() == hipSuccess ? WF_OK : WF_ERR_HIP;
+}
+
+}  // namespace wf

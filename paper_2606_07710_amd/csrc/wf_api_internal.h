@@ -93,6 +93,41 @@ wf_status_t launch_w4_pack(const void *codes, const uint8_t *scales, int rows, i
 wf_status_t launch_w4_quantize(const void *w, int rows, int cols, void *codes, uint8_t *scales,
                                hipStream_t stream);
 
+// Paged KV cache of a batch (paged.hip, paged_attn.hip).  The workspace layouts
+// begin with the zero block, of which the attention reads kPagedZeroBytes at
+// the end (the keys of missing pages).
+constexpr int kPagedZeroBytes = 1 << 16;
+wf_status_t launch_paged_append(wf_dtype_t dt, const wf_paged_cache_t &c,
+                                const wf_paged_batch_t &b, const void *k, const void *v,
+                                size_t kv_stride, const void *q, size_t q_stride, void *q_out,
+                                int n_q_heads, const int32_t *positions, double rope_base,
+                                int n_rows, hipStream_t stream);
+size_t paged_select_workspace_bytes(int n_rows, int n_kv_heads, int max_pages);
+wf_status_t launch_paged_select(wf_dtype_t dt, const void *q, const wf_paged_cache_t &c,
+                                const wf_paged_batch_t &b, int32_t *sel, int n_sel, int n_recent,
+                                int n_rows, int n_q_heads, void *workspace, hipStream_t stream);
+// sel: null for all of a sequence's pages.
+struct PagedPlan {
+    int nb, rg, ks;            // 16-row blocks per wave, row groups, key streams of a workgroup
+    int workgroups;
+    int rows() const { return 16 * nb * rg; }
+};
+PagedPlan plan_paged(wf_dtype_t dt, int max_rows, int n_q_heads, int n_kv_heads, bool sparse);
+size_t paged_attn_workspace_bytes(const PagedPlan &p, int head_dim);
+wf_status_t launch_paged_attn(wf_dtype_t dt, const void *q, const wf_paged_cache_t &c,
+                              const wf_paged_batch_t &b, const int32_t *sel, int n_sel, void *out,
+                              const uint64_t *tree_mask, int n_rows, int n_q_heads,
+                              float softmax_scale, const PagedPlan &p, void *workspace,
+                              hipStream_t stream);
+
+// Log probabilities of tokens (logprob.hip).
+size_t token_logprobs_workspace_bytes(wf_dtype_t dt, int n_rows, int vocab, int n_top);
+wf_status_t launch_token_logprobs(wf_dtype_t dt, const void *logits, size_t row_stride,
+                                  const int32_t *tokens, int n_rows, int vocab, int n_top,
+                                  float *logprob, float *entropy, int32_t *rank,
+                                  int32_t *top_ids, float *top_lp, void *workspace,
+                                  hipStream_t stream);
+
 size_t lmhead_workspace_bytes(int gamma, int vocab);
 // The neural routing policy folded into the LM-head pass (bf16 weights in
 // the LM head's layout; b1, w2, b2 bf16): route = delta[n] > tau.

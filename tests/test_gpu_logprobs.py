@@ -1,0 +1,196 @@
+"""wf_token_logprobs on the GPU against its 64-bit definition.  Allowed errors:
+the differences z - m are exact to 2^-24 of the logits' spread, exponentials to
+2^-22, and the sums join at most a few thousand fp32 terms a lane and 2^8 lanes:
+2^-24 * 2^10 for their common rounding at the very most, 2^-13 in units of the
+entropy's terms; observed errors are some hundred times smaller."""
+import numpy as np
+import pytest
+import torch
+
+import paged_ref as R
+
+wf = pytest.importorskip("paper_2606_07710_amd")
+pytestmark = pytest.mark.gpu
+
+
+def run(x, tokens, n_top, ws=None, **kw):
+    n = x.shape[0]
+    d = dict(device="cuda")
+    lp, ent = torch.full((n,), 9.0, **d), torch.full((n,), 9.0, **d)
+    rank = torch.full((n,), -9, dtype=torch.int32, **d)
+    ids = torch.full((n, n_top), -9, dtype=torch.int32, **d) if n_top else None
+    tops = torch.full((n, n_top), 9.0, **d) if n_top else None
+    wf.wf_token_logprobs(x, tokens, lp, ent, rank, ids, tops, workspace=ws, **kw)
+    return lp, ent, rank, ids, tops
+
+
+def compare(x, tokens, n_top, got=None):
+    lp, ent, rank, ids, tops = got or run(x, tokens, n_top)
+    z = R.f64(x)
+    rlp, rent, rrank, rids, rtops = R.logprobs(z, tokens.cpu().numpy(), n_top)
+    fin = z[np.isfinite(z)]
+    spread = float(fin.max() - fin.min()) if fin.size else 0.0
+    tol = 2.0 ** -13 + 2.0 ** -22 * spread
+
+    def close(a, b, scale=1.0):
+        a = R.f64(a)
+        same = (np.isnan(a) & np.isnan(b)) | (a == b)
+        with np.errstate(invalid="ignore"):
+            near = np.abs(a - b) <= tol * scale
+        assert (same | near).all(), (a[~(same | near)][:4], b[~(same | near)][:4])
+
+    close(lp, rlp)
+    close(ent, rent, 16.0)                    # sums of up to log(vocab) times p
+    assert np.array_equal(rank.cpu().numpy(), rrank)
+    if n_top:
+        assert np.array_equal(ids.cpu().numpy(), rids)
+        close(tops, rtops)
+
+
+def logits(n, vocab, dt, seed, std=3.0):
+    g = torch.Generator("cuda").manual_seed(seed)
+    return (torch.randn(n, vocab, generator=g, device="cuda") * std).to(R.DT[dt])
+
+
+def tokens(n, vocab, seed):
+    g = torch.Generator("cuda").manual_seed(seed + 1000)
+    return torch.randint(0, vocab, (n,), generator=g, device="cuda").int()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("n,vocab,top", [
+    (1, 1, 1), (1, 1, 0), (3, 2, 2), (2, 63, 5), (2, 64, 64), (5, 65, 20), (1, 1000, 64),
+    (4, 2047, 7), (4, 2049, 1), (16, 151936, 20), (1, 128256, 64), (3, 50257, 0), (700, 999, 8),
+    (1100, 4099, 3), (1, 1 << 20, 5),
+])
+def test_sizes(dt, n, vocab, top):
+    print("logprobs", dt, n, vocab, top, flush=True)
+    compare(logits(n, vocab, dt, n + vocab), tokens(n, vocab, n), top)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("shift", [0, 1, 3, 5])
+def test_strides_and_alignment(dt, shift):
+    big = logits(5, 5003, dt, 3)
+    x = big[:, shift: shift + 4001]
+    t = tokens(5, 4001, 4)
+    compare(x, t, 9)
+    one = big.flatten()[shift: shift + 3001].unsqueeze(0)
+    compare(one, t[:1].clamp(max=3000), 4)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("top", [1, 64])
+def test_orders_that_fill_the_lists(dt, top):
+    """Ascending rows (every value enters), equal rows (ties go to the lowest
+    index), few distinct values, descending rows."""
+    v = 9000
+    ramp = torch.linspace(-20, 20, v, device="cuda")
+    rows = [ramp, ramp.flip(0), torch.zeros(v, device="cuda"),
+            (torch.arange(v, device="cuda") % 3).float(), -torch.zeros(v, device="cuda"),
+            torch.where(torch.arange(v, device="cuda") % 7 == 0, 1.0, 0.0),
+            torch.where(torch.arange(v, device="cuda") % 2 == 0, 0.0, -0.0)]
+    x = torch.stack(rows).to(R.DT[dt])
+    compare(x, tokens(len(rows), v, 5), top)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [70, 20000])
+def test_masked_infinite_and_nan_logits(dt, vocab):
+    inf, nan = float("inf"), float("nan")
+    x = logits(9, vocab, dt, 7)
+    x[0, 3:] = -inf                           # three tokens left
+    x[1] = -inf                               # none
+    x[2, 5] = inf
+    x[3, 6] = nan
+    x[4, :] = nan
+    x[5, 1:] = -inf                           # one: entropy 0
+    x[6, 8], x[6, 9] = nan, inf
+    x[7] = torch.where(torch.arange(vocab, device="cuda") % 2 == 0, x[7].float(),
+                       -inf).to(x.dtype)
+    x[8, 60] = nan
+    t = torch.tensor([4, 2, 5, 7, 3, 0, 9, 1, 60], dtype=torch.int32, device="cuda")
+    compare(x, t, 20)
+    t = torch.tensor([1, 69, 4, 6, 0, 5, 8, 2, 3], dtype=torch.int32, device="cuda")
+    compare(x, t, 64)
+
+
+def test_padding_tokens_and_left_out_outputs():
+    x = logits(4, 3000, "f32", 11)
+    t = torch.tensor([-1, 3000, -100, 5], dtype=torch.int32, device="cuda")
+    lp, ent, rank, ids, tops = run(x, t, 3)
+    assert lp[:3].tolist() == [0, 0, 0] and rank[:3].tolist() == [-1, -1, -1]
+    compare(x, t, 3, (lp, ent, rank, ids, tops))
+    # parts of the outputs alone
+    only = torch.empty(4, device="cuda")
+    wf.wf_token_logprobs(x, t, only)
+    assert torch.equal(only, lp)
+    e2 = torch.empty(4, device="cuda")
+    wf.wf_token_logprobs(x, None, None, entropy=e2)
+    assert torch.equal(e2, ent)
+    i2, l2 = torch.empty_like(ids), torch.empty_like(tops)
+    wf.wf_token_logprobs(x, None, None, top_ids=i2, top_logprobs=l2)
+    assert torch.equal(i2, ids) and torch.equal(l2, tops)
+    wf.wf_token_logprobs(x[:0], t[:0], only[:0])             # no rows
+
+
+@pytest.mark.parametrize("big", [1e4, 1e30])
+def test_large_logits(big):
+    x = logits(3, 5000, "f32", 13)
+    x[0] += big if big < 1e6 else 0
+    x[1, 7], x[1, 8] = big, -big
+    x[2, ::2] = -big
+    t = torch.tensor([3, 7, 1], dtype=torch.int32, device="cuda")
+    lp, ent, rank, ids, tops = run(x, t, 5)
+    rlp, rent, rrank, rids, rtops = R.logprobs(R.f64(x), t.cpu().numpy(), 5)
+    # the differences to the row's maximum are exact to 2^-24 of themselves
+    assert np.allclose(R.f64(lp), rlp, rtol=2.0 ** -22, atol=2.0 ** -12)
+    assert np.allclose(R.f64(ent), rent, rtol=2.0 ** -10, atol=2.0 ** -9)
+    assert np.array_equal(rank.cpu().numpy(), rrank) and np.array_equal(ids.cpu().numpy(), rids)
+    assert np.allclose(R.f64(tops), rtops, rtol=2.0 ** -22, atol=2.0 ** -12)
+
+
+def test_captured_call_replays_and_the_workspace_stays_clean():
+    x, t = logits(16, 30000, "f32", 17), tokens(16, 30000, 18)
+    ws = wf.alloc_workspace(wf.wf_token_logprobs_workspace_bytes(x.dtype, 16, 30000, 20), "cuda")
+    out = [torch.empty(16, device="cuda"), torch.empty(16, device="cuda"),
+           torch.empty(16, dtype=torch.int32, device="cuda"),
+           torch.empty(16, 20, dtype=torch.int32, device="cuda"),
+           torch.empty(16, 20, device="cuda")]
+    wf.wf_token_logprobs(x, t, *out, workspace=ws)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        wf.wf_token_logprobs(x, t, *out, workspace=ws)
+    for i in range(3):
+        x.copy_(logits(16, 30000, "f32", 20 + i))
+        for o in out:
+            o.fill_(-3)
+        g.replay()
+        torch.cuda.synchronize()
+        replayed = [o.clone() for o in out]
+        compare(x, t, 20, tuple(replayed))
+        wf.wf_token_logprobs(x, t, *out, workspace=ws)
+        for a, b in zip(out, replayed):
+            assert torch.equal(a, b)
+    assert not ws[: 4 << 20].any()
+
+
+def test_of_the_4_bit_products_logits_beside_the_acceptance_call():
+    """The logits that the 4-bit LM head writes: the same argmax and entropy as
+    the acceptance call reads from them."""
+    g = torch.Generator("cuda").manual_seed(23)
+    w = torch.randn(5000, 512, generator=g, device="cuda").to(torch.bfloat16)
+    h = torch.randn(16, 512, generator=g, device="cuda").to(torch.bfloat16)
+    z = torch.empty(16, 5000, device="cuda")
+    wf.wf_linear_w4(h, wf.W4Weight(*wf.wf_w4_quantize(w)), z)
+    draft = tokens(15, 5000, 24)
+    am = torch.empty(16, dtype=torch.int32, device="cuda")
+    ent = torch.empty(16, device="cuda")
+    acc = torch.empty(3, dtype=torch.int32, device="cuda")
+    wf.wf_lmhead_accept_entropy(None, None, z, draft, 0.5, am, ent, acc)
+    t = torch.cat([draft, am[-1:]])
+    lp, e2, rank, ids, tops = run(z, t, 4)
+    compare(z, t, 4, (lp, e2, rank, ids, tops))
+    assert torch.equal(ids[:, 0], am)
+    assert torch.allclose(ent, e2, rtol=2e-4, atol=2e-4)
