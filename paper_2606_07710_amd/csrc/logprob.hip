@@ -3,16 +3,22 @@
 //
 // A row is cut into `parts`, one workgroup each, and a part into one run per
 // wave.  A wave reads its run front to back in 16-byte pieces; each lane keeps
-// the running maximum m of its values, l = sum e^(z-m) and t = sum e^(z-m)(z-m),
-// so that
-//   log p(z) = z - m - log l,   entropy = log l - t / l,
-// and the wave keeps the run's n best values in LDS: a value enters the list if
-// it beats the n-th best of those before it (the first ones always do), and a
-// full list is cut down to its n best.  Lists hold 64-bit keys, the value's
-// order in the high half and the index's complement in the low one, so that the
-// order of equal values is that of their indexes and no result hangs on which
-// lane came first.  The waves' states and lists meet in LDS, the parts' in
-// memory, where the row's last workgroup joins them in part order.
+// a reference m, which moves up to a value that is larger by more than 8 (so the
+// weights stay below 2^12), l = sum e^(z-m) and t = sum e^(z-m)(z-m), so that
+//   log p(z) = z - m - log l,   entropy = log l - t / l.
+// The wave's best values lie sorted in its lanes, lane i the i-th, as 64-bit
+// keys: the value's order in the high half, the index's complement in the low
+// one, so that the order of equal values is that of their indexes and no result
+// hangs on which lane came first.  The values of a group that beat the n-th best
+// that any wave of the workgroup has, and reach the n-th largest of the lanes'
+// maxima in the group (which n of them do), are gathered in LDS and enter
+// together: all are compared with all.  The sorted lists of the waves, and then,
+// in the row's last workgroup, of the parts, join by the same means: of P lists
+// the (n / r)-th largest of their r-th keys, r = n / P, is reached by n keys, and
+// what reaches it is few more than n.
+//
+// Short rows and few of them are bound by latency, in which the fetching of the
+// code counts: loops that are not hot are kept rolled.
 #include <type_traits>
 
 #include "wf_api_internal.h"
@@ -24,8 +30,14 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
-constexpr int kCap = 512;                  // keys a wave's list holds
 constexpr int kMaxParts = 64;
+constexpr int kLoads = 4;                  // 16-byte loads of a lane in a group
+constexpr int kPartKeys = 1280;            // parts * n_top at most
+// A row's arrival counter has a cache line to itself: counters side by side
+// would queue up at one place of the memory.
+constexpr int kCounterStride = 32;
+constexpr int kMaxSplitRows = 512;
+static_assert(kMaxSplitRows * kCounterStride <= kCounterSlots, "the counters fit the zero block");
 
 struct LogprobParams {
     const void *logits;
@@ -34,205 +46,184 @@ struct LogprobParams {
     float *logprob, *entropy;
     int32_t *rank, *top_ids;
     float *top_lp;
-    int vocab, n_top, parts, part_len;     // part_len: elements, a multiple of kThreads * 8
-    unsigned *arrived;                     // [n_rows], in the zero block
+    int wave_r, wave_want, part_r, part_want;  // bounds of the lists that join
+    int vocab, n_top, parts, part_len;     // part_len: elements, whole groups of the waves
+    unsigned *arrived;                     // [n_rows][kCounterStride], in the zero block
     float *part_state;                     // [rows][parts][4]: m, l, t, rank
-    uint64_t *part_keys;                   // [rows][parts][n_top]
+    uint64_t *part_keys;                   // [rows][parts][n_top], sorted
 };
 
-// The order of fp32 values as unsigned integers: NaN above +inf, -0 as 0.
+// The order of fp32 values as unsigned integers: NaN above +inf, -0 as 0.  No
+// value has order 0.
 __device__ __forceinline__ uint32_t value_order(float x) {
-    if (x != x)
-        return ~0u;
     const uint32_t u = __float_as_uint(x + 0.f);
-    return (u >> 31) ? ~u : u | 0x80000000u;
+    const uint32_t o = (u >> 31) ? ~u : u | 0x80000000u;
+    return x != x ? ~0u : o;
 }
 __device__ __forceinline__ float order_value(uint32_t o) {
     return __uint_as_float((o >> 31) ? o & 0x7fffffffu : ~o);
 }
+
 __device__ __forceinline__ uint64_t make_key(float x, int idx) {
     return ((uint64_t)value_order(x) << 32) | (uint32_t)~(uint32_t)idx;
+}
+
+// op over the lanes of a wave, in a fixed order; the same result in every lane.
+// The steps move values between lanes without LDS: shifts by 1, 2, 4, 8 within
+// the rows of 16, then the rows' last lanes to the rows behind.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp(int identity, int x) {
+    return __builtin_amdgcn_update_dpp(identity, x, CTRL, ROWS, 0xf, false);
+}
+template <typename Op>
+__device__ __forceinline__ int wave_reduce(int x, int identity, Op &&op) {
+    x = op(x, dpp<0x111, 0xf>(identity, x));
+    x = op(x, dpp<0x112, 0xf>(identity, x));
+    x = op(x, dpp<0x114, 0xf>(identity, x));
+    x = op(x, dpp<0x118, 0xf>(identity, x));
+    x = op(x, dpp<0x142, 0xa>(identity, x));
+    x = op(x, dpp<0x143, 0xc>(identity, x));
+    return __builtin_amdgcn_readlane(x, kWave - 1);
+}
+__device__ __forceinline__ float lanes_max(float x) {
+    return __int_as_float(wave_reduce(__float_as_int(x), __float_as_int(-INFINITY), [](int a, int b) {
+        return __float_as_int(fmaxf(__int_as_float(a), __int_as_float(b)));
+    }));
+}
+__device__ __forceinline__ float lanes_sum(float x) {
+    return __int_as_float(wave_reduce(__float_as_int(x), 0, [](int a, int b) {
+        return __float_as_int(__int_as_float(a) + __int_as_float(b));
+    }));
+}
+
+// Running state of a set of logits, and that of the lanes' sets together.
+struct SumState {
+    float m, l, t;
+};
+__device__ __forceinline__ SumState lanes_join(SumState x) {
+    const float m = lanes_max(x.m);
+    // (an empty set: l = t = 0 and m = -inf, which must not become NaN)
+    const float d = x.m == -INFINITY ? 0.f : x.m - m, e = fast_exp2(d * kLog2e);
+    return SumState{m, lanes_sum(x.l * e), lanes_sum((x.t + x.l * d) * e)};
 }
 
 // Orders a wave's LDS stores before its lanes' later loads of them.
 __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
-
-template <int N>
-__device__ __forceinline__ bool has_nan(const float (&x)[N]) {
-    bool any = false;
-#pragma unroll
-    for (int e = 0; e < N; ++e)
-        any |= x[e] != x[e];
-    return any;
+__device__ __forceinline__ uint64_t volatile_load(const uint64_t *p) {
+    return *(const volatile uint64_t *)p;
+}
+__device__ __forceinline__ uint64_t uniform64(uint64_t v) {
+    return ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(v >> 32)) << 32) |
+           (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)v);
+}
+__device__ __forceinline__ uint64_t readlane64(uint64_t v, int lane) {
+    return ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), lane) << 32) |
+           (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
 }
 
-// Running state of a set of logits.
-struct SumState {
-    float m, l, t;
+// Number of the n keys at `list` (LDS; zeros behind them up to a multiple of
+// 8) above each of x and y.  The reads are the same for all lanes.
+__device__ __forceinline__ void count_above(const uint64_t *list, int n, uint64_t x, uint64_t y,
+                                            int &nx, int &ny) {
+#pragma unroll 1
+    for (int j = 0; j < n; j += 8) {
+        uint64_t k[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            k[i] = list[j + i];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            nx += k[i] > x ? 1 : 0;
+            ny += k[i] > y ? 1 : 0;
+        }
+    }
+}
+
+// A wave's n best values: lane i < n holds the i-th key, 0 where there is none.
+struct BestList {
+    uint64_t best, bar;                    // bar: the n-th key (uniform)
+    int n;
+
+    __device__ __forceinline__ void clear() { best = bar = 0; }
+    // Takes in the m <= 64 keys at `from` (LDS, zeros behind them up to a
+    // multiple of 8; all different).  scratch: 64 keys of LDS, the wave's own.
+    __device__ __forceinline__ void take(const uint64_t *from, int m, uint64_t *scratch) {
+        const int lane = threadIdx.x % kWave;
+        const uint64_t key = lane < m ? from[lane] : 0ull;
+        int old_place = lane, new_place = 0, none = 0;
+        count_above(from, m, best, key, old_place, new_place);
+        if (bar | readlane64(best, 0)) {             // (an empty list has none above)
+            scratch[lane] = best;
+            wave_sync();
+            count_above(scratch, n, key, ~0ull, new_place, none);
+            wave_sync();
+        }
+        if (lane < n && old_place < n)
+            scratch[old_place] = best;
+        if (key && new_place < n)
+            scratch[new_place] = key;
+        wave_sync();
+        best = lane < n ? scratch[lane] : 0ull;
+        bar = readlane64(best, n - 1);
+        wave_sync();
+    }
 };
-__device__ __forceinline__ SumState join(SumState x, SumState y) {
-    const float m = fmaxf(x.m, y.m);
-    const float dx = x.m - m, dy = y.m - m;
-    // (an empty side: l = t = 0 and m = -inf, which must not become NaN)
-    const float ex = x.m == -INFINITY ? 0.f : expf(dx), ey = y.m == -INFINITY ? 0.f : expf(dy);
-    const float fx = x.m == -INFINITY ? 0.f : dx, fy = y.m == -INFINITY ? 0.f : dy;
-    SumState r;
-    r.m = m;
-    r.l = x.l * ex + y.l * ey;
-    r.t = (x.t + x.l * fx) * ex + (y.t + y.l * fy) * ey;
-    return r;
-}
-
-// Cuts a list of n keys (n <= kCap, all different) down to its `top` best, in
-// no particular order; returns the least of them.  Called by one wave.
-__device__ __forceinline__ uint64_t keep_best(uint64_t *list, int n, int top) {
-    const int lane = threadIdx.x % kWave;
-    uint64_t k[kCap / kWave];
-#pragma unroll
-    for (int j = 0; j < kCap / kWave; ++j)
-        k[j] = j * kWave + lane < n ? list[j * kWave + lane] : 0ull;
-    // the largest number that at least `top` keys reach, bit by bit from the
-    // top; it is found early where exactly `top` keys reach it
-    uint64_t least = 0;
-    for (int bit = 63; bit >= 0; --bit) {
-        const uint64_t cand = least | (1ull << bit);
-        int count = 0;
-#pragma unroll
-        for (int j = 0; j < kCap / kWave; ++j)
-            count += __popcll(__ballot(k[j] >= cand));
-        if (count >= top) {
-            least = cand;
-            if (count == top)
-                break;
-        }
-    }
-    const uint64_t below = (1ull << lane) - 1ull;
-    int at = 0;
-    uint64_t min_kept = ~0ull;
-    wave_sync();
-#pragma unroll
-    for (int j = 0; j < kCap / kWave; ++j) {
-        const bool take = k[j] >= least && k[j] != 0;
-        const uint64_t mask = __ballot(take);
-        if (take) {
-            list[at + __popcll(mask & below)] = k[j];
-            min_kept = min(min_kept, k[j]);
-        }
-        at += __popcll(mask);
-    }
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1)
-        min_kept = min(min_kept, (uint64_t)__shfl_xor((unsigned long long)min_kept, off, kWave));
-    wave_sync();
-    return min_kept;
-}
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void token_logprobs(LogprobParams a) {
     constexpr int V = 16 / sizeof(T);
-    __shared__ uint64_t lists[kWaves][kCap];
+    constexpr int TILE = kWave * V, U = kLoads;
+    // what enters a wave's list, at most a tile's values at a time; later the
+    // lists of the waves and of the parts
+    constexpr int kGather = TILE;
+    __shared__ __attribute__((aligned(16))) uint64_t keys[2 * kPartKeys + 8];
+    static_assert(kWaves * (kGather + 8) <= 2 * kPartKeys, "the waves' values");
+    uint64_t *joined = keys + kPartKeys;   // what is left of the lists
+    __shared__ int n_joined;
+    __shared__ uint64_t bars[kWaves];
+    __shared__ __attribute__((aligned(16))) uint64_t places[kWaves][kWave];
     __shared__ SumState states[kWaves];
-    __shared__ int ranks[kWaves], counts[kWaves];
+    __shared__ int ranks[kWaves];
     const int row = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
     const int wave = wave_id(), lane = threadIdx.x % kWave;
     const T *z = static_cast<const T *>(a.logits) + (size_t)row * a.stride;
-    auto at = [&](int i) -> float {
+    auto value = [&](T raw) -> float {
         if constexpr (sizeof(T) == 2)
-            return bf16_to_f32(z[i]);
+            return bf16_to_f32(raw);
         else
-            return z[i];
+            return raw;
     };
     const int token = a.tokens ? a.tokens[row] : -1;
     const bool has_token = token >= 0 && token < a.vocab;
-    const float zt = has_token ? at(token) : INFINITY;
-    const bool zt_nan = zt != zt;
+    const float zt = has_token ? value(z[token]) : INFINITY;
+    const uint32_t zt_order = value_order(zt);
+    // What comes before the token: behind it, the values above its own; before
+    // it also the equal ones, which are those above the next lower number (all,
+    // where its logit is -inf: !(x <= NaN)).  NaN counts as above.
+    float zt_below;
+    {
+        const uint32_t u = __float_as_uint(zt + 0.f);
+        zt_below = __uint_as_float(u == 0 ? 0x80000001u : (u >> 31) ? u + 1 : u - 1);
+    }
 
     // ---- this wave's run ----
-    // Elements before `head` and behind the last whole piece are taken one by
-    // one, so that a row may begin at any element.
     const int run = a.part_len / kWaves;
     const int i0 = min(part * a.part_len + wave * run, a.vocab);
     const int i1 = min(i0 + run, a.vocab);
-    uint64_t *list = lists[wave];
-    int n_list = 0;                        // uniform
-    float enter = -INFINITY;               // a value enters if it is larger, or while
-    bool filled = false;                   // the list has not held n_top yet
+    BestList list;
+    list.n = a.n_top;
+    list.clear();
+    uint64_t *buf = keys + wave * (kGather + 8);
+    uint64_t *scratch = places[wave];
+    if (threadIdx.x < kWaves)
+        bars[threadIdx.x] = 0;
+    __syncthreads();
+    uint64_t bar = 0;                      // the highest of the waves' (uniform)
     float m = -INFINITY, l = 0.f, t = 0.f;
-    int ahead = 0;
-    // V values of every lane, a lane's from index base on, the wave's from
-    // `tile` on; full: all of them are there, else the lane's first `valid`.
-    auto take = [&](const float (&x)[V], int tile, int base, int valid, auto full_tag)
-        __attribute__((always_inline)) {
-        constexpr bool FULL = decltype(full_tag)::value;
-        auto there = [&](int e) { return FULL || e < valid; };
-        float mx = -INFINITY;
-#pragma unroll
-        for (int e = 0; e < V; ++e)
-            mx = there(e) ? fmaxf(mx, x[e]) : mx;
-        if (mx > m) {
-            const float f = m == -INFINITY ? 0.f : m - mx;
-            const float s = m == -INFINITY ? 0.f : fast_exp2(f * kLog2e);
-            t = (t + l * f) * s;
-            l *= s;
-            m = mx;
-        }
-        const float mu = m == -INFINITY ? 0.f : m;
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-            const float d = there(e) ? x[e] - mu : -INFINITY;
-            const float w = fast_exp2(d * kLog2e);
-            l += w;
-            t = fmaf(w, fmaxf(d, -1e30f), t);        // (0 * -inf would be NaN)
-        }
-        // ---- the token's rank: whole tiles lie before it or behind it ----
-        if (FULL && !zt_nan && tile + kWave * V <= token) {
-#pragma unroll
-            for (int e = 0; e < V; ++e)
-                ahead += !(x[e] < zt) ? 1 : 0;
-        } else if (FULL && !zt_nan && tile > token) {
-#pragma unroll
-            for (int e = 0; e < V; ++e)
-                ahead += !(x[e] <= zt) ? 1 : 0;
-        } else {
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                const bool before = base + e < token;
-                const bool a_nan = x[e] != x[e];
-                const bool first = zt_nan ? a_nan && before
-                                          : a_nan || x[e] > zt || (x[e] == zt && before);
-                ahead += there(e) && first ? 1 : 0;
-            }
-        }
-        if (a.n_top == 0)
-            return;
-        // ---- the list: what beats the n-th best of the tiles before (values
-        // equal to it have higher indexes here), or, until a list was full, all
-        if (filled && !__ballot(!(mx <= enter)) && !__ballot(has_nan(x)))
-            return;
-        bool in[V];
-#pragma unroll
-        for (int e = 0; e < V; ++e)
-            in[e] = there(e) && (!filled || !(x[e] <= enter));
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-            const uint64_t mask = __ballot(in[e]);
-            if (!mask)
-                continue;
-            const int more = __popcll(mask);
-            if (n_list + more > kCap) {
-                const uint64_t least = keep_best(list, n_list, a.n_top);
-                n_list = a.n_top;
-                filled = true;
-                enter = order_value((uint32_t)(least >> 32));
-            }
-            if (in[e])
-                list[n_list + __popcll(mask & ((1ull << lane) - 1ull))] = make_key(x[e], base + e);
-            n_list += more;
-        }
-        wave_sync();
-    };
+    int ahead = 0;                         // uniform
+
     auto unpack = [&](u32x4 w, float (&x)[V]) {
         if constexpr (sizeof(T) == 2) {
 #pragma unroll
@@ -246,150 +237,312 @@ __global__ __launch_bounds__(kThreads) void token_logprobs(LogprobParams a) {
                 x[e] = __uint_as_float(w[e]);
         }
     };
-    auto singles = [&](int from, int to) {           // fewer than V elements
-        if (from < to) {
-            float x[V] = {};
-            const int i = from + lane;
-            if (i < to)
-                x[0] = at(i);
-            take(x, from, i, i < to ? 1 : 0, std::false_type{});
+    // The sums over V values of every lane; the order of the largest, or, where
+    // NaN or +inf is among them, the highest there is.
+    auto add = [&](const float (&x)[V]) __attribute__((always_inline)) -> uint32_t {
+        float mx = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+            mx = fmaxf(mx, x[e]);
+        if (mx > m + 8.f) {
+            const float f = m == -INFINITY ? 0.f : m - mx;
+            const float s = m == -INFINITY ? 0.f : fast_exp2(f * kLog2e);
+            t = (t + l * f) * s;
+            l *= s;
+            m = mx;
         }
+        const float mu = m == -INFINITY ? 0.f : m;
+        // (sums of a piece first: the chains are V times shorter)
+        float pl = 0.f, pt = 0.f;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const float d = x[e] - mu, p = fast_exp2(d * kLog2e);
+            pl += p;
+            pt = fmaf(p, fmaxf(d, -1e30f), pt);      // (0 * -inf would be NaN)
+        }
+        l += pl;
+        t += pt;
+        return pl != pl ? ~0u : value_order(mx);
     };
+    // Elements before the first 16-byte boundary and behind the last whole piece
+    // go one to a lane, whole groups of U tiles with their loads ahead, what is
+    // left (and the group that has the token) tile by tile.
     const int head =
         min(i1, i0 + (int)(((16 - (reinterpret_cast<uintptr_t>(z + i0) & 15)) & 15) / sizeof(T)));
     const int body = head + (i1 - head) / V * V;
-    constexpr int TILE = kWave * V, U = 4;
-    singles(i0, head);
-    int base = head;
-    for (; base + U * TILE <= body; base += U * TILE) {
+    // A piece of V lies before the token or not; the values before it in its own
+    // piece are counted here where they equal it.
+    if (token >= head && token < body) {
+        const int i = token - (token - head) % V + lane;
+        ahead = __popcll(__ballot(i < token && value(z[min(i, token)]) == zt));
+    }
+    if (zt != zt) {
+        // a NaN's rank: the number of those before it
+        for (int i = i0 + lane; i - lane < min(i1, token); i += kWave) {
+            const float x = value(z[min(i, token)]);
+            ahead += __popcll(__ballot(i < token && i < i1 && x != x));
+        }
+    }
+#pragma unroll 1
+    for (int pos = i0; pos < i1;) {
+        const bool single = pos < head || pos >= body;
+        const int group = pos + U * TILE;
+        const bool whole = !single && group <= body;
+        const int next = whole ? group : pos < head ? head : single ? i1 : min(body, pos + TILE);
+        // a lane's elements in tile u: from index base + u * TILE on, n of them
+        const int base = pos + (single ? lane : lane * V);
+        const int n = base >= next ? 0 : single ? 1 : V;
         u32x4 w[U];
+        uint32_t tops[U] = {};
+        uint32_t top = 0;
+        if (whole) {
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            w[u] = *reinterpret_cast<const u32x4 *>(z + base + u * TILE + lane * V);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
+            for (int u = 0; u < U; ++u)
+                w[u] = *reinterpret_cast<const u32x4 *>(z + pos + u * TILE + lane * V);
+        } else {
+            w[0] = u32x4{0u, 0u, 0u, 0u};
+            if (n == V) {
+                w[0] = *reinterpret_cast<const u32x4 *>(z + base);
+            } else if (n == 1) {
+                if constexpr (sizeof(T) == 2)
+                    w[0][0] = z[base];
+                else
+                    w[0][0] = __float_as_uint(z[base]);
+            }
+        }
+        auto tile = [&](int u, auto full_tag) __attribute__((always_inline)) {
+            constexpr bool FULL = decltype(full_tag)::value;
             float x[V];
             unpack(w[u], x);
-            take(x, base + u * TILE, base + u * TILE + lane * V, V, std::true_type{});
-        }
-    }
-    for (; base < body; base += TILE) {
-        const int i = base + lane * V;
-        u32x4 w = {0u, 0u, 0u, 0u};
-        if (i < body)
-            w = *reinterpret_cast<const u32x4 *>(z + i);
-        float x[V];
-        unpack(w, x);
-        take(x, base, i, i < body ? V : 0, std::false_type{});
-    }
-    singles(body, i1);
-
-    // ---- the waves meet ----
-    SumState s{m, l, t};
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) {
-        SumState o{__shfl_xor(s.m, off, kWave), __shfl_xor(s.l, off, kWave),
-                   __shfl_xor(s.t, off, kWave)};
-        // the lower lane first, so that both sides add alike
-        s = (lane & off) ? join(o, s) : join(s, o);
-        ahead += __shfl_xor(ahead, off, kWave);
-    }
-    if (n_list > a.n_top) {
-        keep_best(list, n_list, a.n_top);
-        n_list = a.n_top;
-    }
-    if (lane == 0) {
-        states[wave] = s;
-        ranks[wave] = ahead;
-        counts[wave] = n_list;
-    }
-    __syncthreads();
-    // Joins the keys of `sets` sets (set i: n(i) keys, key(i, j)) into the first
-    // list, cut to n_top; called by wave 0.
-    int held = 0;
-    auto add = [&](uint64_t k, bool in) {
-        const uint64_t mask = __ballot(in);
-        const int more = __popcll(mask);
-        if (held + more > kCap) {
-            keep_best(lists[0], held, a.n_top);
-            held = a.n_top;
+            for (int e = 0; e < V; ++e)
+                x[e] = FULL || e < n ? x[e] : -INFINITY;
+            tops[u] = add(x);
+            top = max(top, tops[u]);
+            const bool before = base + u * TILE + (FULL ? V : n) <= token;
+            const float above = before ? zt_below : zt;
+            // (one order below it is no less sharp)
+            if (__ballot(tops[u] > zt_order - (before ? 1u : 0u)) && zt == zt)
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    ahead += __popcll(__ballot((FULL || e < n) && !(x[e] <= above)));
+        };
+        if (whole) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                tile(u, std::true_type{});
+        } else {
+            tile(0, std::false_type{});
         }
-        if (in)
-            lists[0][held + __popcll(mask & ((1ull << lane) - 1ull))] = k;
-        held += more;
-        wave_sync();
-    };
-    int all_ahead = 0;
-    if (wave == 0) {
-        held = counts[0];
-        s = states[0];
-        all_ahead = ranks[0];
-        for (int w = 1; w < kWaves; ++w) {
-            s = join(s, states[w]);
-            all_ahead += ranks[w];
-            add(lane < counts[w] ? lists[w][lane] : 0ull, lane < counts[w]);
+        // ---- the list (a value equal to its n-th best is behind it) ----
+        if (a.n_top && __ballot(n > 0 && top >= max((uint32_t)(bar >> 32), 1u))) {
+            // (the waves' bars rise; which one is seen changes no result)
+            const uint64_t b = max(max(volatile_load(bars), volatile_load(bars + 1)),
+                                   max(volatile_load(bars + 2), volatile_load(bars + 3)));
+            bar = uniform64(b);
+            uint32_t need = max((uint32_t)(bar >> 32), 1u);
+            // the n-th largest of the lanes' maxima: the least of those that
+            // fewer than n are above (a lane whose `top` is the NaN mark may hold
+            // less: it counts as 0)
+            const uint32_t o = n > 0 && top != ~0u ? top : 0u;
+            if (__popcll(__ballot(o > need)) >= a.n_top) {
+                uint32_t *tops_lds = reinterpret_cast<uint32_t *>(scratch);
+                tops_lds[lane] = o;
+                wave_sync();
+                int above = 0;
+#pragma unroll 1
+                for (int j = 0; j < kWave; j += 16) {
+                    uint32_t k[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        k[i] = tops_lds[j + i];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        above += k[i] > o ? 1 : 0;
+                }
+                wave_sync();
+                const int reach = wave_reduce(
+                    above < a.n_top ? (int)o : -1, -1,
+                    [](int x, int y) { return (int)min((uint32_t)x, (uint32_t)y); });
+                need = max(need, (uint32_t)reach);
+            }
+            const float need_value = need > 1u ? order_value(need) : -INFINITY;
+            int held = 0;
+            const int tiles = whole ? U : 1;
+#pragma unroll 1
+            for (int u = 0; u <= tiles; ++u) {
+                uint64_t in[V];
+                float x[V];
+                int more = 0;
+                if (u < tiles) {
+                    u32x4 wu = w[0];
+                    uint32_t tu = tops[0];
+#pragma unroll
+                    for (int i = 1; i < U; ++i) {
+                        wu = u == i ? w[i] : wu;
+                        tu = u == i ? tops[i] : tu;
+                    }
+                    if (!__ballot(tu >= need))
+                        continue;
+                    unpack(wu, x);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        in[e] = __ballot(e < n && !(x[e] < need_value));
+                        more += __popcll(in[e]);
+                    }
+                }
+                if (u == tiles || held + more > kGather) {
+                    if (lane < 8)
+                        buf[held + lane] = 0;
+                    wave_sync();
+#pragma unroll 1
+                    for (int i = 0; i < held; i += kWave)
+                        list.take(buf + i, min(held - i, kWave), scratch);
+                    held = 0;
+                }
+                if (more) {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        if (!in[e])
+                            continue;
+                        if ((in[e] >> lane) & 1ull)
+                            buf[held + __popcll(in[e] & ((1ull << lane) - 1ull))] =
+                                make_key(x[e], base + u * TILE + e);
+                        held += __popcll(in[e]);
+                    }
+                }
+            }
+            if (lane == 0)
+                *(volatile uint64_t *)(bars + wave) = list.bar;
+            bar = max(bar, list.bar);
         }
-        if (held > a.n_top) {
-            keep_best(lists[0], held, a.n_top);
-            held = a.n_top;
-        }
+        pos = next;
     }
-    if (a.parts > 1) {
-        const size_t slot = (size_t)row * a.parts + part;
+
+    // ---- the waves meet, then, by the row's last workgroup, the parts ----
+    const size_t first = (size_t)row * a.parts;
+    SumState s{m, l, t};
+    bool last_round = a.parts == 1;
+    int lists = 0;
+#pragma unroll 1
+    for (;;) {
+        s = lanes_join(s);
+        if (lane == 0) {
+            states[wave] = s;
+            ranks[wave] = ahead;
+        }
+        __syncthreads();                   // (the waves' buffers lie in `keys`)
+        if (a.parts == 1 || !last_round) {
+            if (lane < a.n_top)
+                keys[wave * a.n_top + lane] = list.best;
+            lists = kWaves;
+        }
+        if (threadIdx.x == 0)
+            n_joined = 0;
+        __syncthreads();
+        if (a.n_top) {
+            const int r = lists == kWaves ? a.wave_r : a.part_r;
+            const int want = lists == kWaves ? a.wave_want : a.part_want;
+            const uint64_t rth = lane < lists ? keys[lane * a.n_top + r - 1] : 0ull;
+            int above = 0;
+#pragma unroll 4
+            for (int p = 0; p < lists; ++p)
+                above += keys[p * a.n_top + r - 1] > rth ? 1 : 0;
+            // (keys of no value, 0, may be equal: then there is no bound)
+            const uint64_t at = __ballot(lane < lists && above == want - 1);
+            const uint64_t least = at ? readlane64(rth, __builtin_ctzll(at)) : 0ull;
+#pragma unroll 1
+            for (int i = threadIdx.x; i - lane < lists * a.n_top; i += kThreads) {
+                const uint64_t k = i < lists * a.n_top ? keys[i] : 0ull;
+                const uint64_t in = __ballot(k && k >= least);
+                int at = 0;
+                if (in && lane == 0)
+                    at = atomicAdd(&n_joined, __popcll(in));
+                at = __builtin_amdgcn_readfirstlane(at);
+                if (k && k >= least)
+                    joined[at + __popcll(in & ((1ull << lane) - 1ull))] = k;
+            }
+            __syncthreads();
+            list.clear();
+            if (wave == 0) {
+                const int m = n_joined;
+                if (lane < 8)
+                    joined[m + lane] = 0;
+                wave_sync();
+#pragma unroll 1
+                for (int i = 0; i < m; i += kWave)
+                    list.take(joined + i, min(m - i, kWave), scratch);
+            }
+        }
         if (wave == 0) {
+            s = SumState{lane < kWaves ? states[lane].m : -INFINITY,
+                         lane < kWaves ? states[lane].l : 0.f,
+                         lane < kWaves ? states[lane].t : 0.f};
+            s = lanes_join(s);
+            ahead = ranks[0] + ranks[1] + ranks[2] + ranks[3];
+        }
+        if (last_round)
+            break;
+        if (wave == 0) {
+            float *ps = a.part_state + (first + part) * 4;
             if (lane == 0) {
-                float *ps = a.part_state + slot * 4;
-                ps[0] = s.m;
-                ps[1] = s.l;
-                ps[2] = s.t;
-                ps[3] = __int_as_float(all_ahead);
+                store_agent(ps, s.m);
+                store_agent(ps + 1, s.l);
+                store_agent(ps + 2, s.t);
+                store_agent(ps + 3, __int_as_float(ahead));
             }
             if (lane < a.n_top)
-                a.part_keys[slot * a.n_top + lane] = lane < held ? lists[0][lane] : 0ull;
+                store_agent(a.part_keys + (first + part) * a.n_top + lane, list.best);
         }
-        if (!arrive_last(a.arrived + row, a.parts))
+        if (!arrive_last_direct(a.arrived + row * kCounterStride, a.parts))
             return;
         if (threadIdx.x == 0)
-            a.arrived[row] = 0;
-        if (wave != 0)
-            return;
-        held = 0;
-        all_ahead = 0;
+            a.arrived[row * kCounterStride] = 0;
+        // the parts' states, one to a lane of the first wave, and their lists
         s = SumState{-INFINITY, 0.f, 0.f};
-        for (int p = 0; p < a.parts; ++p) {
-            const size_t from = (size_t)row * a.parts + p;
-            const float *ps = a.part_state + from * 4;
-            s = join(s, SumState{ps[0], ps[1], ps[2]});
-            all_ahead += __float_as_int(ps[3]);
-            const uint64_t k = lane < a.n_top ? a.part_keys[from * a.n_top + lane] : 0ull;
-            add(k, k != 0ull);
+        ahead = 0;
+        if (wave == 0) {
+            if (lane < a.parts) {
+                const float *ps = a.part_state + (first + lane) * 4;
+                s = SumState{load_agent(ps), load_agent(ps + 1), load_agent(ps + 2)};
+                ahead = __float_as_int(load_agent(ps + 3));
+            }
+            ahead = wave_reduce(ahead, 0, [](int x, int y) { return x + y; });
         }
-        if (held > a.n_top)
-            keep_best(lists[0], held, a.n_top);
+        if (a.n_top) {
+            const int n = a.parts * a.n_top;
+            constexpr int N = kPartKeys / kThreads;
+            uint64_t got[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int at = i * kThreads + threadIdx.x;
+                got[i] = at < n ? load_agent(a.part_keys + first * a.n_top + at) : 0ull;
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                keys[i * kThreads + threadIdx.x] = got[i];
+            lists = a.parts;
+        }
+        last_round = true;
     }
     if (wave != 0)
         return;
     // ---- results: one wave ----
     // (a row of nothing but -inf has l = 0; +inf or NaN leave NaN in l)
     const float logl = s.l > 0.f ? logf(s.l) : NAN;
-    auto lp = [&](float x) { return (x - s.m) - logl; };
     if (lane == 0) {
         if (a.logprob)
-            a.logprob[row] = has_token ? lp(zt) : 0.f;
+            a.logprob[row] = has_token ? (zt - s.m) - logl : 0.f;
         if (a.rank)
-            a.rank[row] = has_token ? all_ahead : -1;
+            a.rank[row] = has_token ? ahead : -1;
         if (a.entropy)
             a.entropy[row] = logl - s.t / s.l;
     }
     if (lane < a.n_top) {
-        const uint64_t mine = lists[0][lane];
-        int place = 0;
-        for (int j = 0; j < a.n_top; ++j)
-            place += lists[0][j] > mine ? 1 : 0;
-        const uint32_t o = (uint32_t)(mine >> 32);
-        const size_t dst = (size_t)row * a.n_top + place;
-        a.top_ids[dst] = (int32_t)~(uint32_t)mine;
-        a.top_lp[dst] = lp(o == ~0u ? NAN : order_value(o));
+        const uint32_t o = (uint32_t)(list.best >> 32);
+        const size_t dst = (size_t)row * a.n_top + lane;
+        a.top_ids[dst] = (int32_t)~(uint32_t)list.best;
+        a.top_lp[dst] = ((o == ~0u ? NAN : order_value(o)) - s.m) - logl;
     }
 }
 
@@ -398,11 +551,11 @@ struct LogprobPlan {
 };
 
 // Rows are cut where they are too few to fill the chip (about four workgroups a
-// CU), down to two 16-byte pieces of each lane.
-LogprobPlan plan_logprobs(wf_dtype_t dt, int n_rows, int vocab) {
-    const int unit = kThreads * (dt == WF_F32 ? 4 : 8);
-    const int most = std::max(1, std::min(kMaxParts, (vocab + 2 * unit - 1) / (2 * unit)));
-    const int want = std::max(1, 1024 / std::max(n_rows, 1));
+// CU), down to one group of a wave's four 16-byte loads a lane.
+LogprobPlan plan_logprobs(wf_dtype_t dt, int n_rows, int vocab, int n_top) {
+    const int unit = kThreads * (dt == WF_F32 ? 4 : 8) * kLoads;
+    const int most = std::min({kMaxParts, (vocab + unit - 1) / unit, kPartKeys / std::max(n_top, 1)});
+    const int want = std::max(1, 2 * kMaxSplitRows / std::max(n_rows, 1));
     const int parts = std::min(most, want);
     const int len = ((vocab + parts - 1) / parts + unit - 1) / unit * unit;
     return LogprobPlan{(vocab + len - 1) / len, len};
@@ -415,7 +568,7 @@ size_t state_bytes(int n_rows, const LogprobPlan &p) {
 }  // namespace
 
 size_t token_logprobs_workspace_bytes(wf_dtype_t dt, int n_rows, int vocab, int n_top) {
-    const LogprobPlan p = plan_logprobs(dt, n_rows, vocab);
+    const LogprobPlan p = plan_logprobs(dt, n_rows, vocab, n_top);
     return kCounterBytes +
            (p.parts > 1 ? state_bytes(n_rows, p) + (size_t)n_rows * p.parts * n_top * 8 : 0);
 }
@@ -425,7 +578,7 @@ wf_status_t launch_token_logprobs(wf_dtype_t dt, const void *logits, size_t row_
                                   float *logprob, float *entropy, int32_t *rank,
                                   int32_t *top_ids, float *top_lp, void *workspace,
                                   hipStream_t stream) {
-    const LogprobPlan p = plan_logprobs(dt, n_rows, vocab);
+    const LogprobPlan p = plan_logprobs(dt, n_rows, vocab, n_top);
     LogprobParams a{};
     a.logits = logits;
     a.stride = row_stride;
@@ -439,6 +592,14 @@ wf_status_t launch_token_logprobs(wf_dtype_t dt, const void *logits, size_t row_
     a.n_top = n_top;
     a.parts = p.parts;
     a.part_len = p.part_len;
+    // of P lists of n keys, the want-th largest of the r-th keys is reached by
+    // r * want >= n keys
+    auto bound = [&](int lists, int &r, int &want) {
+        r = (std::max(n_top, 1) + lists - 1) / lists;
+        want = (std::max(n_top, 1) + r - 1) / r;
+    };
+    bound(kWaves, a.wave_r, a.wave_want);
+    bound(p.parts, a.part_r, a.part_want);
     char *ws = static_cast<char *>(workspace);
     a.arrived = reinterpret_cast<unsigned *>(ws);
     a.part_state = reinterpret_cast<float *>(ws + kCounterBytes);

@@ -325,9 +325,9 @@ __global__ __launch_bounds__(kThreads) void paged_select(SelectParams a) {
                 best = acc > best ? acc : best;
             }
             if (lp == 0 && p < n_old)
-                keys[p] = id < 0 ? 0ull : score_key(nan ? (double)NAN : best);
+                store_agent(keys + p, id < 0 ? (uint64_t)0 : score_key(nan ? (double)NAN : best));
         }
-        if (!arrive_last(a.arrived + unit, chunks))
+        if (!arrive_last_direct(a.arrived + unit, chunks))
             return;
         if (threadIdx.x == 0)
             a.arrived[unit] = 0;
@@ -343,13 +343,13 @@ __global__ __launch_bounds__(kThreads) void paged_select(SelectParams a) {
     const bool in_lds = choose && n_old <= kLdsKeys;
     if (in_lds) {
         for (int i = threadIdx.x; i < n_old; i += kThreads)
-            lds_keys[i] = keys[i];
+            lds_keys[i] = load_agent(keys + i);
         __syncthreads();
     }
     auto key = [&](int i) -> uint64_t {
         if (!choose)
             return n_top > 0 && paged_page(a.v, b, i) >= 0 ? 1ull : 0ull;
-        return in_lds ? lds_keys[i] : keys[i];
+        return in_lds ? lds_keys[i] : load_agent(keys + i);
     };
     if (choose) {
         uint64_t prefix = 0;

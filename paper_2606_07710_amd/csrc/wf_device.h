@@ -191,4 +191,28 @@ __device__ __forceinline__ bool arrive_last(unsigned *counter, unsigned expected
     return last != 0;
 }
 
+// The same without the L2 write-back and invalidation of the fences, for data
+// that goes past the L2 by itself: what the workgroups hand over is stored with
+// store_agent and read with load_agent, and the wait below holds each wave at
+// the barrier until its stores have arrived.  (With the fences, 608 workgroups
+// that each hand over 20 keys of 16 rows took 31 us instead of 13.)
+template <typename T>
+__device__ __forceinline__ void store_agent(T *p, T v) {
+    __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <typename T>
+__device__ __forceinline__ T load_agent(const T *p) {
+    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ bool arrive_last_direct(unsigned *counter, unsigned expected) {
+    __shared__ int last;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0)
+        last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
+               expected - 1u;
+    __syncthreads();
+    return last != 0;
+}
+
 }  // namespace wf
