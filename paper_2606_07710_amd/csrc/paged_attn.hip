@@ -718,7 +718,9 @@ __global__ __launch_bounds__(256) void paged_attn_f32(PagedAttnParams a) {
 
 // ---------------------------------------------------------------------------
 // Joins the partials of the split item that begins in workgroup blockIdx.x: a
-// wave per row, its lanes over the dims, parts in run order.
+// wave per row, its lanes over the dims, parts in run order.  Bound by the
+// latency of its three trips to memory (with one part's row in flight instead
+// of eight it took 12 us for 32 parts, longer than the attention).
 template <typename T, int DH, int ROWS>
 __global__ __launch_bounds__(256) void paged_attn_join(PagedAttnParams a) {
     const int w0 = blockIdx.x;
@@ -751,13 +753,27 @@ __global__ __launch_bounds__(256) void paged_attn_join(PagedAttnParams a) {
             lp = src[1] * f;
         }
         l += wave_sum(lp);
+        // eight parts' rows in flight (past the last part: the last again, with
+        // factor 0)
         const int n = min(parts - p0, kWave);
-        for (int p = 0; p < n; ++p) {
-            const float fp = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), p));
-            const float *src = a.part_o + (slot(p0 + p) * ROWS + row) * DH + lane * E;
+        for (int p = 0; p < n; p += 8) {
+            float x[8][E];
 #pragma unroll
-            for (int e = 0; e < E; ++e)
-                o[e] = fmaf(src[e], fp, o[e]);
+            for (int i = 0; i < 8; ++i) {
+                const float *src =
+                    a.part_o + (slot(min(p0 + p + i, parts - 1)) * ROWS + row) * DH + lane * E;
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    x[i][e] = src[e];
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float fp = __uint_as_float(
+                    __builtin_amdgcn_readlane(__float_as_uint(f), min(p + i, kWave - 1)));
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    o[e] = p + i < n ? fmaf(x[i][e], fp, o[e]) : o[e];
+            }
         }
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
