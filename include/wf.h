@@ -872,8 +872,10 @@ size_t wf_paged_verify_attn_workspace_bytes(wf_dtype_t dt, int32_t n_rows,
  *   s = max_h sum_d q_d (q_d >= 0 ? hi[d] : lo[d]),  q_d = q[r][h][d],
  *
  * formed in fp64.  sel[r][g] receives the n_sel - n_recent old pages of the
- * largest scores (the lower page among equals; a NaN score before all others;
- * pages without an entry in the table never) and the recent ones, as logical
+ * largest scores (the lower page among equals; before all others those whose
+ * score has something not finite in it, a bound of the page or an element of
+ * the group's q; pages without an entry in the table never) and the recent
+ * ones, as logical
  * page numbers in ascending order, then -1.  Every old page is complete and
  * visible to its row, so the selection is causal for chains, blocks and trees.
  * q [n_rows][n_q_heads][head_dim]; sel [n_rows][n_kv_heads][n_sel] int32.

@@ -107,10 +107,6 @@ __device__ __forceinline__ SumState lanes_join(SumState x) {
     return SumState{m, lanes_sum(x.l * e), lanes_sum((x.t + x.l * d) * e)};
 }
 
-// Orders a wave's LDS stores before its lanes' later loads of them.
-__device__ __forceinline__ void wave_sync() {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-}
 __device__ __forceinline__ uint64_t volatile_load(const uint64_t *p) {
     return *(const volatile uint64_t *)p;
 }

@@ -225,52 +225,158 @@ __global__ __launch_bounds__(kThreads) void paged_append(AppendParams a) {
 }
 
 // ---------------------------------------------------------------------------
-// Selection.  The workgroups of one (row, KV head) share its old pages, at
-// least kScorePages each: DH / V lanes to a page, V dimensions each,
-//   s = max_h sum_d q_d (q_d >= 0 ? hi_d : lo_d)
-// in fp64 (bf16 products are exact and their sums all but exact there, so the
-// order of the pages does not hang on the order of the sums), and stores the
-// scores as 64-bit keys of the same order.  The last workgroup of the (row,
-// head) finds the n_top-th largest key digit by digit and lists the pages at
-// or above it in page order.
+// Selection, in two launches.
+//
+// Scores:  s = max_h sum_d q_d (q_d >= 0 ? hi_d : lo_d)
+//            = max_h sum_d max(q_d, 0) hi_d + min(q_d, 0) lo_d,
+// in fp64 (bf16 products are exact there and their sums all but exact, so the
+// order of the pages does not hang on the order of the sums), as products of the
+// fp64 matrix instruction: 16 query rows -- the heads of a group, and as many of
+// the sequence's rows as fit -- with the bounds of 16 pages.  A lane holds a
+// quarter of the dims of one query row and of one page; which dims meet in a
+// step is the same for both.  Bound by the matrix unit, 64 cycles for each of
+// DH / 2 steps a tile (each lane summing by itself, with sums over lanes at the
+// end, took 89 us where this takes SCORETIME: 16 sequences of up to 32K tokens).
+//
+// Choice:  a workgroup per (row, KV head) finds the n_top-th largest key digit
+// by digit and lists the pages at or above it in page order.
 // ---------------------------------------------------------------------------
-constexpr int kScorePages = 64;
-constexpr int kLdsKeys = 2048;
+typedef double f64x4 __attribute__((ext_vector_type(4)));
 
 struct SelectParams {
     PagedView v;
     const void *q, *bounds;
     int32_t *sel;
     uint64_t *keys;                // [n_rows * n_kv_heads][max_pages]
-    unsigned *arrived;             // [n_rows * n_kv_heads], in the zero block
     int n_sel, n_recent, group, n_q_heads;
+    int pack;                      // rows of a sequence that share a tile
 };
 
-// A key of a score: larger scores have larger keys, NaN the largest; 0 is kept
-// for pages without an entry.
+// A key of a score: larger scores have larger keys; a score that is not finite
+// (something not finite went into it) has the largest; 0 is kept for pages
+// without an entry.
 __device__ __forceinline__ uint64_t score_key(double s) {
-    if (s != s)
+    if (!(fabs(s) < INFINITY))
         return ~0ull;
     const uint64_t u = __builtin_bit_cast(uint64_t, s + 0.0);
     return (u >> 63) ? ~u : u | (1ull << 63);
 }
 
+// The first recent page of a sequence's row, that is, the number of its old ones.
+__device__ __forceinline__ int old_pages(const SelectParams &a, const Seq &s, int row) {
+    return max(((s.ctx + row) >> a.v.page_shift) + 1 - a.n_recent, 0);
+}
+
 template <typename T, int DH>
-__global__ __launch_bounds__(kThreads) void paged_select(SelectParams a) {
+__global__ __launch_bounds__(kThreads) void paged_scores(SelectParams a) {
     using E = Elem<T>;
-    constexpr int V = E::kVec;
-    constexpr int LPP = DH / V;                      // lanes per page
-    constexpr int WAVES = kThreads / kWave;
+    constexpr int V = E::kVec, PIECES = DH / 4 / V, WAVES = kThreads / kWave;
+    __shared__ double sc[WAVES][16][17];
+    const int g = blockIdx.x % a.v.n_kv_heads;
+    long long first, total;
+    const int b = paged_find<kThreads>(
+        a.v.n_seqs, blockIdx.x / a.v.n_kv_heads,
+        [&](int i) { return (paged_seq(a.v, i, a.v.max_rows).rows + a.pack - 1) / a.pack; }, &first,
+        &total);
+    if (b < 0)
+        return;
+    const Seq s = paged_seq(a.v, b, a.v.max_rows);
+    const int row0 = (int)(blockIdx.x / a.v.n_kv_heads - first) * a.pack;
+    const int rows = min(s.rows - row0, a.pack);
+    const int n_old = old_pages(a, s, row0 + rows - 1);
+    if (n_old <= a.n_sel - a.n_recent)               // all of them are selected
+        return;
+    const int wave = wave_id(), lane = threadIdx.x % kWave;
+    const int m16 = lane & 15, c4 = lane >> 4;
+    const int heads = min(a.group, 16);              // of a row in a tile
+    for (int p0 = (blockIdx.y * WAVES + wave) * 16; p0 < n_old; p0 += gridDim.y * WAVES * 16) {
+        const int p = p0 + m16;
+        const int id = p < n_old ? paged_page(a.v, b, p) : -1;
+        u32x4 lo[PIECES], hi[PIECES];
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i)
+            lo[i] = hi[i] = u32x4{0u, 0u, 0u, 0u};
+        if (id >= 0) {
+            const T *src = static_cast<const T *>(a.bounds) +
+                           ((size_t)id * a.v.n_kv_heads + g) * 2 * DH + c4 * (DH / 4);
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+                lo[i] = *reinterpret_cast<const u32x4 *>(src + i * V);
+                hi[i] = *reinterpret_cast<const u32x4 *>(src + DH + i * V);
+            }
+        }
+        double best[4];                              // of (row, page) lane + 64 j
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            best[j] = -INFINITY;
+        bool odd[4] = {};
+        for (int h0 = 0; h0 < a.group; h0 += 16) {
+            const int row = m16 / heads, h = h0 + m16 % heads;
+            const bool live = row < rows && h < a.group;
+            const T *qp = static_cast<const T *>(a.q) +
+                          ((size_t)(s.r0 + row0 + (live ? row : 0)) * a.n_q_heads + g * a.group +
+                           (live ? h : 0)) * DH + c4 * (DH / 4);
+            f64x4 acc = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+                float q[V], l[V], u[V];
+                E::unpack(*reinterpret_cast<const u32x4 *>(qp + i * V), q);
+                E::unpack(lo[i], l);
+                E::unpack(hi[i], u);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    // (not max and min, which would lose a NaN)
+                    const float up = q[e] >= 0.f || q[e] != q[e] ? q[e] : 0.f;
+                    const float dn = q[e] < 0.f ? q[e] : 0.f;
+                    acc = __builtin_amdgcn_mfma_f64_16x16x4f64((double)(live ? up : 0.f),
+                                                               (double)u[e], acc, 0, 0, 0);
+                    acc = __builtin_amdgcn_mfma_f64_16x16x4f64((double)(live ? dn : 0.f),
+                                                               (double)l[e], acc, 0, 0, 0);
+                }
+            }
+            // lane (m16, c4) has rows 4 i + c4 of column m16
+            wave_sync();
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                sc[wave][4 * i + c4][m16] = acc[i];
+            wave_sync();
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int at = lane + kWave * j, r = at / 16;
+                if (r < rows)
+                    for (int h2 = 0; h2 < min(heads, a.group - h0); ++h2) {
+                        const double x = sc[wave][r * heads + h2][at % 16];
+                        odd[j] |= !(fabs(x) < INFINITY);
+                        best[j] = x > best[j] ? x : best[j];
+                    }
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int at = lane + kWave * j, r = at / 16, page = p0 + at % 16;
+            const int its = __shfl(id, at % 16, kWave);
+            if (r < rows && page < n_old)
+                a.keys[((size_t)(s.r0 + row0 + r) * a.v.n_kv_heads + g) * a.v.max_pages + page] =
+                    its < 0 ? 0ull : score_key(odd[j] ? (double)NAN : best[j]);
+        }
+    }
+}
+
+constexpr int kLdsKeys = 2048;
+
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void paged_choose(SelectParams a) {
+    constexpr int WAVES = THREADS / kWave;
     __shared__ int seq_of_row;
     const int unit = blockIdx.x;
-    const int r = unit / a.v.n_kv_heads, g = unit % a.v.n_kv_heads;
+    const int r = unit / a.v.n_kv_heads;
     if (threadIdx.x == 0)
         seq_of_row = -1;
     __syncthreads();
-    for (int s = threadIdx.x; s < a.v.n_seqs; s += kThreads) {
-        const Seq q = paged_seq(a.v, s, a.v.max_rows);
+    for (int i = threadIdx.x; i < a.v.n_seqs; i += THREADS) {
+        const Seq q = paged_seq(a.v, i, a.v.max_rows);
         if (r >= q.r0 && r < q.r0 + q.rows)
-            seq_of_row = s;
+            seq_of_row = i;
     }
     __syncthreads();
     const int b = uniform(seq_of_row);
@@ -278,60 +384,11 @@ __global__ __launch_bounds__(kThreads) void paged_select(SelectParams a) {
         return;
     const Seq s = paged_seq(a.v, b, a.v.max_rows);
     const int newest = (s.ctx + r - s.r0) >> a.v.page_shift;
-    const int n_old = max(newest + 1 - a.n_recent, 0);
+    const int n_old = old_pages(a, s, r - s.r0);
     const int n_top = a.n_sel - a.n_recent;
     const int wave = wave_id(), lane = threadIdx.x % kWave;
-    uint64_t *keys = a.keys + (size_t)unit * a.v.max_pages;
+    const uint64_t *keys = a.keys + (size_t)unit * a.v.max_pages;
     const bool choose = n_old > n_top && n_top > 0;
-
-    // the workgroups of a (row, head) that have pages to score
-    const int chunks =
-        choose ? min((n_old + kScorePages - 1) / kScorePages, (int)gridDim.y) : 1;
-    if ((int)blockIdx.y >= chunks)
-        return;
-    if (choose) {
-        constexpr int PPW = kWave / LPP;             // pages at a time of a wave
-        const int lp = lane % LPP;
-        for (int p0 = (blockIdx.y * WAVES + wave) * PPW; p0 < n_old; p0 += chunks * WAVES * PPW) {
-            const int p = p0 + lane / LPP;
-            const int id = p < n_old ? paged_page(a.v, b, p) : -1;
-            float lo[V], hi[V];
-            if (id >= 0) {
-                const T *src = static_cast<const T *>(a.bounds) +
-                               ((size_t)id * a.v.n_kv_heads + g) * 2 * DH + lp * V;
-                E::unpack(*reinterpret_cast<const u32x4 *>(src), lo);
-                E::unpack(*reinterpret_cast<const u32x4 *>(src + DH), hi);
-            } else {
-#pragma unroll
-                for (int e = 0; e < V; ++e)
-                    lo[e] = hi[e] = 0.f;
-            }
-            double best = -INFINITY;
-            bool nan = false;
-            for (int h = 0; h < a.group; ++h) {
-                float q[V];
-                E::unpack(*reinterpret_cast<const u32x4 *>(
-                              static_cast<const T *>(a.q) +
-                              ((size_t)r * a.n_q_heads + g * a.group + h) * DH + lp * V),
-                          q);
-                double acc = 0.0;
-#pragma unroll
-                for (int e = 0; e < V; ++e)
-                    acc = fma((double)q[e], (double)(q[e] >= 0.f ? hi[e] : lo[e]), acc);
-#pragma unroll
-                for (int off = 1; off < LPP; off <<= 1)
-                    acc += __shfl_xor(acc, off, kWave);
-                nan |= acc != acc;
-                best = acc > best ? acc : best;
-            }
-            if (lp == 0 && p < n_old)
-                store_agent(keys + p, id < 0 ? (uint64_t)0 : score_key(nan ? (double)NAN : best));
-        }
-        if (!arrive_last_direct(a.arrived + unit, chunks))
-            return;
-        if (threadIdx.x == 0)
-            a.arrived[unit] = 0;
-    }
 
     // ---- the smallest selected key ----
     __shared__ uint64_t lds_keys[kLdsKeys];
@@ -340,29 +397,41 @@ __global__ __launch_bounds__(kThreads) void paged_select(SelectParams a) {
     __shared__ int digit, above;
     uint64_t least = 1;                              // all pages with an entry
     int equal_quota = n_old;                         // of the pages at `least`
-    const bool in_lds = choose && n_old <= kLdsKeys;
-    if (in_lds) {
-        for (int i = threadIdx.x; i < n_old; i += kThreads)
-            lds_keys[i] = load_agent(keys + i);
-        __syncthreads();
-    }
+    const bool in_lds = n_old <= kLdsKeys;
+    if (in_lds)
+        for (int i = threadIdx.x; i < n_old; i += THREADS)
+            lds_keys[i] = choose ? keys[i] : n_top > 0 && paged_page(a.v, b, i) >= 0 ? 1ull : 0ull;
     auto key = [&](int i) -> uint64_t {
-        if (!choose)
-            return n_top > 0 && paged_page(a.v, b, i) >= 0 ? 1ull : 0ull;
-        return in_lds ? lds_keys[i] : load_agent(keys + i);
+        if (in_lds)
+            return lds_keys[i];
+        return choose ? keys[i] : n_top > 0 && paged_page(a.v, b, i) >= 0 ? 1ull : 0ull;
     };
     if (choose) {
         uint64_t prefix = 0;
         int need = n_top;
         int shift = 56;
         for (;; shift -= 8) {
-            for (int i = threadIdx.x; i < 256; i += kThreads)
+            for (int i = threadIdx.x; i < 256; i += THREADS)
                 hist[i] = 0;
             __syncthreads();
-            for (int i = threadIdx.x; i < n_old; i += kThreads) {
-                const uint64_t k = key(i);
-                if (shift == 56 || (k >> (shift + 8)) == (prefix >> (shift + 8)))
-                    atomicAdd(&hist[(k >> shift) & 255], 1);
+            for (int i0 = wave * kWave; i0 < n_old; i0 += THREADS) {
+                const int i = i0 + lane;
+                const uint64_t k = i < n_old ? key(i) : 0ull;
+                const bool in = i < n_old &&
+                                (shift == 56 || (k >> (shift + 8)) == (prefix >> (shift + 8)));
+                const int d = (int)(k >> shift) & 255;
+                // many keys share their first digits: those of the wave's first
+                // such key go in as one
+                const uint64_t live = __ballot(in);
+                if (!live)
+                    continue;
+                const int lead = __builtin_ctzll(live);
+                const int d0 = __builtin_amdgcn_readlane(d, lead);
+                const uint64_t same = __ballot(in && d == d0);
+                if (lane == lead)
+                    atomicAdd(&hist[d0], __popcll(same));
+                else if (in && d != d0)
+                    atomicAdd(&hist[d], 1);
             }
             __syncthreads();
             // the digit of the need-th largest key: bins from the top on
@@ -403,6 +472,8 @@ __global__ __launch_bounds__(kThreads) void paged_select(SelectParams a) {
         equal_quota = shift == 0 ? need : n_old;
         if (least == 0)                              // fewer pages than n_top have entries
             least = 1, equal_quota = n_old;
+    } else {
+        __syncthreads();
     }
 
     // ---- list them in page order: a run of pages per wave ----
@@ -452,7 +523,7 @@ __global__ __launch_bounds__(kThreads) void paged_select(SelectParams a) {
     }
     // the recent pages, and -1 behind them
     const int recent = newest + 1 - n_old;
-    for (int i = listed + threadIdx.x; i < a.n_sel; i += kThreads)
+    for (int i = listed + threadIdx.x; i < a.n_sel; i += THREADS)
         out[i] = i - listed < recent ? n_old + i - listed : -1;
 }
 
@@ -510,27 +581,31 @@ wf_status_t launch_paged_select(wf_dtype_t dt, const void *q, const wf_paged_cac
     a.q = q;
     a.bounds = c.bounds;
     a.sel = sel;
-    a.arrived = static_cast<unsigned *>(workspace);
     a.keys = reinterpret_cast<uint64_t *>(static_cast<char *>(workspace) + kCounterBytes);
     a.n_sel = n_sel;
     a.n_recent = n_recent;
     a.group = n_q_heads / c.n_kv_heads;
     a.n_q_heads = n_q_heads;
-    // (the table may be far wider than the sequences are long: no more
-    // workgroups than fill the chip a few times)
-    const int units = n_rows * c.n_kv_heads;
-    const int chunks = (b.max_pages + kScorePages - 1) / kScorePages;
+    a.pack = std::min(std::max(16 / a.group, 1), b.max_rows);
+    // (a sequence's last pack may be short; the table may be far wider than the
+    // sequences are long: no more workgroups than fill the chip a few times)
+    const int packs = std::min(n_rows, n_rows / a.pack + std::min(b.n_seqs, n_rows));
+    const int units = packs * c.n_kv_heads;
+    const int chunks = (b.max_pages + 63) / 64;
     const dim3 grid(units, std::min(chunks, std::max(2048 / units, 1)));
     const dim3 block(kThreads);
-    if (dt == WF_BF16) {
-        if (c.head_dim == 128)
-            hipLaunchKernelGGL((paged_select<uint16_t, 128>), grid, block, 0, stream, a);
+    if (n_sel > n_recent) {
+        if (dt == WF_BF16) {
+            if (c.head_dim == 128)
+                hipLaunchKernelGGL((paged_scores<uint16_t, 128>), grid, block, 0, stream, a);
+            else
+                hipLaunchKernelGGL((paged_scores<uint16_t, 64>), grid, block, 0, stream, a);
+        } else if (c.head_dim == 128)
+            hipLaunchKernelGGL((paged_scores<float, 128>), grid, block, 0, stream, a);
         else
-            hipLaunchKernelGGL((paged_select<uint16_t, 64>), grid, block, 0, stream, a);
-    } else if (c.head_dim == 128)
-        hipLaunchKernelGGL((paged_select<float, 128>), grid, block, 0, stream, a);
-    else
-        hipLaunchKernelGGL((paged_select<float, 64>), grid, block, 0, stream, a);
+            hipLaunchKernelGGL((paged_scores<float, 64>), grid, block, 0, stream, a);
+    }
+    hipLaunchKernelGGL((paged_choose<kThreads>), dim3(n_rows * c.n_kv_heads), block, 0, stream, a);
     return hipGetLastError() == hipSuccess ? WF_OK : WF_ERR_HIP;
 }
 

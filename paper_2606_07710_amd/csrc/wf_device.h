@@ -161,6 +161,11 @@ __device__ __forceinline__ int wave_id() {
     return __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
 }
 
+// Orders a wave's LDS stores before its lanes' later loads of them.
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
 // Halves of a device-scope fence.
 __device__ __forceinline__ void fence_release_agent() {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");

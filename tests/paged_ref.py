@@ -123,7 +123,7 @@ def attention(rnd, tree=None, sel=None, scale=None):
     return out, err
 
 
-def select(rnd, n_sel, n_recent, rows_of=None):
+def select(rnd, n_sel, n_recent):
     """The selection [n][Hkv][n_sel]; rows of no sequence hold -7."""
     bounds, q = f64(rnd.bounds), f64(rnd.q)
     grp, n_pool = rnd.hq // rnd.hkv, rnd.k.shape[0]
@@ -140,11 +140,10 @@ def select(rnd, n_sel, n_recent, rows_of=None):
                         continue
                     lo, hi = bounds[t, g]
                     qq = q[r, g * grp:(g + 1) * grp]
+                    odd = not (np.isfinite(bounds[t, g]).all() and np.isfinite(qq).all())
                     with np.errstate(invalid="ignore"):
-                        s = (qq * np.where(qq >= 0, hi, lo)).sum(-1)
-                    s = np.inf if np.isnan(s).any() else s.max()
-                    nan = np.isnan((qq * np.where(qq >= 0, hi, lo)).sum(-1)).any()
-                    score.append((0 if nan else 1, -s, p))
+                        s = (qq * np.where(qq >= 0, hi, lo)).sum(-1).max()
+                    score.append((0, 0.0, p) if odd else (1, -s, p))
                 top = sorted(p for _, _, p in sorted(score)[: n_sel - n_recent])
                 got = top + list(range(n_old, newest + 1))
                 out[r, g] = got + [-1] * (n_sel - len(got))
