@@ -71,18 +71,14 @@ __device__ __forceinline__ uint64_t make_key(float x, int idx) {
 // op over the lanes of a wave, in a fixed order; the same result in every lane.
 // The steps move values between lanes without LDS: shifts by 1, 2, 4, 8 within
 // the rows of 16, then the rows' last lanes to the rows behind.
-template <int CTRL, int ROWS>
-__device__ __forceinline__ int dpp(int identity, int x) {
-    return __builtin_amdgcn_update_dpp(identity, x, CTRL, ROWS, 0xf, false);
-}
 template <typename Op>
 __device__ __forceinline__ int wave_reduce(int x, int identity, Op &&op) {
-    x = op(x, dpp<0x111, 0xf>(identity, x));
-    x = op(x, dpp<0x112, 0xf>(identity, x));
-    x = op(x, dpp<0x114, 0xf>(identity, x));
-    x = op(x, dpp<0x118, 0xf>(identity, x));
-    x = op(x, dpp<0x142, 0xa>(identity, x));
-    x = op(x, dpp<0x143, 0xc>(identity, x));
+    x = op(x, dpp<kRowShr1, 0xf>(identity, x));
+    x = op(x, dpp<kRowShr2, 0xf>(identity, x));
+    x = op(x, dpp<kRowShr4, 0xf>(identity, x));
+    x = op(x, dpp<kRowShr8, 0xf>(identity, x));
+    x = op(x, dpp<kRowBcast15, 0xa>(identity, x));
+    x = op(x, dpp<kRowBcast31, 0xc>(identity, x));
     return __builtin_amdgcn_readlane(x, kWave - 1);
 }
 __device__ __forceinline__ float lanes_max(float x) {

@@ -48,15 +48,19 @@ __device__ __forceinline__ float nan_min(float a, float b) { return (a < b || a 
 __device__ __forceinline__ float nan_max(float a, float b) { return (a > b || a != a) ? a : b; }
 
 // ---------------------------------------------------------------------------
-// Append.  A workgroup takes one page that the batch writes and one KV head's
-// K and V rows in it, or the group of query heads that reads that head: rows
-// move in 16-byte pieces, a thread holding both halves of its rotation pairs.
+// Append.  A workgroup takes one page that the batch writes and a run of KV
+// heads with the query heads that read them.  It forms the sines and cosines of
+// the page's new rows once, in LDS; then each of its waves takes one head's rows
+// after the other, in 16-byte pieces, a thread holding both halves of its
+// rotation pairs:
 //   k' = R(pos) k: (lo, hi) -> (lo cos - hi sin, hi cos + lo sin), the angle
 //   pos * theta_i in turns, reduced to half a turn in fp64 (an fp32 product
 //   would be off by a part in a hundred of a radian at 64K positions), sine and
 //   cosine in fp32.
 // The bounds are taken anew from all of the page's valid rows, older ones
-// included, so they never depend on what the page held before.
+// included, so they never depend on what the page held before.  Prompts are
+// bound by memory (with the angles formed by every head's workgroup, 11000 rows
+// of 48 heads took 92 us, with the run of heads APPTIME).
 // ---------------------------------------------------------------------------
 struct AppendParams {
     PagedView v;
@@ -65,15 +69,21 @@ struct AppendParams {
     void *k, *vc, *bounds, *q_out;
     const int32_t *positions;
     size_t kv_stride, q_stride;    // elements
-    int group, n_q_heads;
+    int group, n_q_heads;          // 0 without q
+    int run;                       // KV heads of a workgroup
 };
 
 template <typename T, int DH>
 __global__ __launch_bounds__(kThreads) void paged_append(AppendParams a) {
     using E = Elem<T>;
-    constexpr int V = E::kVec;
-    constexpr int LPR = DH / 2 / V;                  // threads per row
-    constexpr int ROWS = kThreads / LPR;             // rows at a time
+    constexpr int V = E::kVec, H = DH / 2;
+    constexpr int LPR = H / V;                       // lanes per row
+    constexpr int ROWS = kWave / LPR;                // rows of a wave at a time
+    constexpr int WAVES = kThreads / kWave;
+    // cosines and sines of the page's rows, [page_size][H + 4] each (padded, so
+    // that the rows of a wave start in different banks)
+    extern __shared__ __attribute__((aligned(16))) float trig[];
+    constexpr int TST = H + 4;
     const int page = 1 << a.v.page_shift;
     const int any_rows = a.v.n_rows;
     long long first, total;
@@ -93,68 +103,17 @@ __global__ __launch_bounds__(kThreads) void paged_append(AppendParams a) {
     // page rows [from, to) are new, [0, from) older
     const int from = max(s.ctx - p0, 0), to = min(s.ctx + s.rows - p0, page);
     const int row0 = s.r0 + p0 - s.ctx;              // the call's row of page row 0
-    const int c = threadIdx.x % LPR, rt = threadIdx.x / LPR;
-
-    float cs[V], sn[V];
-    auto angle = [&](int r) {
-        const int pos = a.positions ? a.positions[r] : s.ctx + (r - s.r0);
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-            const double t = (double)pos * a.turns[c * V + e];
-            sincospif(2.f * (float)(t - rint(t)), &sn[e], &cs[e]);
-        }
-    };
-    auto rotate = [&](const T *src, u32x4 &lo, u32x4 &hi, float (&fl)[V], float (&fh)[V]) {
-        float x[V], y[V];
-        E::unpack(*reinterpret_cast<const u32x4 *>(src + c * V), x);
-        E::unpack(*reinterpret_cast<const u32x4 *>(src + DH / 2 + c * V), y);
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-            fl[e] = x[e] * cs[e] - y[e] * sn[e];
-            fh[e] = y[e] * cs[e] + x[e] * sn[e];
-        }
-        lo = E::pack(fl);
-        hi = E::pack(fh);
-    };
-
-    if ((int)blockIdx.y >= a.v.n_kv_heads) {
-        // ---- the query heads of a group ----
-        const int h0 = ((int)blockIdx.y - a.v.n_kv_heads) * a.group;
-        for (int base = from; base < to; base += ROWS) {
-            const int nr = min(to - base, ROWS);
-            int have = -1;
-            for (int p = rt; p < nr * a.group; p += ROWS) {
-                const int r = row0 + base + p % nr, h = h0 + p / nr;
-                if (r != have)
-                    angle(r);
-                have = r;
-                u32x4 lo, hi;
-                float fl[V], fh[V];
-                rotate(static_cast<const T *>(a.q_in) + r * a.q_stride + (size_t)h * DH, lo, hi,
-                       fl, fh);
-                T *dst = static_cast<T *>(a.q_out) + ((size_t)r * a.n_q_heads + h) * DH;
-                *reinterpret_cast<u32x4 *>(dst + c * V) = lo;
-                *reinterpret_cast<u32x4 *>(dst + DH / 2 + c * V) = hi;
-            }
-        }
-        return;
-    }
-
-    // ---- one KV head ----
     const int id = paged_page(a.v, b, lp);
-    if (id < 0)
-        return;
-    const int g = blockIdx.y;
-    const size_t head = (size_t)id * a.v.n_kv_heads + g;
-    T *kp = static_cast<T *>(a.k) + (head << a.v.page_shift) * DH;
-    T *vp = static_cast<T *>(a.vc) + (head << a.v.page_shift) * DH;
+    const int wave = wave_id(), lane = threadIdx.x % kWave;
+    const int c = lane % LPR, rt = lane / LPR;
+    const int g0 = blockIdx.y * a.run, n_kv = min(a.run, a.v.n_kv_heads - g0);
+    const int n_heads = n_kv * (1 + a.group);        // KV heads, then query heads
+
+    float *cs = trig, *sn = trig + page * TST;
+
+    // smallest and largest of what the lane has seen of a head's keys
     float mn[2 * V], mx[2 * V];
-#pragma unroll
-    for (int e = 0; e < 2 * V; ++e) {
-        mn[e] = INFINITY;
-        mx[e] = -INFINITY;
-    }
-    auto count = [&](u32x4 lo, u32x4 hi) {
+    auto count = [&](const u32x4 &lo, const u32x4 &hi) {
         float x[V], y[V];
         E::unpack(lo, x);
         E::unpack(hi, y);
@@ -166,61 +125,117 @@ __global__ __launch_bounds__(kThreads) void paged_append(AppendParams a) {
             mx[V + e] = nan_max(mx[V + e], y[e]);
         }
     };
-    for (int r = from + rt; r < to; r += ROWS) {
-        const size_t src = (size_t)(row0 + r) * a.kv_stride + (size_t)g * DH;
-        const T *vs = static_cast<const T *>(a.v_in) + src;
-        const u32x4 v0 = *reinterpret_cast<const u32x4 *>(vs + c * V);
-        const u32x4 v1 = *reinterpret_cast<const u32x4 *>(vs + DH / 2 + c * V);
-        angle(row0 + r);
-        u32x4 lo, hi;
-        float fl[V], fh[V];
-        rotate(static_cast<const T *>(a.k_in) + src, lo, hi, fl, fh);
-        T *kd = kp + (size_t)r * DH, *vd = vp + (size_t)r * DH;
-        *reinterpret_cast<u32x4 *>(kd + c * V) = lo;
-        *reinterpret_cast<u32x4 *>(kd + DH / 2 + c * V) = hi;
-        *reinterpret_cast<u32x4 *>(vd + c * V) = v0;
-        *reinterpret_cast<u32x4 *>(vd + DH / 2 + c * V) = v1;
-        if (a.bounds)
-            count(lo, hi);
-    }
-    if (!a.bounds)
-        return;
-    for (int r = rt; r < from; r += ROWS) {
-        const T *kd = kp + (size_t)r * DH;
-        count(*reinterpret_cast<const u32x4 *>(kd + c * V),
-              *reinterpret_cast<const u32x4 *>(kd + DH / 2 + c * V));
-    }
-    // over the rows of a wave, then over the waves
-#pragma unroll
-    for (int off = LPR; off < kWave; off <<= 1)
+    // the older rows of KV head h
+    auto older = [&](int h) {
 #pragma unroll
         for (int e = 0; e < 2 * V; ++e) {
-            mn[e] = nan_min(mn[e], __shfl_xor(mn[e], off, kWave));
-            mx[e] = nan_max(mx[e], __shfl_xor(mx[e], off, kWave));
+            mn[e] = INFINITY;
+            mx[e] = -INFINITY;
         }
-    constexpr int WAVES = kThreads / kWave;
-    __shared__ float red[WAVES][2][DH];
-    if (threadIdx.x % kWave < LPR) {
-        const int w = threadIdx.x / kWave;
+        const T *kp = static_cast<const T *>(a.k) +
+                      (((size_t)id * a.v.n_kv_heads + h) << a.v.page_shift) * DH;
+        constexpr int U = 4;                         // rows of a lane in flight
+        for (int r0 = rt; r0 < from; r0 += U * ROWS) {
+            u32x4 w[U][2];
 #pragma unroll
-        for (int e = 0; e < 2 * V; ++e) {
-            const int d = (e < V ? 0 : DH / 2) + c * V + e % V;
-            red[w][0][d] = mn[e];
-            red[w][1][d] = mx[e];
+            for (int u = 0; u < U; ++u) {
+                // (past the last row: that one again)
+                const T *src = kp + (size_t)min(r0 + u * ROWS, from - 1) * DH;
+                w[u][0] = *reinterpret_cast<const u32x4 *>(src + c * V);
+                w[u][1] = *reinterpret_cast<const u32x4 *>(src + H + c * V);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                count(w[u][0], w[u][1]);
         }
+    };
+    const bool bounds = a.bounds && id >= 0;
+    if (bounds && wave < n_kv)
+        older(g0 + wave);
+
+    for (int at = threadIdx.x; at < (to - from) * H; at += kThreads) {
+        const int r = at / H, i = at % H;
+        const int pos = a.positions ? a.positions[row0 + from + r] : p0 + from + r;
+        const double x = (double)pos * a.turns[i];
+        sincospif(2.f * (float)(x - rint(x)), &sn[r * TST + i], &cs[r * TST + i]);
     }
     __syncthreads();
-    if (threadIdx.x < 2 * DH) {
-        const int which = threadIdx.x / DH, d = threadIdx.x % DH;
-        float x = red[0][which][d];
+    for (int head = wave; head < n_heads; head += WAVES) {
+        const bool is_q = head >= n_kv;
+        if (!is_q && id < 0)
+            continue;
+        const int h = is_q ? g0 * a.group + head - n_kv : g0 + head;
+        const size_t unit = (size_t)max(id, 0) * a.v.n_kv_heads + h;
+        const size_t head_row = unit << a.v.page_shift;
+        if (!is_q && bounds && head != wave)
+            older(h);
+        for (int r = from + rt; r < to; r += ROWS) {
+            const size_t in_row = row0 + r;
+            const T *src = is_q ? static_cast<const T *>(a.q_in) + in_row * a.q_stride +
+                                      (size_t)h * DH
+                                : static_cast<const T *>(a.k_in) + in_row * a.kv_stride +
+                                      (size_t)h * DH;
+            T *dst = is_q ? static_cast<T *>(a.q_out) + (in_row * a.n_q_heads + h) * DH
+                          : static_cast<T *>(a.k) + (head_row + r) * DH;
+            float x[V], y[V], lo[V], hi[V];
+            E::unpack(*reinterpret_cast<const u32x4 *>(src + c * V), x);
+            E::unpack(*reinterpret_cast<const u32x4 *>(src + H + c * V), y);
+            if (!is_q) {
+                const T *vs = static_cast<const T *>(a.v_in) + in_row * a.kv_stride +
+                              (size_t)h * DH;
+                T *vd = static_cast<T *>(a.vc) + (head_row + r) * DH;
+                const u32x4 v0 = *reinterpret_cast<const u32x4 *>(vs + c * V);
+                const u32x4 v1 = *reinterpret_cast<const u32x4 *>(vs + H + c * V);
+                *reinterpret_cast<u32x4 *>(vd + c * V) = v0;
+                *reinterpret_cast<u32x4 *>(vd + H + c * V) = v1;
+            }
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w)
-            x = which ? nan_max(x, red[w][1][d]) : nan_min(x, red[w][0][d]);
-        T *dst = static_cast<T *>(a.bounds) + (head * 2 + which) * DH + d;
-        if constexpr (sizeof(T) == 2)
-            *dst = f32_to_bf16(x);                   // exact: x is a stored value
-        else
-            *dst = x;
+            for (int e = 0; e < V; e += 4) {
+                const int at = (r - from) * TST + c * V + e;
+                const f32x4 co = *reinterpret_cast<const f32x4 *>(cs + at);
+                const f32x4 si = *reinterpret_cast<const f32x4 *>(sn + at);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    lo[e + i] = x[e + i] * co[i] - y[e + i] * si[i];
+                    hi[e + i] = y[e + i] * co[i] + x[e + i] * si[i];
+                }
+            }
+            const u32x4 wlo = E::pack(lo), whi = E::pack(hi);
+            *reinterpret_cast<u32x4 *>(dst + c * V) = wlo;
+            *reinterpret_cast<u32x4 *>(dst + H + c * V) = whi;
+            if (!is_q && bounds)
+                count(wlo, whi);                     // as stored
+        }
+        if (is_q || !bounds)
+            continue;
+        // Over the wave's ROWS rows: first the upper half of the lanes hands its
+        // minima to the lower one for that one's maxima.
+        float keep[2 * V];
+        const bool up = lane & 32;
+#pragma unroll
+        for (int e = 0; e < 2 * V; ++e) {
+            const float other = __shfl_xor(up ? mn[e] : mx[e], 32, kWave);
+            keep[e] = up ? nan_max(mx[e], other) : nan_min(mn[e], other);
+        }
+#pragma unroll
+        for (int off = LPR; off < 32; off <<= 1)
+#pragma unroll
+            for (int e = 0; e < 2 * V; ++e) {
+                const float other = __shfl_xor(keep[e], off, kWave);
+                keep[e] = up ? nan_max(keep[e], other) : nan_min(keep[e], other);
+            }
+        if ((lane & 31) < LPR) {
+            T *dst = static_cast<T *>(a.bounds) + (unit * 2 + (up ? 1 : 0)) * DH;
+            float x[V], y[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                x[e] = keep[e];
+                y[e] = keep[V + e];
+            }
+            // (exact: they are stored values)
+            *reinterpret_cast<u32x4 *>(dst + c * V) = E::pack(x);
+            *reinterpret_cast<u32x4 *>(dst + H + c * V) = E::pack(y);
+        }
     }
 }
 
@@ -554,17 +569,20 @@ wf_status_t launch_paged_append(wf_dtype_t dt, const wf_paged_cache_t &c,
     // more than they fill
     const int pages = (int)std::min<long long>(
         n_rows, n_rows / c.page_size + 2ll * std::min(b.n_seqs, n_rows));
-    const dim3 grid(pages, c.n_kv_heads * (q ? 2 : 1));
+    // as many workgroups as fill the chip four times over, no more than heads
+    a.run = std::max(1, c.n_kv_heads / std::max(1, 1024 / pages));
+    const dim3 grid(pages, (c.n_kv_heads + a.run - 1) / a.run);
     const dim3 block(kThreads);
+    const size_t lds = (size_t)2 * c.page_size * (c.head_dim / 2 + 4) * sizeof(float);
     if (dt == WF_BF16) {
         if (c.head_dim == 128)
-            hipLaunchKernelGGL((paged_append<uint16_t, 128>), grid, block, 0, stream, a);
+            hipLaunchKernelGGL((paged_append<uint16_t, 128>), grid, block, lds, stream, a);
         else
-            hipLaunchKernelGGL((paged_append<uint16_t, 64>), grid, block, 0, stream, a);
+            hipLaunchKernelGGL((paged_append<uint16_t, 64>), grid, block, lds, stream, a);
     } else if (c.head_dim == 128)
-        hipLaunchKernelGGL((paged_append<float, 128>), grid, block, 0, stream, a);
+        hipLaunchKernelGGL((paged_append<float, 128>), grid, block, lds, stream, a);
     else
-        hipLaunchKernelGGL((paged_append<float, 64>), grid, block, 0, stream, a);
+        hipLaunchKernelGGL((paged_append<float, 64>), grid, block, lds, stream, a);
     return hipGetLastError() == hipSuccess ? WF_OK : WF_ERR_HIP;
 }
 

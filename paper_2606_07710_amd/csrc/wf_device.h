@@ -5,6 +5,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 namespace wf {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -152,6 +154,33 @@ __device__ __forceinline__ RowState wave_merge(RowState s) {
 
 __device__ __forceinline__ float state_entropy(RowState s) {
     return log1pf(s.sp) - s.t / (1.f + s.sp);
+}
+
+// A lane's value from another lane without LDS (data-parallel primitives): CTRL
+// names the move, ROWS the rows of 16 lanes that receive; the rest, and lanes
+// whose source lies outside the row, get `identity`.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp(int identity, int x) {
+    return __builtin_amdgcn_update_dpp(identity, x, CTRL, ROWS, 0xf, false);
+}
+constexpr int kRowShr1 = 0x111, kRowShr2 = 0x112, kRowShr4 = 0x114, kRowShr8 = 0x118;
+constexpr int kRowBcast15 = 0x142, kRowBcast31 = 0x143;   // a row's last lane to the rows behind
+
+// Sum of a value over the lanes up to and with the own one.
+__device__ __forceinline__ long long wave_scan_add(long long x) {
+    auto step = [&](auto ctrl, auto rows) {
+        constexpr int C = decltype(ctrl)::value, R = decltype(rows)::value;
+        const int lo = dpp<C, R>(0, (int)(unsigned)x), hi = dpp<C, R>(0, (int)(x >> 32));
+        x += (long long)(((unsigned long long)(unsigned)hi << 32) | (unsigned)lo);
+    };
+    using std::integral_constant;
+    step(integral_constant<int, kRowShr1>{}, integral_constant<int, 0xf>{});
+    step(integral_constant<int, kRowShr2>{}, integral_constant<int, 0xf>{});
+    step(integral_constant<int, kRowShr4>{}, integral_constant<int, 0xf>{});
+    step(integral_constant<int, kRowShr8>{}, integral_constant<int, 0xf>{});
+    step(integral_constant<int, kRowBcast15>{}, integral_constant<int, 0xa>{});
+    step(integral_constant<int, kRowBcast31>{}, integral_constant<int, 0xc>{});
+    return x;
 }
 
 // Index of the calling wave in its workgroup, as a wave-uniform (scalar)

@@ -68,12 +68,7 @@ __device__ __forceinline__ int paged_find(int n_seqs, long long at, F &&count, l
         if (b0 + i < n_seqs)
             mine += count(b0 + i);
     const int lane = threadIdx.x % kWave;
-    long long incl = mine;
-#pragma unroll
-    for (int off = 1; off < kWave; off <<= 1) {
-        const long long o = __shfl_up(incl, off, kWave);
-        incl += lane >= off ? o : 0;
-    }
+    const long long incl = wave_scan_add(mine);
     if (threadIdx.x == 0)
         found = -1;
     if (lane == kWave - 1)
