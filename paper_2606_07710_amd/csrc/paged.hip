@@ -88,7 +88,7 @@ __global__ __launch_bounds__(kThreads) void paged_append(AppendParams a) {
     const int any_rows = a.v.n_rows;
     long long first, total;
     const int b = paged_find<kThreads>(
-        a.v.n_seqs, blockIdx.x,
+        a.v.n_seqs, [](long long) { return (long long)blockIdx.x; },
         [&](int s) {
             const Seq q = paged_seq(a.v, s, any_rows);
             return q.rows ? ((q.ctx + q.rows - 1) >> a.v.page_shift) - (q.ctx >> a.v.page_shift) + 1
@@ -290,7 +290,7 @@ __global__ __launch_bounds__(kThreads) void paged_scores(SelectParams a) {
     const int g = blockIdx.x % a.v.n_kv_heads;
     long long first, total;
     const int b = paged_find<kThreads>(
-        a.v.n_seqs, blockIdx.x / a.v.n_kv_heads,
+        a.v.n_seqs, [&](long long) { return (long long)(blockIdx.x / a.v.n_kv_heads); },
         [&](int i) { return (paged_seq(a.v, i, a.v.max_rows).rows + a.pack - 1) / a.pack; }, &first,
         &total);
     if (b < 0)

@@ -60,55 +60,59 @@ __device__ __forceinline__ long long dense_units(const PagedAttnParams &a, const
     return (long long)a.v.n_kv_heads * groups * chunks;
 }
 
-// The run of workgroup w of W that share `total` units, and the workgroup that
-// has unit u.
-__device__ __forceinline__ long long run_begin(long long total, int W, int w) {
-    const long long q = total / W, r = total % W;
-    return q * w + min((long long)w, r);
-}
-__device__ __forceinline__ int run_owner(long long total, int W, long long u) {
-    const long long q = total / W, r = total % W;
-    return (int)(u < r * (q + 1) ? u / (q + 1) : r + (u - r * (q + 1)) / q);
-}
+// Runs of `total` units for W workgroups: the first `more` of them have len + 1.
+// (Units count in 32 bits: 2^31 chunks are more than a day's work of 2^47 bytes;
+// a batch with more of them is not run at all.)
+struct Runs {
+    int len, more;
+    __device__ __forceinline__ Runs(int total, int W) : len(total / W) { more = total - len * W; }
+    __device__ __forceinline__ int begin(int w) const { return len * w + min(w, more); }
+    __device__ __forceinline__ int owner(int u) const {
+        const int split = more * (len + 1);
+        return u < split ? u / (len + 1) : more + (u - split) / len;
+    }
+};
 
 // ---------------------------------------------------------------------------
 // Pages of a key list: 64 of them at a time in the lanes of a wave.
-template <bool SPARSE>
+// ROW_BYTES: of a key.
+template <bool SPARSE, int ROW_BYTES>
 struct Pages {
-    int phys, lpos;                // of list page base + lane; phys -1: none
+    // of list page base + lane: where its KV head's keys start in the pool, in
+    // bytes (hi < 0: no such page), and the position of its first key
+    int lo, hi, pos;
     int base;
 
     __device__ __forceinline__ void load(const PagedAttnParams &a, const Item &it, int at) {
         base = at;
         const int i = at + (int)(threadIdx.x % kWave);
+        int p = i;
         if constexpr (SPARSE) {
-            const int newest = (it.n_keys - 1) >> a.v.page_shift;
-            int p = -1;
-            if (i < a.n_sel)
-                p = a.sel[((size_t)it.r0 * a.v.n_kv_heads + it.g) * a.n_sel + i];
-            const bool ok = p >= 0 && p <= newest;
-            phys = ok ? paged_page(a.v, it.b, p) : -1;
-            lpos = p << a.v.page_shift;
-        } else {
-            const bool ok = (i << a.v.page_shift) < it.n_keys;
-            phys = ok ? paged_page(a.v, it.b, i) : -1;
-            lpos = i << a.v.page_shift;
+            p = i < a.n_sel
+                    ? a.sel[((size_t)it.r0 * a.v.n_kv_heads + it.g) * a.n_sel + i] : -1;
+            if (p > (it.n_keys - 1) >> a.v.page_shift)
+                p = -1;
+        } else if (i > (it.n_keys - 1) >> a.v.page_shift) {
+            p = -1;
         }
+        const int id = p >= 0 ? paged_page(a.v, it.b, p) : -1;
+        const size_t off = (((size_t)max(id, 0) * a.v.n_kv_heads + it.g) << a.v.page_shift) *
+                           ROW_BYTES;
+        lo = (int)(unsigned)off;
+        hi = id < 0 ? -1 : (int)(off >> 32);
+        pos = p << a.v.page_shift;
     }
-    // whether list key k's page is among the 64 (k wave-uniform)
-    __device__ __forceinline__ bool has(const PagedAttnParams &a, int k) const {
-        return (k >> a.v.page_shift) < base + kWave;
-    }
-    // 16 keys from list key k on (k % 16 == 0): their position, how many of them
-    // there are, and their row in the pool's [page][head][row] order
-    __device__ __forceinline__ void find(const PagedAttnParams &a, const Item &it, int k, int &pos,
-                                         int &n, size_t &row) const {
+    // 16 keys from list key k on (k % 16 == 0, wave-uniform, its page among the
+    // 64): their position, how many of them there are, where in the pool
+    __device__ __forceinline__ void find(const PagedAttnParams &a, const Item &it, int k, int &at,
+                                         int &n, size_t &off) const {
         const int lane = (k >> a.v.page_shift) - base;
-        const int ph = __builtin_amdgcn_readlane(phys, lane);
-        const int off = k & ((1 << a.v.page_shift) - 1);
-        pos = __builtin_amdgcn_readlane(lpos, lane) + off;
-        n = ph < 0 ? 0 : min(max(it.n_keys - pos, 0), 16);
-        row = (((size_t)max(ph, 0) * a.v.n_kv_heads + it.g) << a.v.page_shift) + off;
+        const int in = k & ((1 << a.v.page_shift) - 1);
+        const int h = __builtin_amdgcn_readlane(hi, lane);
+        at = SPARSE ? __builtin_amdgcn_readlane(pos, lane) + in : k;
+        n = h < 0 ? 0 : min(max(it.n_keys - at, 0), 16);
+        off = (((size_t)(unsigned)h << 32) | (unsigned)__builtin_amdgcn_readlane(lo, lane)) +
+              (unsigned)(in * ROW_BYTES);
     }
 };
 
@@ -121,12 +125,15 @@ struct Rows {
 
     __device__ __forceinline__ void set(const PagedAttnParams &a, const Item &it, int row0) {
         const int m16 = threadIdx.x & 15;
+        // (q < 2^14 and at most 256 heads: (q + 1/2) / heads is at least 2^-9 away
+        // from a whole number, the product off by less than 2^-15)
+        const float per_row = __builtin_amdgcn_rcpf((float)it.heads);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
             // rows past the item's repeat its last one and are not stored
             const int q = min(it.first + row0 + nb * 16 + m16, it.n_q - 1);
-            i[nb] = q / it.heads;
-            h[nb] = it.h0 + q % it.heads;
+            i[nb] = (int)(((float)q + 0.5f) * per_row);
+            h[nb] = it.h0 + q - i[nb] * it.heads;
         }
     }
     __device__ __forceinline__ void load_mask(const PagedAttnParams &a, const Item &it, int seq_i) {
@@ -197,46 +204,51 @@ __device__ __forceinline__ void store_item(const PagedAttnParams &a, const Item 
 // piece of an item in it, and store(item, whole, slot) after it.
 template <bool SPARSE, int ROWS, int THREADS, typename Segment, typename Store>
 __device__ __forceinline__ void walk(const PagedAttnParams &a, Segment &&segment, Store &&store) {
-    const int W = gridDim.x, w = blockIdx.x;
-    long long total, at, end;
+    const int w = blockIdx.x;
     Item it;
-    long long item0 = 0;           // the item's first unit
-    int active = W;                // workgroups that have units
-    // ---- where the run begins ----
+    int item0 = 0;                 // the item's first unit
     int item = 0;                  // dense: item of the sequence; sparse: of all
+    int b = 0, total = 0;
     Seq s{0, 0, 0};
     const int sparse_groups = (a.group + ROWS - 1) / ROWS;
     const int sparse_chunks =
         SPARSE ? (int)((((long long)a.n_sel << a.v.page_shift) + kChunk - 1) / kChunk) : 0;
-    int b = 0;
+    // ---- where the run begins ----
+    auto workgroups = [&](int n) { return min((int)gridDim.x, max(n, 1)); };
     if constexpr (SPARSE) {
-        total = (long long)a.v.n_rows * a.v.n_kv_heads * sparse_groups * sparse_chunks;
+        total = a.v.n_rows * a.v.n_kv_heads * sparse_groups * sparse_chunks;
     } else {
-        // (the run's first unit depends on the total, which the search finds:
-        // the total first, then the sequence)
-        long long first;
-        auto units = [&](int i) { return dense_units<ROWS>(a, paged_seq(a.v, i, a.v.max_rows)); };
-        paged_find<THREADS>(a.v.n_seqs, -1, units, &first, &total);
-        active = (int)min((long long)W, max(total, 1ll));
-        if (w < active && total > 0) {
-            b = paged_find<THREADS>(a.v.n_seqs, run_begin(total, active, w), units, &first, &total);
+        long long first, all;
+        b = paged_find<THREADS>(
+            a.v.n_seqs,
+            [&](long long n) -> long long {
+                if (n > 0x7fffffff)
+                    return n;
+                const int of = workgroups((int)n);
+                return w < of ? Runs((int)n, of).begin(w) : n;
+            },
+            [&](int i) { return dense_units<ROWS>(a, paged_seq(a.v, i, a.v.max_rows)); }, &first,
+            &all);
+        if (b >= 0) {
             s = paged_seq(a.v, b, a.v.max_rows);
-            item0 = first;
+            item0 = (int)first;
+            total = (int)all;
         }
     }
-    active = (int)min((long long)W, max(total, 1ll));
+    const int active = workgroups(total);
+    const Runs runs(total, active);
     int tail_owner = -1;           // last workgroup of the split item that begins here
     Item tail{};
     if (w < active && total > 0) {
-        at = run_begin(total, active, w);
-        end = run_begin(total, active, w + 1);
+        int at = runs.begin(w);
+        const int end = runs.begin(w + 1);
         if constexpr (SPARSE) {
-            item = (int)(at / sparse_chunks);
-            item0 = (long long)item * sparse_chunks;
+            item = at / sparse_chunks;
+            item0 = item * sparse_chunks;
         } else {
             const int chunks = (s.ctx + s.rows + kChunk - 1) / kChunk;
-            item = (int)((at - item0) / chunks);
-            item0 += (long long)item * chunks;
+            item = (at - item0) / chunks;
+            item0 += item * chunks;
         }
         int row_now = -1;
         while (at < end) {
@@ -286,8 +298,8 @@ __device__ __forceinline__ void walk(const PagedAttnParams &a, Segment &&segment
                 it.n_keys = s.ctx + s.rows;
                 it.chunks = (it.n_keys + kChunk - 1) / kChunk;
             }
-            const int chunk0 = (int)(at - item0);
-            const int n = (int)min((long long)(it.chunks - chunk0), end - at);
+            const int chunk0 = at - item0;
+            const int n = min(it.chunks - chunk0, end - at);
             const bool whole = n == it.chunks;
             const bool tail_piece = chunk0 == 0 && !whole;
             if (!SPARSE || it.b >= 0) {
@@ -297,7 +309,7 @@ __device__ __forceinline__ void walk(const PagedAttnParams &a, Segment &&segment
                 store(it, whole, 2 * w + (tail_piece ? 1 : 0));
             }
             if (tail_piece && it.b >= 0) {
-                tail_owner = run_owner(total, active, item0 + it.chunks - 1);
+                tail_owner = runs.owner(item0 + it.chunks - 1);
                 tail = it;
             }
             at += n;
@@ -362,17 +374,21 @@ __global__ __launch_bounds__(64 * KS * RG) void paged_attn_bf16(PagedAttnParams 
     const int stream = wave % KS, rgi = wave / KS;
     const float sl2 = a.sl2;
 
-    // A lane's byte offset within the 16 keys of a wave load, for each of the
-    // LPH loads of K and of V (the swizzles repeat after 16 keys).
-    unsigned koff[LPH], voff[LPH];
-    constexpr int RPL = 1024 / RB;                    // rows per load
-    const int lrow = lane / GRAN;
+    // This wave's loads of a tile: RG waves share the LPH loads that 16 keys of K
+    // (or V) take, or (LPH < RG) a half's go to some waves and the other's to the
+    // others.  A lane's byte offset in the 16 keys, swizzled (the swizzles repeat
+    // after 16 keys):
+    constexpr int NJ = LPH >= RG ? LPH / RG : 1;
+    constexpr int RPL = 1024 / RB;                    // keys per load
+    unsigned koff[NJ], voff[NJ], row_of[NJ];
 #pragma unroll
-    for (int j = 0; j < LPH; ++j) {
-        const int kl = j * RPL + lrow, pg = lane % GRAN;
-        koff[j] = (unsigned)((pg ^ (kl & (GRAN - 1))) * 16);
+    for (int ji = 0; ji < NJ; ++ji) {
+        const int j = LPH >= RG ? rgi + ji * RG : rgi % LPH;
+        const int kl = j * RPL + lane / GRAN, pg = lane % GRAN;
         const int seg = (pg >> 1) ^ (kl & (SEGS - 1));
-        voff[j] = (unsigned)((2 * seg + (pg & 1)) * 16);
+        row_of[ji] = kl;
+        koff[ji] = (unsigned)((pg ^ (kl & (GRAN - 1))) * 16);
+        voff[ji] = (unsigned)((2 * seg + (pg & 1)) * 16);
     }
 
     bf16x8 qf[NB][KC];
@@ -404,7 +420,7 @@ __global__ __launch_bounds__(64 * KS * RG) void paged_attn_bf16(PagedAttnParams 
             for (int md = 0; md < MD; ++md)
                 o[md][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
-        Pages<SPARSE> pages;
+        Pages<SPARSE, RB> pages;
         pages.load(a, it, (k_begin + stream * kTile) >> a.v.page_shift);
 
         // position and number of the keys in the two halves of a stage's tile
@@ -414,41 +430,38 @@ __global__ __launch_bounds__(64 * KS * RG) void paged_attn_bf16(PagedAttnParams 
         Where ring_where[NBUF - 1];
 
         auto issue = [&](int st) __attribute__((always_inline)) -> Where {
-            const int t = KS * st + stream;
-            const int kb = k_begin + t * kTile;
+            const int kb = k_begin + (KS * st + stream) * kTile;
             const unsigned slot = lds_addr(smem) + ((st % NBUF) * KS + stream) * TILE;
+            if ((kb + 16) >> a.v.page_shift >= pages.base + kWave)
+                pages.load(a, it, kb >> a.v.page_shift);
             Where wh;
-            const char *ks[2], *vs[2];
-#pragma unroll
-            for (int hf = 0; hf < 2; ++hf) {
-                wh.pos[hf] = wh.n[hf] = 0;
-                size_t row = 0;
-                const int k = kb + 16 * hf;
-                if (k < k_end) {
-                    if (!pages.has(a, k))
-                        pages.load(a, it, k >> a.v.page_shift);
-                    pages.find(a, it, k, wh.pos[hf], wh.n[hf], row);
-                }
-                const bool some = wh.n[hf] > 0;
-                ks[hf] = some ? static_cast<const char *>(a.k) + row * RB : a.zeros;
-                vs[hf] = some ? static_cast<const char *>(a.vc) + row * RB : a.zeros;
+            size_t off[2];
+            pages.find(a, it, kb, wh.pos[0], wh.n[0], off[0]);
+            if (a.v.page_shift > 4) {                // the same page
+                wh.pos[1] = wh.pos[0] + 16;
+                wh.n[1] = wh.n[0] < 16 ? 0 : min(max(it.n_keys - wh.pos[1], 0), 16);
+                off[1] = off[0] + 16 * RB;
+            } else {
+                pages.find(a, it, kb + 16, wh.pos[1], wh.n[1], off[1]);
             }
+            const bool whole = wh.n[0] + wh.n[1] == 32;
 #pragma unroll
             for (int jr = 0; jr < LPW; ++jr) {
-                const int L = rgi + jr * RG;
-                const bool is_v = L >= NLOAD / 2;
-                const int jj = L % (NLOAD / 2);
-                const int hf = jj / LPH, j = jj % LPH;
-                // keys that are not there repeat the half's last one
-                unsigned off = 0;
-#pragma unroll
-                for (int x = 0; x < LPH; ++x)
-                    if (j == x)
-                        off = (is_v ? voff[x] : koff[x]);
-                const int r = min(j * RPL + lrow, max((hf ? wh.n[1] : wh.n[0]) - 1, 0));
-                const char *ksrc = hf ? ks[1] : ks[0], *vsrc = hf ? vs[1] : vs[0];
-                lds_dma16_so(is_v ? vsrc : ksrc, off + r * RB,
-                             slot + (is_v ? HALF : 0) + jj * 1024);
+                const bool is_v = jr >= LPW / 2;
+                const int hf = LPH >= RG ? jr / NJ % 2 : rgi / LPH;
+                const int ji = LPH >= RG ? jr % NJ : 0;
+                const int j = LPH >= RG ? rgi + ji * RG : rgi % LPH;
+                const char *src = static_cast<const char *>(is_v ? a.vc : a.k) + (hf ? off[1] : off[0]);
+                unsigned row = row_of[ji];
+                if (!whole) {
+                    // keys that are not there repeat the half's last one, or are
+                    // zeros
+                    const int n = hf ? wh.n[1] : wh.n[0];
+                    src = n ? src : a.zeros;
+                    row = min(row, (unsigned)max(n - 1, 0));
+                }
+                lds_dma16_so(src, (is_v ? voff[ji] : koff[ji]) + row * RB,
+                             slot + (is_v ? HALF : 0) + (hf * LPH + j) * 1024);
             }
             return wh;
         };
@@ -474,10 +487,27 @@ __global__ __launch_bounds__(64 * KS * RG) void paged_attn_bf16(PagedAttnParams 
                         s[mb][nb] = mfma16x16x32(kop, qf[nb][kk], s[mb][nb]);
                 }
             }
-            // masks, where a half is short or reaches into the block
+            // V^T, while the scores are formed: two transposing reads per 16 dims
+            typedef short v4i16 __attribute__((ext_vector_type(4)));
+            typedef short v8i16 __attribute__((ext_vector_type(8)));
+            const int q4 = m16 & 3, qk = m16 >> 2;
+            bf16x8 vop[MD];
 #pragma unroll
-            for (int mb = 0; mb < 2; ++mb)
-                if (wh.n[mb] < 16 || wh.pos[mb] + 15 >= it.ctx) {
+            for (int md = 0; md < MD; ++md) {
+                v4i16 half[2];
+#pragma unroll
+                for (int hh = 0; hh < 2; ++hh) {
+                    const int kl = 16 * hh + 4 * c4 + qk;
+                    half[hh] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                        (WF_LDS(v4i16) *)(vt + kl * RB + (md ^ (kl & (SEGS - 1))) * 32 + q4 * 8));
+                }
+                const v8i16 both = __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7);
+                vop[md] = __builtin_bit_cast(bf16x8, both);
+            }
+            // masks, where a half is short or reaches into the block
+            if (wh.n[0] + wh.n[1] < 32 || max(wh.pos[0], wh.pos[1]) + 15 >= it.ctx) {
+#pragma unroll
+                for (int mb = 0; mb < 2; ++mb)
 #pragma unroll
                     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -489,25 +519,26 @@ __global__ __launch_bounds__(64 * KS * RG) void paged_attn_bf16(PagedAttnParams 
                             const bool vis = (4 * c4 + i < wh.n[mb]) & ((j < 0) | seen);
                             s[mb][nb][i] = vis ? s[mb][nb][i] : -INFINITY;
                         }
-                }
-            // The reference maximum of a row moves only when a score outgrows
-            // it by 8 log2 units: weights stay below 2^8, exact either way.
-            bool grow = false;
+            }
+            // The reference maximum of a row moves only when a score outgrows it
+            // by 8 log2 units: weights stay below 2^8, exact either way.  Only
+            // then (and at the first keys) do the row's four lanes compare notes.
             float mx[NB];
+            bool grow = false;
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
-                float m = fmaxf(fmaxf(fmaxf(s[0][nb][0], s[0][nb][1]), fmaxf(s[0][nb][2], s[0][nb][3])),
-                                fmaxf(fmaxf(s[1][nb][0], s[1][nb][1]), fmaxf(s[1][nb][2], s[1][nb][3])));
-                m = fmaxf(m, __shfl_xor(m, 16, kWave));
-                mx[nb] = fmaxf(m, __shfl_xor(m, 32, kWave));
+                mx[nb] = fmaxf(fmaxf(fmaxf(s[0][nb][0], s[0][nb][1]), fmaxf(s[0][nb][2], s[0][nb][3])),
+                               fmaxf(fmaxf(s[1][nb][0], s[1][nb][1]), fmaxf(s[1][nb][2], s[1][nb][3])));
                 grow |= (mx[nb] - mref[nb]) * sl2 > 8.f;
             }
             if (__ballot(grow)) {
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
-                    const bool up = (mx[nb] - mref[nb]) * sl2 > 8.f;
-                    const float alpha = up ? fast_exp2((mref[nb] - mx[nb]) * sl2) : 1.f;
-                    mref[nb] = up ? mx[nb] : mref[nb];
+                    float m = fmaxf(mx[nb], __shfl_xor(mx[nb], 16, kWave));
+                    m = fmaxf(m, __shfl_xor(m, 32, kWave));
+                    const bool up = (m - mref[nb]) * sl2 > 8.f;
+                    const float alpha = up ? fast_exp2((mref[nb] - m) * sl2) : 1.f;
+                    mref[nb] = up ? m : mref[nb];
                     lrow_sum[nb] *= alpha;
 #pragma unroll
                     for (int md = 0; md < MD; ++md)
@@ -534,23 +565,11 @@ __global__ __launch_bounds__(64 * KS * RG) void paged_attn_bf16(PagedAttnParams 
                                   pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7])};
                 pb[nb] = __builtin_bit_cast(bf16x8, pv);
             }
-            typedef short v4i16 __attribute__((ext_vector_type(4)));
-            typedef short v8i16 __attribute__((ext_vector_type(8)));
-            const int q4 = m16 & 3, qk = m16 >> 2;
 #pragma unroll
-            for (int md = 0; md < MD; ++md) {
-                v4i16 half[2];
-#pragma unroll
-                for (int hh = 0; hh < 2; ++hh) {
-                    const int kl = 16 * hh + 4 * c4 + qk;
-                    half[hh] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (WF_LDS(v4i16) *)(vt + kl * RB + (md ^ (kl & (SEGS - 1))) * 32 + q4 * 8));
-                }
-                const v8i16 both = __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7);
+            for (int md = 0; md < MD; ++md)
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb)
-                    o[md][nb] = mfma16x16x32(__builtin_bit_cast(bf16x8, both), pb[nb], o[md][nb]);
-            }
+                    o[md][nb] = mfma16x16x32(vop[md], pb[nb], o[md][nb]);
         };
 
         // q is in before the first copy goes out, so that the compiler waits
@@ -560,7 +579,7 @@ __global__ __launch_bounds__(64 * KS * RG) void paged_attn_bf16(PagedAttnParams 
 #pragma unroll
             for (int kk = 0; kk < KC; ++kk)
                 asm volatile("" : "+v"(qf[nb][kk]));
-        asm volatile("" : "+v"(pages.phys), "+v"(pages.lpos));
+        asm volatile("" : "+v"(pages.lo), "+v"(pages.hi), "+v"(pages.pos));
 #pragma unroll
         for (int i = 0; i < NBUF - 1; ++i)
             if (i < n_steps)
@@ -644,16 +663,17 @@ __global__ __launch_bounds__(256) void paged_attn_f32(PagedAttnParams a) {
             o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
         float mref = -INFINITY, lsum = 0.f;
-        Pages<SPARSE> pages;
+        Pages<SPARSE, DH * 4> pages;
         pages.load(a, it, (k_begin + 16 * stream) >> a.v.page_shift);
         for (int k = k_begin + 16 * stream; k < k_end; k += 16 * KS) {
-            if (!pages.has(a, k))
+            if (k >> a.v.page_shift >= pages.base + kWave)
                 pages.load(a, it, k >> a.v.page_shift);
             int pos, nk;
-            size_t row;
-            pages.find(a, it, k, pos, nk, row);
+            size_t off;
+            pages.find(a, it, k, pos, nk, off);
             if (nk == 0)
                 continue;
+            const size_t row = off / (DH * 4);
             const float *kp = static_cast<const float *>(a.k) + (row + min(m16, nk - 1)) * DH;
             f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -717,10 +737,12 @@ __global__ __launch_bounds__(256) void paged_attn_f32(PagedAttnParams a) {
 }
 
 // ---------------------------------------------------------------------------
-// Joins the partials of the split item that begins in workgroup blockIdx.x: a
-// wave per row, its lanes over the dims, parts in run order.  Bound by the
-// latency of its three trips to memory (with one part's row in flight instead
-// of eight it took 12 us for 32 parts, longer than the attention).
+// Joins the partials of the split item that begins in workgroup blockIdx.x, in
+// run order: 16 lanes to a row, a sixteenth of its dims each, 16 rows to a
+// workgroup.  Bound by the latency of its three trips to memory (with one part's
+// row in flight instead of eight it took 12 us for 32 parts, longer than the
+// attention; with a wave to a row, four times the workgroups, 10 us for 128
+// items of 64 rows).
 template <typename T, int DH, int ROWS>
 __global__ __launch_bounds__(256) void paged_attn_join(PagedAttnParams a) {
     const int w0 = blockIdx.x;
@@ -728,71 +750,80 @@ __global__ __launch_bounds__(256) void paged_attn_join(PagedAttnParams a) {
     const int w1 = m[0];
     if (w1 < 0)
         return;
-    const int row = blockIdx.y * 4 + wave_id();
+    const int row = blockIdx.y * 16 + threadIdx.x / 16;
     const int q = m[4] + row;
     if (q >= m[5])
         return;
-    const int lane = threadIdx.x % kWave;
-    constexpr int E = DH / kWave;
+    const int sub = threadIdx.x % 16, lane0 = threadIdx.x % kWave & ~15;
+    constexpr int E = DH / 16;
     const int parts = w1 - w0 + 1;
     auto slot = [&](int p) { return (size_t)(p == 0 ? 2 * w0 + 1 : 2 * (w0 + p)); };
+    auto over16 = [&](float x, auto op) {
+#pragma unroll
+        for (int off = 1; off < 16; off <<= 1)
+            x = op(x, __shfl_xor(x, off, kWave));
+        return x;
+    };
     float mm = -INFINITY;
-    for (int p = lane; p < parts; p += kWave)
+    for (int p = sub; p < parts; p += 16)
         mm = fmaxf(mm, a.part_ml[(slot(p) * ROWS + row) * 2]);
-    mm = wave_max(mm);
+    mm = over16(mm, [](float x, float y) { return fmaxf(x, y); });
     const float muse = mm == -INFINITY ? 0.f : mm;
     float l = 0.f, o[E];
 #pragma unroll
     for (int e = 0; e < E; ++e)
         o[e] = 0.f;
-    for (int p0 = 0; p0 < parts; p0 += kWave) {
+    for (int p0 = 0; p0 < parts; p0 += 16) {
         float f = 0.f, lp = 0.f;
-        if (p0 + lane < parts) {
-            const float *src = a.part_ml + (slot(p0 + lane) * ROWS + row) * 2;
+        if (p0 + sub < parts) {
+            const float *src = a.part_ml + (slot(p0 + sub) * ROWS + row) * 2;
             f = fast_exp2((src[0] - muse) * a.sl2);
             lp = src[1] * f;
         }
-        l += wave_sum(lp);
+        l += over16(lp, [](float x, float y) { return x + y; });
         // eight parts' rows in flight (past the last part: the last again, with
         // factor 0)
-        const int n = min(parts - p0, kWave);
+        const int n = min(parts - p0, 16);
         for (int p = 0; p < n; p += 8) {
-            float x[8][E];
+            f32x4 x[8][E / 4];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float *src =
-                    a.part_o + (slot(min(p0 + p + i, parts - 1)) * ROWS + row) * DH + lane * E;
+                    a.part_o + (slot(min(p0 + p + i, parts - 1)) * ROWS + row) * DH + sub * E;
 #pragma unroll
-                for (int e = 0; e < E; ++e)
-                    x[i][e] = src[e];
+                for (int e = 0; e < E / 4; ++e)
+                    x[i][e] = *reinterpret_cast<const f32x4 *>(src + 4 * e);
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float fp = __uint_as_float(
-                    __builtin_amdgcn_readlane(__float_as_uint(f), min(p + i, kWave - 1)));
+                const float fp = __shfl(f, lane0 + p + i, kWave);
 #pragma unroll
                 for (int e = 0; e < E; ++e)
-                    o[e] = p + i < n ? fmaf(x[i][e], fp, o[e]) : o[e];
+                    o[e] = p + i < n ? fmaf(x[i][e / 4][e % 4], fp, o[e]) : o[e];
             }
         }
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+        o[e] *= inv;
     T *dst = static_cast<T *>(a.out) +
-             ((size_t)(m[1] + q / m[3]) * a.n_q_heads + m[2] + q % m[3]) * DH + lane * E;
+             ((size_t)(m[1] + q / m[3]) * a.n_q_heads + m[2] + q % m[3]) * DH + sub * E;
     if constexpr (sizeof(T) == 4) {
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-            dst[e] = o[e] * inv;
-    } else if constexpr (E == 2) {
-        *reinterpret_cast<uint32_t *>(dst) = pack_bf16x2(o[0] * inv, o[1] * inv);
+        for (int e = 0; e < E; e += 4)
+            *reinterpret_cast<f32x4 *>(dst + e) = f32x4{o[e], o[e + 1], o[e + 2], o[e + 3]};
     } else {
-        dst[0] = f32_to_bf16(o[0] * inv);
+#pragma unroll
+        for (int e = 0; e < E; e += 4)
+            *reinterpret_cast<u32x2 *>(dst + e) =
+                u32x2{pack_bf16x2(o[e], o[e + 1]), pack_bf16x2(o[e + 2], o[e + 3])};
     }
 }
 
 template <typename T, int DH, int ROWS>
 void join(const PagedAttnParams &a, int workgroups, hipStream_t stream) {
-    hipLaunchKernelGGL((paged_attn_join<T, DH, ROWS>), dim3(workgroups, ROWS / 4), dim3(256), 0,
+    hipLaunchKernelGGL((paged_attn_join<T, DH, ROWS>), dim3(workgroups, ROWS / 16), dim3(256), 0,
                        stream, a);
 }
 
@@ -819,8 +850,10 @@ wf_status_t launch(wf_dtype_t dt, const PagedAttnParams &a, const PagedPlan &p,
         launch_bf16<DH, 1, 1, 4, 2, false>(a, W, stream);
     } else if (p.rg == 2) {
         launch_bf16<DH, 1, 2, 2, 2, false>(a, W, stream);
-    } else {
+    } else if (p.nb == 1) {
         launch_bf16<DH, 1, 4, 1, 3, false>(a, W, stream);
+    } else {
+        launch_bf16<DH, 2, 4, 1, 3, false>(a, W, stream);
     }
     return hipGetLastError() == hipSuccess ? WF_OK : WF_ERR_HIP;
 }
@@ -842,7 +875,7 @@ PagedPlan plan_paged(wf_dtype_t dt, int max_rows, int n_q_heads, int n_kv_heads,
         return PagedPlan{1, 1, 4, kWorkgroups};
     if (rows <= 32)
         return PagedPlan{1, 2, 2, 2 * kWorkgroups};
-    return PagedPlan{1, 4, 1, 2 * kWorkgroups};
+    return PagedPlan{rows <= 64 ? 1 : 2, 4, 1, 2 * kWorkgroups};
 }
 
 size_t paged_attn_workspace_bytes(const PagedPlan &p, int head_dim) {

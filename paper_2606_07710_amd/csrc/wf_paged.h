@@ -50,12 +50,12 @@ __device__ __forceinline__ long long uniform64(long long x) {
     return (long long)(((unsigned long long)hi << 32) | lo);
 }
 
-// Where unit `at` of a ragged list lies: sequence b owns count(b) units, in
-// order.  All threads of the workgroup call this with the same `at`; *total
-// receives the number of units, and the result is the owning sequence (-1 if
-// there are fewer units), with *first its first unit.
-template <int THREADS, typename F>
-__device__ __forceinline__ int paged_find(int n_seqs, long long at, F &&count, long long *first,
+// Where unit at(total) of a ragged list lies: sequence b owns count(b) units, in
+// order, `total` of them in all (also *total).  All threads of the workgroup
+// call this alike; the result is the owning sequence (-1 if there is no such
+// unit), with *first its first unit.
+template <int THREADS, typename F, typename At>
+__device__ __forceinline__ int paged_find(int n_seqs, At &&at_of, F &&count, long long *first,
                                           long long *total) {
     constexpr int WAVES = THREADS / kWave;
     __shared__ long long wave_sums[WAVES];
@@ -80,6 +80,7 @@ __device__ __forceinline__ int paged_find(int n_seqs, long long at, F &&count, l
         before += w < (int)(threadIdx.x / kWave) ? wave_sums[w] : 0;
         all += wave_sums[w];
     }
+    const long long at = at_of(uniform64(all));
     long long lo = before + incl - mine;
     if (at >= lo && at < lo + mine) {
         int b = b0;
