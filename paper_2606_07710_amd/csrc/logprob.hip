@@ -68,19 +68,7 @@ __device__ __forceinline__ uint64_t make_key(float x, int idx) {
     return ((uint64_t)value_order(x) << 32) | (uint32_t)~(uint32_t)idx;
 }
 
-// op over the lanes of a wave, in a fixed order; the same result in every lane.
-// The steps move values between lanes without LDS: shifts by 1, 2, 4, 8 within
-// the rows of 16, then the rows' last lanes to the rows behind.
-template <typename Op>
-__device__ __forceinline__ int wave_reduce(int x, int identity, Op &&op) {
-    x = op(x, dpp<kRowShr1, 0xf>(identity, x));
-    x = op(x, dpp<kRowShr2, 0xf>(identity, x));
-    x = op(x, dpp<kRowShr4, 0xf>(identity, x));
-    x = op(x, dpp<kRowShr8, 0xf>(identity, x));
-    x = op(x, dpp<kRowBcast15, 0xa>(identity, x));
-    x = op(x, dpp<kRowBcast31, 0xc>(identity, x));
-    return __builtin_amdgcn_readlane(x, kWave - 1);
-}
+// Over the lanes of a wave.
 __device__ __forceinline__ float lanes_max(float x) {
     return __int_as_float(wave_reduce(__float_as_int(x), __float_as_int(-INFINITY), [](int a, int b) {
         return __float_as_int(fmaxf(__int_as_float(a), __int_as_float(b)));

@@ -87,17 +87,16 @@ __global__ __launch_bounds__(kThreads) void paged_append(AppendParams a) {
     const int page = 1 << a.v.page_shift;
     const int any_rows = a.v.n_rows;
     long long first, total;
+    Seq s;
     const int b = paged_find<kThreads>(
-        a.v.n_seqs, [](long long) { return (long long)blockIdx.x; },
-        [&](int s) {
-            const Seq q = paged_seq(a.v, s, any_rows);
+        a.v, any_rows, [](long long) { return (long long)blockIdx.x; },
+        [&](const Seq &q) {
             return q.rows ? ((q.ctx + q.rows - 1) >> a.v.page_shift) - (q.ctx >> a.v.page_shift) + 1
                           : 0;
         },
-        &first, &total);
+        &first, &total, &s);
     if (b < 0)
         return;
-    const Seq s = paged_seq(a.v, b, any_rows);
     const int lp = (s.ctx >> a.v.page_shift) + (int)(blockIdx.x - first);
     const int p0 = lp << a.v.page_shift;
     // page rows [from, to) are new, [0, from) older
@@ -282,30 +281,47 @@ __device__ __forceinline__ int old_pages(const SelectParams &a, const Seq &s, in
     return max(((s.ctx + row) >> a.v.page_shift) + 1 - a.n_recent, 0);
 }
 
+// The score tiles, [sequence][KV head][pack of rows][16 pages], laid end to end,
+// go out in equal runs to the workgroups, in turn to a run's waves.
 template <typename T, int DH>
 __global__ __launch_bounds__(kThreads) void paged_scores(SelectParams a) {
     using E = Elem<T>;
     constexpr int V = E::kVec, PIECES = DH / 4 / V, WAVES = kThreads / kWave;
     __shared__ double sc[WAVES][16][17];
-    const int g = blockIdx.x % a.v.n_kv_heads;
+    const int n_top = a.n_sel - a.n_recent;
+    // a sequence's tiles of a pack, none where all old pages are selected
+    auto tiles_of = [&](const Seq &q) {
+        const int n_old = q.rows ? old_pages(a, q, q.rows - 1) : 0;
+        return n_old > n_top ? (n_old + 15) / 16 : 0;
+    };
+    auto count = [&](const Seq &q) {
+        return (long long)tiles_of(q) * a.v.n_kv_heads * ((q.rows + a.pack - 1) / a.pack);
+    };
     long long first, total;
-    const int b = paged_find<kThreads>(
-        a.v.n_seqs, [&](long long) { return (long long)(blockIdx.x / a.v.n_kv_heads); },
-        [&](int i) { return (paged_seq(a.v, i, a.v.max_rows).rows + a.pack - 1) / a.pack; }, &first,
-        &total);
-    if (b < 0)
-        return;
-    const Seq s = paged_seq(a.v, b, a.v.max_rows);
-    const int row0 = (int)(blockIdx.x / a.v.n_kv_heads - first) * a.pack;
-    const int rows = min(s.rows - row0, a.pack);
-    const int n_old = old_pages(a, s, row0 + rows - 1);
-    if (n_old <= a.n_sel - a.n_recent)               // all of them are selected
-        return;
+    Seq s;
+    int b = paged_find<kThreads>(
+        a.v, a.v.max_rows, [&](long long n) { return n * blockIdx.x / gridDim.x; }, count, &first,
+        &total, &s);
+    const long long end = total * (blockIdx.x + 1) / gridDim.x;
     const int wave = wave_id(), lane = threadIdx.x % kWave;
+    long long at = total * blockIdx.x / gridDim.x + wave;
+    if (b < 0 || at >= end)
+        return;
     const int m16 = lane & 15, c4 = lane >> 4;
     const int heads = min(a.group, 16);              // of a row in a tile
-    for (int p0 = (blockIdx.y * WAVES + wave) * 16; p0 < n_old; p0 += gridDim.y * WAVES * 16) {
-        const int p = p0 + m16;
+    int tiles = tiles_of(s), packs = (s.rows + a.pack - 1) / a.pack;
+    for (; at < end; at += WAVES) {
+        while (at >= first + (long long)tiles * packs * a.v.n_kv_heads) {
+            first += (long long)tiles * packs * a.v.n_kv_heads;
+            s = paged_seq(a.v, ++b, a.v.max_rows);
+            tiles = tiles_of(s);
+            packs = (s.rows + a.pack - 1) / a.pack;
+        }
+        const int unit = (int)(at - first);          // < 2^31: see the limits
+        const int tile = unit % tiles, pack = unit / tiles % packs, g = unit / tiles / packs;
+        const int row0 = pack * a.pack, rows = min(s.rows - row0, a.pack);
+        const int n_old = old_pages(a, s, row0 + rows - 1);
+        const int p0 = tile * 16, p = p0 + m16;
         const int id = p < n_old ? paged_page(a.v, b, p) : -1;
         u32x4 lo[PIECES], hi[PIECES];
 #pragma unroll
@@ -331,36 +347,39 @@ __global__ __launch_bounds__(kThreads) void paged_scores(SelectParams a) {
             const T *qp = static_cast<const T *>(a.q) +
                           ((size_t)(s.r0 + row0 + (live ? row : 0)) * a.n_q_heads + g * a.group +
                            (live ? h : 0)) * DH + c4 * (DH / 4);
-            f64x4 acc = {0.0, 0.0, 0.0, 0.0};
+            // two sums, so that a step need not wait for the one before it
+            f64x4 up_sum = {0.0, 0.0, 0.0, 0.0}, dn_sum = up_sum;
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) {
                 float q[V], l[V], u[V];
-                E::unpack(*reinterpret_cast<const u32x4 *>(qp + i * V), q);
+                u32x4 w = *reinterpret_cast<const u32x4 *>(qp + i * V);
+                w = live ? w : u32x4{0u, 0u, 0u, 0u};
+                E::unpack(w, q);
                 E::unpack(lo[i], l);
                 E::unpack(hi[i], u);
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    // (not max and min, which would lose a NaN)
-                    const float up = q[e] >= 0.f || q[e] != q[e] ? q[e] : 0.f;
+                    // (a NaN goes with the first: the score is odd either way)
                     const float dn = q[e] < 0.f ? q[e] : 0.f;
-                    acc = __builtin_amdgcn_mfma_f64_16x16x4f64((double)(live ? up : 0.f),
-                                                               (double)u[e], acc, 0, 0, 0);
-                    acc = __builtin_amdgcn_mfma_f64_16x16x4f64((double)(live ? dn : 0.f),
-                                                               (double)l[e], acc, 0, 0, 0);
+                    const float up = q[e] < 0.f ? 0.f : q[e];
+                    up_sum = __builtin_amdgcn_mfma_f64_16x16x4f64((double)up, (double)u[e], up_sum,
+                                                                  0, 0, 0);
+                    dn_sum = __builtin_amdgcn_mfma_f64_16x16x4f64((double)dn, (double)l[e], dn_sum,
+                                                                  0, 0, 0);
                 }
             }
             // lane (m16, c4) has rows 4 i + c4 of column m16
             wave_sync();
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                sc[wave][4 * i + c4][m16] = acc[i];
+                sc[wave][4 * i + c4][m16] = up_sum[i] + dn_sum[i];
             wave_sync();
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int at = lane + kWave * j, r = at / 16;
+                const int to = lane + kWave * j, r = to / 16;
                 if (r < rows)
                     for (int h2 = 0; h2 < min(heads, a.group - h0); ++h2) {
-                        const double x = sc[wave][r * heads + h2][at % 16];
+                        const double x = sc[wave][r * heads + h2][to % 16];
                         odd[j] |= !(fabs(x) < INFINITY);
                         best[j] = x > best[j] ? x : best[j];
                     }
@@ -368,8 +387,8 @@ __global__ __launch_bounds__(kThreads) void paged_scores(SelectParams a) {
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int at = lane + kWave * j, r = at / 16, page = p0 + at % 16;
-            const int its = __shfl(id, at % 16, kWave);
+            const int to = lane + kWave * j, r = to / 16, page = p0 + to % 16;
+            const int its = __shfl(id, to % 16, kWave);
             if (r < rows && page < n_old)
                 a.keys[((size_t)(s.r0 + row0 + r) * a.v.n_kv_heads + g) * a.v.max_pages + page] =
                     its < 0 ? 0ull : score_key(odd[j] ? (double)NAN : best[j]);
@@ -410,6 +429,7 @@ __global__ __launch_bounds__(THREADS) void paged_choose(SelectParams a) {
     __shared__ int hist[256];
     __shared__ int wave_count[2][WAVES];
     __shared__ int digit, above;
+    __shared__ uint64_t same[2][WAVES];
     uint64_t least = 1;                              // all pages with an entry
     int equal_quota = n_old;                         // of the pages at `least`
     const bool in_lds = n_old <= kLdsKeys;
@@ -422,9 +442,34 @@ __global__ __launch_bounds__(THREADS) void paged_choose(SelectParams a) {
         return choose ? keys[i] : n_top > 0 && paged_page(a.v, b, i) >= 0 ? 1ull : 0ull;
     };
     if (choose) {
-        uint64_t prefix = 0;
+        // (the keys' common leading digits need no counting)
+        uint64_t ones = ~0ull, zeros = ~0ull;
+        for (int i = threadIdx.x; i < n_old; i += THREADS) {
+            ones &= key(i);
+            zeros &= ~key(i);
+        }
+        auto all_of = [](uint64_t x) -> uint64_t {
+            auto both = [](int u, int v) { return u & v; };
+            return ((uint64_t)(uint32_t)wave_reduce((int)(x >> 32), -1, both) << 32) |
+                   (uint32_t)wave_reduce((int)(uint32_t)x, -1, both);
+        };
+        ones = all_of(ones);
+        zeros = all_of(zeros);
+        if (lane == 0) {
+            same[0][wave] = ones;
+            same[1][wave] = zeros;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            ones &= same[0][w];
+            zeros &= same[1][w];
+        }
+        const uint64_t differ = uniform64((long long)~(ones | zeros));
+        int shift = differ ? (63 - __builtin_clzll(differ)) / 8 * 8 : 0;
+        uint64_t prefix = shift < 56 ? uniform64((long long)ones) >> (shift + 8) << (shift + 8) : 0;
+        const int top_shift = shift;
         int need = n_top;
-        int shift = 56;
         for (;; shift -= 8) {
             for (int i = threadIdx.x; i < 256; i += THREADS)
                 hist[i] = 0;
@@ -433,7 +478,8 @@ __global__ __launch_bounds__(THREADS) void paged_choose(SelectParams a) {
                 const int i = i0 + lane;
                 const uint64_t k = i < n_old ? key(i) : 0ull;
                 const bool in = i < n_old &&
-                                (shift == 56 || (k >> (shift + 8)) == (prefix >> (shift + 8)));
+                                (shift == top_shift ||
+                                 (k >> (shift + 8)) == (prefix >> (shift + 8)));
                 const int d = (int)(k >> shift) & 255;
                 // many keys share their first digits: those of the wave's first
                 // such key go in as one
@@ -457,12 +503,7 @@ __global__ __launch_bounds__(THREADS) void paged_choose(SelectParams a) {
                     mine[j] = hist[255 - (4 * lane + j)];
                     sum += mine[j];
                 }
-                int incl = sum;
-#pragma unroll
-                for (int off = 1; off < kWave; off <<= 1) {
-                    const int o = __shfl_up(incl, off, kWave);
-                    incl += lane >= off ? o : 0;
-                }
+                const int incl = (int)wave_scan_add(sum);
                 int before = incl - sum;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
@@ -605,12 +646,10 @@ wf_status_t launch_paged_select(wf_dtype_t dt, const void *q, const wf_paged_cac
     a.group = n_q_heads / c.n_kv_heads;
     a.n_q_heads = n_q_heads;
     a.pack = std::min(std::max(16 / a.group, 1), b.max_rows);
-    // (a sequence's last pack may be short; the table may be far wider than the
-    // sequences are long: no more workgroups than fill the chip a few times)
-    const int packs = std::min(n_rows, n_rows / a.pack + std::min(b.n_seqs, n_rows));
-    const int units = packs * c.n_kv_heads;
-    const int chunks = (b.max_pages + 63) / 64;
-    const dim3 grid(units, std::min(chunks, std::max(2048 / units, 1)));
+    // two workgroups a CU share the tiles evenly; there are at most this many
+    const long long tiles = (long long)std::min(n_rows, n_rows / a.pack + b.n_seqs) *
+                            c.n_kv_heads * ((b.max_pages + 15) / 16);
+    const dim3 grid((unsigned)std::min<long long>(512, (tiles + 3) / 4));
     const dim3 block(kThreads);
     if (n_sel > n_recent) {
         if (dt == WF_BF16) {

@@ -219,18 +219,18 @@ __device__ __forceinline__ void walk(const PagedAttnParams &a, Segment &&segment
         total = a.v.n_rows * a.v.n_kv_heads * sparse_groups * sparse_chunks;
     } else {
         long long first, all;
+        Seq q;
         b = paged_find<THREADS>(
-            a.v.n_seqs,
+            a.v, a.v.max_rows,
             [&](long long n) -> long long {
                 if (n > 0x7fffffff)
                     return n;
                 const int of = workgroups((int)n);
                 return w < of ? Runs((int)n, of).begin(w) : n;
             },
-            [&](int i) { return dense_units<ROWS>(a, paged_seq(a.v, i, a.v.max_rows)); }, &first,
-            &all);
+            [&](const Seq &o) { return dense_units<ROWS>(a, o); }, &first, &all, &q);
         if (b >= 0) {
-            s = paged_seq(a.v, b, a.v.max_rows);
+            s = q;
             item0 = (int)first;
             total = (int)all;
         }

@@ -166,6 +166,20 @@ __device__ __forceinline__ int dpp(int identity, int x) {
 constexpr int kRowShr1 = 0x111, kRowShr2 = 0x112, kRowShr4 = 0x114, kRowShr8 = 0x118;
 constexpr int kRowBcast15 = 0x142, kRowBcast31 = 0x143;   // a row's last lane to the rows behind
 
+// op over the lanes of a wave, in a fixed order; the same result in every lane.
+// The steps move values between lanes without LDS: shifts by 1, 2, 4, 8 within
+// the rows of 16, then the rows' last lanes to the rows behind.
+template <typename Op>
+__device__ __forceinline__ int wave_reduce(int x, int identity, Op &&op) {
+    x = op(x, dpp<kRowShr1, 0xf>(identity, x));
+    x = op(x, dpp<kRowShr2, 0xf>(identity, x));
+    x = op(x, dpp<kRowShr4, 0xf>(identity, x));
+    x = op(x, dpp<kRowShr8, 0xf>(identity, x));
+    x = op(x, dpp<kRowBcast15, 0xa>(identity, x));
+    x = op(x, dpp<kRowBcast31, 0xc>(identity, x));
+    return __builtin_amdgcn_readlane(x, kWave - 1);
+}
+
 // Sum of a value over the lanes up to and with the own one.
 __device__ __forceinline__ long long wave_scan_add(long long x) {
     auto step = [&](auto ctrl, auto rows) {

@@ -50,23 +50,27 @@ __device__ __forceinline__ long long uniform64(long long x) {
     return (long long)(((unsigned long long)hi << 32) | lo);
 }
 
-// Where unit at(total) of a ragged list lies: sequence b owns count(b) units, in
-// order, `total` of them in all (also *total).  All threads of the workgroup
-// call this alike; the result is the owning sequence (-1 if there is no such
-// unit), with *first its first unit.
+// Where unit at(total) of a ragged list lies: sequence b owns count(its Seq)
+// units, in order, `total` of them in all (also *total).  All threads of the
+// workgroup call this alike, once in a kernel; the result is the owning sequence
+// (-1 if there is no such unit), with *first its first unit and *seq its rows.
 template <int THREADS, typename F, typename At>
-__device__ __forceinline__ int paged_find(int n_seqs, At &&at_of, F &&count, long long *first,
-                                          long long *total) {
+__device__ __forceinline__ int paged_find(const PagedView &a, int max_rows, At &&at_of, F &&count,
+                                          long long *first, long long *total, Seq *seq) {
     constexpr int WAVES = THREADS / kWave;
     __shared__ long long wave_sums[WAVES];
     __shared__ long long found_first;
     __shared__ int found;
-    const int per = (n_seqs + THREADS - 1) / THREADS;
+    __shared__ Seq found_seq;
+    const int per = (a.n_seqs + THREADS - 1) / THREADS;
     const int b0 = threadIdx.x * per;
     long long mine = 0;
+    Seq s{0, 0, 0};
     for (int i = 0; i < per; ++i)
-        if (b0 + i < n_seqs)
-            mine += count(b0 + i);
+        if (b0 + i < a.n_seqs) {
+            s = paged_seq(a, b0 + i, max_rows);
+            mine += count(s);
+        }
     const int lane = threadIdx.x % kWave;
     const long long incl = wave_scan_add(mine);
     if (threadIdx.x == 0)
@@ -84,19 +88,23 @@ __device__ __forceinline__ int paged_find(int n_seqs, At &&at_of, F &&count, lon
     long long lo = before + incl - mine;
     if (at >= lo && at < lo + mine) {
         int b = b0;
-        for (long long n = count(b); at >= lo + n; n = count(b)) {
-            lo += n;
-            ++b;
-        }
+        if (per > 1)
+            for (;; ++b) {
+                s = paged_seq(a, b, max_rows);
+                const long long n = count(s);
+                if (at < lo + n)
+                    break;
+                lo += n;
+            }
         found = b;
         found_first = lo;
+        found_seq = s;
     }
     __syncthreads();
     *first = uniform64(found_first);
     *total = uniform64(all);
-    const int b = uniform(found);
-    __syncthreads();
-    return b;
+    *seq = Seq{uniform(found_seq.r0), uniform(found_seq.rows), uniform(found_seq.ctx)};
+    return uniform(found);
 }
 
 }  // namespace wf
