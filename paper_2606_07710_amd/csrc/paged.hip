@@ -133,7 +133,7 @@ __global__ __launch_bounds__(kThreads) void paged_append(AppendParams a) {
         }
         const T *kp = static_cast<const T *>(a.k) +
                       (((size_t)id * a.v.n_kv_heads + h) << a.v.page_shift) * DH;
-        constexpr int U = 4;                         // rows of a lane in flight
+        constexpr int U = 8;                         // rows of a lane in flight
         for (int r0 = rt; r0 < from; r0 += U * ROWS) {
             u32x4 w[U][2];
 #pragma unroll
@@ -159,7 +159,10 @@ __global__ __launch_bounds__(kThreads) void paged_append(AppendParams a) {
         sincospif(2.f * (float)(x - rint(x)), &sn[r * TST + i], &cs[r * TST + i]);
     }
     __syncthreads();
-    for (int head = wave; head < n_heads; head += WAVES) {
+    // (a single KV head, with its older rows, is work enough for the first wave)
+    const bool apart = n_kv == 1 && a.group > 0;
+    for (int head = wave; head < (apart && wave == 0 ? 1 : n_heads);
+         head += apart ? WAVES - 1 : WAVES) {
         const bool is_q = head >= n_kv;
         if (!is_q && id < 0)
             continue;
@@ -207,22 +210,32 @@ __global__ __launch_bounds__(kThreads) void paged_append(AppendParams a) {
         }
         if (is_q || !bounds)
             continue;
-        // Over the wave's ROWS rows: first the upper half of the lanes hands its
-        // minima to the lower one for that one's maxima.
+        // over the wave's ROWS rows
         float keep[2 * V];
         const bool up = lane & 32;
+        auto pick = [&](float x, float y) { return up ? nan_max(x, y) : nan_min(x, y); };
+        typedef unsigned u32pair __attribute__((ext_vector_type(2)));
 #pragma unroll
         for (int e = 0; e < 2 * V; ++e) {
-            const float other = __shfl_xor(up ? mn[e] : mx[e], 32, kWave);
-            keep[e] = up ? nan_max(mx[e], other) : nan_min(mn[e], other);
+            // the halves' minima side by side in the lower lanes, their maxima in
+            // the upper ones
+            u32pair w = __builtin_bit_cast(
+                u32pair, __builtin_amdgcn_permlane32_swap(__float_as_uint(mn[e]),
+                                                          __float_as_uint(mx[e]), false, false));
+            keep[e] = pick(__uint_as_float(w[0]), __uint_as_float(w[1]));
+            // rows of 16 lanes: each with its neighbour
+            w = __builtin_bit_cast(
+                u32pair, __builtin_amdgcn_permlane16_swap(__float_as_uint(keep[e]),
+                                                          __float_as_uint(keep[e]), false, false));
+            keep[e] = pick(__uint_as_float(w[0]), __uint_as_float(w[1]));
+            if constexpr (LPR <= 8)
+                keep[e] = pick(keep[e], __int_as_float(dpp<kRowRor8, 0xf>(
+                                            0, __float_as_int(keep[e]))));
+            if constexpr (LPR <= 4)
+                keep[e] = pick(keep[e], __int_as_float(dpp<kRowRor4, 0xf>(
+                                            0, __float_as_int(keep[e]))));
         }
-#pragma unroll
-        for (int off = LPR; off < 32; off <<= 1)
-#pragma unroll
-            for (int e = 0; e < 2 * V; ++e) {
-                const float other = __shfl_xor(keep[e], off, kWave);
-                keep[e] = up ? nan_max(keep[e], other) : nan_min(keep[e], other);
-            }
+        static_assert(LPR == 4 || LPR == 8 || LPR == 16, "the lanes of a row");
         if ((lane & 31) < LPR) {
             T *dst = static_cast<T *>(a.bounds) + (unit * 2 + (up ? 1 : 0)) * DH;
             float x[V], y[V];
@@ -433,9 +446,21 @@ __global__ __launch_bounds__(THREADS) void paged_choose(SelectParams a) {
     uint64_t least = 1;                              // all pages with an entry
     int equal_quota = n_old;                         // of the pages at `least`
     const bool in_lds = n_old <= kLdsKeys;
-    if (in_lds)
-        for (int i = threadIdx.x; i < n_old; i += THREADS)
-            lds_keys[i] = choose ? keys[i] : n_top > 0 && paged_page(a.v, b, i) >= 0 ? 1ull : 0ull;
+    if (in_lds) {
+        // (all of a thread's loads at once)
+        constexpr int N = kLdsKeys / THREADS;
+        uint64_t got[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const int i = j * THREADS + threadIdx.x;
+            got[j] = i >= n_old ? 0ull
+                     : choose   ? keys[i]
+                                : (n_top > 0 && paged_page(a.v, b, i) >= 0 ? 1ull : 0ull);
+        }
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            lds_keys[j * THREADS + threadIdx.x] = got[j];
+    }
     auto key = [&](int i) -> uint64_t {
         if (in_lds)
             return lds_keys[i];
@@ -662,7 +687,7 @@ wf_status_t launch_paged_select(wf_dtype_t dt, const void *q, const wf_paged_cac
         else
             hipLaunchKernelGGL((paged_scores<float, 64>), grid, block, 0, stream, a);
     }
-    hipLaunchKernelGGL((paged_choose<kThreads>), dim3(n_rows * c.n_kv_heads), block, 0, stream, a);
+    hipLaunchKernelGGL((paged_choose<512>), dim3(n_rows * c.n_kv_heads), dim3(512), 0, stream, a);
     return hipGetLastError() == hipSuccess ? WF_OK : WF_ERR_HIP;
 }
 
