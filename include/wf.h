@@ -848,7 +848,9 @@ wf_status_t wf_paged_append(wf_dtype_t dt, const wf_paged_cache_t *cache,
  * (wf_paged_append); positions behind them are not read.  Values of block
  * rows that a row does not see have to be finite.  A row that sees no key
  * (pages missing) gets zeros.  Limits as for wf_verify_attn; n_rows *
- * n_q_heads <= 2^22.
+ * n_q_heads <= 2^22.  (A batch whose keys, counted once for every KV head and 16
+ * to 128 of its query rows, are 2^38 and more is not run: outputs stay as they
+ * were.)
  * workspace >= wf_paged_verify_attn_workspace_bytes(...) bytes. */
 wf_status_t wf_paged_verify_attn(wf_dtype_t dt, const void *q,
                                  const wf_paged_cache_t *cache,
@@ -895,7 +897,9 @@ size_t wf_paged_select_workspace_bytes(int32_t n_rows, int32_t n_kv_heads,
  * head g restricted to the pages sel[r][g][0 .. n_sel) (logical page numbers
  * in any order, as wf_paged_select writes them; entries that are negative, or
  * past the row's own page, are passed over; a page listed twice counts twice).
- * Limits: 1 <= n_sel <= 1024; the rest as there.
+ * Bits of tree_mask above the row's own are ignored.  Limits: 1 <= n_sel <= 1024;
+ * n_rows * n_kv_heads * n_sel * page_size < 2^38 (for groups of up to 16 query
+ * heads); the rest as there.
  * workspace >= wf_paged_sparse_attn_workspace_bytes(...) bytes. */
 wf_status_t wf_paged_sparse_attn(wf_dtype_t dt, const void *q,
                                  const wf_paged_cache_t *cache,

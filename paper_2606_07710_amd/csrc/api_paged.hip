@@ -1,6 +1,7 @@
 // api_paged.hip -- the extern "C" boundary of the paged cache and of the token
 // log probabilities: argument validation on the host, workspace queries and
 // dispatch.  Nothing is enqueued unless every check passes.
+#include <climits>
 #include <cmath>
 
 #include "wf_api_internal.h"
@@ -174,6 +175,12 @@ wf_status_t wf_paged_sparse_attn(wf_dtype_t dt, const void *q, const wf_paged_ca
                                  int32_t n_q_heads, float softmax_scale, void *workspace,
                                  size_t workspace_bytes, void *stream) {
     if (n_sel < 1 || n_sel > kMaxSelected || !sel || !aligned4(sel))
+        return WF_ERR_INVALID_ARG;
+    // (chunks of 128 listed keys are counted in 32 bits)
+    if (cache && cache->n_kv_heads > 0 && n_rows > 0 &&
+        (long long)n_rows * cache->n_kv_heads *
+                ((n_q_heads / cache->n_kv_heads + 15) / 16) *
+                (((long long)n_sel * cache->page_size + 127) / 128) > INT32_MAX)
         return WF_ERR_INVALID_ARG;
     return attn_common(dt, q, cache, batch, sel, n_sel, out, tree_mask, n_rows, n_q_heads,
                        softmax_scale, workspace, workspace_bytes, stream);

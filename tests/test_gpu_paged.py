@@ -62,6 +62,9 @@ APPENDS = [
     ([(3, 40), (70, 5)], 16, 3, 1, 64, "f32", True, 0),
     ([(2, 100000), (1, 65535)], 64, 8, 1, 128, "f32", False, 0),
     ([(1, i) for i in range(300)], 16, 2, 1, 64, "bf16", False, 0),
+    ([(128, 256), (5, 250), (100, 77)], 128, 8, 4, 128, "bf16", False, 0),
+    ([(2, 33)], 32, 80, 1, 128, "bf16", False, 0),
+    ([(1, 7 * i % 50) if i % 9 == 4 else (0, 3) for i in range(1024)], 16, 2, 2, 64, "f32", False, 0),
 ]
 
 
@@ -150,6 +153,10 @@ ATTN = [
     ([(8, 256)], 16, 8, 2, 64, "f32", False, 0),
     ([(5, 40), (1, 0), (16, 200)], 32, 8, 2, 128, "f32", False, 1),
     ([(30, 100), (7, 15)], 16, 4, 1, 64, "f32", True, 0),
+    ([(1 if i % 3 else 2, i % 40) for i in range(700)], 16, 2, 1, 64, "bf16", False, 0),
+    ([(3, 20) if i in (0, 500, 1023) else (0, i) for i in range(1024)], 32, 8, 2, 128, "bf16", True, 5),
+    ([(40, 700), (1, 3)], 128, 24, 8, 128, "bf16", False, 0),
+    ([(64, 64), (2, 500)], 64, 64, 2, 64, "bf16", False, 0),
 ]
 
 
@@ -477,6 +484,43 @@ def test_results_repeat_and_stay_in_their_buffers():
     assert torch.equal(runs[0], runs[1]) and torch.equal(runs[0], runs[2])
     assert (guard[0] == 5).all() and (guard[-1] == 5).all() and (big[need:] == 0xa5).all()
     assert not big[: 4 << 20].any()
+
+
+def test_two_rounds_at_once_on_two_streams():
+    """Two batches with workspaces of their own, launched side by side."""
+    sets = [setup_round([(4, 900), (16, 300), (1, 130)], seed=71),
+            setup_round([(9, 500), (2, 1000), (16, 44), (1, 2)], seed=72)]
+    alone = []
+    for rnd, io, ws in sets:
+        run_round(rnd, io, ws)
+        torch.cuda.synchronize()
+        alone.append({n: io[n].clone() for n in ("out", "sel", "some")})
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        for (rnd, io, ws), st in zip(sets, streams):
+            run_round(rnd, io, ws, stream=st)
+        torch.cuda.synchronize()
+        for (rnd, io, ws), ref in zip(sets, alone):
+            for n, t in ref.items():
+                assert torch.equal(io[n], t), n
+
+
+def test_select_of_broken_lists_stays_in_range():
+    rnd = R.Round([(2, 640), (3, 900), (1, 320)], 16, 4, 2, 64, seed=73, max_rows=4).on_gpu()
+    for start, ctx in (([0, 4, 2, 6], None), ([0, 2, 5, 9], None), ([0, 2, 5, 6], [640, -3, 1 << 29]),
+                       ([3, 2, 1, 0], None)):
+        rnd.batch.row_start.copy_(torch.tensor(start, dtype=torch.int32))
+        rnd.batch.ctx_len.copy_(torch.tensor(ctx, dtype=torch.int32) if ctx else rnd.ctx)
+        sel = torch.full((rnd.n, 2, 8), -7, dtype=torch.int32, device="cuda")
+        wf.wf_paged_select(rnd.dq, rnd.cache, rnd.batch, sel, 2)
+        assert ((sel >= -7) & (sel < rnd.table.shape[1])).all()
+    # the sequences whose numbers hold are served as ever
+    rnd.batch.row_start.copy_(torch.tensor([0, 2, 5, 6], dtype=torch.int32))
+    rnd.batch.ctx_len.copy_(torch.tensor([640, -3, 320], dtype=torch.int32))
+    wf.wf_paged_select(rnd.dq, rnd.cache, rnd.batch, sel.fill_(-7), 2)
+    want = R.select(rnd, 8, 2)
+    assert np.array_equal(sel.cpu().numpy()[[0, 1, 5]], want[[0, 1, 5]])
+    assert (sel[2:5] == -7).all()
 
 
 def test_copies_of_a_cache_have_their_own_memory():

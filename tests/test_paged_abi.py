@@ -137,6 +137,12 @@ def test_selections_are_checked(kw):
     assert _select(**kw) == 1
 
 
+def test_sparse_work_is_counted_in_32_bits():
+    assert _sparse(dict(hkv=32, page=128), n=1 << 17, ns=1024) == 1
+    assert _sparse(dict(hkv=32, page=128), n=1 << 16, ns=1024) == 1
+    assert _sparse(dict(hkv=32, page=128), n=(1 << 16) - 1, ns=1024, ws=None) == 3
+
+
 @pytest.mark.parametrize("cache,batch,kw", [
     (dict(bounds=None), {}, {}), ({}, {}, dict(nr=0)), ({}, {}, dict(nr=11)),
     (dict(page=16), dict(pages=65537), {}), ({}, {}, dict(n=(1 << 16) + 1))])
