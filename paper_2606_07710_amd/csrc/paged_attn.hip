@@ -392,9 +392,20 @@ __global__ __launch_bounds__(64 * KS * RG) void paged_attn_bf16(PagedAttnParams 
         const int kl = j * RPL + lane / GRAN, pg = lane % GRAN;
         const int seg = (pg >> 1) ^ (kl & (SEGS - 1));
         row_of[ji] = kl;
-        koff[ji] = (unsigned)((pg ^ (kl & (GRAN - 1))) * 16);
-        voff[ji] = (unsigned)((2 * seg + (pg & 1)) * 16);
+        koff[ji] = (unsigned)(kl * RB + (pg ^ (kl & (GRAN - 1))) * 16);
+        voff[ji] = (unsigned)(kl * RB + (2 * seg + (pg & 1)) * 16);
     }
+    // Where a lane's operands lie in its stream's tile: K's granules (16 keys
+    // further on by an immediate offset), V's segments.
+    const WF_LDS(char) *const tile0 = (const WF_LDS(char) *)smem + stream * TILE;
+    int kread[KC], vread[MD];
+    const int q4 = m16 & 3, qk = m16 >> 2;
+#pragma unroll
+    for (int kk = 0; kk < KC; ++kk)
+        kread[kk] = m16 * RB + ((4 * kk + c4) ^ (m16 & (GRAN - 1))) * 16;
+#pragma unroll
+    for (int md = 0; md < MD; ++md)
+        vread[md] = (4 * c4 + qk) * RB + (md ^ ((4 * c4 + qk) & (SEGS - 1))) * 32 + q4 * 8;
 
     bf16x8 qf[NB][KC];
     f32x4 o[MD][NB];
@@ -434,9 +445,12 @@ __global__ __launch_bounds__(64 * KS * RG) void paged_attn_bf16(PagedAttnParams 
         };
         Where ring_where[NBUF - 1];
 
-        auto issue = [&](int st) __attribute__((always_inline)) -> Where {
+        // (the ring's buffer is known where a step is compiled, so that addresses
+        // in it are immediates)
+        auto issue = [&](auto bi, int st) __attribute__((always_inline)) -> Where {
             const int kb = k_begin + (KS * st + stream) * kTile;
-            const unsigned slot = lds_addr(smem) + ((st % NBUF) * KS + stream) * TILE;
+            const unsigned slot =
+                lds_addr(smem) + stream * TILE + decltype(bi)::value * (KS * TILE);
             if ((kb + 16) >> a.v.page_shift >= pages.base + kWave)
                 pages.load(a, it, kb >> a.v.page_shift);
             Where wh;
@@ -449,44 +463,51 @@ __global__ __launch_bounds__(64 * KS * RG) void paged_attn_bf16(PagedAttnParams 
             } else {
                 pages.find(a, it, kb + 16, wh.pos[1], wh.n[1], off[1]);
             }
-            const bool whole = wh.n[0] + wh.n[1] == 32;
+            auto copy = [&](auto whole_tag) __attribute__((always_inline)) {
+                constexpr bool WHOLE = decltype(whole_tag)::value;
 #pragma unroll
-            for (int jr = 0; jr < LPW; ++jr) {
-                const bool is_v = jr >= LPW / 2;
-                const int hf = LPH >= RG ? jr / NJ % 2 : rgi / LPH;
-                const int ji = LPH >= RG ? jr % NJ : 0;
-                const int j = LPH >= RG ? rgi + ji * RG : rgi % LPH;
-                const char *src = static_cast<const char *>(is_v ? a.vc : a.k) + (hf ? off[1] : off[0]);
-                unsigned row = row_of[ji];
-                if (!whole) {
-                    // keys that are not there repeat the half's last one, or are
-                    // zeros
-                    const int n = hf ? wh.n[1] : wh.n[0];
-                    src = n ? src : a.zeros;
-                    row = min(row, (unsigned)max(n - 1, 0));
+                for (int jr = 0; jr < LPW; ++jr) {
+                    const bool is_v = jr >= LPW / 2;
+                    const int hf = LPH >= RG ? jr / NJ % 2 : rgi / LPH;
+                    const int ji = LPH >= RG ? jr % NJ : 0;
+                    const int j = LPH >= RG ? rgi + ji * RG : rgi % LPH;
+                    const char *src =
+                        static_cast<const char *>(is_v ? a.vc : a.k) + (hf ? off[1] : off[0]);
+                    unsigned at = is_v ? voff[ji] : koff[ji];
+                    if constexpr (!WHOLE) {
+                        // keys that are not there repeat the half's last one, or
+                        // are zeros
+                        const int n = hf ? wh.n[1] : wh.n[0];
+                        src = n ? src : a.zeros;
+                        at -= (row_of[ji] - min(row_of[ji], (unsigned)max(n - 1, 0))) * RB;
+                    }
+                    // (the copy takes scalars; these are, but the compiler may hold
+                    // them in vector registers)
+                    lds_dma16_so<NT>(
+                        reinterpret_cast<const char *>(uniform64(reinterpret_cast<intptr_t>(src))),
+                        at, uniform((int)(slot + (is_v ? HALF : 0) + (hf * LPH + j) * 1024)));
                 }
-                lds_dma16_so<NT>(src, (is_v ? voff[ji] : koff[ji]) + row * RB,
-                                 slot + (is_v ? HALF : 0) + (hf * LPH + j) * 1024);
-            }
+            };
+            if (wh.n[0] + wh.n[1] == 32)
+                copy(std::true_type{});
+            else
+                copy(std::false_type{});
             return wh;
         };
 
-        auto compute = [&](int st, const Where &wh) __attribute__((always_inline)) {
-            const WF_LDS(char) *kt =
-                (const WF_LDS(char) *)smem + ((st % NBUF) * KS + stream) * TILE;
+        auto compute = [&](auto bi, const Where &wh) __attribute__((always_inline)) {
+            const WF_LDS(char) *kt = tile0 + decltype(bi)::value * (KS * TILE);
             const WF_LDS(char) *vt = kt + HALF;
             f32x4 s[2][NB];
 #pragma unroll
             for (int mb = 0; mb < 2; ++mb) {
-                const int kl = 16 * mb + m16;
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb)
                     s[mb][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int kk = 0; kk < KC; ++kk) {
-                    const int pg = (4 * kk + c4) ^ (kl & (GRAN - 1));
                     const bf16x8 kop = __builtin_bit_cast(
-                        bf16x8, *(const WF_LDS(u32x4) *)(kt + kl * RB + pg * 16));
+                        bf16x8, *(const WF_LDS(u32x4) *)(kt + kread[kk] + 16 * mb * RB));
 #pragma unroll
                     for (int nb = 0; nb < NB; ++nb)
                         s[mb][nb] = mfma16x16x32(kop, qf[nb][kk], s[mb][nb]);
@@ -495,17 +516,14 @@ __global__ __launch_bounds__(64 * KS * RG) void paged_attn_bf16(PagedAttnParams 
             // V^T, while the scores are formed: two transposing reads per 16 dims
             typedef short v4i16 __attribute__((ext_vector_type(4)));
             typedef short v8i16 __attribute__((ext_vector_type(8)));
-            const int q4 = m16 & 3, qk = m16 >> 2;
             bf16x8 vop[MD];
 #pragma unroll
             for (int md = 0; md < MD; ++md) {
                 v4i16 half[2];
 #pragma unroll
-                for (int hh = 0; hh < 2; ++hh) {
-                    const int kl = 16 * hh + 4 * c4 + qk;
+                for (int hh = 0; hh < 2; ++hh)
                     half[hh] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (WF_LDS(v4i16) *)(vt + kl * RB + (md ^ (kl & (SEGS - 1))) * 32 + q4 * 8));
-                }
+                        (WF_LDS(v4i16) *)(vt + vread[md] + 16 * hh * RB));
                 const v8i16 both = __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7);
                 vop[md] = __builtin_bit_cast(bf16x8, both);
             }
@@ -585,14 +603,16 @@ __global__ __launch_bounds__(64 * KS * RG) void paged_attn_bf16(PagedAttnParams 
             for (int kk = 0; kk < KC; ++kk)
                 asm volatile("" : "+v"(qf[nb][kk]));
         asm volatile("" : "+v"(pages.lo), "+v"(pages.hi), "+v"(pages.pos));
-#pragma unroll
-        for (int i = 0; i < NBUF - 1; ++i)
-            if (i < n_steps)
-                ring_where[i] = issue(i);
-        for (int st = 0; st < n_steps; ++st) {
+        if (0 < n_steps)
+            ring_where[0] = issue(ic<0>{}, 0);
+        if constexpr (NBUF > 2)
+            if (1 < n_steps)
+                ring_where[1] = issue(ic<1>{}, 1);
+        auto step = [&](auto bi, int st) __attribute__((always_inline)) {
+            constexpr int B = decltype(bi)::value;
             // stage st is in LDS once only the later stages' copies are out
-            if (NBUF > 2 && n_steps - 1 - st >= NBUF - 2)
-                wait_vmcnt<(NBUF - 2) * LPW>();
+            if (NBUF > 2 && st + 1 < n_steps)
+                wait_vmcnt<LPW>();
             else
                 wait_vmcnt<0>();
             // ... for every wave that copied a part of it, and every wave is
@@ -602,13 +622,21 @@ __global__ __launch_bounds__(64 * KS * RG) void paged_attn_bf16(PagedAttnParams 
             else
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             const Where now = ring_where[0];
-#pragma unroll
-            for (int i = 0; i + 1 < NBUF - 1; ++i)
-                ring_where[i] = ring_where[i + 1];
+            if constexpr (NBUF > 2)
+                ring_where[0] = ring_where[1];
             if (st + NBUF - 1 < n_steps)
-                ring_where[NBUF - 2] = issue(st + NBUF - 1);
+                ring_where[NBUF - 2] = issue(ic<(B + NBUF - 1) % NBUF>{}, st + NBUF - 1);
             if (RG == 1 || KS * st + stream < n_tiles)
-                compute(st, now);
+                compute(bi, now);
+        };
+        static_assert(NBUF == 2 || NBUF == 3, "the steps of a turn of the ring");
+        for (int st = 0; st < n_steps; st += NBUF) {
+            step(ic<0>{}, st);
+            if (st + 1 < n_steps)
+                step(ic<1>{}, st + 1);
+            if constexpr (NBUF > 2)
+                if (st + 2 < n_steps)
+                    step(ic<2>{}, st + 2);
         }
         // ---- the streams' rows meet in LDS ----
         __syncthreads();
