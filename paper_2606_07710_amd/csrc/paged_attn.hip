@@ -797,6 +797,19 @@ __global__ __launch_bounds__(256) void paged_attn_join(PagedAttnParams a) {
             x = op(x, __shfl_xor(x, off, kWave));
         return x;
     };
+    // eight parts' rows at a time (past the last part: the last again, with
+    // factor 0), the first eight before their factors are known
+    f32x4 x[8][E / 4];
+    auto fetch = [&](int p0) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float *src = a.part_o + (slot(min(p0 + i, parts - 1)) * ROWS + row) * DH + sub * E;
+#pragma unroll
+            for (int e = 0; e < E / 4; ++e)
+                x[i][e] = *reinterpret_cast<const f32x4 *>(src + 4 * e);
+        }
+    };
+    fetch(0);
     float mm = -INFINITY;
     for (int p = sub; p < parts; p += 16)
         mm = fmaxf(mm, a.part_ml[(slot(p) * ROWS + row) * 2]);
@@ -814,25 +827,15 @@ __global__ __launch_bounds__(256) void paged_attn_join(PagedAttnParams a) {
             lp = src[1] * f;
         }
         l += over16(lp, [](float x, float y) { return x + y; });
-        // eight parts' rows in flight (past the last part: the last again, with
-        // factor 0)
-        const int n = min(parts - p0, 16);
-        for (int p = 0; p < n; p += 8) {
-            f32x4 x[8][E / 4];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float *src =
-                    a.part_o + (slot(min(p0 + p + i, parts - 1)) * ROWS + row) * DH + sub * E;
-#pragma unroll
-                for (int e = 0; e < E / 4; ++e)
-                    x[i][e] = *reinterpret_cast<const f32x4 *>(src + 4 * e);
-            }
+        for (int p = 0; p < min(parts - p0, 16); p += 8) {
+            if (p0 + p)
+                fetch(p0 + p);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float fp = __shfl(f, lane0 + p + i, kWave);
 #pragma unroll
                 for (int e = 0; e < E; ++e)
-                    o[e] = p + i < n ? fmaf(x[i][e / 4][e % 4], fp, o[e]) : o[e];
+                    o[e] = p0 + p + i < parts ? fmaf(x[i][e / 4][e % 4], fp, o[e]) : o[e];
             }
         }
     }
