@@ -150,6 +150,32 @@ def test_large_logits(big):
     assert np.allclose(R.f64(tops), rtops, rtol=2.0 ** -22, atol=2.0 ** -12)
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [70, 5000, 60000])
+def test_logits_masked_with_the_lowest_number(dt, vocab):
+    """A mask of the type's lowest value, before, between and behind what is
+    left, and beside its largest: weights of exactly 0, so the rows' results are
+    those of the same rows with -inf there."""
+    low, high = torch.finfo(R.DT[dt]).min, torch.finfo(R.DT[dt]).max
+    x = logits(8, vocab, dt, 41)
+    at = torch.arange(vocab, device="cuda")
+    keep = torch.stack([at >= vocab - 3, at < 3, at % 9 == 4, at == vocab // 2, at % 2 == 1,
+                        at < 0, at == 5, (at >= vocab // 4) & (at < vocab // 2)])
+    x = torch.where(keep, x.float(), low).to(x.dtype)
+    x[6, 5] = high
+    t = torch.stack([k.nonzero()[0, 0] if k.any() else at[7] for k in keep]).int()
+    lp, ent, rank, ids, tops = run(x, t, 3)
+    rlp, rent, rrank, rids, rtops = R.logprobs(R.f64(x), t.cpu().numpy(), 3)
+    # as `compare` has it, the spread that of the values left (under 2^5)
+    assert np.allclose(R.f64(lp), rlp, rtol=0, atol=2.0 ** -13 + 2.0 ** -17)
+    assert np.allclose(R.f64(ent), rent, rtol=0, atol=16 * (2.0 ** -13 + 2.0 ** -17))
+    assert np.array_equal(rank.cpu().numpy(), rrank) and np.array_equal(ids.cpu().numpy(), rids)
+    # (differences of 2^128 and more are -inf in fp32; 2^-22 of the larger ones)
+    with np.errstate(over="ignore"):
+        assert np.allclose(R.f64(tops), rtops.astype(np.float32), rtol=2.0 ** -22,
+                           atol=2.0 ** -13 + 2.0 ** -17)
+
+
 def test_captured_call_replays_and_the_workspace_stays_clean():
     x, t = logits(16, 30000, "f32", 17), tokens(16, 30000, 18)
     ws = wf.alloc_workspace(wf.wf_token_logprobs_workspace_bytes(x.dtype, 16, 30000, 20), "cuda")
