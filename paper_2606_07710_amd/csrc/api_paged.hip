@@ -177,7 +177,7 @@ wf_status_t wf_paged_sparse_attn(wf_dtype_t dt, const void *q, const wf_paged_ca
     if (n_sel < 1 || n_sel > kMaxSelected || !sel || !aligned4(sel))
         return WF_ERR_INVALID_ARG;
     // (chunks of 128 listed keys are counted in 32 bits)
-    if (cache && cache->n_kv_heads > 0 && n_rows > 0 &&
+    if (cache && attn_sizes_ok(n_rows, n_q_heads, cache->n_kv_heads) &&
         (long long)n_rows * cache->n_kv_heads *
                 ((n_q_heads / cache->n_kv_heads + 15) / 16) *
                 (((long long)n_sel * cache->page_size + 127) / 128) > INT32_MAX)

@@ -17,6 +17,13 @@
 //   P   = exp2((S - m) * scale * log2 e), online maximum and sum per row
 //   O^T += V^T P^T   A from transposing reads of the LDS copy of the V tile
 // fp32: the same with the fp32 matrix instruction, operands from memory.
+//
+// What bounds it (32 heads over 8 of 128, attention and join): decoding 128
+// requests of up to 16K keys moves 3.0 GB in 462 us, 6.5 TB/s; 45 rows' selections
+// of 122 pages of 32 keys 0.68 GB in 109 us, 6.2 TB/s.  Blocks of 16 rows (16 requests
+// of up to 8K, 183 MB, 46 us) and draft trees (4 of 61 nodes, 55 MB and 11.5 GFLOP,
+// 43 us) are bound by the issue of the loads and of exp2 and by the partials, one
+// request of 1K keys (9.5 us) by launch and dependent trips.
 #include "wf_lds_dma.h"
 #include "wf_paged.h"
 
@@ -772,10 +779,11 @@ __global__ __launch_bounds__(256) void paged_attn_f32(PagedAttnParams a) {
 // ---------------------------------------------------------------------------
 // Joins the partials of the split item that begins in workgroup blockIdx.x, in
 // run order: 16 lanes to a row, a sixteenth of its dims each, 16 rows to a
-// workgroup.  Bound by the latency of its three trips to memory (with one part's
-// row in flight instead of eight it took 12 us for 32 parts, longer than the
+// workgroup.  Bound by the latency of its three trips to memory: 2.5 us for the parts
+// of one request's heads, 12 for 32 MB of draft trees' partials (with one part's
+// row in flight instead of eight 12 us for 32 parts, longer than the
 // attention; with a wave to a row, four times the workgroups, 10 us for 128
-// items of 64 rows).
+// items of 64 rows; sixteen rows in flight gain nothing).
 template <typename T, int DH, int ROWS>
 __global__ __launch_bounds__(256) void paged_attn_join(PagedAttnParams a) {
     const int w0 = blockIdx.x;
@@ -904,7 +912,15 @@ size_t ml_bytes(const PagedPlan &p) {
 }  // namespace
 
 // Rows that share each key's bytes: the query heads of a group and, dense, the
-// sequence's rows.
+// sequence's rows.  Up to 16 rows and fp32: four key streams, four waves with
+// rings of their own, one workgroup a CU (two streams and two workgroups a CU:
+// one request of 1K 9.98 us instead of 9.5, selected pages 12.7 instead of 12.3,
+// 128 requests of up to 16K the same).  More rows: a tile serves all waves, so two
+// workgroups a CU hide each other's barriers (one: draft trees of 4 requests 54.6
+// us instead of 47.8), and 768 workgroups write more partials than they balance
+// (blocks of 16 of 16 requests 47 us instead of 43.5).  Items of 256 rows, which
+// read keys half as often, leave too little work in flight (trees 53 us instead
+// of 45).
 PagedPlan plan_paged(wf_dtype_t dt, int max_rows, int n_q_heads, int n_kv_heads, bool sparse) {
     const int rows = n_q_heads / n_kv_heads * (sparse ? 1 : max_rows);
     if (dt == WF_F32 || sparse || rows <= 16)
