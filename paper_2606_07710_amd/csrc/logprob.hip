@@ -185,7 +185,6 @@ __global__ __launch_bounds__(kThreads) void token_logprobs(LogprobParams a) {
     const int token = a.tokens ? a.tokens[row] : -1;
     const bool has_token = token >= 0 && token < a.vocab;
     const float zt = has_token ? value(z[token]) : INFINITY;
-    const uint32_t zt_order = value_order(zt);
     // What comes before the token: behind it, the values above its own; before
     // it also the equal ones, which are those above the next lower number (all,
     // where its logit is -inf: !(x <= NaN)).  NaN counts as above.
@@ -224,9 +223,9 @@ __global__ __launch_bounds__(kThreads) void token_logprobs(LogprobParams a) {
                 x[e] = __uint_as_float(w[e]);
         }
     };
-    // The sums over V values of every lane; the order of the largest, or, where
-    // NaN or +inf is among them, the highest there is.
-    auto add = [&](const float (&x)[V]) __attribute__((always_inline)) -> uint32_t {
+    // The sums over V values of every lane; the largest, or, where NaN or +inf is
+    // among them, NaN.
+    auto add = [&](const float (&x)[V]) __attribute__((always_inline)) -> float {
         float mx = -INFINITY;
 #pragma unroll
         for (int e = 0; e < V; ++e)
@@ -242,13 +241,15 @@ __global__ __launch_bounds__(kThreads) void token_logprobs(LogprobParams a) {
         float pl = 0.f, pt = 0.f;
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            const float d = x[e] - mu, p = fast_exp2(d * kLog2e);
+            // (0 * -inf would be NaN; a NaN stays one)
+            const float d = __builtin_elementwise_maximum(x[e] - mu, -1e30f);
+            const float p = fast_exp2(d * kLog2e);
             pl += p;
-            pt = fmaf(p, fmaxf(d, -1e30f), pt);      // (0 * -inf would be NaN)
+            pt = fmaf(p, d, pt);
         }
         l += pl;
         t += pt;
-        return pl != pl ? ~0u : value_order(mx);
+        return fmaf(pl, 0.f, mx);
     };
     // Elements before the first 16-byte boundary and behind the last whole piece
     // go one to a lane, whole groups of U tiles with their loads ahead, what is
@@ -279,8 +280,10 @@ __global__ __launch_bounds__(kThreads) void token_logprobs(LogprobParams a) {
         const int base = pos + (single ? lane : lane * V);
         const int n = base >= next ? 0 : single ? 1 : V;
         u32x4 w[U];
-        uint32_t tops[U] = {};
-        uint32_t top = 0;
+        float tops[U], top = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            tops[u] = -INFINITY;
         if (whole) {
 #pragma unroll
             for (int u = 0; u < U; ++u)
@@ -304,11 +307,10 @@ __global__ __launch_bounds__(kThreads) void token_logprobs(LogprobParams a) {
             for (int e = 0; e < V; ++e)
                 x[e] = FULL || e < n ? x[e] : -INFINITY;
             tops[u] = add(x);
-            top = max(top, tops[u]);
+            top = __builtin_elementwise_maximum(top, tops[u]);
             const bool before = base + u * TILE + (FULL ? V : n) <= token;
             const float above = before ? zt_below : zt;
-            // (one order below it is no less sharp)
-            if (__ballot(tops[u] > zt_order - (before ? 1u : 0u)) && zt == zt)
+            if (__ballot(!(tops[u] <= above)) && zt == zt)
 #pragma unroll
                 for (int e = 0; e < V; ++e)
                     ahead += __popcll(__ballot((FULL || e < n) && !(x[e] <= above)));
@@ -321,16 +323,17 @@ __global__ __launch_bounds__(kThreads) void token_logprobs(LogprobParams a) {
             tile(0, std::false_type{});
         }
         // ---- the list (a value equal to its n-th best is behind it) ----
-        if (a.n_top && __ballot(n > 0 && top >= max((uint32_t)(bar >> 32), 1u))) {
+        const uint32_t top_order = n > 0 ? value_order(top) : 0u;
+        if (a.n_top && __ballot(top_order >= max((uint32_t)(bar >> 32), 1u))) {
             // (the waves' bars rise; which one is seen changes no result)
             const uint64_t b = max(max(volatile_load(bars), volatile_load(bars + 1)),
                                    max(volatile_load(bars + 2), volatile_load(bars + 3)));
             bar = uniform64(b);
             uint32_t need = max((uint32_t)(bar >> 32), 1u);
             // the n-th largest of the lanes' maxima: the least of those that
-            // fewer than n are above (a lane whose `top` is the NaN mark may hold
-            // less: it counts as 0)
-            const uint32_t o = n > 0 && top != ~0u ? top : 0u;
+            // fewer than n are above (a lane whose `top` is NaN may hold less: it
+            // counts as 0)
+            const uint32_t o = top == top ? top_order : 0u;
             if (__popcll(__ballot(o > need)) >= a.n_top) {
                 uint32_t *tops_lds = reinterpret_cast<uint32_t *>(scratch);
                 tops_lds[lane] = o;
@@ -362,13 +365,13 @@ __global__ __launch_bounds__(kThreads) void token_logprobs(LogprobParams a) {
                 int more = 0;
                 if (u < tiles) {
                     u32x4 wu = w[0];
-                    uint32_t tu = tops[0];
+                    float tu = tops[0];
 #pragma unroll
                     for (int i = 1; i < U; ++i) {
                         wu = u == i ? w[i] : wu;
                         tu = u == i ? tops[i] : tu;
                     }
-                    if (!__ballot(tu >= need))
+                    if (!__ballot(value_order(tu) >= need))
                         continue;
                     unpack(wu, x);
 #pragma unroll
