@@ -35,6 +35,7 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kMaxParts = 64;
 constexpr int kLoads = 4;                  // 16-byte loads of a lane in a group
+constexpr int kInserts = 8;                // values that enter a list one by one
 constexpr int kPartKeys = 1280;            // parts * n_top at most
 // A row's arrival counter has a cache line to itself: counters side by side
 // queue up at one place of the memory (16 rows without alternatives: 15.6 us,
@@ -134,6 +135,15 @@ struct BestList {
     int n;
 
     __device__ __forceinline__ void clear() { best = bar = 0; }
+    // Takes in one key (uniform), no key of the list.
+    __device__ __forceinline__ void insert(uint64_t key) {
+        const int lane = threadIdx.x % kWave, place = __popcll(__ballot(best > key));
+        const uint64_t before =
+            ((uint64_t)(uint32_t)dpp<kWaveShr1, 0xf>(0, (int)(uint32_t)(best >> 32)) << 32) |
+            (uint32_t)dpp<kWaveShr1, 0xf>(0, (int)(uint32_t)best);
+        best = lane >= n || lane < place ? best : lane == place ? key : before;
+        bar = readlane64(best, n - 1);
+    }
     // Takes in the m <= 64 keys at `from` (LDS, zeros behind them up to a
     // multiple of 8; all different).  scratch: 64 keys of LDS, the wave's own.
     __device__ __forceinline__ void take(const uint64_t *from, int m, uint64_t *scratch) {
@@ -371,13 +381,30 @@ __global__ __launch_bounds__(kThreads) void token_logprobs(LogprobParams a) {
                         wu = u == i ? w[i] : wu;
                         tu = u == i ? tops[i] : tu;
                     }
-                    if (!__ballot(value_order(tu) >= need))
+                    uint64_t lanes = __ballot(n > 0 && value_order(tu) >= need);
+                    if (!lanes)
                         continue;
                     unpack(wu, x);
 #pragma unroll
                     for (int e = 0; e < V; ++e) {
                         in[e] = __ballot(e < n && !(x[e] < need_value));
                         more += __popcll(in[e]);
+                    }
+                    // a few for a list that is full, each the largest of its lane's
+                    if (list.bar && more <= kInserts && more == __popcll(lanes) && !__ballot(tu != tu)) {
+                        int at = 0;
+#pragma unroll
+                        for (int e = 1; e < V; ++e)
+                            at = x[e] == tu ? e : at;
+                        at += base + u * TILE;
+#pragma unroll 1
+                        for (; lanes; lanes &= lanes - 1) {
+                            const int from = __builtin_ctzll(lanes);
+                            list.insert(make_key(
+                                __int_as_float(__builtin_amdgcn_readlane(__float_as_int(tu), from)),
+                                __builtin_amdgcn_readlane(at, from)));
+                        }
+                        continue;
                     }
                 }
                 if (u == tiles || held + more > kGather) {

@@ -165,6 +165,7 @@ __device__ __forceinline__ int dpp(int identity, int x) {
 }
 constexpr int kRowShr1 = 0x111, kRowShr2 = 0x112, kRowShr4 = 0x114, kRowShr8 = 0x118;
 constexpr int kRowRor4 = 0x124, kRowRor8 = 0x128;         // rotations within a row
+constexpr int kWaveShr1 = 0x138;                          // from the lane before
 constexpr int kRowBcast15 = 0x142, kRowBcast31 = 0x143;   // a row's last lane to the rows behind
 
 // op over the lanes of a wave, in a fixed order; the same result in every lane.
