@@ -266,12 +266,17 @@ __global__ __launch_bounds__(kThreads) void paged_append(AppendParams a) {
 // order of the pages does not hang on the order of the sums), as products of the
 // fp64 matrix instruction: 16 query rows -- the heads of a group, and as many of
 // the sequence's rows as fit -- with the bounds of 16 pages.  A lane holds a
-// quarter of the dims of one query row and of one page; which dims meet in a
-// step is the same for both.  Bound by the matrix unit, 64 cycles for each of
-// DH / 2 steps a tile (each lane summing by itself, with sums over lanes at the
-// end, took 89 us where this takes 29: 45 rows of 16 sequences of up to 32K
-// tokens).  The tiles are dealt out evenly to 512 workgroups (256: 46 us,
-// 1024: 45 us for the whole selection, which takes 37).
+// quarter of the dims of one query row and of one page, 64 bytes of them next to
+// its neighbours' at a time; which dims meet in a step is the same for both.
+// Bound by the matrix unit, 64 cycles for each of DH / 2 steps a tile, and by the
+// vector work, which does not go on beside fp64 products, whichever wave's they
+// are: a product with two conversions takes 87 cycles.  So there is little of it
+// (two instructions split q, nothing is masked that is not looked at), and none
+// between products.  45 rows of 16 sequences of up to 32K tokens take 24 us (89
+// with each lane summing by itself and sums over lanes at the end, 29 with the
+// conversions between the products; the next tile's operands loaded ahead, 48
+// registers to move, 10 more; q kept converted for a pack's tiles, 128 registers, 6
+// more).  The tiles are dealt out evenly to 512 workgroups (256 or 1024: 8 more).
 //
 // Choice:  a workgroup per (row, KV head) finds the n_top-th largest key digit
 // by digit and lists the pages at or above it in page order.
@@ -331,88 +336,121 @@ __global__ __launch_bounds__(kThreads) void paged_scores(SelectParams a) {
     const int m16 = lane & 15, c4 = lane >> 4;
     const int heads = min(a.group, 16);              // of a row in a tile
     int tiles = tiles_of(s), packs = (s.rows + a.pack - 1) / a.pack;
-    for (; at < end; at += WAVES) {
-        while (at >= first + (long long)tiles * packs * a.v.n_kv_heads) {
+    // A tile: rows [row, row + rows) of the call, KV head g, 16 pages from p0 on, of
+    // which the lane has one; n_old of the sequence's are old to the last row.
+    struct Tile {
+        int row, rows, g, n_old, p0, id;
+    };
+    auto locate = [&](long long to) {
+        while (to >= first + (long long)tiles * packs * a.v.n_kv_heads) {
             first += (long long)tiles * packs * a.v.n_kv_heads;
             s = paged_seq(a.v, ++b, a.v.max_rows);
             tiles = tiles_of(s);
             packs = (s.rows + a.pack - 1) / a.pack;
         }
-        const int unit = (int)(at - first);          // < 2^31: see the limits
-        const int tile = unit % tiles, pack = unit / tiles % packs, g = unit / tiles / packs;
-        const int row0 = pack * a.pack, rows = min(s.rows - row0, a.pack);
-        const int n_old = old_pages(a, s, row0 + rows - 1);
-        const int p0 = tile * 16, p = p0 + m16;
-        const int id = p < n_old ? paged_page(a.v, b, p) : -1;
-        u32x4 lo[PIECES], hi[PIECES];
+        const int unit = (int)(to - first);          // < 2^31: see the limits
+        const int tile = unit % tiles, pack = unit / tiles % packs;
+        const int row0 = pack * a.pack;
+        Tile w;
+        w.g = unit / tiles / packs;
+        w.row = s.r0 + row0;
+        w.rows = min(s.rows - row0, a.pack);
+        w.n_old = old_pages(a, s, row0 + w.rows - 1);
+        w.p0 = tile * 16;
+        w.id = w.p0 + m16 < w.n_old ? paged_page(a.v, b, w.p0 + m16) : -1;
+        return w;
+    };
+    // (a page that is not there has another's bounds, a row that is not there
+    // another's q: what comes of them is not looked at)
+    auto load_bounds = [&](const Tile &w, u32x4 (&lo)[PIECES], u32x4 (&hi)[PIECES]) {
+        const T *src = static_cast<const T *>(a.bounds) +
+                       ((size_t)max(w.id, 0) * a.v.n_kv_heads + w.g) * 2 * DH + c4 * V;
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            lo[i] = *reinterpret_cast<const u32x4 *>(src + i * 4 * V);
+            hi[i] = *reinterpret_cast<const u32x4 *>(src + DH + i * 4 * V);
+        }
+    };
+    auto load_q = [&](const Tile &w, int h0, u32x4 (&q)[PIECES]) {
+        const int row = min(m16 / heads, w.rows - 1), h = min(h0 + m16 % heads, a.group - 1);
+        const T *src = static_cast<const T *>(a.q) +
+                       ((size_t)(w.row + row) * a.n_q_heads + w.g * a.group + h) * DH +
+                       c4 * V;
 #pragma unroll
         for (int i = 0; i < PIECES; ++i)
-            lo[i] = hi[i] = u32x4{0u, 0u, 0u, 0u};
-        if (id >= 0) {
-            const T *src = static_cast<const T *>(a.bounds) +
-                           ((size_t)id * a.v.n_kv_heads + g) * 2 * DH + c4 * (DH / 4);
-#pragma unroll
-            for (int i = 0; i < PIECES; ++i) {
-                lo[i] = *reinterpret_cast<const u32x4 *>(src + i * V);
-                hi[i] = *reinterpret_cast<const u32x4 *>(src + DH + i * V);
-            }
-        }
-        double best[4];                              // of (row, page) lane + 64 j
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            best[j] = -INFINITY;
-        bool odd[4] = {};
+            q[i] = *reinterpret_cast<const u32x4 *>(src + i * 4 * V);
+    };
+    for (; at < end; at += WAVES) {
+        const Tile now = locate(at);
+        u32x4 lo[PIECES], hi[PIECES], qw[PIECES];
+        load_bounds(now, lo, hi);
+        load_q(now, 0, qw);
+        double best = -INFINITY;
+        bool odd = false;
         for (int h0 = 0; h0 < a.group; h0 += 16) {
-            const int row = m16 / heads, h = h0 + m16 % heads;
-            const bool live = row < rows && h < a.group;
-            const T *qp = static_cast<const T *>(a.q) +
-                          ((size_t)(s.r0 + row0 + (live ? row : 0)) * a.n_q_heads + g * a.group +
-                           (live ? h : 0)) * DH + c4 * (DH / 4);
-            // two sums, so that a step need not wait for the one before it
-            f64x4 up_sum = {0.0, 0.0, 0.0, 0.0}, dn_sum = up_sum;
+            if (h0)
+                load_q(now, h0, qw);
+            f64x4 sum = {0.0, 0.0, 0.0, 0.0};
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) {
                 float q[V], l[V], u[V];
-                u32x4 w = *reinterpret_cast<const u32x4 *>(qp + i * V);
-                w = live ? w : u32x4{0u, 0u, 0u, 0u};
-                E::unpack(w, q);
+                E::unpack(qw[i], q);
                 E::unpack(lo[i], l);
                 E::unpack(hi[i], u);
+                double up[V], dn[V], ud[V], ld[V];
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    // (a NaN goes with the first: the score is odd either way)
-                    const float dn = q[e] < 0.f ? q[e] : 0.f;
-                    const float up = q[e] < 0.f ? 0.f : q[e];
-                    up_sum = __builtin_amdgcn_mfma_f64_16x16x4f64((double)up, (double)u[e], up_sum,
-                                                                  0, 0, 0);
-                    dn_sum = __builtin_amdgcn_mfma_f64_16x16x4f64((double)dn, (double)l[e], dn_sum,
-                                                                  0, 0, 0);
+                    // (not finite: one of the two is NaN or infinite, the score odd)
+                    const float x = __builtin_amdgcn_fmed3f(q[e], 0.f, INFINITY);
+                    up[e] = (double)x;
+                    dn[e] = (double)(q[e] - x);
+                    ud[e] = (double)u[e];
+                    ld[e] = (double)l[e];
                 }
+                // (a conversion between two products would wait for the first of them
+                // and hold up the second)
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    sum = __builtin_amdgcn_mfma_f64_16x16x4f64(up[e], ud[e], sum, 0, 0, 0);
+                    sum = __builtin_amdgcn_mfma_f64_16x16x4f64(dn[e], ld[e], sum, 0, 0, 0);
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
             // lane (m16, c4) has rows 4 i + c4 of column m16
             wave_sync();
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                sc[wave][4 * i + c4][m16] = up_sum[i] + dn_sum[i];
+                sc[wave][4 * i + c4][m16] = sum[i];
             wave_sync();
+            const int live = min(heads, a.group - h0);
+            // four rows at a time (there is one where the group has several parts)
+#pragma unroll 1
+            for (int r0 = 0; r0 < now.rows; r0 += 4) {
+                const int r = r0 + c4, page = now.p0 + m16;
+                if (h0 == 0) {
+                    best = -INFINITY;
+                    odd = false;
+                }
+                if (r >= now.rows)
+                    continue;
+                // (four heads at a time, the last one again past the last)
+#pragma unroll 1
+                for (int h2 = 0; h2 < live; h2 += 4) {
+                    double x[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int to = lane + kWave * j, r = to / 16;
-                if (r < rows)
-                    for (int h2 = 0; h2 < min(heads, a.group - h0); ++h2) {
-                        const double x = sc[wave][r * heads + h2][to % 16];
-                        odd[j] |= !(fabs(x) < INFINITY);
-                        best[j] = x > best[j] ? x : best[j];
+                    for (int k = 0; k < 4; ++k)
+                        x[k] = sc[wave][r * heads + min(h2 + k, live - 1)][m16];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        odd |= !(fabs(x[k]) < INFINITY);
+                        best = x[k] > best ? x[k] : best;
                     }
+                }
+                if (h0 + 16 >= a.group && page < now.n_old)
+                    a.keys[((size_t)(now.row + r) * a.v.n_kv_heads + now.g) * a.v.max_pages +
+                           page] = now.id < 0 ? 0ull : score_key(odd ? (double)NAN : best);
             }
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int to = lane + kWave * j, r = to / 16, page = p0 + to % 16;
-            const int its = __shfl(id, to % 16, kWave);
-            if (r < rows && page < n_old)
-                a.keys[((size_t)(s.r0 + row0 + r) * a.v.n_kv_heads + g) * a.v.max_pages + page] =
-                    its < 0 ? 0ull : score_key(odd[j] ? (double)NAN : best[j]);
         }
     }
 }
