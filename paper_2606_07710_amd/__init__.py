@@ -1064,11 +1064,10 @@ def _paged(cache, batch, dev):
     return cache.ref, batch.ref
 
 
-def _row_stride(t, name):
-    """The distance of t's rows [n][heads][D] in elements; the rest is dense."""
-    n, heads, dh = t.shape
+def _row_stride(t, n, heads, dh, name):
+    """The distance of t's rows [n][heads][dh] in elements; the rest is dense."""
     s = t.stride()
-    if t.numel() and ((dh > 1 and s[2] != 1) or (heads > 1 and s[1] != dh)):
+    if n and ((dh > 1 and s[2] != 1) or (heads > 1 and s[1] != dh)):
         raise ValueError(f"the heads of a row of {name} must lie side by side")
     return s[0] if n > 1 else heads * dh
 
@@ -1081,33 +1080,33 @@ def wf_paged_append(k, v, cache, batch, rope_base, q=None, q_out=None, positions
     fused projection.  positions [n] int32: what to rotate by, where that is not
     the row's position (draft trees)."""
     dev, raw = _at(stream)
-    shape = tuple(k.shape)
+    shape, dtype = k.shape, cache.dtype
     n, hkv, dh = shape
-    if tuple(v.shape) != shape or k.dtype != cache.dtype or v.dtype != cache.dtype or \
+    if v.shape != shape or k.dtype != dtype or v.dtype != dtype or \
             hkv != cache.n_kv_heads or dh != cache.head_dim:
         raise ValueError("k and v must match each other and the cache")
-    stride = _row_stride(k, "k")
-    if _row_stride(v, "v") != stride:
+    stride = _row_stride(k, n, hkv, dh, "k")
+    if _row_stride(v, n, hkv, dh, "v") != stride:
         raise ValueError("k and v must have the same strides")
-    qs, hq, qp = 0, 0, None
+    if k.get_device() != dev or v.get_device() != dev:
+        raise ValueError("k and v must be tensors on the current device")
+    qs, hq, qp, qo = 0, 0, None, None
     if (q is None) != (q_out is None):
         raise ValueError("q and q_out come together")
     if q is not None:
-        hq = q.shape[1]
-        if tuple(q.shape) != (n, hq, dh) or tuple(q_out.shape) != (n, hq, dh) or \
-                q.dtype != cache.dtype or q_out.dtype != cache.dtype:
+        qshape = q.shape
+        if len(qshape) != 3 or qshape[0] != n or qshape[2] != dh or q_out.shape != qshape or \
+                q.dtype != dtype or q_out.dtype != dtype:
             raise ValueError("q and q_out must be [n][Hq][D], of the cache's type")
-        qs, qp = _row_stride(q, "q"), q.data_ptr()
-    for t in (k, v) if q is None else (k, v, q):
-        if t.get_device() != dev:
-            raise ValueError("k, v and q must be tensors on the current device")
-    if positions is not None and (tuple(positions.shape) != (n,)
-                                  or positions.dtype != torch.int32):
+        if q.get_device() != dev:
+            raise ValueError("q must be a tensor on the current device")
+        hq = qshape[1]
+        qs, qp, qo = _row_stride(q, n, hq, dh, "q"), q.data_ptr(), _ptr(q_out, dev, "q_out")
+    if positions is not None and (positions.shape != (n,) or positions.dtype != torch.int32):
         raise ValueError("positions must be [n] int32")
     _check(lib.wf_paged_append(cache.code, *_paged(cache, batch, dev), k.data_ptr(), v.data_ptr(),
-                               stride, qp, qs, _ptr(q_out, dev, "q_out"), hq,
-                               _ptr(positions, dev, "positions"), rope_base, n, raw),
-           "wf_paged_append")
+                               stride, qp, qs, qo, hq, _ptr(positions, dev, "positions"),
+                               rope_base, n, raw), "wf_paged_append")
 
 
 def _code_of(dtype):
