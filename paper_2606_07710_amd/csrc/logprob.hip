@@ -19,9 +19,10 @@
 //
 // Short rows and few of them are bound by latency, in which the fetching of the
 // code counts: loops that are not hot are kept rolled.  16 fp32 rows of 151936
-// with 20 alternatives take 16 us, most of it the lists' two meetings; 2000 bf16
-// rows with 5 (608 MB) take 158 us, 3.8 TB/s, bound by the vector unit (0.74
-// busy: an exponential and six more instructions a value).
+// with 20 alternatives take 16 us (7 without: the rest are the lists, from a
+// group's values to their two meetings); 2000 bf16 rows with 5 (608 MB) take 146
+// us, 4.2 TB/s, bound by the vector unit (0.73 busy: 14 instructions a value, an
+// exponential among them).
 #include <type_traits>
 
 #include "wf_api_internal.h"
@@ -35,7 +36,10 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kMaxParts = 64;
 constexpr int kLoads = 4;                  // 16-byte loads of a lane in a group
-constexpr int kInserts = 8;                // values that enter a list one by one
+// Up to so many values of a tile enter a full list one by one, a compare and
+// seven moves each, more of them together (2000 rows with 5 alternatives: 167 ->
+// 163 us; into an empty list one by one, 16 rows with 20 take 17.5 us, not 16).
+constexpr int kInserts = 8;
 constexpr int kPartKeys = 1280;            // parts * n_top at most
 // A row's arrival counter has a cache line to itself: counters side by side
 // queue up at one place of the memory (16 rows without alternatives: 15.6 us,
