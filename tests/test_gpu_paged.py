@@ -316,6 +316,28 @@ def test_select_ties_missing_pages_and_nan():
     assert sel[1, 1].tolist() == [0, 1, 2, 4, 39, 40, -1, -1, -1]
 
 
+@pytest.mark.parametrize("dt,dh", [("bf16", 64), ("bf16", 128), ("f32", 64), ("f32", 128)])
+def test_select_of_queries_that_are_not_finite(dt, dh):
+    """Such a query makes every page's score of its own row and group odd (the
+    first pages are chosen), and nobody else's; signed zeros and the type's
+    largest numbers are scores like others."""
+    rnd = R.Round([(6, 900), (1, 400)], 16, 8, 2, dh, dt, seed=67)
+    inf, nan, big = float("inf"), float("nan"), torch.finfo(rnd.q.dtype).max
+    rnd.q[0, 1, 3] = inf
+    rnd.q[1, 6, dh - 1] = -inf
+    rnd.q[2, 0, 0], rnd.q[2, 7, 9] = nan, -nan
+    rnd.q[3, :, ::2] = -0.0
+    rnd.q[4, 2, 5], rnd.q[4, 5, 6] = big, -big
+    rnd.q[5] = 0.0
+    rnd.on_gpu()
+    sel = torch.empty((rnd.n, 2, 11), dtype=torch.int32, device="cuda")
+    wf.wf_paged_select(rnd.dq, rnd.cache, rnd.batch, sel, 2)
+    got = sel.cpu().numpy()
+    assert np.array_equal(got, R.select(rnd, 11, 2))
+    assert got[0, 0, :9].tolist() == list(range(9)) == got[1, 1, :9].tolist()
+    assert got[0, 1, :9].tolist() != list(range(9)) != got[6, 0, :9].tolist()
+
+
 # ---- attention over selected pages -------------------------------------------------
 
 SPARSES = [
