@@ -10,9 +10,9 @@
 // keys: the value's order in the high half, the index's complement in the low
 // one, so that the order of equal values is that of their indexes and no result
 // hangs on which lane came first.  The values of a group that beat the n-th best
-// that any wave of the workgroup has, and reach the n-th largest of the lanes'
-// maxima in the group (which n of them do), are gathered in LDS and enter
-// together: all are compared with all.  The sorted lists of the waves, and then,
+// that any wave of the workgroup has, and reach what n of the lanes' maxima in
+// the group reach, are gathered in LDS and enter together: all are compared with
+// all.  The sorted lists of the waves, and then,
 // in the row's last workgroup, of the parts, join by the same means: of P lists
 // the (n / r)-th largest of their r-th keys, r = n / P, is reached by n keys, and
 // what reaches it is few more than n.
@@ -344,30 +344,76 @@ __global__ __launch_bounds__(kThreads) void token_logprobs(LogprobParams a) {
                                    max(volatile_load(bars + 2), volatile_load(bars + 3)));
             bar = uniform64(b);
             uint32_t need = max((uint32_t)(bar >> 32), 1u);
-            // the n-th largest of the lanes' maxima: the least of those that
-            // fewer than n are above (a lane whose `top` is NaN may hold less: it
-            // counts as 0)
-            const uint32_t o = top == top ? top_order : 0u;
-            if (__popcll(__ballot(o > need)) >= a.n_top) {
-                uint32_t *tops_lds = reinterpret_cast<uint32_t *>(scratch);
-                tops_lds[lane] = o;
-                wave_sync();
-                int above = 0;
+            // A number that n values reach and few more.  (A lane whose maximum is NaN
+            // may hold less: it counts as 0.)
+            if (a.n_top <= kWave / 2) {
+                // the n-th largest of the lanes' maxima: the least of those that
+                // fewer than n are above
+                const uint32_t o = top == top ? top_order : 0u;
+                if (__popcll(__ballot(o > need)) >= a.n_top) {
+                    uint32_t *tops_lds = reinterpret_cast<uint32_t *>(scratch);
+                    tops_lds[lane] = o;
+                    wave_sync();
+                    int above = 0;
 #pragma unroll 1
-                for (int j = 0; j < kWave; j += 16) {
-                    uint32_t k[16];
+                    for (int j = 0; j < kWave; j += 16) {
+                        uint32_t k[16];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        k[i] = tops_lds[j + i];
+                        for (int i = 0; i < 16; ++i)
+                            k[i] = tops_lds[j + i];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        above += k[i] > o ? 1 : 0;
+                        for (int i = 0; i < 16; ++i)
+                            above += k[i] > o ? 1 : 0;
+                    }
+                    wave_sync();
+                    const int reach = wave_reduce(
+                        above < a.n_top ? (int)o : -1, -1,
+                        [](int x, int y) { return (int)min((uint32_t)x, (uint32_t)y); });
+                    need = max(need, (uint32_t)reach);
                 }
-                wave_sync();
-                const int reach = wave_reduce(
-                    above < a.n_top ? (int)o : -1, -1,
-                    [](int x, int y) { return (int)min((uint32_t)x, (uint32_t)y); });
-                need = max(need, (uint32_t)reach);
+            } else {
+                // by halving, one that n of the lanes' maxima in the tiles reach and
+                // at most a quarter more: the least of 64 lanes' maxima is reached by
+                // a quarter of all values (16 rows of 151936 with 64 alternatives: 41
+                // -> 31 us; with 20 the same, with 5 half a us more than the above)
+                uint32_t o[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    o[u] = n > 0 && (u == 0 || whole) && tops[u] == tops[u] ? value_order(tops[u])
+                                                                            : 0u;
+                auto reach = [&](uint32_t x) {
+                    int c = 0;
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+                        c += __popcll(__ballot(o[u] >= x));
+                    return c;
+                };
+                if (reach(need + 1u) >= a.n_top) {
+                    uint32_t most = o[0];
+#pragma unroll
+                    for (int u = 1; u < U; ++u)
+                        most = max(most, o[u]);
+                    // (every lane reaches the least of the lanes', 64 of them)
+                    const uint32_t least = (uint32_t)wave_reduce((int)most, -1, [](int x, int y) {
+                        return (int)min((uint32_t)x, (uint32_t)y);
+                    });
+                    uint32_t past = 1u + (uint32_t)wave_reduce((int)most, 0, [](int x, int y) {
+                        return (int)max((uint32_t)x, (uint32_t)y);
+                    });
+                    need = max(need, least);
+#pragma unroll 1
+                    while (past - need > 1u) {
+                        const uint32_t mid = need + (past - need) / 2u;
+                        const int c = reach(mid);
+                        if (c < a.n_top) {
+                            past = mid;
+                            continue;
+                        }
+                        need = mid;
+                        if (c <= a.n_top + a.n_top / 4)
+                            break;
+                    }
+                }
             }
             const float need_value = need > 1u ? order_value(need) : -INFINITY;
             int held = 0;

@@ -61,7 +61,7 @@ def tokens(n, vocab, seed):
 @pytest.mark.parametrize("n,vocab,top", [
     (1, 1, 1), (1, 1, 0), (3, 2, 2), (2, 63, 5), (2, 64, 64), (5, 65, 20), (1, 1000, 64),
     (4, 2047, 7), (4, 2049, 1), (16, 151936, 20), (1, 128256, 64), (3, 50257, 0), (700, 999, 8),
-    (1100, 4099, 3), (1, 1 << 20, 5),
+    (1100, 4099, 3), (1, 1 << 20, 5), (3, 30011, 33), (2, 5000, 48), (600, 9001, 40),
 ])
 def test_sizes(dt, n, vocab, top):
     print("logprobs", dt, n, vocab, top, flush=True)
