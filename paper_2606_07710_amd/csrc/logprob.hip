@@ -442,10 +442,10 @@ __global__ __launch_bounds__(kThreads) void token_logprobs(LogprobParams a) {
                     }
                     // a few for a list that is full, each the largest of its lane's
                     if (list.bar && more <= kInserts && more == __popcll(lanes) && !__ballot(tu != tu)) {
-                        int at = 0;
+                        int at = 0;                  // (behind the n-th lie no values)
 #pragma unroll
                         for (int e = 1; e < V; ++e)
-                            at = x[e] == tu ? e : at;
+                            at = e < n && x[e] == tu ? e : at;
                         at += base + u * TILE;
 #pragma unroll 1
                         for (; lanes; lanes &= lanes - 1) {

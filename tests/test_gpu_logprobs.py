@@ -220,3 +220,28 @@ def test_of_the_4_bit_products_logits_beside_the_acceptance_call():
     compare(z, t, 4, (lp, e2, rank, ids, tops))
     assert torch.equal(ids[:, 0], am)
     assert torch.allclose(ent, e2, rtol=2e-4, atol=2e-4)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("top", [1, 5, 64])
+@pytest.mark.parametrize("vocab,shift", [(1023, 0), (1027, 0), (4098, 1), (9007, 3), (20013, 5)])
+def test_a_zero_above_negative_logits_at_the_ends_of_the_runs(dt, top, vocab, shift):
+    """Rows whose best values are zeros (of either sign) next to the unaligned
+    ends of the rows and of the parts that a row is read in: the elements there
+    go one to a lane, and a zero is also what is left in such a lane."""
+    print("zeros", dt, top, vocab, shift, flush=True)
+    g = torch.Generator("cuda").manual_seed(vocab + top)
+    at = sorted({p for e in (0, 1024, 2048, 4096, 8192, vocab) for p in range(e - 8, e + 8)
+                 if 0 <= p < vocab})
+    n = len(at) + 3
+    x = torch.full((n, vocab + 8), 50.0, dtype=R.DT[dt], device="cuda")[:, shift: shift + vocab]
+    x.copy_(-1.0 - torch.randn(n, vocab, generator=g, device="cuda").abs())
+    for r, p in enumerate(at):
+        x[r, p] = 0.0 if r % 3 else -0.0
+    x[-3, -3:] = torch.tensor([0.0, -0.0, 0.0])           # several of them
+    x[-2, at] = 0.0
+    x[-1, ::2] = -0.0
+    t = torch.tensor(at + [vocab - 1, at[-1], 1], dtype=torch.int32, device="cuda")
+    compare(x, t, top)
+    ids = run(x, t, top)[3]
+    assert torch.equal(ids[: len(at), 0], t[: len(at)])
