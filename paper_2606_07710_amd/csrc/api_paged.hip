@@ -56,9 +56,10 @@ bool select_sizes_ok(int n_rows, int n_kv_heads, int max_pages) {
 }
 
 wf_status_t attn_common(wf_dtype_t dt, const void *q, const wf_paged_cache_t *c,
-                        const wf_paged_batch_t *b, const int32_t *sel, int n_sel, void *out,
-                        const uint64_t *tree_mask, int n_rows, int n_q_heads, float softmax_scale,
-                        void *workspace, size_t workspace_bytes, void *stream) {
+                        const wf_paged_batch_t *b, bool sparse, const int32_t *sel, int n_sel,
+                        void *out, const uint64_t *tree_mask, int n_rows, int n_q_heads,
+                        float softmax_scale, void *workspace, size_t workspace_bytes,
+                        void *stream) {
     const wf_status_t st = check_cache(dt, c);
     if (st != WF_OK)
         return st;
@@ -67,9 +68,10 @@ wf_status_t attn_common(wf_dtype_t dt, const void *q, const wf_paged_cache_t *c,
         return WF_ERR_INVALID_ARG;
     if (n_rows == 0)
         return WF_OK;
-    if (!q || !out || !aligned16(q) || !aligned16(out) || !aligned16(tree_mask))
+    if (!q || !out || !aligned16(q) || !aligned16(out) || !aligned16(tree_mask) ||
+        (sparse && (!sel || !aligned4(sel))))
         return WF_ERR_INVALID_ARG;
-    const wf::PagedPlan p = wf::plan_paged(dt, b->max_rows, n_q_heads, c->n_kv_heads, sel);
+    const wf::PagedPlan p = wf::plan_paged(dt, b->max_rows, n_q_heads, c->n_kv_heads, sparse);
     if (!workspace || !aligned16(workspace) ||
         workspace_bytes < wf::paged_attn_workspace_bytes(p, c->head_dim))
         return WF_ERR_WORKSPACE;
@@ -124,7 +126,7 @@ wf_status_t wf_paged_verify_attn(wf_dtype_t dt, const void *q, const wf_paged_ca
                                  const uint64_t *tree_mask, int32_t n_rows, int32_t n_q_heads,
                                  float softmax_scale, void *workspace, size_t workspace_bytes,
                                  void *stream) {
-    return attn_common(dt, q, cache, batch, nullptr, 0, out, tree_mask, n_rows, n_q_heads,
+    return attn_common(dt, q, cache, batch, false, nullptr, 0, out, tree_mask, n_rows, n_q_heads,
                        softmax_scale, workspace, workspace_bytes, stream);
 }
 
@@ -174,7 +176,7 @@ wf_status_t wf_paged_sparse_attn(wf_dtype_t dt, const void *q, const wf_paged_ca
                                  void *out, const uint64_t *tree_mask, int32_t n_rows,
                                  int32_t n_q_heads, float softmax_scale, void *workspace,
                                  size_t workspace_bytes, void *stream) {
-    if (n_sel < 1 || n_sel > kMaxSelected || !sel || !aligned4(sel))
+    if (n_sel < 1 || n_sel > kMaxSelected)
         return WF_ERR_INVALID_ARG;
     // (chunks of 128 listed keys are counted in 32 bits)
     if (cache && attn_sizes_ok(n_rows, n_q_heads, cache->n_kv_heads) &&
@@ -182,7 +184,7 @@ wf_status_t wf_paged_sparse_attn(wf_dtype_t dt, const void *q, const wf_paged_ca
                 ((n_q_heads / cache->n_kv_heads + 15) / 16) *
                 (((long long)n_sel * cache->page_size + 127) / 128) > INT32_MAX)
         return WF_ERR_INVALID_ARG;
-    return attn_common(dt, q, cache, batch, sel, n_sel, out, tree_mask, n_rows, n_q_heads,
+    return attn_common(dt, q, cache, batch, true, sel, n_sel, out, tree_mask, n_rows, n_q_heads,
                        softmax_scale, workspace, workspace_bytes, stream);
 }
 

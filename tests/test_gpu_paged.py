@@ -575,3 +575,20 @@ def test_pages_past_32_bits():
     want = R.rotate(R.f64(rnd.new_k), np.array([300, 301])[:, None, None], BASE)
     got = k[n_pages - 81, :, 300 - 256: 302 - 256].transpose(0, 1)
     check(got, want, R.rotation_error(R.f64(rnd.new_k), want, "bf16"))
+
+
+def test_a_round_without_rows():
+    """Every request idle: no tensor has a row, and every call of the round
+    returns."""
+    rnd = R.Round([(0, 30), (0, 0)], 16, 8, 2, 64, seed=99, max_rows=4).on_gpu()
+    assert rnd.n == 0
+    q, out = rnd.dq, torch.empty_like(rnd.dq)
+    sel = torch.empty((0, 2, 5), dtype=torch.int32, device="cuda")
+    kv = rnd.new_k.cuda()
+    wf.wf_paged_append(kv, kv, rnd.cache, rnd.batch, BASE, q=q, q_out=out)
+    wf.wf_paged_append(kv, kv, rnd.cache, rnd.batch, BASE)
+    wf.wf_paged_verify_attn(q, rnd.cache, rnd.batch, out)
+    wf.wf_paged_select(q, rnd.cache, rnd.batch, sel, 2)
+    wf.wf_paged_sparse_attn(q, rnd.cache, rnd.batch, sel, out)
+    torch.cuda.synchronize()
+    assert torch.equal(rnd.dk.cpu(), rnd.k) and torch.equal(rnd.db.cpu(), rnd.bounds)

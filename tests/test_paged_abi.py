@@ -212,3 +212,16 @@ def test_handles_refuse_what_does_not_fit():
         wf.PagedBatch(i(2, 3), i(2), i(2))
     with pytest.raises(TypeError):
         wf.PagedBatch(i(2, 3), i(3).long(), i(2))
+
+
+@pytest.mark.parametrize("call,tensors", [
+    (_append, ("k", "v", "q", "qo")), (_append, ("k", "v")), (_attn, ("q", "out", "ws")),
+    (_select, ("q", "sel", "ws")), (_sparse, ("q", "sel", "out", "ws"))])
+def test_no_rows_are_a_no_op_with_empty_tensors(call, tensors):
+    """An empty tensor's pointer is null."""
+    assert call(n=0, **{t: None for t in tensors}) == 0
+
+
+def test_selections_are_needed_where_there_are_rows():
+    assert _sparse(sel=None, ws=None) == 1 and _select(sel=None, ws=None) == 1
+    assert _sparse(n=0, sel=None, ns=0) == 1 and _sparse(n=0, sel=None, ns=1025) == 1
