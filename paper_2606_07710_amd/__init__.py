@@ -1110,7 +1110,11 @@ def wf_paged_append(k, v, cache, batch, rope_base, q=None, q_out=None, positions
 
 
 def _code_of(dtype):
-    return dtype if isinstance(dtype, int) else (WF_F32 if dtype == torch.float32 else WF_BF16)
+    """The code of a torch dtype, or the code itself."""
+    code = dtype if isinstance(dtype, int) else _DTYPE_CODES.get(dtype)
+    if code is None:
+        raise TypeError(f"unsupported dtype {dtype}; use float32 or bfloat16")
+    return code
 
 
 def wf_paged_verify_attn_workspace_bytes(dtype, n_rows, n_seqs, max_rows, n_q_heads, n_kv_heads,

@@ -225,3 +225,15 @@ def test_no_rows_are_a_no_op_with_empty_tensors(call, tensors):
 def test_selections_are_needed_where_there_are_rows():
     assert _sparse(sel=None, ws=None) == 1 and _select(sel=None, ws=None) == 1
     assert _sparse(n=0, sel=None, ns=0) == 1 and _sparse(n=0, sel=None, ns=1025) == 1
+
+
+@pytest.mark.parametrize("query,sizes", [
+    (wf.wf_paged_verify_attn_workspace_bytes, (8, 4, 16, 32, 8, 128)),
+    (wf.wf_paged_sparse_attn_workspace_bytes, (8, 32, 8, 128, 64, 10)),
+    (wf.wf_token_logprobs_workspace_bytes, (16, 1000, 5))])
+def test_workspace_queries_refuse_other_types(query, sizes):
+    assert query(torch.float32, *sizes) == query(wf.WF_F32, *sizes) >= 4 << 20
+    assert query(torch.bfloat16, *sizes) == query(wf.WF_BF16, *sizes) >= 4 << 20
+    for dtype in (torch.float16, torch.float64, torch.int32, torch.float8_e4m3fn, None, "bf16"):
+        with pytest.raises(TypeError):
+            query(dtype, *sizes)
