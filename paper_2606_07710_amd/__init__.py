@@ -977,7 +977,21 @@ def wf_linear_w4(x, weight, out, residual=None, workspace=None, stream=None):
     return out
 
 
-class PagedCache:
+class _Fixed:
+    """A handle whose numbers and tensors stay those that the calls hold: once it
+    is made, none of them can be assigned."""
+    _held = frozenset()
+
+    def __setattr__(self, name, value):
+        if name in self._held:
+            raise AttributeError(f"{name} of a {type(self).__name__} cannot change: make another")
+        super().__setattr__(name, value)
+
+    def _hold(self):
+        self.__dict__["_held"] = frozenset(self.__dict__) | {"_held"}
+
+
+class PagedCache(_Fixed):
     """One layer's paged K/V cache (wf.h): a pool of pages that the sequences of
     a batch share.
 
@@ -986,7 +1000,7 @@ class PagedCache:
              largest key per dimension (kept by wf_paged_append, read by
              wf_paged_select), or None
 
-    The tensors stay the ones it was made of (the calls hold their addresses); a
+    The tensors and sizes stay the ones it was made of (the calls hold them); a
     deep copy has its own."""
 
     def __init__(self, k, v, bounds=None):
@@ -1006,6 +1020,7 @@ class PagedCache:
         self.struct = PagedCacheStruct(_ptr(k, dev, "k"), _ptr(v, dev, "v"),
                                        _ptr(bounds, dev, "bounds"), n, page, hkv, dh)
         self.ref = ctypes.byref(self.struct)
+        self._hold()
 
     k = property(lambda self: self._tensors[0])
     v = property(lambda self: self._tensors[1])
@@ -1025,11 +1040,12 @@ def alloc_paged_cache(n_pages, page_size, n_kv_heads, head_dim, dtype, device,
     return PagedCache(k, v, b)
 
 
-class PagedBatch:
+class PagedBatch(_Fixed):
     """A ragged batch over paged caches (wf.h): int32 device tensors page_table
     [n_seqs][max_pages], row_start [n_seqs + 1] and ctx_len [n_seqs], which the
     caller may refill between calls (and between a captured graph's replays), and
-    the most rows that a sequence has in an attention or selection call."""
+    the most rows that a sequence has in an attention or selection call.  The
+    tensors and sizes, max_rows among them, stay the ones it was made of."""
 
     def __init__(self, page_table, row_start, ctx_len, max_rows=64):
         n, max_pages = page_table.shape
@@ -1049,6 +1065,7 @@ class PagedBatch:
                                        _ptr(ctx_len, dev, "ctx_len"), n, max_pages,
                                        self.max_rows)
         self.ref = ctypes.byref(self.struct)
+        self._hold()
 
     page_table = property(lambda self: self._tensors[0])
     row_start = property(lambda self: self._tensors[1])

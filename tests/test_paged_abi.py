@@ -1,6 +1,7 @@
 """What the paged-cache calls and the token log probabilities refuse, on the
 CPU: no call here reaches the GPU (pointers are never dereferenced by the
 checks), and what their Python wrappers refuse before the library is called."""
+import copy
 import ctypes
 
 import pytest
@@ -237,3 +238,41 @@ def test_workspace_queries_refuse_other_types(query, sizes):
     for dtype in (torch.float16, torch.float64, torch.int32, torch.float8_e4m3fn, None, "bf16"):
         with pytest.raises(TypeError):
             query(dtype, *sizes)
+
+
+class _Device:
+    """As much of a device tensor as the handles look at."""
+
+    def __init__(self, shape, dtype):
+        self.shape, self.dtype, self.device = torch.Size(shape), dtype, torch.device("cuda", 0)
+
+    def get_device(self):
+        return 0
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return FAKE
+
+
+def test_handles_keep_what_the_calls_hold():
+    """The calls read a handle's struct: its numbers cannot be changed beside it."""
+    kv = _Device((3, 2, 16, 64), torch.bfloat16)
+    cache = wf.PagedCache(kv, kv, _Device((3, 2, 2, 64), torch.bfloat16))
+    i32 = [_Device(s, torch.int32) for s in ((4, 9), (5,), (4,))]
+    batch = wf.PagedBatch(*i32, max_rows=8)
+    assert batch.max_rows == batch.struct.max_rows == 8 and cache.head_dim == 64
+    for handle, names in ((batch, ("max_rows", "n_seqs", "max_pages", "dev", "struct", "ref",
+                                   "page_table", "row_start", "ctx_len", "_tensors")),
+                          (cache, ("head_dim", "page_size", "n_pages", "n_kv_heads", "code", "dtype",
+                                   "device", "dev", "struct", "ref", "k", "v", "bounds"))):
+        for name in names:
+            before = getattr(handle, name)
+            with pytest.raises(AttributeError):
+                setattr(handle, name, 16)
+            assert getattr(handle, name) is before
+        handle.note = 1                        # the caller's own names are the caller's
+        handle.note = 2
+    again = copy.copy(batch)
+    assert again.struct.max_rows == 8 and again.row_start is batch.row_start
