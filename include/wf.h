@@ -797,7 +797,9 @@ size_t wf_linear_w4_workspace_bytes(int32_t n_rows, int32_t n_out, int32_t k_in)
  *
  * A sequence whose numbers break these rules (row_start decreasing or outside
  * [0, n_rows], more than max_rows rows, a negative context, positions past
- * max_pages * page_size) is skipped: nothing of it is read or written.
+ * max_pages * page_size) is skipped: nothing of it is read or written.  The
+ * others are served.  Where a decreasing row_start gives a row to two of them,
+ * what its rows of q_out, out and sel hold afterwards is not defined.
  * Limits: 1 <= n_seqs <= 1024; page_size in {16, 32, 64, 128}; 1 <= max_pages,
  * max_pages * page_size <= 2^26; 1 <= n_pages; 0 <= n_rows <= 2^20 (0 is a
  * no-op); head_dim in {64, 128}; WF_F32 or WF_BF16, one type for the cache and

@@ -79,8 +79,9 @@ struct AppendParams {
     int run;                       // KV heads of a workgroup
 };
 
+// The unit-th page that the batch writes; returns how many there are.
 template <typename T, int DH>
-__global__ __launch_bounds__(kThreads) void paged_append(AppendParams a) {
+__device__ __forceinline__ long long append_page(const AppendParams &a, long long unit) {
     using E = Elem<T>;
     constexpr int V = E::kVec, H = DH / 2;
     constexpr int LPR = H / V;                       // lanes per row
@@ -95,15 +96,15 @@ __global__ __launch_bounds__(kThreads) void paged_append(AppendParams a) {
     long long first, total;
     Seq s;
     const int b = paged_find<kThreads>(
-        a.v, any_rows, [](long long) { return (long long)blockIdx.x; },
+        a.v, any_rows, [&](long long) { return unit; },
         [&](const Seq &q) {
             return q.rows ? ((q.ctx + q.rows - 1) >> a.v.page_shift) - (q.ctx >> a.v.page_shift) + 1
                           : 0;
         },
         &first, &total, &s);
     if (b < 0)
-        return;
-    const int lp = (s.ctx >> a.v.page_shift) + (int)(blockIdx.x - first);
+        return total;
+    const int lp = (s.ctx >> a.v.page_shift) + (int)(unit - first);
     const int p0 = lp << a.v.page_shift;
     // page rows [from, to) are new, [0, from) older
     const int from = max(s.ctx - p0, 0), to = min(s.ctx + s.rows - p0, page);
@@ -255,6 +256,16 @@ __global__ __launch_bounds__(kThreads) void paged_append(AppendParams a) {
             *reinterpret_cast<u32x4 *>(dst + H + c * V) = E::pack(y);
         }
     }
+    return total;
+}
+
+// A workgroup has one page, unless a decreasing row_start gives rows to several
+// sequences: then there may be more pages than the host counts.
+template <typename T, int DH>
+__global__ __launch_bounds__(kThreads) void paged_append(AppendParams a) {
+    for (long long unit = blockIdx.x; append_page<T, DH>(a, unit) > unit + gridDim.x;
+         unit += gridDim.x)
+        __syncthreads();
 }
 
 // ---------------------------------------------------------------------------
@@ -685,8 +696,8 @@ wf_status_t launch_paged_append(wf_dtype_t dt, const wf_paged_cache_t &c,
     a.q_stride = q_stride;
     a.n_q_heads = n_q_heads;
     a.group = q ? n_q_heads / c.n_kv_heads : 0;
-    // at most this many pages receive rows: a sequence's rows reach one page
-    // more than they fill
+    // at most this many pages receive rows, each row of one sequence: a sequence's
+    // rows reach one page more than they fill
     const int pages = (int)std::min<long long>(
         n_rows, n_rows / c.page_size + 2ll * std::min(b.n_seqs, n_rows));
     // as many workgroups as fill the chip four times over, no more than heads

@@ -52,8 +52,8 @@ __device__ __forceinline__ long long uniform64(long long x) {
 
 // Where unit at(total) of a ragged list lies: sequence b owns count(its Seq)
 // units, in order, `total` of them in all (also *total).  All threads of the
-// workgroup call this alike, once in a kernel; the result is the owning sequence
-// (-1 if there is no such unit), with *first its first unit and *seq its rows.
+// workgroup call this alike, once or again after a barrier; the result is the owning
+// sequence (-1 if there is no such unit), with *first its first unit and *seq its rows.
 template <int THREADS, typename F, typename At>
 __device__ __forceinline__ int paged_find(const PagedView &a, int max_rows, At &&at_of, F &&count,
                                           long long *first, long long *total, Seq *seq) {

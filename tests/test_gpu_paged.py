@@ -592,3 +592,63 @@ def test_a_round_without_rows():
     wf.wf_paged_sparse_attn(q, rnd.cache, rnd.batch, sel, out)
     torch.cuda.synchronize()
     assert torch.equal(rnd.dk.cpu(), rnd.k) and torch.equal(rnd.db.cpu(), rnd.bounds)
+
+
+def test_append_of_lists_that_give_rows_twice():
+    """Sequences whose own numbers hold are served, each in its pages, also where a
+    decreasing row_start between them gives them the same rows; the others leave
+    everything as it was."""
+    say("append, rows given twice")
+    n, ctx = 200, 5
+    rnd = R.Round([(n, ctx)] * 8, 16, 4, 2, 64, seed=81).on_gpu()
+    starts = [0, n] * 4 + [0]
+    rnd.batch.row_start.copy_(torch.tensor(starts, dtype=torch.int32))
+    q, new_k, new_v = (x[:n] for x in (rnd.q, rnd.new_k, rnd.new_v))
+    out = torch.full((n, 4, 64), 7.0, dtype=q.dtype, device="cuda")
+    wf.wf_paged_append(new_k.cuda(), new_v.cuda(), rnd.cache, rnd.batch, BASE, q=q.cuda(),
+                       q_out=out)
+    rnd.start, rnd.q = starts[:-1], q
+    rnd.lens = [(n if b % 2 == 0 else 0, ctx) for b in range(8)]
+    k, ek, v, qo, eq, touched = expected_append(rnd, None, rnd.k, rnd.v, rnd.bounds, q)
+    assert len(touched) == 4 * 13
+    check(rnd.dk, k, ek, "k")
+    assert np.array_equal(R.f64(rnd.dv), v)
+    check(out, qo, eq, "q")                    # (their rows are at the same positions)
+    ref, stored = rnd.bounds.clone(), rnd.dk.cpu()
+    for p, lp, b in touched:
+        x = stored[p, :, : min(16, ctx + n - lp * 16)]
+        ref[p, :, 0], ref[p, :, 1] = x.amin(1), x.amax(1)
+    assert torch.equal(rnd.db.cpu(), ref)
+
+
+@pytest.mark.parametrize("start,ctx,served", [
+    ([0, 3, 7, 9], [30, -1, 40], [0, 2]), ([0, 3, 7, 9], [1 << 30, 20, 2000], [1]),
+    ([-1, 3, 7, 9], None, [1, 2]), ([0, 3, 7, 10], None, [0, 1]), ([0, 3, 2, 9], None, [0, 2]),
+    ([9, 7, 3, 0], None, []), ([0, 1 << 30, 7, 9], None, [2])])
+def test_append_of_broken_lists(start, ctx, served):
+    """Sequences whose numbers do not hold leave pages, bounds and q_out alone."""
+    rnd = R.Round([(3, 30), (4, 20), (2, 40)], 16, 4, 2, 64, seed=83).on_gpu()
+    rnd.batch.row_start.copy_(torch.tensor(start, dtype=torch.int32))
+    if ctx:
+        rnd.batch.ctx_len.copy_(torch.tensor(ctx, dtype=torch.int32))
+    out = torch.full_like(rnd.dq, 7.0)
+    # (rows that two sequences have are rotated by either's positions: without q)
+    twice = start == [0, 3, 2, 9]
+    wf.wf_paged_append(rnd.new_k.cuda(), rnd.new_v.cuda(), rnd.cache, rnd.batch, BASE,
+                       **({} if twice else dict(q=rnd.dq, q_out=out)))
+    torch.cuda.synchronize()
+    lens = rnd.lens
+    rnd.start = start[:-1]
+    rnd.lens = [(start[b + 1] - start[b] if b in served else 0, c) for b, (_, c) in enumerate(lens)]
+    if twice:
+        # five rows more than its pages were made for fit them all the same
+        assert rnd.lens[2] == (7, 40)
+    k, ek, v, qo, eq, touched = expected_append(rnd, None, rnd.k, rnd.v, rnd.bounds, rnd.q)
+    check(rnd.dk, k, ek, "k")
+    assert np.array_equal(R.f64(rnd.dv), v)
+    if not twice:
+        check(out, qo, eq, "q")
+        assert (R.f64(out)[np.isnan(qo)] == 7.0).all()
+    pages = {p for p, _, _ in touched}
+    rest = [p for p in range(rnd.k.shape[0]) if p not in pages]
+    assert torch.equal(rnd.db.cpu()[rest], rnd.bounds[rest])
