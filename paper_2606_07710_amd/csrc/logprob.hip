@@ -36,6 +36,10 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kMaxParts = 64;
 constexpr int kLoads = 4;                  // 16-byte loads of a lane in a group
+// Groups after which a lane's sums go into a second pair, so that rows of millions
+// of values are no chain of as many roundings: kLoads * kFold pieces in one sum and,
+// in the longest run there can be, 2^28 values in 2^18 groups, 2^10 such sums.
+constexpr int kFold = 256;
 // Up to so many values of a tile enter a full list one by one, a compare and
 // seven moves each, more of them together (2000 rows with 5 alternatives: 167 ->
 // 163 us; into an empty list one by one, 16 rows with 20 take 17.5 us, not 16).
@@ -101,6 +105,13 @@ __device__ __forceinline__ SumState lanes_join(SumState x) {
     const float m = lanes_max(x.m);
     const float d = shift(x.m, m), e = fast_exp2(d * kLog2e);
     return SumState{m, lanes_sum(x.l * e), lanes_sum((x.t + x.l * d) * e)};
+}
+// The sums l and t from reference m into `all`, whose reference is no larger; they
+// begin anew.
+__device__ __forceinline__ void fold(SumState &all, float m, float &l, float &t) {
+    const float d = shift(all.m, m), e = fast_exp2(d * kLog2e);
+    all = SumState{m, fmaf(all.l, e, l), fmaf(all.t + all.l * d, e, t)};
+    l = t = 0.f;
 }
 
 __device__ __forceinline__ uint64_t volatile_load(const uint64_t *p) {
@@ -222,6 +233,7 @@ __global__ __launch_bounds__(kThreads) void token_logprobs(LogprobParams a) {
     __syncthreads();
     uint64_t bar = 0;                      // the highest of the waves' (uniform)
     float m = -INFINITY, l = 0.f, t = 0.f;
+    SumState all{-INFINITY, 0.f, 0.f};     // of the groups before the last kFold
     int ahead = 0;                         // uniform
 
     auto unpack = [&](u32x4 w, float (&x)[V]) {
@@ -284,8 +296,13 @@ __global__ __launch_bounds__(kThreads) void token_logprobs(LogprobParams a) {
             ahead += __popcll(__ballot(i < token && i < i1 && x != x));
         }
     }
+    int next_fold = i0 + kFold * U * TILE;
 #pragma unroll 1
     for (int pos = i0; pos < i1;) {
+        if (pos >= next_fold) {
+            fold(all, m, l, t);
+            next_fold = pos + kFold * U * TILE;
+        }
         const bool single = pos < head || pos >= body;
         const int group = pos + U * TILE;
         const bool whole = !single && group <= body;
@@ -487,7 +504,8 @@ __global__ __launch_bounds__(kThreads) void token_logprobs(LogprobParams a) {
 
     // ---- the waves meet, then, by the row's last workgroup, the parts ----
     const size_t first = (size_t)row * a.parts;
-    SumState s{m, l, t};
+    fold(all, m, l, t);
+    SumState s = all;
     bool last_round = a.parts == 1;
     int lists = 0;
 #pragma unroll 1

@@ -245,3 +245,31 @@ def test_a_zero_above_negative_logits_at_the_ends_of_the_runs(dt, top, vocab, sh
     compare(x, t, top)
     ids = run(x, t, top)[3]
     assert torch.equal(ids[: len(at), 0], t[: len(at)])
+
+
+def test_sums_of_long_rows():
+    """The longest row there can be, in few parts: 2^28 times the logits 1/4, 0, 0,
+    0.  A lane has 52428 pieces of four, whose sum 3.336 is no multiple of the
+    steps of a large fp32 number: added one after the other they would be off by
+    the same amount each time, by 4.5e-4 in all.  Allowed, as for short rows, are
+    1100 terms' roundings, 6.6e-5, which the entropy has 1.3 times (its second
+    sum is 0.18 of the first), and 2^-20 for the logarithm of about 21."""
+    vocab, top = 1 << 30, 64
+    print("long row", flush=True)
+    x = torch.zeros((1, vocab), device="cuda")
+    x[0, ::4] = 0.25
+    t = torch.tensor([(1 << 29) + 4], dtype=torch.int32, device="cuda")
+    lp, ent, rank, ids, tops = run(x, t, top)
+    total = vocab / 4 * (np.exp(0.25) + 3.0)
+    p = np.array([np.exp(0.25), 1.0]) / total
+    entropy = -vocab / 4 * (p[0] * np.log(p[0]) + 3 * p[1] * np.log(p[1]))
+    assert abs(float(lp[0]) - np.log(p[0])) <= 2.0 ** -13
+    assert np.abs(R.f64(tops) - np.log(p[0])).max() <= 2.0 ** -13
+    assert abs(float(ent[0]) - entropy) <= 2.0 ** -13
+    assert int(rank[0]) == (1 << 27) + 1
+    assert torch.equal(ids[0].cpu(), torch.arange(0, 4 * top, 4, dtype=torch.int32))
+    # a token of the lower ones, at the end
+    t.fill_(vocab - 1)
+    lp, _, rank, _, _ = run(x, t, 0)
+    assert abs(float(lp[0]) - np.log(p[1])) <= 2.0 ** -13
+    assert int(rank[0]) == vocab - 1
