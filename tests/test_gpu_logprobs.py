@@ -273,3 +273,99 @@ def test_sums_of_long_rows():
     lp, _, rank, _, _ = run(x, t, 0)
     assert abs(float(lp[0]) - np.log(p[1])) <= 2.0 ** -13
     assert int(rank[0]) == vocab - 1
+
+
+U = 2.0 ** -24
+
+
+def chain(vocab, dt):
+    """Terms that a value passes on its way into a row's sum, at most: a lane's
+    pieces (the fewest lanes: one part), the values of a piece, the sums over
+    lanes, waves and parts."""
+    per = 4 if dt == "f32" else 8
+    return -(-vocab // (256 * per)) + 3 + per + 6 + 2 + 6
+
+
+def bounds(z, tokens, dt):
+    """Errors of a row's log probabilities (at z, an array) and entropy.  A lane's
+    reference lies at most 8 below its largest value, so exponents are at most d + 8,
+    d = max - z.  A weight e^(z - m): the difference and the product with log2 e
+    (a constant with an error of its own) round by U of the exponent each, the
+    exponential is good to 2 U, and the moves and joins, of d + 8 together and at most
+    d / 8 + 5 of them, do the same again: 6 d + 64 units."""
+    n, vocab = z.shape
+    m = z.max(1, keepdims=True)
+    d = m - z
+    w = np.exp(-d)
+    total = w.sum(1, keepdims=True)
+    p = w / total
+    c = chain(vocab, dt)
+    a = (p * d).sum(1)
+    in_l = 6 * a + 64 + c
+    in_t = (p * (d + 8) * (6 * d + 65 + c)).sum(1) + 6 * (a + 16)
+    log_l = 2 * (8 + np.log(vocab))                     # 2 U of the logarithm
+
+    def of(zt):
+        return U * (in_l + log_l + (m[:, 0] - zt + 8) + np.abs(zt - m[:, 0] - np.log(total[:, 0])))
+
+    return of, U * (in_l * (1 + a + 8) + in_t + log_l + a + 8 + np.log(vocab))
+
+
+def compare_closely(x, tokens, n_top, dt):
+    z = R.f64(x)
+    lp, ent, rank, ids, tops = run(x, tokens, n_top)
+    rlp, rent, rrank, rids, rtops = R.logprobs(z, tokens.cpu().numpy(), n_top)
+    of, entropy = bounds(z, tokens, dt)
+    assert np.array_equal(rank.cpu().numpy(), rrank) and np.array_equal(ids.cpu().numpy(), rids)
+    at = np.arange(len(z))
+    assert (np.abs(R.f64(lp) - rlp) <= of(z[at, tokens.cpu().numpy()])).all()
+    for i in range(n_top):
+        assert (np.abs(R.f64(tops)[:, i] - rtops[:, i]) <= of(z[at, rids[:, i]])).all()
+    assert (np.abs(R.f64(ent) - rent) <= entropy).all(), (R.f64(ent) - rent, entropy)
+    assert (lp <= 0).all() and (tops <= 0).all() and (ent >= 0).all()
+    return R.f64(lp) - rlp, R.f64(tops) - rtops, R.f64(ent) - rent
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("n,vocab,top", [
+    (16, 151936, 20), (511, 700, 3), (512, 5000, 5), (513, 5000, 5), (600, 9001, 20), (1, 50257, 64)])
+def test_errors_of_ordinary_rows(dt, n, vocab, top):
+    """Each value within its bound, and, where there are many, in the mean square:
+    log l, the difference and the result round to a step of at most 2^-20 (values
+    of 8 to 16), half of it at most, a third of that squared on the average, and a
+    chain of up to 100 roundings of a sum is off by sqrt(100 / 3) U at random: 4e-7
+    together; the exponential's own 2 U may be the same for all values."""
+    print("ordinary", dt, n, vocab, top, flush=True)
+    lp, tops, ent = compare_closely(logits(n, vocab, dt, n + vocab), tokens(n, vocab, n), top, dt)
+    if n > 500:
+        assert np.sqrt((lp ** 2).mean()) <= 2.0 ** -20
+        assert np.sqrt((tops ** 2).mean()) <= 2.0 ** -20
+        # t / l is up to 16 from a reference, its two sums as above
+        assert np.sqrt((ent ** 2).mean()) <= 2.0 ** -18
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [4999, 151936])
+@pytest.mark.parametrize("where", ["first", "middle", "last"])
+def test_errors_of_rows_with_one_likely_token(dt, vocab, where):
+    """One token 4 to 30 above the rest.  From 12 on the rest is more than 8 below
+    it, so the row's reference is that token, its weight is 1 without an error, and
+    the entropy, log(1 + s) + sum p d, is a sum of terms above 0: within (6 d + 64
+    + chain) U of itself, twice (weights and their sums), but that s is lost in
+    1 + s where it lies below the roundings of the sums of which 1 is a term."""
+    print("likely", dt, vocab, where, flush=True)
+    gaps = [4, 5, 6, 7, 8, 9, 10, 12, 13, 14, 16, 18, 20, 24, 30]
+    g = torch.Generator("cuda").manual_seed(vocab)
+    x = (-2.0 - torch.rand(len(gaps), vocab, generator=g, device="cuda")).to(R.DT[dt])
+    at = {"first": 0, "middle": vocab // 2, "last": vocab - 1}[where]
+    x[:, at] = torch.tensor(gaps, device="cuda").to(x.dtype) - 2.0
+    t = torch.full((len(gaps),), at, dtype=torch.int32, device="cuda")
+    t[::3] = 7 if at != 7 else 8
+    _, _, ent = compare_closely(x, t, 5, dt)
+    z, c = R.f64(x), chain(vocab, dt)
+    ref = R.logprobs(z, t.cpu().numpy(), 0)[1]
+    for i, gap in enumerate(gaps):
+        if gap >= 12:
+            rest = np.exp(np.delete(z[i], at) - z[i, at]).sum()
+            allowed = 2 * U * (6 * (gap + 1) + 64 + c) * ref[i] + min(rest, (c + 16) * U)
+            assert abs(ent[i]) <= allowed, (gap, ent[i], ref[i], allowed)

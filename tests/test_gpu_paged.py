@@ -652,3 +652,80 @@ def test_append_of_broken_lists(start, ctx, served):
     pages = {p for p, _, _ in touched}
     rest = [p for p in range(rnd.k.shape[0]) if p not in pages]
     assert torch.equal(rnd.db.cpu()[rest], rnd.bounds[rest])
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("lens,tree", [
+    ([(4, 70), (2, 33)], False), ([(61, 300), (1, 1500)], True), ([(16, 900), (1, 40)], False),
+    ([(1, 2000)], False), ([(2, 2000)], False)])
+def test_attention_of_large_whole_numbers(dt, lens, tree):
+    """Scores of up to 2^27, of whole numbers: every sum of products is exact, two
+    scores are equal or at least 2^17 apart, so the weights are 1 for the largest
+    score's keys and 0 for the others, and the output is the mean of those keys'
+    values, off by its fp32 sum and its own rounding."""
+    say("large whole numbers", dt, lens, tree)
+    rnd = R.Round(lens, 16, 8, 2, 64, dt, seed=91)
+    g = torch.Generator().manual_seed(92)
+    whole = lambda t: torch.randint(-3, 4, t.shape, generator=g).to(t.dtype)  # noqa: E731
+    rnd.k, rnd.q = whole(rnd.k), whole(rnd.q) * 2.0 ** 20
+    rnd.q[0] = 0.0                             # every key alike
+    rnd.on_gpu()
+    words = trees(rnd, 93) if tree else None
+    mask = R.masks64(words) if tree else None
+    out = torch.full_like(rnd.dq, 7.0)
+    wf.wf_paged_verify_attn(rnd.dq, rnd.cache, rnd.batch, out, tree_mask=mask)
+    keys = max(r + c for r, c in lens)
+    sums = (keys + 8) * 2.0 ** -24 * float(rnd.v.abs().max())
+    ref, _ = R.attention(rnd, words)
+    check(out, ref, np.abs(ref) * (R.HALF_STEP[dt] + 2.0 ** -22) + sums, "dense")
+    assert rnd.n == 1 or np.abs(ref).max() > 1
+    # every second page
+    n_pages = -(-keys // 16)
+    sel = torch.full((rnd.n, 2, n_pages), -1, dtype=torch.int32)
+    sel[:, :, ::2] = torch.arange(0, n_pages, 2, dtype=torch.int32)
+    some = torch.full_like(rnd.dq, 7.0)
+    wf.wf_paged_sparse_attn(rnd.dq, rnd.cache, rnd.batch, sel.cuda(), some, tree_mask=mask)
+    ref, _ = R.attention(rnd, words, sel)
+    check(some, ref, np.abs(ref) * (R.HALF_STEP[dt] + 2.0 ** -22) + sums, "selected")
+
+
+@pytest.mark.parametrize("lens,tree", [
+    ([(1, 3000)] * 4, False), ([(16, 900), (16, 1500)], False), ([(61, 1200)], True)])
+def test_attention_error_in_the_mean_square(lens, tree):
+    """bf16: a rounding at random to 8 bits is off by 2^-8 / sqrt(3) at the foot of
+    a binade and by sqrt(3 / (8 ln 2)) = 0.7355 of that over numbers spread evenly
+    over their logarithm: 0.00166.  The output has one such rounding, and every
+    weight one before its product with V; nothing else is held in 16 bits.  A
+    tenth for distributions that are not quite that; partial rows in bf16, one
+    rounding more, would be a sixth above."""
+    say("mean square", lens, tree)
+    rnd = R.Round(lens, 32, 8, 2, 128, "bf16", seed=95, std=1.1).on_gpu()
+    words = trees(rnd, 96) if tree else None
+    mask = R.masks64(words) if tree else None
+    ref, _ = R.attention(rnd, words)
+    # what the weights' roundings come to: sqrt(sum (p v)^2), element by element
+    parts = np.zeros_like(ref)
+    k, v, q = R.f64(rnd.k), R.f64(rnd.v), R.f64(rnd.q)
+    for b, (rows, ctx) in enumerate(lens):
+        for i in range(rows):
+            at = R.visible(rnd, b, i, words)
+            ids = rnd.table[b].numpy()[at // 32]
+            for h in range(8):
+                kk, vv = k[ids, h // 4, at % 32], v[ids, h // 4, at % 32]
+                z = kk @ q[rnd.start[b] + i, h] * 128 ** -0.5
+                w = np.exp(z - z.max())
+                w /= w.sum()
+                parts[rnd.start[b] + i, h] = np.sqrt((w * w) @ (vv * vv))
+    step = 2.0 ** -8 / 3 ** 0.5 * 0.7355
+    allowed = 1.1 * step * np.sqrt((ref ** 2).mean() + (parts ** 2).mean())
+    n_pages = rnd.table.shape[1]
+    every = torch.arange(n_pages, dtype=torch.int32).repeat(rnd.n, 2, 1).cuda()
+    for what in ("dense", "selected"):
+        out = torch.full_like(rnd.dq, 7.0)
+        if what == "dense":
+            wf.wf_paged_verify_attn(rnd.dq, rnd.cache, rnd.batch, out, tree_mask=mask)
+        else:
+            wf.wf_paged_sparse_attn(rnd.dq, rnd.cache, rnd.batch, every, out, tree_mask=mask)
+        error = np.sqrt(((R.f64(out) - ref) ** 2).mean())
+        say(what, error / np.sqrt((ref ** 2).mean()), allowed / np.sqrt((ref ** 2).mean()))
+        assert error <= allowed, (what, error, allowed)
