@@ -793,7 +793,9 @@ size_t wf_linear_w4_workspace_bytes(int32_t n_rows, int32_t n_out, int32_t k_in)
  *               outside [0, n_pages) name no page: nothing is stored there
  *               and no row sees keys there.
  *   max_rows    the most rows that a sequence has in an attention or
- *               selection call, at most 64 (the append takes any number)
+ *               selection call, at most 64 (the append takes any number).  The
+ *               attention's tiles are made for it: a batch of single tokens
+ *               under max_rows 64 takes a fifth longer than under 1
  *
  * A sequence whose numbers break these rules (row_start decreasing or outside
  * [0, n_rows], more than max_rows rows, a negative context, positions past
@@ -803,8 +805,9 @@ size_t wf_linear_w4_workspace_bytes(int32_t n_rows, int32_t n_out, int32_t k_in)
  * Limits: 1 <= n_seqs <= 1024; page_size in {16, 32, 64, 128}; 1 <= max_pages,
  * max_pages * page_size <= 2^26; 1 <= n_pages; 0 <= n_rows <= 2^20 (0 is a
  * no-op); head_dim in {64, 128}; WF_F32 or WF_BF16, one type for the cache and
- * the call's tensors.  Two sequences must not share a page that a call
- * writes.
+ * the call's tensors.  A page that a call writes must have one entry only
+ * among those of the batch's sequences (sequences may share pages that are
+ * read).
  * ---------------------------------------------------------------------- */
 typedef struct {
     void *k, *v, *bounds;
@@ -827,6 +830,9 @@ typedef struct {
  * cache has bounds, those of every page that received a row become the
  * bounds of its rows up to the sequence's newest position, as stored; older
  * contents count for nothing, so rows taken back by a rollback leave no trace.
+ * An accepted path of a draft tree, whose rows do not lie together, is appended
+ * again from the old context on: keys moved within the pages by other means
+ * leave bounds behind that are not theirs.
  * k, v   n_rows rows of [n_kv_heads][head_dim], kv_row_stride ELEMENTS apart;
  * q      n_rows rows of [n_q_heads][head_dim], q_row_stride apart, or NULL
  *        (q_out is then not written); q_out [n_rows][n_q_heads][head_dim],

@@ -1044,8 +1044,9 @@ class PagedBatch(_Fixed):
     """A ragged batch over paged caches (wf.h): int32 device tensors page_table
     [n_seqs][max_pages], row_start [n_seqs + 1] and ctx_len [n_seqs], which the
     caller may refill between calls (and between a captured graph's replays), and
-    the most rows that a sequence has in an attention or selection call.  The
-    tensors and sizes, max_rows among them, stay the ones it was made of."""
+    the most rows that a sequence has in an attention or selection call, which the
+    attention's tiles are made for.  The tensors and sizes, max_rows among them, stay
+    the ones it was made of."""
 
     def __init__(self, page_table, row_start, ctx_len, max_rows=64):
         n, max_pages = page_table.shape

@@ -729,3 +729,37 @@ def test_attention_error_in_the_mean_square(lens, tree):
         error = np.sqrt(((R.f64(out) - ref) ** 2).mean())
         say(what, error / np.sqrt((ref ** 2).mean()), allowed / np.sqrt((ref ** 2).mean()))
         assert error <= allowed, (what, error, allowed)
+
+
+def test_an_accepted_tree_path_is_appended_again():
+    """A draft tree's rows lie in their order in the tree.  The path that is
+    accepted becomes the cache by being appended from the old context on: pages,
+    bounds and what later rows see of them are those of a cache that never held
+    the rest of the tree."""
+    say("accepted path")
+    ctx, rows, path = 57, 12, [0, 3, 4, 8, 11, 6, 9]      # over the end of a page of 16
+    rnd = R.Round([(rows, ctx)], 16, 4, 2, 64, seed=97).on_gpu()
+    alone = R.Round([(rows, ctx)], 16, 4, 2, 64, seed=97).on_gpu()
+    one = dict(dtype=torch.int32, device="cuda")
+    depth = torch.arange(rows, **one) // 2 + ctx
+    k, v = rnd.new_k.cuda(), rnd.new_v.cuda()
+    wf.wf_paged_append(k, v, rnd.cache, rnd.batch, BASE, positions=depth)
+    n = len(path)
+    for r in (rnd, alone):
+        again = wf.PagedBatch(r.batch.page_table, torch.tensor([0, n], **one),
+                              torch.tensor([ctx], **one), 64)
+        wf.wf_paged_append(k[path], v[path], r.cache, again, BASE)
+    new = ctx + n                              # positions up to there count
+    pages = rnd.table[0, : -(-new // 16)].tolist()
+    assert new % 16 == 0 and torch.equal(rnd.db[pages], alone.db[pages])
+    assert torch.equal(rnd.dk[pages], alone.dk[pages]) and torch.equal(rnd.dv[pages], alone.dv[pages])
+    out, sel = [], []
+    for r in (rnd, alone):
+        later = wf.PagedBatch(r.batch.page_table, torch.tensor([0, 2], **one),
+                              torch.tensor([new], **one), 2)
+        wf.wf_paged_append(k[:2], v[:2], r.cache, later, BASE)
+        sel.append(torch.empty((2, 2, 3), **one))
+        wf.wf_paged_select(rnd.dq[:2], r.cache, later, sel[-1], 1)
+        out.append(torch.empty_like(rnd.dq[:2]))
+        wf.wf_paged_verify_attn(rnd.dq[:2], r.cache, later, out[-1])
+    assert torch.equal(*out) and torch.equal(*sel)
