@@ -20,9 +20,9 @@
 // Short rows and few of them are bound by latency, in which the fetching of the
 // code counts: loops that are not hot are kept rolled.  16 fp32 rows of 151936
 // with 20 alternatives take 16 us (7 without: the rest are the lists, from a
-// group's values to their two meetings); 2000 bf16 rows with 5 (608 MB) take 146
-// us, 4.2 TB/s, bound by the vector unit (0.73 busy: 14 instructions a value, an
-// exponential among them).
+// group's values to their two meetings); 2000 bf16 rows with 5 (608 MB) take 147
+// us, 4.1 TB/s, bound by the vector unit (0.74 busy: 14 instructions a value, an
+// exponential among them), 125 without.
 #include <type_traits>
 
 #include "wf_api_internal.h"
@@ -41,13 +41,13 @@ constexpr int kLoads = 4;                  // 16-byte loads of a lane in a group
 // in the longest run there can be, 2^28 values in 2^18 groups, 2^10 such sums.
 constexpr int kFold = 256;
 // Up to so many values of a tile enter a full list one by one, a compare and
-// seven moves each, more of them together (2000 rows with 5 alternatives: 167 ->
-// 163 us; into an empty list one by one, 16 rows with 20 take 17.5 us, not 16).
+// seven moves each, more of them together (2000 bf16 rows with 5 alternatives: 157 ->
+// 149 us in a graph; into an empty list one by one, 16 rows with 20 take 1.5 longer).
 constexpr int kInserts = 8;
 constexpr int kPartKeys = 1280;            // parts * n_top at most
 // A row's arrival counter has a cache line to itself: counters side by side
-// queue up at one place of the memory (16 rows without alternatives: 15.6 us,
-// apart 10.8).
+// queue up at one place of the memory (16 rows without alternatives: 13.1 us in a
+// graph, apart 7.6).
 constexpr int kCounterStride = 32;
 constexpr int kMaxSplitRows = 512;
 static_assert(kMaxSplitRows * kCounterStride <= kCounterSlots, "the counters fit the zero block");
@@ -636,7 +636,7 @@ struct LogprobPlan {
 
 // Rows are cut where they are too few to fill the chip (about four workgroups a
 // CU), down to one group of a wave's loads a lane.  (2000 rows in four parts each
-// took 221 us, whole 173: every part begins its lists anew.)
+// take 201 us, whole 148: every part begins its lists anew.)
 LogprobPlan plan_logprobs(wf_dtype_t dt, int n_rows, int vocab, int n_top) {
     const int unit = kThreads * (dt == WF_F32 ? 4 : 8) * kLoads;
     const int most = std::min({kMaxParts, (vocab + unit - 1) / unit, kPartKeys / std::max(n_top, 1)});

@@ -63,10 +63,12 @@ __device__ __forceinline__ float nan_max(float a, float b) {
 //   cosine in fp32.
 // The bounds are taken anew from all of the page's valid rows, older ones
 // included, so they never depend on what the page held before.  Prompts are
-// bound by memory: 11000 rows of 32 + 8 + 8 heads, 277 MB, take 53 us, 5.2 TB/s
-// (92 us with the angles formed anew by every head's workgroup).  64 rows of 64
-// sequences take 6 us, the latency of a table entry, then a page's rows and the
-// stores.
+// bound by memory: 11000 rows of 32 + 8 + 8 heads, 277 MB, take 63 us, 4.4 TB/s, in
+// pages of 16 (on inputs that the last-level cache still holds 54; there, with the
+// angles formed anew by every head's workgroup, 92).  In pages of 128 they take 88:
+// the sines and cosines of a page are 70 KB of LDS, two workgroups a CU.  64 rows of
+// 64 sequences take 7 us in pages of 64 and of 128, the latency of a table entry,
+// then a page's rows and the stores.
 // ---------------------------------------------------------------------------
 struct AppendParams {
     PagedView v;

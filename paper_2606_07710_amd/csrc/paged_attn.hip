@@ -16,11 +16,18 @@
 //   S^T = K Q^T    A = 16 keys x 32 dims from the LDS copy of the K tile
 //   P   = exp2((S - m) * scale * log2 e), online maximum and sum per row
 //   O^T += V^T P^T   A from transposing reads of the LDS copy of the V tile
+// P goes into the second product in bf16, the type that the matrix instruction
+// takes beside V, as in the dense kernel; its sum is of the unrounded weights, and
+// all else is fp32 up to the output.  So a weight is off by half a step, 2^-8, at
+// most, and the output by 0.0022 of itself in the mean square, where its own
+// rounding alone is 0.0017.  (The rest of each weight as a second bf16 operand gives
+// 0.0017: decoding takes 0.3 % longer, blocks 2 %, trees 45 -> 48 us, and an infinite
+// V beside a weight without a rest becomes NaN.)
 // fp32: the same with the fp32 matrix instruction, operands from memory.
 //
 // What bounds it (32 heads over 8 of 128, attention and join): decoding 128
 // requests of up to 16K keys moves 3.0 GB in 462 us, 6.5 TB/s; 45 rows' selections
-// of 122 pages of 32 keys 0.68 GB in 109 us, 6.2 TB/s.  Blocks of 16 rows (16 requests
+// of 122 pages of 32 keys 0.68 GB in 110 us, 6.2 TB/s.  Blocks of 16 rows (16 requests
 // of up to 8K, 183 MB, 46 us) and draft trees (4 of 61 nodes, 55 MB and 11.5 GFLOP,
 // 43 us) are bound by the issue of the loads and of exp2 and by the partials, one
 // request of 1K keys (9.5 us) by launch and dependent trips.
